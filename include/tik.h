@@ -49,12 +49,25 @@ typedef int tik_status;
 #define TIK_DEV_WAIT_EXPIRED 4     /* an in-kernel bounded wait ran out (outputs invalid) */
 #define TIK_DEV_BAD_POSITION 8     /* token position outside the cos/sin table: token left untouched */
 #define TIK_DEV_BAD_CONTEXT 16     /* decode: ctx_lens[b] > max_ctx_len: that slot attends keys 0..max_ctx_len-1 only */
+#define TIK_DEV_BAD_TOKEN 32       /* embedding: token id outside [0,V): row of zeros, no gradient */
 
 #define TIK_OP_ATTN_TRAIN_FWD 0
 #define TIK_OP_ATTN_PREFILL 1
 #define TIK_OP_ATTN_DECODE 2
 #define TIK_OP_TOKEN_LOGPROB 3
 #define TIK_OP_ATTN_TRAIN_BWD 4
+#define TIK_OP_EMBEDDING_BWD 5
+#define TIK_OP_BLOCK_NORM_BWD 6
+#define TIK_OP_GRAD_NORM 7
+
+/* element types of tensors that may have either */
+#define TIK_DTYPE_BF16 0
+#define TIK_DTYPE_FP32 1
+
+/* the gate of tik_block_norm */
+#define TIK_GATE_NONE 0
+#define TIK_GATE_CHANNEL 1         /* bf16 [H]: one factor per channel */
+#define TIK_GATE_TOKEN 2           /* bf16 [T]: one factor per token */
 
 /* Create / destroy the per-device context (host memory plus one small device status
  * word).  `device` is a CUDA ordinal.  tik_create is the only call that allocates. */
@@ -79,6 +92,9 @@ int tik_selftest_host(void);
  * device that holds max_clusters clusters of the cluster kernel at one time, 0 when another kernel takes it.
  * tik_selftest_bwd_dq: the dQ grid of a tik_attn_train_bwd call: 1 when its query tiles are fastest, 0 when its heads
  * are, and the query heads of a CTA. */
+/* tik_selftest_context: a stand-in context without a device, for tests of argument checks (tik_destroy frees it): calls
+ * that are refused return as with a real one; it is not to be used for anything else. */
+tik_status tik_selftest_context(tik_ctx** out, int sm_count);
 #define TIK_LINEAR_NARROW 0        /* one unit of few weight rows per CTA */
 #define TIK_LINEAR_UNITS 1         /* persistent CTAs over column units */
 #define TIK_LINEAR_PAIR_UNITS 2    /* persistent CTA pairs over 256-column units */
@@ -93,8 +109,10 @@ int tik_selftest_bwd_dq(int64_t S, int64_t total_tokens, int max_seqlen, int Hq,
 unsigned long long tik_kernel_launches(void);
 
 /* Scratch bytes an operator needs.  rows_or_batch: decode batch B, log-prob rows T, or the number
- * of sequences S for train forward / prefill.  max_ctx: the host's bound on a context length
- * (decode, prefill) or sequence length (train forward).  H, V only for the log-prob op.  Returns 0
+ * of sequences S for train forward / prefill, tokens T for the embedding and block-norm gradients, the
+ * number of tensors for the gradient norm.  max_ctx: the host's bound on a context length
+ * (decode, prefill) or sequence length (train forward).  H for the log-prob op and the embedding and
+ * block-norm gradients, V for the log-prob op and the embedding gradient.  Returns 0
  * when no scratch is needed or usable (train forward / prefill outside the range that the
  * persistent schedule handles: they then run without scratch). */
 size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d,
@@ -263,6 +281,80 @@ tik_status tik_swiglu(tik_ctx* ctx, const void* gate_up, void* out, int64_t T, i
  * 64, N a multiple of 8.  No workspace. */
 tik_status tik_linear(tik_ctx* ctx, const void* x, const void* weight, void* y, int64_t T, int K,
                       int N, void* stream);
+
+/* Embedding lookup with scaling (no paper counterpart: where a token's row enters the policy-update
+ * forward and every rollout step): y[t] = scale * table[ids[t]].
+ *   ids int32 [T], table bf16 [V][H] -> y bf16 [T][H]; the product in fp32, one rounding (scale 1: an
+ *   exact copy).  An id outside [0, V) gives a row of zeros and raises TIK_DEV_BAD_TOKEN.
+ * H must be a multiple of 8.  Needs no workspace. */
+tik_status tik_embedding(tik_ctx* ctx, const int32_t* ids, const void* table, void* y, float scale, int64_t T,
+                         int V, int H, void* stream);
+
+/* Gradient of tik_embedding with respect to the table:
+ *   g[v] = scale * sum over t with ids[t] == v of d_y[t]
+ *   accumulate == 0:  d_table = g: every row is written, with zeros where no token has that id
+ *   accumulate != 0:  d_table[v] += g[v] for the ids that occur; other rows are neither read nor written
+ *   (the later micro-batches of a step, or a table that is tied to lm_head and holds its gradient)
+ * d_y bf16 [T][H], ids int32 [T], d_table bf16 or fp32 [V][H] by table_dtype (TIK_DTYPE_*).  Tokens are sorted by id,
+ * equal ids by position, and a row's tokens are summed in fp32 in that order in a shape that depends on their
+ * number only: no atomics on values, the same bits on every call, whatever other ids the batch holds.  One rounding of
+ * g (accumulate: of d_table + g).  Ids outside [0, V) have no gradient and raise TIK_DEV_BAD_TOKEN.
+ * T == 0 with accumulate == 0 writes zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes. */
+tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, void* d_table, int table_dtype,
+                             int accumulate, float scale, int64_t T, int V, int H, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/* The step between two blocks of a layer in one pass: norm after the block, gate, scaled residual sum,
+ * norm before the next block (no paper counterpart; tik_rmsnorm with a residual is the case without
+ * post_weight and gate and with branch_scale 1, bit for bit).  Per token t with block output x[t]:
+ *   n = x * rsqrt(mean_j x_j^2 + eps) * post_weight        (post_weight NULL: n = x)
+ *   s = bf16(residual + branch_scale * gate * n)           (gate_kind: TIK_GATE_*)
+ *   y = s * rsqrt(mean_j s_j^2 + eps) * weight             (weight and y both NULL: no next norm)
+ * x, residual, s, y bf16 [T][H]; post_weight, weight bf16 [H]; gate bf16 [H] or [T].  s may be residual (in
+ * place), s or y may be x; else outputs do not overlap inputs.  fp32 arithmetic, one rounding of s and one of y (y
+ * from the rounded s, which the next layer reads).  A row's result depends on that row only, not on T.
+ * H must be a multiple of 8 and <= 8192. */
+tik_status tik_block_norm(tik_ctx* ctx, const void* x, const void* residual, const void* post_weight,
+                          const void* gate, int gate_kind, float branch_scale, const void* weight, void* s, void* y,
+                          float eps, int64_t T, int H, void* stream);
+
+/* Backward of tik_block_norm; with x NULL of the plain norm y = tik_rmsnorm(s, weight).  Given d_y = dL/dy and d_s =
+ * dL/ds (what reaches the residual stream from further on; either may be NULL for zeros, d_y exactly when weight is):
+ *   r = rsqrt(mean s^2 + eps), q = d_y * weight:  G = d_s + r * (q - s r^2 mean(q s)),  d_weight = sum_t d_y s r
+ *   d_residual = G;  d_n = branch_scale * gate * G;  d_gate = branch_scale * sum G n  (over t, or per token over the channels)
+ *   rx = rsqrt(mean x^2 + eps), p = d_n * post_weight:  d_x = rx * (p - x rx^2 mean(p x)),  d_post_weight = sum_t d_n x rx
+ *   (post_weight NULL: d_x = d_n)
+ * x and s are the forward's input and output (the rounding of s counts as the identity).  d_residual, d_x bf16 [T][H]
+ * (d_x NULL exactly when x is), each may be one of d_y, d_s, x, s; d_weight, d_post_weight fp32 [H], d_gate fp32 [H] or
+ * [T]: each exactly when its factor is given, overwritten (zeros for T == 0).  fp32 arithmetic; sums over tokens in one fixed
+ * order without atomics: the same inputs give the same bits on every call.
+ * ws: tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, ..., H, 0) bytes. */
+tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, const void* x, const void* s,
+                              const void* post_weight, const void* gate, int gate_kind, float branch_scale,
+                              const void* weight, float eps, void* d_x, void* d_residual, float* d_weight,
+                              float* d_post_weight, float* d_gate, int64_t T, int H, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/* Global gradient norm over n tensors: norm = sqrt(sum_i sum_j grads[i][j]^2).
+ *   grads: HOST array of n device pointers, numel and dtypes (TIK_DTYPE_*): HOST arrays, read during the call.  A
+ *   tensor's elements are contiguous, its base aligned to its element; no further alignment is asked for, and numel[i] may
+ *   be 0 (then grads[i] may be NULL).  norm: device fp32 [1].
+ * Squares of 64 elements or fewer are summed in fp32 (in fp64 where they leave its range), everything above in fp64 in one fixed
+ * order: the same list gives the same bits on every call and every device.  Infinities and NaN pass into the norm.
+ * ws: tik_workspace_bytes(TIK_OP_GRAD_NORM, n, ...) bytes. */
+tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* numel, const int* dtypes, int n,
+                         float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/* Clipping by the global norm: out[i] = grads[i] * (max_norm / norm) when max_norm < norm < infinity, else the gradients as
+ * they are: in place nothing is read or written then, and a norm that is not finite leaves every gradient alone for the
+ * caller to see.  out NULL: in place; else a HOST array of device pointers of the same types and sizes (out[i] may be
+ * grads[i]).  The factor is the fp32 quotient; products in fp32, one rounding.
+ * norm: device fp32 [1].  norm_given == 0: computed first, as by tik_grad_norm, and stored there; else read, e.g. after a
+ * sharded trainer has combined its ranks' norms.  max_norm must be finite and > 0.  Tensors that are written may not overlap
+ * each other or another input (TIK_ERR_INVALID_ARG).  ws as for tik_grad_norm (norm_given: may be NULL). */
+tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* out, const int64_t* numel,
+                         const int* dtypes, int n, float max_norm, float* norm, int norm_given, void* ws,
+                         size_t ws_bytes, void* stream);
 
 /* Decode attention without any allocation (the paper has no counterpart; this variant
  * exists for deployments of this library).  Same arguments, kernels and output bits as

@@ -242,3 +242,79 @@ def attn_bwd_packed(q, k, v, dout, cu_seqlens, scale: float, f32: bool = False):
         ctypes.c_int(d), ctypes.c_double(scale), _p(dq), _p(dk), _p(dv))
     assert rc == 0
     return dq, dk, dv
+
+
+# ---------------------------------------------------------------- around the attention backward (numpy, fp64)
+
+def _f64(a):
+    return None if a is None else np.asarray(a, dtype=np.float64)
+
+
+def embedding_bwd(d_y, ids, vocab: int, scale: float):
+    """(scale * sum of the rows of d_y [T,H] with each id [vocab,H], the same sum of magnitudes, rows per id [vocab])."""
+    d_y, ids = _f64(d_y), np.asarray(ids, dtype=np.int64)
+    ok = (ids >= 0) & (ids < vocab)
+    out, mag = np.zeros((vocab, d_y.shape[1])), np.zeros((vocab, d_y.shape[1]))
+    np.add.at(out, ids[ok], scale * d_y[ok])
+    np.add.at(mag, ids[ok], abs(scale) * np.abs(d_y[ok]))
+    return out, mag, np.bincount(ids[ok], minlength=vocab)
+
+
+def _norm_rows(v, eps: float):
+    return 1.0 / np.sqrt((v * v).mean(axis=1, keepdims=True) + eps)
+
+
+def _gate(gate):
+    """A gate [H] or [T,1] (or None) as a factor that broadcasts to [T,H]."""
+    if gate is None:
+        return np.ones((1, 1))
+    gate = _f64(gate)
+    return gate[None, :] if gate.ndim == 1 else gate
+
+
+def block_norm(x, residual, eps: float, post_weight=None, gate=None, branch_scale: float = 1.0):
+    """(residual + branch_scale * gate * norm(x; post_weight), the branch alone); the sum before it is rounded."""
+    x, residual, post_weight = _f64(x), _f64(residual), _f64(post_weight)
+    n = x if post_weight is None else x * _norm_rows(x, eps) * post_weight
+    u = branch_scale * _gate(gate) * n
+    return residual + u, u
+
+
+def block_norm_bwd(d_y, d_s, x, s, weight, eps: float, post_weight=None, gate=None, branch_scale: float = 1.0):
+    """Gradients of y = norm(s; weight), s = residual + branch_scale * gate * norm(x; post_weight), and the sums of
+    magnitudes that a rounding error of each scales with: ({name: value}, {name: magnitude})."""
+    d_y, d_s, x, s, weight, post_weight = (_f64(a) for a in (d_y, d_s, x, s, weight, post_weight))
+    out, mag = {}, {}
+    G, mG = np.zeros_like(s), np.zeros_like(s)
+    if d_s is not None:
+        G, mG = G + d_s, mG + np.abs(d_s)
+    if weight is not None:
+        r, q = _norm_rows(s, eps), d_y * weight
+        G = G + r * q - r ** 3 * s * (q * s).mean(axis=1, keepdims=True)
+        mG = mG + r * np.abs(q) + r ** 3 * np.abs(s) * np.abs(q * s).mean(axis=1, keepdims=True)
+        out["d_weight"], mag["d_weight"] = (d_y * s * r).sum(axis=0), np.abs(d_y * s * r).sum(axis=0)
+    out["d_residual"], mag["d_residual"] = G, mG
+    if x is None:
+        return out, mag
+    f = branch_scale * _gate(gate)
+    rx = _norm_rows(x, eps)
+    n = x if post_weight is None else x * rx * post_weight
+    dn, mdn = f * G, np.abs(f) * mG
+    if gate is not None:
+        axis, keep = (0, False) if np.ndim(gate) == 1 else (1, True)
+        out["d_gate"] = branch_scale * (G * n).sum(axis=axis, keepdims=keep)
+        mag["d_gate"] = abs(branch_scale) * (mG * np.abs(n)).sum(axis=axis, keepdims=keep)
+    if post_weight is None:
+        out["d_x"], mag["d_x"] = dn, mdn
+        return out, mag
+    out["d_post_weight"], mag["d_post_weight"] = (dn * x * rx).sum(axis=0), (mdn * np.abs(x * rx)).sum(axis=0)
+    p, mp = dn * post_weight, mdn * np.abs(post_weight)
+    out["d_x"] = rx * p - rx ** 3 * x * (p * x).mean(axis=1, keepdims=True)
+    mag["d_x"] = rx * mp + rx ** 3 * np.abs(x) * (mp * np.abs(x)).mean(axis=1, keepdims=True)
+    return out, mag
+
+
+def grad_norm(grads) -> float:
+    """Square root of the sum of the squares of all elements of a list of arrays."""
+    with np.errstate(all="ignore"):
+        return float(np.sqrt(sum(float((_f64(g) ** 2).sum()) for g in grads)))

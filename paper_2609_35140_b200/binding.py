@@ -19,7 +19,8 @@ from . import build as _build
 
 OK = 0
 OP_ATTN_TRAIN_FWD, OP_ATTN_PREFILL, OP_ATTN_DECODE, OP_TOKEN_LOGPROB, OP_ATTN_TRAIN_BWD = 0, 1, 2, 3, 4
-DEV_BAD_BLOCK, DEV_BAD_TARGET, DEV_WAIT_EXPIRED, DEV_BAD_POSITION, DEV_BAD_CONTEXT = 1, 2, 4, 8, 16
+OP_EMBEDDING_BWD, OP_BLOCK_NORM_BWD, OP_GRAD_NORM = 5, 6, 7
+DEV_BAD_BLOCK, DEV_BAD_TARGET, DEV_WAIT_EXPIRED, DEV_BAD_POSITION, DEV_BAD_CONTEXT, DEV_BAD_TOKEN = 1, 2, 4, 8, 16, 32
 
 _lib = None
 _native = None
@@ -72,13 +73,20 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.tik_attn_train_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, f32,
                                        vp, sz, vp]
     lib.tik_token_logprob.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, f32, vp, sz, vp]
+    lib.tik_embedding.argtypes = [vp, vp, vp, vp, f32, i64, i32, i32, vp]
+    lib.tik_embedding_bwd.argtypes = [vp, vp, vp, vp, i32, i32, f32, i64, i32, i32, vp, sz, vp]
+    lib.tik_block_norm.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, f32, i64, i32, vp]
+    lib.tik_block_norm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, f32, vp, vp, vp, vp, vp, i64, i32, vp, sz, vp]
+    lib.tik_grad_norm.argtypes = [vp, vp, vp, vp, i32, vp, vp, sz, vp]
+    lib.tik_grad_clip.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp, i32, vp, sz, vp]
     lib.tik_attn_decode_static.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                            i32, f32, vp, vp]
     lib.tik_attn_decode_static.restype = i32
     for name in ("tik_create", "tik_destroy", "tik_device_status", "tik_attn_train_fwd",
                  "tik_kv_cache_write", "tik_attn_prefill", "tik_attn_decode", "tik_token_logprob",
                  "tik_qk_norm_rope_kv_write", "tik_rmsnorm", "tik_swiglu", "tik_linear",
-                 "tik_attn_train_bwd"):
+                 "tik_attn_train_bwd", "tik_embedding", "tik_embedding_bwd", "tik_block_norm", "tik_block_norm_bwd",
+                 "tik_grad_norm", "tik_grad_clip"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -209,6 +217,46 @@ def tik_token_logprob(hidden, lm_head, target_ids, inv_temperature: float = 1.0,
                       lse: Optional[torch.Tensor] = None):
     """hidden [T,H], lm_head [V,H] bf16, target_ids int32 [T] -> logprob fp32 [T]."""
     return (_native or _load_native()).token_logprob(hidden, lm_head, target_ids, inv_temperature, ws, logprob, lse)
+
+
+def tik_embedding(ids, table, scale: float = 1.0, y: Optional[torch.Tensor] = None):
+    """scale * table[ids]: ids int32 [T], table [V,H] bf16 -> y [T,H].  Ids outside [0,V): zeros and DEV_BAD_TOKEN."""
+    return (_native or _load_native()).embedding(ids, table, scale, y)
+
+
+def tik_embedding_bwd(d_y, ids, vocab: int, scale: float = 1.0, d_table: Optional[torch.Tensor] = None,
+                      accumulate: bool = False, ws: Optional[torch.Tensor] = None):
+    """Gradient of tik_embedding with respect to the table: d_y [T,H] bf16, ids int32 [T] -> d_table [vocab,H] (bf16, or the
+    bf16 or fp32 tensor passed).  accumulate: added to d_table, whose other rows are left alone.  Deterministic."""
+    return (_native or _load_native()).embedding_bwd(d_y, ids, vocab, scale, d_table, bool(accumulate), ws)
+
+
+def tik_block_norm(x, residual, weight, eps: float, post_weight=None, gate=None, branch_scale: float = 1.0,
+                   s: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
+    """The step between two blocks: s = residual + branch_scale * gate * norm(x; post_weight), y = norm(s; weight), all [T,H]
+    bf16.  post_weight, gate ([H] per channel or [T,1] per token) and weight may be None (no norm of x, no gate, no y).
+    Returns (y, s); s may be residual itself (in place)."""
+    return (_native or _load_native()).block_norm(x, residual, weight, eps, post_weight, gate, branch_scale, s, y)
+
+
+def tik_block_norm_bwd(d_y, d_s, x, s, weight, eps: float, post_weight=None, gate=None, branch_scale: float = 1.0,
+                       ws: Optional[torch.Tensor] = None):
+    """Backward of tik_block_norm (x, s: its input and output; x None: of tik_rmsnorm(s, weight)).  d_s None: zeros; d_y None
+    where weight is.  Returns (d_x, d_residual, d_weight, d_post_weight, d_gate), fp32 for the last three, None for
+    what is absent.  Deterministic."""
+    return (_native or _load_native()).block_norm_bwd(d_y, d_s, x, s, weight, eps, post_weight, gate, branch_scale, ws)
+
+
+def tik_grad_norm(grads, norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """sqrt of the sum of squares over a list of contiguous bf16 / fp32 tensors -> norm fp32 [1] (device)."""
+    return (_native or _load_native()).grad_norm(grads, norm, ws)
+
+
+def tik_grad_clip(grads, max_norm: float, norm: Optional[torch.Tensor] = None, out=None,
+                  ws: Optional[torch.Tensor] = None):
+    """grads *= max_norm / norm where max_norm < norm < inf, in place or into the tensors of `out`; returns norm.  norm: None =
+    computed here; a tensor fp32 [1] = taken from there (a sharded trainer's combined norm)."""
+    return (_native or _load_native()).grad_clip(grads, max_norm, norm, out, ws)
 
 
 STATIC_SCRATCH_BYTES = 8 << 20

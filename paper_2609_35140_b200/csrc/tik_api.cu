@@ -192,6 +192,13 @@ int tik_selftest_host(void) {
     if (once.run(ok_step, DeviceOnce::MAX_DEVICES + 5) != cudaSuccess || runs != 5) return 8;
     return 0;
 }
+tik_status tik_selftest_context(tik_ctx** out, int sm_count) {
+    if (!out) return TIK_ERR_INVALID_ARG;
+    *out = new (std::nothrow) tik_ctx();
+    if (!*out) return TIK_ERR_CUDA;
+    (*out)->sm_count = sm_count;
+    return TIK_OK;
+}
 int tik_selftest_linear(int64_t T, int K, int N, int sm_count, int* ctas, int* cols) {
     LinearParams p{};
     p.T = T;
@@ -228,7 +235,6 @@ const char* tik_contract_id(void) { return TIK_CONTRACT_ID; }
 size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d, int64_t max_ctx, int H,
                            int V) {
     (void)Hkv;
-    (void)H;
     if (op == TIK_OP_ATTN_TRAIN_FWD || op == TIK_OP_ATTN_PREFILL) {
         // rows_or_batch = number of sequences S, max_ctx = the host's bound on a sequence's positions
         if (rows_or_batch <= 0 || max_ctx <= 0 || !attn_persist_supported(rows_or_batch, max_ctx)) return 0;
@@ -251,6 +257,9 @@ size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d
         if (rows_or_batch <= 0) return 0;
         return static_cast<size_t>(rows_or_batch) * Hq * sizeof(float);
     }
+    if (op == TIK_OP_EMBEDDING_BWD) return rows_or_batch > 0 && H > 0 && V > 0 ? embed_bwd_bytes(rows_or_batch, V, H) : 0;
+    if (op == TIK_OP_BLOCK_NORM_BWD) return rows_or_batch > 0 && H > 0 ? block_norm_bwd_bytes(rows_or_batch, H) : 0;
+    if (op == TIK_OP_GRAD_NORM) return rows_or_batch > 0 ? grad_norm_bytes(rows_or_batch) : 0;
     return 0;
 }
 
@@ -737,6 +746,198 @@ tik_status tik_linear(tik_ctx* ctx, const void* x, const void* weight, void* y, 
     p.a_rows = a_rows;
     cudaError_t e = launch_linear(tmA, tmB, tmY, p, c.pair, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_linear");
+}
+
+tik_status tik_embedding(tik_ctx* ctx, const int32_t* ids, const void* table, void* y, float scale, int64_t T, int V,
+                         int H, void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    if (T < 0 || V <= 0 || H <= 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative or zero size");
+    if (!std::isfinite(scale)) return fail(ctx, TIK_ERR_INVALID_ARG, "scale must be finite");
+    if (H % 8 != 0) return fail(ctx, TIK_ERR_UNSUPPORTED, "H must be a multiple of 8");
+    if (T == 0) return TIK_OK;
+    if (!ids || !table || !y) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (!aligned16(table) || !aligned16(y)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    if (T >= (1ll << 31)) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31");
+    EmbedParams p{};
+    p.ids = ids;
+    p.table = static_cast<const __nv_bfloat16*>(table);
+    p.y = static_cast<__nv_bfloat16*>(y);
+    p.scale = scale;
+    p.T = T;
+    p.V = V;
+    p.H = H;
+    p.dev_status = ctx->dev_status;
+    cudaError_t e = launch_embed(p, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_embedding");
+}
+
+tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, void* d_table, int table_dtype,
+                             int accumulate, float scale, int64_t T, int V, int H, void* ws, size_t ws_bytes,
+                             void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    if (T < 0 || V <= 0 || H <= 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative or zero size");
+    if (!std::isfinite(scale)) return fail(ctx, TIK_ERR_INVALID_ARG, "scale must be finite");
+    if (table_dtype != TIK_DTYPE_BF16 && table_dtype != TIK_DTYPE_FP32) return fail(ctx, TIK_ERR_INVALID_ARG, "unknown element type");
+    if (H % 8 != 0) return fail(ctx, TIK_ERR_UNSUPPORTED, "H must be a multiple of 8");
+    if (T == 0 && accumulate) return TIK_OK;
+    if (!d_table || (T > 0 && (!d_y || !ids))) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (!aligned16(d_y) || !aligned16(d_table) || !aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    if (T >= (1ll << 30)) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^30");
+    if (V >= (1 << 30)) return fail(ctx, TIK_ERR_UNSUPPORTED, "V must be < 2^30");
+    const size_t need = tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, 0, 0, 0, 0, H, V);
+    if (need > 0 && (!ws || ws_bytes < need)) return fail(ctx, TIK_ERR_WORKSPACE, "embedding gradient workspace too small");
+    EmbedParams p{};
+    p.ids = ids;
+    p.d_y = static_cast<const __nv_bfloat16*>(d_y);
+    p.d_table = d_table;
+    p.fp32 = table_dtype == TIK_DTYPE_FP32;
+    p.accumulate = accumulate != 0;
+    p.scale = scale;
+    p.T = T;
+    p.V = V;
+    p.H = H;
+    p.dev_status = ctx->dev_status;
+    cudaError_t e = launch_embed_bwd(p, ws, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_embedding_bwd");
+}
+
+// what both directions of the step between two blocks ask of their arguments
+static tik_status check_block_norm(tik_ctx* ctx, const void* post_weight, const void* gate, int gate_kind, float branch_scale,
+                                   const void* weight, float eps, int64_t T, int H) {
+    if (T < 0 || H <= 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative or zero size");
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(ctx, TIK_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    if (!std::isfinite(branch_scale)) return fail(ctx, TIK_ERR_INVALID_ARG, "branch_scale must be finite");
+    if (gate_kind != TIK_GATE_NONE && gate_kind != TIK_GATE_CHANNEL && gate_kind != TIK_GATE_TOKEN)
+        return fail(ctx, TIK_ERR_INVALID_ARG, "unknown gate kind");
+    if ((gate_kind != TIK_GATE_NONE) != (gate != nullptr) && (T > 0 || gate)) return fail(ctx, TIK_ERR_INVALID_ARG, "gate and gate_kind disagree");
+    if (H % 8 != 0 || H > 8192) return fail(ctx, TIK_ERR_UNSUPPORTED, "H must be a multiple of 8 and <= 8192");
+    if (!aligned16(post_weight) || !aligned16(weight) || (gate_kind == TIK_GATE_CHANNEL && !aligned16(gate)))
+        return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    if (T >= (1ll << 31)) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31");
+    return TIK_OK;
+}
+
+tik_status tik_block_norm(tik_ctx* ctx, const void* x, const void* residual, const void* post_weight, const void* gate,
+                          int gate_kind, float branch_scale, const void* weight, void* s, void* y, float eps, int64_t T,
+                          int H, void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    tik_status st = check_block_norm(ctx, post_weight, gate, gate_kind, branch_scale, weight, eps, T, H);
+    if (st != TIK_OK) return st;
+    if (T == 0) return TIK_OK;
+    if (!x || !residual || !s) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (!weight != !y) return fail(ctx, TIK_ERR_INVALID_ARG, "weight and y go together");
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(s) || !aligned16(y))
+        return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    BlockNormParams p{};
+    p.x = static_cast<const __nv_bfloat16*>(x);
+    p.residual = static_cast<const __nv_bfloat16*>(residual);
+    p.post_weight = static_cast<const __nv_bfloat16*>(post_weight);
+    p.gate = static_cast<const __nv_bfloat16*>(gate);
+    p.weight = static_cast<const __nv_bfloat16*>(weight);
+    p.s = static_cast<__nv_bfloat16*>(s);
+    p.y = static_cast<__nv_bfloat16*>(y);
+    p.gate_kind = gate_kind;
+    p.branch_scale = branch_scale;
+    p.eps = eps;
+    p.T = T;
+    p.H = H;
+    cudaError_t e = launch_block_norm(p, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_block_norm");
+}
+
+tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, const void* x, const void* s,
+                              const void* post_weight, const void* gate, int gate_kind, float branch_scale,
+                              const void* weight, float eps, void* d_x, void* d_residual, float* d_weight,
+                              float* d_post_weight, float* d_gate, int64_t T, int H, void* ws, size_t ws_bytes,
+                              void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    tik_status st = check_block_norm(ctx, post_weight, gate, gate_kind, branch_scale, weight, eps, T, H);
+    if (st != TIK_OK) return st;
+    if (!weight != !d_weight || !post_weight != !d_post_weight) return fail(ctx, TIK_ERR_INVALID_ARG, "a weight and its gradient go together");
+    if (T > 0) {
+        if (!s || !d_residual || (!d_y && !d_s)) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+        if (!d_y != !weight) return fail(ctx, TIK_ERR_INVALID_ARG, "d_y and weight go together");
+        if (!x != !d_x) return fail(ctx, TIK_ERR_INVALID_ARG, "x and d_x go together");
+        if (!x && (post_weight || gate)) return fail(ctx, TIK_ERR_INVALID_ARG, "post_weight and gate need x");
+        if (!gate != !d_gate) return fail(ctx, TIK_ERR_INVALID_ARG, "gate and d_gate go together");
+    }
+    if (!aligned16(d_y) || !aligned16(d_s) || !aligned16(x) || !aligned16(s) || !aligned16(d_x) || !aligned16(d_residual) || !aligned16(ws))
+        return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    const size_t need = tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, 0, 0, 0, 0, H, 0);
+    if (need > 0 && (!ws || ws_bytes < need)) return fail(ctx, TIK_ERR_WORKSPACE, "block norm gradient workspace too small");
+    BlockNormParams p{};
+    p.d_y = static_cast<const __nv_bfloat16*>(d_y);
+    p.d_s = static_cast<const __nv_bfloat16*>(d_s);
+    p.x = static_cast<const __nv_bfloat16*>(x);
+    p.s = static_cast<__nv_bfloat16*>(const_cast<void*>(s));
+    p.post_weight = static_cast<const __nv_bfloat16*>(post_weight);
+    p.gate = static_cast<const __nv_bfloat16*>(gate);
+    p.weight = static_cast<const __nv_bfloat16*>(weight);
+    p.gate_kind = gate_kind;
+    p.branch_scale = branch_scale;
+    p.eps = eps;
+    p.T = T;
+    p.H = H;
+    p.d_x = static_cast<__nv_bfloat16*>(d_x);
+    p.d_residual = static_cast<__nv_bfloat16*>(d_residual);
+    p.d_weight = d_weight;
+    p.d_post_weight = d_post_weight;
+    p.d_gate = d_gate;
+    p.part = static_cast<float*>(ws);
+    cudaError_t e = launch_block_norm_bwd(p, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_block_norm_bwd");
+}
+
+static tik_status check_grads(tik_ctx* ctx, const void* const* grads, const int64_t* numel, const int* dtypes, int n) {
+    if (n < 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative size");
+    if (n > 0 && (!grads || !numel || !dtypes)) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (numel[i] < 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative size");
+        if (dtypes[i] != TIK_DTYPE_BF16 && dtypes[i] != TIK_DTYPE_FP32) return fail(ctx, TIK_ERR_INVALID_ARG, "unknown element type");
+        if (numel[i] > 0 && !grads[i]) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+        if (numel[i] >= (1ll << 40) || (total += numel[i]) >= (1ll << 40))
+            return fail(ctx, TIK_ERR_UNSUPPORTED, "the tensors must have less than 2^40 elements");
+        if (reinterpret_cast<uintptr_t>(grads[i]) & (dtypes[i] == TIK_DTYPE_FP32 ? 3u : 1u))
+            return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
+    }
+    return TIK_OK;
+}
+
+tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* numel, const int* dtypes, int n,
+                         float* norm, void* ws, size_t ws_bytes, void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    tik_status st = check_grads(ctx, grads, numel, dtypes, n);
+    if (st != TIK_OK) return st;
+    if (!norm) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (!aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    const size_t need = tik_workspace_bytes(TIK_OP_GRAD_NORM, n, 0, 0, 0, 0, 0, 0);
+    if (need > 0 && (!ws || ws_bytes < need)) return fail(ctx, TIK_ERR_WORKSPACE, "gradient norm workspace too small");
+    cudaError_t e = launch_grad_norm(grads, numel, dtypes, n, norm, static_cast<double*>(ws), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_grad_norm");
+}
+
+tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes,
+                         int n, float max_norm, float* norm, int norm_given, void* ws, size_t ws_bytes, void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    tik_status st = check_grads(ctx, grads, numel, dtypes, n);
+    if (st != TIK_OK) return st;
+    if (!(max_norm > 0.0f) || !std::isfinite(max_norm)) return fail(ctx, TIK_ERR_INVALID_ARG, "max_norm must be finite and > 0");
+    if (!norm) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    for (int i = 0; out && i < n; ++i) {
+        if (numel[i] > 0 && !out[i]) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+        if (reinterpret_cast<uintptr_t>(out[i]) & (dtypes[i] == TIK_DTYPE_FP32 ? 3u : 1u))
+            return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
+    }
+    bool no_memory = false;
+    if (grad_ranges_overlap(grads, out, numel, dtypes, n, &no_memory))
+        return fail(ctx, TIK_ERR_INVALID_ARG, no_memory ? "out of host memory" : "tensors to be written overlap");
+    if (!aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    const size_t need = norm_given ? 0 : tik_workspace_bytes(TIK_OP_GRAD_NORM, n, 0, 0, 0, 0, 0, 0);
+    if (need > 0 && (!ws || ws_bytes < need)) return fail(ctx, TIK_ERR_WORKSPACE, "gradient norm workspace too small");
+    cudaError_t e = launch_grad_clip(grads, out, numel, dtypes, n, max_norm, norm, norm_given != 0, static_cast<double*>(ws),
+                                     static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_grad_clip");
 }
 
 tik_status tik_attn_train_bwd(tik_ctx* ctx, const void* q, const void* k, const void* v, const void* o,

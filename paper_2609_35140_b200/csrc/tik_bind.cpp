@@ -18,6 +18,7 @@
 
 #include <mutex>
 #include <string>
+#include <vector>
 
 #include "../../include/tik.h"
 
@@ -343,6 +344,230 @@ PyObject* linear(Args a) {
     return wrap(y_in, made);
 }
 
+// a tensor of the current device
+const at::Tensor& on(int device, const at::Tensor& t) {
+    if (!t.is_cuda() || t.get_device() != device) raise_tik("tensors must be on the current CUDA device");
+    return t;
+}
+const at::Tensor* on(int device, const at::Tensor* t) { return t ? &on(device, *t) : nullptr; }
+void want_sizes(const at::Tensor& t, at::IntArrayRef sizes, const char* what) {
+    if (t.sizes() != sizes) raise(PyExc_ValueError, std::string(what) + " has the wrong shape");
+}
+void want_sizes(const at::Tensor* t, at::IntArrayRef sizes, const char* what) {
+    if (t) want_sizes(*t, sizes, what);
+}
+
+PyObject* embedding(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const at::Tensor &ids = on(dev, a.tensor()), &table = on(dev, a.tensor());
+    const float scale = a.real();
+    const at::Tensor* y_in = on(dev, a.opt());
+    want_rank(ids, 1);
+    want_rank(table, 2);
+    at::Tensor made;
+    const int64_t T = ids.size(0);
+    const int V = dim(table, 0), H = dim(table, 1);
+    want_sizes(y_in, {T, H}, "y");
+    const at::Tensor& y = out_or(y_in, made, {T, H}, at::kBFloat16, table);
+    void *tp = bf(table), *yp = bf(y), *st = stream();
+    const int32_t* ip = i32(ids);
+    check(unlocked([&] { return tik_embedding(ctx, ip, tp, yp, scale, T, V, H, st); }), ctx);
+    return wrap(y_in, made);
+}
+
+int element_type(const at::Tensor& t) {
+    if (t.scalar_type() == at::kBFloat16) return TIK_DTYPE_BF16;
+    if (t.scalar_type() == at::kFloat) return TIK_DTYPE_FP32;
+    raise_tik(std::string("expected bf16 or fp32, got ") + at::toString(t.scalar_type()));
+}
+
+PyObject* embedding_bwd(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const at::Tensor &dy = on(dev, a.tensor()), &ids = on(dev, a.tensor());
+    const int V = a.int32();
+    const float scale = a.real();
+    const at::Tensor* table_in = on(dev, a.opt());
+    const int accumulate = a.int32();
+    const at::Tensor* ws_in = on(dev, a.opt());
+    want_rank(dy, 2);
+    const int64_t T = dy.size(0);
+    const int H = dim(dy, 1);
+    want_sizes(ids, {T}, "ids");
+    if (V <= 0) raise(PyExc_ValueError, "vocab must be positive");
+    want_sizes(table_in, {V, H}, "d_table");
+    if (accumulate && !table_in) raise(PyExc_ValueError, "accumulate needs d_table");
+    const Scratch ws = sized_ws(ws_in, tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, 0, 0, 0, 0, H, V), dy);
+    at::Tensor made;
+    const at::Tensor& table = out_or(table_in, made, {V, H}, at::kBFloat16, dy);
+    const int type = element_type(table);
+    void *gp = bf(dy), *tp = ptr(table), *st = stream();
+    const int32_t* ip = i32(ids);
+    check(unlocked([&] { return tik_embedding_bwd(ctx, gp, ip, tp, type, accumulate, scale, T, V, H, ws.p, ws.bytes, st); }), ctx);
+    return wrap(table_in, made);
+}
+
+// TIK_GATE_* of a gate [H] or [T,1]
+int gate_kind(const at::Tensor* gate, int64_t T, int64_t H) {
+    if (!gate) return TIK_GATE_NONE;
+    if (gate->dim() == 2) {
+        want_sizes(*gate, {T, 1}, "gate");
+        return TIK_GATE_TOKEN;
+    }
+    want_sizes(*gate, {H}, "gate");
+    return TIK_GATE_CHANNEL;
+}
+
+PyObject* block_norm(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const at::Tensor &x = on(dev, a.tensor()), &res = on(dev, a.tensor());
+    const at::Tensor* w = on(dev, a.opt());
+    const float eps = a.real();
+    const at::Tensor *post = on(dev, a.opt()), *gate = on(dev, a.opt());
+    const float branch_scale = a.real();
+    const at::Tensor *s_in = on(dev, a.opt()), *y_in = on(dev, a.opt());
+    want_rank(x, 2);
+    const int64_t T = x.size(0);
+    const int H = dim(x, 1), kind = gate_kind(gate, T, H);
+    want_sizes(res, {T, H}, "residual");
+    want_sizes(w, {H}, "weight");
+    want_sizes(post, {H}, "post_weight");
+    want_sizes(s_in, {T, H}, "s");
+    want_sizes(y_in, {T, H}, "y");
+    if (y_in && !w) raise(PyExc_ValueError, "y needs weight");
+    at::Tensor made_s, made_y;
+    const at::Tensor& s = out_or(s_in, made_s, {T, H}, at::kBFloat16, x);
+    const at::Tensor* y = w ? &out_or(y_in, made_y, {T, H}, at::kBFloat16, x) : nullptr;
+    void *xp = bf(x), *rp = bf(res), *wp = bf(w), *pp = bf(post), *gp = bf(gate), *sp = bf(s), *yp = bf(y), *st = stream();
+    check(unlocked([&] { return tik_block_norm(ctx, xp, rp, pp, gp, kind, branch_scale, wp, sp, yp, eps, T, H, st); }), ctx);
+    PyObject* a0 = Py_None;
+    if (w) a0 = wrap(y_in, made_y);
+    else Py_INCREF(Py_None);
+    PyObject* a1 = wrap(s_in, made_s);
+    return Py_BuildValue("(NN)", a0, a1);
+}
+
+PyObject* block_norm_bwd(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const at::Tensor *dy = on(dev, a.opt()), *ds = on(dev, a.opt()), *x = on(dev, a.opt());
+    const at::Tensor& s = on(dev, a.tensor());
+    const at::Tensor* w = on(dev, a.opt());
+    const float eps = a.real();
+    const at::Tensor *post = on(dev, a.opt()), *gate = on(dev, a.opt());
+    const float branch_scale = a.real();
+    const at::Tensor* ws_in = on(dev, a.opt());
+    want_rank(s, 2);
+    const int64_t T = s.size(0);
+    const int H = dim(s, 1), kind = gate_kind(gate, T, H);
+    want_sizes(dy, {T, H}, "d_y");
+    want_sizes(ds, {T, H}, "d_s");
+    want_sizes(x, {T, H}, "x");
+    want_sizes(w, {H}, "weight");
+    want_sizes(post, {H}, "post_weight");
+    if (!dy != !w) raise(PyExc_ValueError, "d_y and weight go together");
+    if (!dy && !ds) raise(PyExc_ValueError, "neither d_y nor d_s");
+    if (!x && (post || gate)) raise(PyExc_ValueError, "post_weight and gate need x");
+    const Scratch ws = sized_ws(ws_in, tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, 0, 0, 0, 0, H, 0), s);
+    at::Tensor made[5];
+    made[1] = empty({T, H}, at::kBFloat16, s);
+    if (x) made[0] = empty({T, H}, at::kBFloat16, s);
+    if (w) made[2] = empty({H}, at::kFloat, s);
+    if (post) made[3] = empty({H}, at::kFloat, s);
+    if (gate) made[4] = empty(gate->sizes(), at::kFloat, s);
+    auto opt = [](const at::Tensor& t) { return t.defined() ? &t : nullptr; };
+    void *dyp = bf(dy), *dsp = bf(ds), *xp = bf(x), *sp = bf(s), *wp = bf(w), *pp = bf(post), *gp = bf(gate), *dxp = bf(opt(made[0])),
+         *drp = bf(made[1]), *st = stream();
+    float *dwp = f32(opt(made[2])), *dpp = f32(opt(made[3])), *dgp = f32(opt(made[4]));
+    check(unlocked([&] { return tik_block_norm_bwd(ctx, dyp, dsp, xp, sp, pp, gp, kind, branch_scale, wp, eps, dxp, drp, dwp, dpp, dgp,
+                                                   T, H, ws.p, ws.bytes, st); }), ctx);
+    PyObject* out[5];
+    for (int i = 0; i < 5; ++i) {
+        out[i] = Py_None;
+        if (made[i].defined()) out[i] = THPVariable_Wrap(made[i]);
+        else Py_INCREF(Py_None);
+    }
+    return Py_BuildValue("(NNNNN)", out[0], out[1], out[2], out[3], out[4]);
+}
+
+// A Python list or tuple of gradients as the arrays of the C interface.
+struct GradArgs {
+    std::vector<void*> ptrs;
+    std::vector<int64_t> numel;
+    std::vector<int> types;
+    int n = 0;
+    GradArgs(PyObject* list, int device) {
+        if (!PyList_Check(list) && !PyTuple_Check(list)) raise(PyExc_TypeError, "expected a list or tuple of tensors");
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(list);
+        if (count > INT32_MAX) raise(PyExc_OverflowError, "too many tensors");
+        n = static_cast<int>(count);
+        ptrs.reserve(n);
+        numel.reserve(n);
+        types.reserve(n);
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            PyObject* o = PySequence_Fast_GET_ITEM(list, i);
+            if (!THPVariable_Check(o)) raise(PyExc_TypeError, std::string("expected a tensor, got ") + Py_TYPE(o)->tp_name);
+            const at::Tensor& t = on(device, THPVariable_Unpack(o));
+            types.push_back(element_type(t));
+            ptrs.push_back(ptr(t));
+            numel.push_back(t.numel());
+        }
+    }
+};
+
+// the norm's own tensor: given or made
+const at::Tensor& norm_of(const at::Tensor* given, at::Tensor& made, int device) {
+    if (given) {
+        want_sizes(*given, {1}, "norm");
+        return *given;
+    }
+    return made = at::detail::empty_cuda({1}, at::kFloat, at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)), std::nullopt);
+}
+Scratch grad_ws(const at::Tensor* given, int n, const at::Tensor& like) {
+    return sized_ws(given, tik_workspace_bytes(TIK_OP_GRAD_NORM, n, 0, 0, 0, 0, 0, 0), like);
+}
+
+PyObject* grad_norm(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const GradArgs g(a.next(), dev);
+    const at::Tensor *norm_in = on(dev, a.opt()), *ws_in = on(dev, a.opt());
+    at::Tensor made;
+    const at::Tensor& norm = norm_of(norm_in, made, dev);
+    const Scratch ws = grad_ws(ws_in, g.n, norm);
+    float* np = f32(&norm);
+    void* st = stream();
+    check(unlocked([&] { return tik_grad_norm(ctx, g.ptrs.data(), g.numel.data(), g.types.data(), g.n, np, ws.p, ws.bytes, st); }), ctx);
+    return wrap(norm_in, made);
+}
+
+PyObject* grad_clip(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const GradArgs g(a.next(), dev);
+    const float max_norm = a.real();
+    const at::Tensor* norm_in = on(dev, a.opt());
+    PyObject* out_list = a.next();
+    const at::Tensor* ws_in = on(dev, a.opt());
+    std::vector<void*> to;
+    if (out_list != Py_None) {
+        GradArgs out(out_list, dev);
+        if (out.numel != g.numel || out.types != g.types) raise(PyExc_ValueError, "out has other types or sizes than grads");
+        to.swap(out.ptrs);
+    }
+    at::Tensor made;
+    const at::Tensor& norm = norm_of(norm_in, made, dev);
+    Scratch ws;
+    if (!norm_in || ws_in) ws = grad_ws(ws_in, g.n, norm);
+    float* np = f32(&norm);
+    void* st = stream();
+    check(unlocked([&] { return tik_grad_clip(ctx, g.ptrs.data(), out_list != Py_None ? to.data() : nullptr, g.numel.data(), g.types.data(),
+                                              g.n, max_norm, np, norm_in != nullptr, ws.p, ws.bytes, st); }), ctx);
+    return wrap(norm_in, made);
+}
+
 PyObject* attn_prefill(Args a) {
     tik_ctx* ctx = context(current_device());
     const at::Tensor& q = a.tensor();
@@ -480,7 +705,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {
     TIK_DEF(init), TIK_DEF(context_handle), TIK_DEF(attn_train_fwd), TIK_DEF(attn_train_bwd), TIK_DEF(kv_cache_write),
     TIK_DEF(qk_norm_rope_kv_write), TIK_DEF(rmsnorm), TIK_DEF(swiglu), TIK_DEF(linear), TIK_DEF(attn_prefill),
-    TIK_DEF(attn_prefill_kv), TIK_DEF(attn_decode), TIK_DEF(attn_decode_static), TIK_DEF(token_logprob),
+    TIK_DEF(attn_prefill_kv), TIK_DEF(attn_decode), TIK_DEF(attn_decode_static), TIK_DEF(token_logprob), TIK_DEF(embedding),
+    TIK_DEF(embedding_bwd), TIK_DEF(block_norm), TIK_DEF(block_norm_bwd), TIK_DEF(grad_norm), TIK_DEF(grad_clip),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_tikbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -107,6 +107,20 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return *reinterpret_cast<uint32_t*>(&t);
 }
 
+// eight bf16 <-> eight fp32
+__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
+    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(r[i] << 16);              // bf16 -> fp32 is exact
+        f[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                      pack_bf16x2(f[6], f[7]));
+}
+
 // Two-wide forms of the same IEEE operations (fma.rn / add.rn on f32 pairs): identical bits to
 // the scalar intrinsics, half the issue slots.
 __device__ __forceinline__ void fma_rn_x2(float& d0, float& d1, float a0, float a1, float b, float c) {

@@ -15,19 +15,6 @@ namespace tik {
 constexpr int HN_THREADS = 128;
 constexpr unsigned SW_VEC_MAX = 0xfffff000u;      // SwiGLU output vectors per launch
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(r[i] << 16);              // bf16 -> fp32 is exact
-        f[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ uint4 pack8(const float* f) {
-    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
-                      pack_bf16x2(f[6], f[7]));
-}
-
 // One CTA per row; NV = 16-byte vectors per thread (H <= 1024 * NV).
 template <int NV, bool RESIDUAL>
 __global__ void __launch_bounds__(HN_THREADS) rmsnorm_kernel(const NormParams p) {

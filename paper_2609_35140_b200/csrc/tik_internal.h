@@ -204,6 +204,58 @@ struct NormParams {
 cudaError_t launch_rmsnorm(const NormParams& p, cudaStream_t stream);
 cudaError_t launch_swiglu(const void* gate_up, void* out, long long T, int I, cudaStream_t stream);
 
+struct EmbedParams {
+    const int32_t* ids;          // [T]
+    const __nv_bfloat16* table;  // [V][H] (lookup)
+    __nv_bfloat16* y;            // [T][H] (lookup)
+    const __nv_bfloat16* d_y;    // [T][H] (gradient)
+    void* d_table;               // [V][H] bf16 or fp32 (gradient)
+    int fp32, accumulate;
+    float scale;
+    long long T;
+    int V, H;
+    int32_t *sorted, *order;     // scratch [T]: ids in ascending order (V for those out of range), their tokens
+    int* dev_status;
+};
+size_t embed_bwd_bytes(int64_t T, int V, int H);
+cudaError_t launch_embed(const EmbedParams& p, cudaStream_t stream);
+cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream);
+
+// The step between two blocks (tik_block_norm) and its gradient.
+constexpr int GATE_CHANNEL = 1, GATE_TOKEN = 2;
+struct BlockNormParams {
+    const __nv_bfloat16* x;      // [T][H] block output (gradient: or null)
+    const __nv_bfloat16* residual;
+    const __nv_bfloat16* post_weight;    // [H] or null
+    const __nv_bfloat16* gate;   // [H], [T] or null
+    const __nv_bfloat16* weight; // [H] or null
+    __nv_bfloat16* s;            // [T][H]
+    __nv_bfloat16* y;            // [T][H] or null
+    int gate_kind;
+    float branch_scale, eps;
+    long long T;
+    int H;
+    // gradient only
+    const __nv_bfloat16* d_y;    // [T][H] or null
+    const __nv_bfloat16* d_s;    // [T][H] or null
+    __nv_bfloat16* d_x;          // [T][H] or null
+    __nv_bfloat16* d_residual;   // [T][H]
+    float *d_weight, *d_post_weight, *d_gate;
+    float* part;                 // scratch [CTAs][2][H]: sums over a CTA's tokens
+};
+size_t block_norm_bwd_bytes(int64_t T, int H);
+cudaError_t launch_block_norm(const BlockNormParams& p, cudaStream_t stream);
+cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream);
+
+// Gradient norm and clipping over host lists of n tensors; n <= 0 is fine.  norm_known: *norm is read, else written.
+size_t grad_norm_bytes(int64_t n);
+cudaError_t launch_grad_norm(const void* const* grads, const int64_t* numel, const int* dtypes, int n, float* norm, double* part,
+                             cudaStream_t stream);
+cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, float max_norm,
+                             float* norm, bool norm_known, double* part, cudaStream_t stream);
+// whether two of the ranges that a clip writes, or one of them and another range that it reads, share a byte (or no memory)
+bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, bool* no_memory);
+
 struct LinearParams {
     __nv_bfloat16* y;            // [T][N]
     int64_t T;

@@ -16,6 +16,7 @@ constexpr int TIK_DEV_BAD_TARGET = 2;     // target id outside [0, V)
 constexpr int TIK_DEV_WAIT_EXPIRED = 4;   // a bounded wait ran out
 constexpr int TIK_DEV_BAD_POSITION = 8;   // token position outside the cos/sin table
 constexpr int TIK_DEV_BAD_CONTEXT = 16;   // decode: ctx_lens[b] above the host's max_ctx_len
+constexpr int TIK_DEV_BAD_TOKEN = 32;     // embedding: token id outside [0, V)
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
