@@ -796,6 +796,7 @@ tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, 
     p.T = T;
     p.V = V;
     p.H = H;
+    p.sm_count = ctx->sm_count;
     p.dev_status = ctx->dev_status;
     cudaError_t e = launch_embed_bwd(p, ws, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_embedding_bwd");

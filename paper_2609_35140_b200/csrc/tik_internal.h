@@ -214,12 +214,16 @@ struct EmbedParams {
     float scale;
     long long T;
     int V, H;
-    int32_t *sorted, *order;     // scratch [T]: ids in ascending order (V for those out of range), their tokens
+    int32_t* order;              // scratch [T]: tokens by id, equal ids by position
+    uint4* place;                // scratch [T]: what begins at a place of that order (tik_embed.cu)
+    uint2* keys[2];              // scratch [T] each: (id, token) between the passes of the sort
+    float* part;                 // scratch [2 (T / 32 + 1)][H]: sums of a long run's pieces
+    int sm_count;
     int* dev_status;
 };
 size_t embed_bwd_bytes(int64_t T, int V, int H);
 cudaError_t launch_embed(const EmbedParams& p, cudaStream_t stream);
-cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream);
+cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream);     // fills in the scratch
 
 // The step between two blocks (tik_block_norm) and its gradient.
 constexpr int GATE_CHANNEL = 1, GATE_TOKEN = 2;
