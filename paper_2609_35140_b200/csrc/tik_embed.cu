@@ -57,24 +57,33 @@ __device__ __forceinline__ long long emb_slot(long long place, uint32_t len) {
 __device__ __forceinline__ int emb_key(const EmbedParams& p, int id) { return id >= 0 && id < p.V ? id : p.V; }
 
 // Calls of few tokens: a token's place is the number of tokens before it in the order, counted by comparing all pairs.
-// Lanes are tokens; the warps of a CTA share the tokens that they are compared with.
+// Lanes are tokens; the warps of a CTA share the tokens that they are compared with, from shared memory (out of L2 every
+// load of the chain waits behind the zeros that are being written meanwhile).
 constexpr int EMB_RANK_TOKENS = 4096;
 constexpr int EMB_RANK_WARPS = 8;
 __global__ void __launch_bounds__(EMB_RANK_WARPS * 32) embed_rank_kernel(const EmbedParams p) {
+    __shared__ alignas(16) int keys[EMB_RANK_TOKENS];
     __shared__ int count[EMB_RANK_WARPS][3][32];
     pdl_wait();
     pdl_launch_dependents();
     const int T = static_cast<int>(p.T), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int t = blockIdx.x * 32 + lane;
-    const int mine = t < T ? emb_key(p, p.ids[t]) : -1;
+    const int padded = (T + 4 * EMB_RANK_WARPS - 1) / (4 * EMB_RANK_WARPS) * (4 * EMB_RANK_WARPS);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < padded; i += EMB_RANK_WARPS * 32) keys[i] = i < T ? emb_key(p, p.ids[i]) : 0x7fffffff;
+    __syncthreads();
+    const int t = blockIdx.x * 32 + lane, mine = t < T ? keys[t] : -1;
     int less = 0, same = 0, same_before = 0;
-    const int per = (T + EMB_RANK_WARPS - 1) / EMB_RANK_WARPS, to = min(T, per * (warp + 1));
-#pragma unroll 8
-    for (int i = per * warp; i < to; ++i) {
-        const int k = emb_key(p, p.ids[i]);
-        less += k < mine;
-        same += k == mine;
-        same_before += k == mine && i < t;
+    const int per = padded / EMB_RANK_WARPS;
+#pragma unroll 4
+    for (int i = per * warp; i < per * (warp + 1); i += 4) {
+        const int4 k4 = *reinterpret_cast<const int4*>(keys + i);
+        const int k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            less += k[j] < mine;
+            same += k[j] == mine;
+            same_before += k[j] == mine && i + j < t;
+        }
     }
     count[warp][0][lane] = less;
     count[warp][1][lane] = same;
@@ -100,55 +109,62 @@ __global__ void __launch_bounds__(EMB_RANK_WARPS * 32) embed_rank_kernel(const E
 
 // Other calls: a stable radix sort by one cluster of eight CTAs, whose 256 warps own consecutive stretches of the list.  Per
 // digit: each warp counts its digits, the CTAs exchange their counts through distributed shared memory, and each
-// warp moves its elements, in order, to where the elements before them end.
+// warp moves its elements, in order, to where the elements before them end.  ON_CHIP: the list stays in the CTAs' shared
+// memory between the passes (up to EMB_CHIP_TOKENS), which the zeros written meanwhile do not slow down; else in global memory.
 constexpr int EMB_CLUSTER = 8, EMB_SORT_THREADS = 1024, EMB_SORT_WARPS = EMB_SORT_THREADS / 32;
-constexpr int EMB_BINS = 512;
-constexpr size_t EMB_SORT_SMEM = (EMB_SORT_WARPS * EMB_BINS + EMB_BINS + 32) * sizeof(int);
+constexpr int EMB_BINS = 512, EMB_CHIP_TOKENS = 65536;
+struct EmbedSortSmem {
+    int hist[EMB_SORT_WARPS][EMB_BINS];
+    int total[EMB_BINS], base[EMB_BINS];
+    int warp_sum[EMB_SORT_WARPS];
+    int first_head[EMB_SORT_WARPS], last_head[EMB_SORT_WARPS];
+    int cta_first_head, cta_last_head;
+    uint2 edge;                                              // the CTA's last element
+};
+// elements of a warp's stretch: whole windows of 32
+inline __host__ __device__ int emb_stretch(int T) {
+    return ((T + EMB_CLUSTER * EMB_SORT_WARPS - 1) / (EMB_CLUSTER * EMB_SORT_WARPS) + 31) / 32 * 32;
+}
 
 __device__ __forceinline__ int ld_cluster_int(uint32_t addr) {
     int v;
     asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
-// first place of [0, n) whose key is >= key, found by a whole warp (keys ascending)
-__device__ __forceinline__ int emb_lower_bound(const uint2* keys, int n, uint32_t key, int lane) {
-    int lo = 0, hi = n;                      // keys before lo are < key, keys from hi on are not
-    while (lo < hi) {
-        const int step = (hi - lo + 31) / 32, probe = lo + step * (lane + 1) - 1;
-        const unsigned below = __ballot_sync(0xffffffffu, probe < hi && __ldcg(&keys[probe]).x < key);
-        const int c = __popc(below);
-        hi = min(hi, lo + step * (c + 1) - 1);
-        lo += step * c;
-    }
-    return lo;
+__device__ __forceinline__ void st_cluster_uint2(uint32_t addr, uint2 v) {
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
 }
 
+template <bool ON_CHIP>
 __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const EmbedParams p, int passes, int digit_bits) {
-    extern __shared__ int emb_smem[];
-    int* hist = emb_smem;                                        // [warps][bins]
-    int* total = hist + EMB_SORT_WARPS * EMB_BINS;               // [bins] of this CTA
-    int* warp_sum = total + EMB_BINS;
+    extern __shared__ __align__(16) unsigned char emb_smem[];
+    EmbedSortSmem& sm = *reinterpret_cast<EmbedSortSmem*>(emb_smem);
+    uint2* list = reinterpret_cast<uint2*>(emb_smem + sizeof(EmbedSortSmem));        // ON_CHIP: two buffers of a CTA's stretch
     const int T = static_cast<int>(p.T), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_ctarank();
     pdl_wait();
     pdl_launch_dependents();
     const int bins = 1 << digit_bits;
-    const int per = ((T + EMB_CLUSTER * EMB_SORT_WARPS - 1) / (EMB_CLUSTER * EMB_SORT_WARPS) + 31) / 32 * 32;
-    const long long from = static_cast<long long>(per) * (rank * EMB_SORT_WARPS + warp);
+    const int per = emb_stretch(T), chunk = per * EMB_SORT_WARPS;
+    const long long cta_from = static_cast<long long>(chunk) * rank, from = cta_from + per * warp;
     const int first = static_cast<int>(from < T ? from : T), last = static_cast<int>(from + per < T ? from + per : T);
-    int* mine = hist + warp * EMB_BINS;
+    int* mine = sm.hist[warp];
+    // elements of this CTA's stretch before pass `pass` (pass == passes: sorted)
+    auto element = [&](int pass, int i) {
+        if (pass == 0) return make_uint2(emb_key(p, p.ids[i]), i);
+        if (ON_CHIP) return list[(pass & 1) * chunk + static_cast<int>(i - cta_from)];
+        return __ldcg(&p.keys[pass & 1][i]);
+    };
+    cluster_sync_all();                                      // every CTA runs before any writes to another's shared memory
     for (int pass = 0; pass < passes; ++pass) {
-        const uint2* src = p.keys[(pass + 1) & 1];               // pass 0 reads the ids
-        uint2* dst = p.keys[pass & 1];
         const int shift = pass * digit_bits;
-        auto element = [&](int i) { return pass == 0 ? make_uint2(emb_key(p, p.ids[i]), i) : __ldcg(&src[i]); };
         for (int i = lane; i < bins; i += 32) mine[i] = 0;
         __syncwarp();
         for (int i0 = first; i0 < last; i0 += 32) {
             const int i = i0 + lane;
             const unsigned here = __ballot_sync(0xffffffffu, i < last);
             if (i < last) {
-                const int digit = (element(i).x >> shift) & (bins - 1);
+                const int digit = (element(pass, i).x >> shift) & (bins - 1);
                 const unsigned peers = __match_any_sync(here, digit);
                 if (lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
             }
@@ -156,22 +172,22 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
         }
         __syncthreads();
         int sum = 0;
-        if (tid < bins) {                                        // a bin's counts -> counts of the warps before
+        if (tid < bins) {                                    // a bin's counts -> counts of the warps before
 #pragma unroll
             for (int w = 0; w < EMB_SORT_WARPS; ++w) {
-                const int n = hist[w * EMB_BINS + tid];
-                hist[w * EMB_BINS + tid] = sum;
+                const int n = sm.hist[w][tid];
+                sm.hist[w][tid] = sum;
                 sum += n;
             }
-            total[tid] = sum;
+            sm.total[tid] = sum;
         }
         __syncwarp();
         cluster_sync_all();
-        int before = 0, all = 0;                                 // of the CTAs before, of the cluster
+        int before = 0, all = 0;                             // of the CTAs before, of the cluster
         if (tid < bins) {
 #pragma unroll
             for (uint32_t r = 0; r < EMB_CLUSTER; ++r) {
-                const int n = ld_cluster_int(mapa_cluster(smem_u32(total + tid), r));
+                const int n = ld_cluster_int(mapa_cluster(smem_u32(sm.total + tid), r));
                 before += r < rank ? n : 0;
                 all += n;
             }
@@ -182,47 +198,116 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
             const int n = __shfl_up_sync(0xffffffffu, scan, off);
             if (lane >= off) scan += n;
         }
-        if (lane == 31) warp_sum[warp] = scan;
+        if (lane == 31) sm.warp_sum[warp] = scan;
         __syncthreads();
-        int base = scan - all + before;
-        for (int w = 0; w < warp; ++w) base += warp_sum[w];
-        if (tid < bins) {
+        int below = lane < warp ? sm.warp_sum[lane] : 0;
 #pragma unroll
-            for (int w = 0; w < EMB_SORT_WARPS; ++w) hist[w * EMB_BINS + tid] += base;
-        }
+        for (int off = 16; off >= 1; off >>= 1) below += __shfl_xor_sync(0xffffffffu, below, off);
+        if (tid < bins) sm.base[tid] = scan - all + before + below;
         __syncthreads();
         for (int i0 = first; i0 < last; i0 += 32) {
             const int i = i0 + lane;
             const unsigned here = __ballot_sync(0xffffffffu, i < last);
             if (i < last) {
-                const uint2 e = element(i);
+                const uint2 e = element(pass, i);
                 const int digit = (e.x >> shift) & (bins - 1);
                 const unsigned peers = __match_any_sync(here, digit);
-                const int at = mine[digit] + __popc(peers & ((1u << lane) - 1));
+                const int at = sm.base[digit] + mine[digit] + __popc(peers & ((1u << lane) - 1));
                 __syncwarp(here);
                 if (lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
-                __stcg(&dst[at], e);
+                if (ON_CHIP) {
+                    const uint32_t to = static_cast<uint32_t>(at) / static_cast<uint32_t>(chunk);
+                    st_cluster_uint2(mapa_cluster(smem_u32(list + ((pass + 1) & 1) * chunk + (at - static_cast<int>(to) * chunk)), to), e);
+                } else {
+                    __stcg(&p.keys[(pass + 1) & 1][at], e);
+                }
             }
             __syncwarp();
         }
         cluster_sync_all();
     }
-    // records: a warp takes 32 places at a time and looks for the ends of the two runs that may reach beyond them
-    const uint2* keys = p.keys[(passes - 1) & 1];
+    // Records need the ends of each run.  Heads (first places of runs) of a warp's windows, the first and the last of its stretch,
+    // then of its CTA; what a stretch does not hold, the closest stretch before or after it does.
+    if (tid == 0 && cta_from < T) sm.edge = element(passes, static_cast<int>(cta_from + chunk < T ? cta_from + chunk : T) - 1);
+    cluster_sync_all();
+    constexpr int NONE_BEFORE = -1, NONE_AFTER = 0x7fffffff;
+    auto heads_of = [&](int i0) {
+        const int i = i0 + lane;
+        const uint32_t key = i < T ? element(passes, i).x : 0xffffffffu;
+        uint32_t left = __shfl_up_sync(0xffffffffu, key, 1);
+        if (lane == 0) {
+            left = 0xfffffffeu;
+            if (i0 > cta_from) left = element(passes, i0 - 1).x;
+            else if (rank > 0) left = ld_cluster_int(mapa_cluster(smem_u32(&sm.edge), rank - 1));
+        }
+        return __ballot_sync(0xffffffffu, key != left);      // (places from T on: the first of them is a head)
+    };
+    int first_head = NONE_AFTER, last_head = NONE_BEFORE;
+    for (int i0 = first; i0 < last; i0 += 32) {
+        const unsigned heads = heads_of(i0);
+        if (heads == 0) continue;
+        if (first_head == NONE_AFTER) first_head = i0 + __ffs(heads) - 1;
+        last_head = i0 + 31 - __clz(heads);
+    }
+    if (lane == 0) {
+        sm.first_head[warp] = first_head;
+        sm.last_head[warp] = last_head;
+    }
+    __syncthreads();
+    int before = NONE_BEFORE, after = NONE_AFTER;            // closest heads outside the stretch
+    {
+        int cta_first = sm.first_head[lane], cta_last = sm.last_head[lane];
+        before = lane < warp ? cta_last : NONE_BEFORE;
+        after = lane > warp ? cta_first : NONE_AFTER;
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) {
+            before = max(before, __shfl_xor_sync(0xffffffffu, before, off));
+            after = min(after, __shfl_xor_sync(0xffffffffu, after, off));
+            cta_first = min(cta_first, __shfl_xor_sync(0xffffffffu, cta_first, off));
+            cta_last = max(cta_last, __shfl_xor_sync(0xffffffffu, cta_last, off));
+        }
+        if (tid == 0) {
+            sm.cta_first_head = cta_first;
+            sm.cta_last_head = cta_last;
+        }
+    }
+    __syncwarp();
+    cluster_sync_all();
+    {
+        int cta_first = NONE_AFTER, cta_last = NONE_BEFORE;
+        if (lane < EMB_CLUSTER) {
+            if (lane > static_cast<int>(rank)) cta_first = ld_cluster_int(mapa_cluster(smem_u32(&sm.cta_first_head), lane));
+            if (lane < static_cast<int>(rank)) cta_last = ld_cluster_int(mapa_cluster(smem_u32(&sm.cta_last_head), lane));
+        }
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) {
+            cta_first = min(cta_first, __shfl_xor_sync(0xffffffffu, cta_first, off));
+            cta_last = max(cta_last, __shfl_xor_sync(0xffffffffu, cta_last, off));
+        }
+        before = max(before, cta_last);
+        after = min(min(after, cta_first), T);
+    }
     const uint32_t bad = p.V;
+    int next = -1;                                           // the first head behind the window
     for (int i0 = first; i0 < last; i0 += 32) {
         const int i = i0 + lane;
-        const uint2 e = i < T ? __ldcg(&keys[i]) : make_uint2(0xffffffffu, 0);
-        const uint32_t left = __shfl_up_sync(0xffffffffu, e.x, 1), edge_l = i0 > 0 ? __ldcg(&keys[i0 - 1]).x : 0xfffffffeu;
-        const unsigned heads = __ballot_sync(0xffffffffu, e.x != (lane == 0 ? edge_l : left));
-        const uint32_t k0 = __shfl_sync(0xffffffffu, e.x, 0), k31 = __shfl_sync(0xffffffffu, e.x, 31);
-        const uint32_t edge_r = i0 + 32 < T ? __ldcg(&keys[i0 + 32]).x : 0xfffffffeu;
-        const int begin = heads & 1 ? i0 : emb_lower_bound(keys, T, k0, lane);
-        const int end = k31 == edge_r ? emb_lower_bound(keys, T, k31 + 1, lane) : i0 + 32;
+        const unsigned heads = heads_of(i0);
+        const unsigned to_lane = 0xffffffffu >> (31 - lane);
+        if (next < i0 + 32) {
+            next = after;
+            for (int j0 = i0 + 32; j0 < last; j0 += 32) {
+                const unsigned more = heads_of(j0);
+                if (more) {
+                    next = j0 + __ffs(more) - 1;
+                    break;
+                }
+            }
+        }
         if (i < last) {
-            const unsigned upto = heads & (0xffffffffu >> (31 - lane)), after = heads & ~(0xffffffffu >> (31 - lane));
-            const int head = upto ? i0 + 31 - __clz(upto) : begin;
-            const int tail = after ? i0 + __ffs(after) - 1 : min(end, T);
+            const uint2 e = element(passes, i);
+            const unsigned upto = heads & to_lane, behind = heads & ~to_lane;
+            const int head = upto ? i0 + 31 - __clz(upto) : before;
+            const int tail = behind ? i0 + __ffs(behind) - 1 : next;
             uint4 rec = emb_record(e.x, i - head, tail - head, e.y);
             if (e.x == bad) {
                 rec.y = 0;
@@ -231,29 +316,43 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
             p.order[i] = e.y;
             p.place[i] = rec;
         }
+        if (heads) before = i0 + 31 - __clz(heads);
     }
+    cluster_sync_all();                                      // no CTA leaves while another may read its shared memory
 }
 
-// 16 bytes of bf16 or 32 of fp32 of a table row
+// eight columns of a table row: what is there, and the new value
+template <bool FP32>
+struct EmbedOld {
+    uint4 v[FP32 ? 2 : 1];
+};
+template <bool FP32>
+__device__ __forceinline__ void emb_old(const EmbedParams& p, long long at, EmbedOld<FP32>& old) {
+    const uint4* d = reinterpret_cast<const uint4*>(p.d_table) + (FP32 ? 2 : 1) * at;
+#pragma unroll
+    for (int i = 0; i < (FP32 ? 2 : 1); ++i) old.v[i] = __ldcg(d + i);
+}
 template <bool FP32, bool ACC>
-__device__ __forceinline__ void emb_store(const EmbedParams& p, long long at, float (&sum)[8]) {
-    float old[8] = {};
+__device__ __forceinline__ void emb_store(const EmbedParams& p, long long at, const float (&sum)[8], const EmbedOld<FP32>& old) {
+    float f[8] = {};
+    if (ACC && FP32) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint4 v = old.v[FP32 ? i : 0];
+            f[4 * i] = __uint_as_float(v.x), f[4 * i + 1] = __uint_as_float(v.y);
+            f[4 * i + 2] = __uint_as_float(v.z), f[4 * i + 3] = __uint_as_float(v.w);
+        }
+    } else if (ACC) {
+        unpack8(old.v[0], f);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __fmaf_rn(p.scale, sum[e], f[e]);
     if (FP32) {
         float4* d = reinterpret_cast<float4*>(p.d_table) + 2 * at;
-        if (ACC) {
-            const float4 a = __ldcg(d), b = __ldcg(d + 1);
-            old[0] = a.x, old[1] = a.y, old[2] = a.z, old[3] = a.w, old[4] = b.x, old[5] = b.y, old[6] = b.z, old[7] = b.w;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = __fmaf_rn(p.scale, sum[e], old[e]);
-        d[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-        d[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        d[0] = make_float4(f[0], f[1], f[2], f[3]);
+        d[1] = make_float4(f[4], f[5], f[6], f[7]);
     } else {
-        uint4* d = reinterpret_cast<uint4*>(p.d_table) + at;
-        if (ACC) unpack8(__ldcg(d), old);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = __fmaf_rn(p.scale, sum[e], old[e]);
-        *d = pack8(sum);
+        reinterpret_cast<uint4*>(p.d_table)[at] = pack8(f);
     }
 }
 __device__ __forceinline__ void emb_add(float (&sum)[8], const uint4& v) {
@@ -267,7 +366,7 @@ __device__ __forceinline__ void emb_add(float (&sum)[8], const uint4& v) {
 // every CTA marks which of its share of the rows occur, and one warp copies zeros over the others by bulk stores,
 // which take no other warp's issue slots.  The sort releases its dependents behind its own wait, so whatever came
 // before it has completed when this grid starts, and it writes neither ids nor table.
-constexpr int EMB_SUM_THREADS = 1024, EMB_SUM_WARPS = EMB_SUM_THREADS / 32;
+constexpr int EMB_SUM_THREADS = 512, EMB_SUM_WARPS = EMB_SUM_THREADS / 32;
 constexpr int EMB_MARK_ROWS = 32768;                         // rows marked at a time
 constexpr int EMB_ZEROS = 8192;                              // bytes of a bulk store
 template <bool FP32, bool ACC>
@@ -319,50 +418,94 @@ __global__ void __launch_bounds__(EMB_SUM_THREADS) embed_sum_kernel(const EmbedP
         }
     }
     pdl_wait();
-    // An item is a piece's 512 columns.  A warp looks up 32 of its items at a time and sums four of them side by side.
-    const int slices = (vpr + 63) / 64;
-    const long long items = p.T * slices, stride = static_cast<long long>(gridDim.x) * EMB_SUM_WARPS;
-    for (long long base = blockIdx.x * EMB_SUM_WARPS + warp; base < items; base += 32 * stride) {
-        const long long item = base + lane * stride;
-        const int at_place = static_cast<int>(item / slices), at_slice = static_cast<int>(item - static_cast<long long>(at_place) * slices);
-        uint4 rec = make_uint4(0, 0, 0, 0);
-        if (item < items) rec = __ldcg(&p.place[at_place]);
-        unsigned todo = __ballot_sync(0xffffffffu, rec.y != 0);
-        while (todo) {
-            const int l = __ffs(todo) - 1;
-            todo &= todo - 1;
-            const int place = __shfl_sync(0xffffffffu, at_place, l), key = __shfl_sync(0xffffffffu, rec.x, l);
-            const int c0 = __shfl_sync(0xffffffffu, at_slice, l) * 64 + lane;
-            const uint32_t info = __shfl_sync(0xffffffffu, rec.y, l);
-            const int len = info & EMB_LEN;
-            const int token = lane < len ? __ldcg(&p.order[place + lane]) : 0;
-            const uint4* dy = reinterpret_cast<const uint4*>(p.d_y) + c0;
-            const bool in0 = c0 < vpr, in1 = c0 + 32 < vpr;
-            float s0[8] = {}, s1[8] = {};
-#pragma unroll 4
-            for (int r = 0; r < len; ++r) {
-                const uint4* row = dy + static_cast<long long>(__shfl_sync(0xffffffffu, token, r)) * vpr;
-                uint4 a = make_uint4(0, 0, 0, 0), b = a;
-                if (in0) a = __ldcg(row);
-                if (in1) b = __ldcg(row + 32);
-                emb_add(s0, a);
-                emb_add(s1, b);
+    // A warp has the same NV * 256 columns of consecutive places.  It looks up 32 places at a time and goes through the rows of
+    // the pieces that begin there, whichever piece they belong to, U at a time: most pieces are one row, and one
+    // after the other they would leave a few hundred bytes per warp in flight.
+    constexpr int NV = ACC ? 1 : 2, U = ACC && FP32 ? 6 : 8; // (16-byte vectors per lane: the old values need registers too)
+    struct Item {
+        int place, key, len, start;
+    };
+    __shared__ Item list[EMB_SUM_WARPS][32];
+    const int slices = (vpr + 32 * NV - 1) / (32 * NV), warps = gridDim.x * EMB_SUM_WARPS, me = blockIdx.x * EMB_SUM_WARPS + warp;
+    const int groups = warps >= slices ? warps / slices : 1, group = warps >= slices ? me / slices : 0;
+    const int per = static_cast<int>((p.T + groups - 1) / groups);
+    const long long places_from = static_cast<long long>(per) * group;
+    const int places_to = static_cast<int>(group >= groups ? 0 : places_from + per < T ? places_from + per : T);
+    for (int slice = me % slices; slice < slices; slice += warps) {
+        const int c0 = slice * 32 * NV + lane;
+        bool in[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) in[v] = c0 + 32 * v < vpr;
+        const uint4* dy = reinterpret_cast<const uint4*>(p.d_y) + c0;
+        float sum[NV][8] = {};
+        for (long long p0 = places_from; p0 < places_to; p0 += 32) {
+            uint4 rec = make_uint4(0, 0, 0, 0);
+            if (p0 + lane < places_to) rec = __ldcg(&p.place[p0 + lane]);
+            const int len = rec.y & EMB_LEN;
+            int end = len;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int n = __shfl_up_sync(0xffffffffu, end, off);
+                if (lane >= off) end += n;
             }
-            if (info & EMB_MANY) {
-                float4* to = reinterpret_cast<float4*>(p.part + emb_slot(place, len) * p.H) + 2 * c0;
-                if (in0) {
-                    to[0] = make_float4(s0[0], s0[1], s0[2], s0[3]);
-                    to[1] = make_float4(s0[4], s0[5], s0[6], s0[7]);
+            const int rows = __shfl_sync(0xffffffffu, end, 31), start = end - len;
+            const unsigned pieces = __ballot_sync(0xffffffffu, len > 0), before_lane = (1u << lane) - 1;
+            if (len > 0)
+                list[warp][__popc(pieces & before_lane)] = {static_cast<int>(p0) + lane, static_cast<int>(rec.x),
+                                                            static_cast<int>(rec.y & (EMB_LEN | EMB_MANY)), start};
+            __syncwarp();
+            for (int r0 = 0; r0 < rows; r0 += 32) {
+                // lane l: row r0 + l, its piece (the o-th) and its token
+                const unsigned starts = __reduce_or_sync(0xffffffffu, len > 0 && start >= r0 && start < r0 + 32 ? 1u << (start - r0) : 0u);
+                const int o = __popc(__ballot_sync(0xffffffffu, len > 0 && start < r0)) + __popc(starts & (before_lane * 2 + 1)) - 1;
+                int token = 0;
+                bool at_end = false;
+                if (r0 + lane < rows) {
+                    const Item& it = list[warp][o];
+                    const int r = r0 + lane - it.start;
+                    token = __ldcg(&p.order[it.place + r]);
+                    at_end = r + 1 == static_cast<int>(it.len & EMB_LEN);
                 }
-                if (in1) {
-                    to[64] = make_float4(s1[0], s1[1], s1[2], s1[3]);
-                    to[65] = make_float4(s1[4], s1[5], s1[6], s1[7]);
+                const unsigned ends = __ballot_sync(0xffffffffu, at_end);
+                const int n = rows - r0 < 32 ? rows - r0 : 32;
+                for (int j = 0; j < n; j += U) {
+                    uint4 row[U][NV];
+                    EmbedOld<FP32> old[ACC ? U : 1][NV];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const uint4* from = dy + static_cast<long long>(__shfl_sync(0xffffffffu, token, (j + u) & 31)) * vpr;
+                        const int ou = __shfl_sync(0xffffffffu, o, (j + u) & 31);
+#pragma unroll
+                        for (int v = 0; v < NV; ++v)
+                            if (j + u < n && in[v]) {
+                                row[u][v] = __ldcg(from + 32 * v);
+                                if (ACC && (ends >> (j + u) & 1)) emb_old(p, static_cast<long long>(list[warp][ou].key) * vpr + c0 + 32 * v, old[ACC ? u : 0][v]);
+                            }
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (j + u >= n) break;
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) emb_add(sum[v], row[u][v]);
+                        const int ou = __shfl_sync(0xffffffffu, o, j + u);
+                        if (!(ends >> (j + u) & 1)) continue;
+                        const Item it = list[warp][ou];
+#pragma unroll
+                        for (int v = 0; v < NV; ++v) {
+                            if (in[v] && (it.len & EMB_MANY)) {
+                                float4* to = reinterpret_cast<float4*>(p.part + emb_slot(it.place, it.len & EMB_LEN) * p.H) + 2 * (c0 + 32 * v);
+                                to[0] = make_float4(sum[v][0], sum[v][1], sum[v][2], sum[v][3]);
+                                to[1] = make_float4(sum[v][4], sum[v][5], sum[v][6], sum[v][7]);
+                            } else if (in[v]) {
+                                emb_store<FP32, ACC>(p, static_cast<long long>(it.key) * vpr + c0 + 32 * v, sum[v], old[ACC ? u : 0][v]);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) sum[v][e] = 0.0f;
+                        }
+                    }
                 }
-            } else {
-                const long long at = static_cast<long long>(key) * vpr + c0;
-                if (in0) emb_store<FP32, ACC>(p, at, s0);
-                if (in1) emb_store<FP32, ACC>(p, at + 32, s1);
             }
+            __syncwarp();
         }
     }
     if (!ACC && warp == 0) tma_store_wait_all();
@@ -410,7 +553,10 @@ __global__ void __launch_bounds__(EMB_FOLD_WARPS * 32) embed_fold_kernel(const E
 #pragma unroll
                 for (int w = 1; w < EMB_FOLD_WARPS; ++w) s[e] = __fadd_rn(s[e], sums[w][e][lane]);
             }
-            emb_store<FP32, ACC>(p, static_cast<long long>(static_cast<int>(rec.x)) * vpr + c, s);
+            const long long at = static_cast<long long>(static_cast<int>(rec.x)) * vpr + c;
+            EmbedOld<FP32> old;
+            if (ACC) emb_old(p, at, old);
+            emb_store<FP32, ACC>(p, at, s, old);
         }
         __syncthreads();
     }
@@ -419,7 +565,7 @@ __global__ void __launch_bounds__(EMB_FOLD_WARPS * 32) embed_fold_kernel(const E
 static size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 size_t embed_bwd_bytes(int64_t T, int, int H) {
     const size_t n = static_cast<size_t>(T);
-    return align16(4 * n) + 16 * n + (T > EMB_RANK_TOKENS ? 2 * 8 * n : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;
+    return align16(4 * n) + 16 * n + (T > EMB_CHIP_TOKENS ? 2 * 8 * n : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;
 }
 
 cudaError_t launch_embed(const EmbedParams& p, cudaStream_t stream) {
@@ -439,21 +585,27 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
     char* at = static_cast<char*>(ws);
     p.place = reinterpret_cast<uint4*>(at);
     at += 16 * p.T;
-    if (p.T > EMB_RANK_TOKENS)
+    const bool on_chip = p.T <= EMB_CHIP_TOKENS;
+    if (!on_chip)
         for (int i = 0; i < 2; ++i, at += 8 * p.T) p.keys[i] = reinterpret_cast<uint2*>(at);
     p.order = reinterpret_cast<int32_t*>(at);
     p.part = reinterpret_cast<float*>(at + align16(4 * p.T));
     cudaError_t e = cudaSuccess;
     if (p.T > EMB_RANK_TOKENS) {
         static DeviceOnce configured;
+        const size_t base = sizeof(EmbedSortSmem), list = 2ull * sizeof(uint2) * EMB_SORT_WARPS;      // per element of a stretch
         e = configured.run([&]() {
-            return cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(EMB_SORT_SMEM));
+            const cudaError_t e1 = cudaFuncSetAttribute(embed_sort_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                        static_cast<int>(base + list * emb_stretch(EMB_CHIP_TOKENS)));
+            return e1 != cudaSuccess ? e1 : cudaFuncSetAttribute(embed_sort_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                                 static_cast<int>(base));
         });
         if (e != cudaSuccess) return e;
         int bits = 1;
         while (p.V >> bits) ++bits;                          // keys are 0 .. V
         const int passes = (bits + 8) / 9, digit_bits = (bits + passes - 1) / passes;
-        e = launch_pdl(embed_sort_kernel, dim3(EMB_CLUSTER), EMB_SORT_THREADS, EMB_SORT_SMEM, stream, EMB_CLUSTER, p, passes, digit_bits);
+        e = launch_pdl(on_chip ? embed_sort_kernel<true> : embed_sort_kernel<false>, dim3(EMB_CLUSTER), EMB_SORT_THREADS,
+                       base + (on_chip ? list * emb_stretch(static_cast<int>(p.T)) : 0), stream, EMB_CLUSTER, p, passes, digit_bits);
     } else if (p.T > 0) {
         e = launch_pdl(embed_rank_kernel, dim3(static_cast<unsigned>((p.T + 31) / 32)), EMB_RANK_WARPS * 32, 0, stream, 1, p);
     }

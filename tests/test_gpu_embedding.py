@@ -95,7 +95,9 @@ def _ids(kind, T, V, rng):
     (1, 1, 8, "one"), (1, 5000, 72, "uniform"), (2, 3, 3584, "one"), (31, 40, 64, "falling"), (33, 1000, 1536, "distinct"),
     (64, 64, 200, "one"), (65, 64, 200, "one"), (127, 2, 264, "uniform"), (128, 9, 64, "few"), (129, 151936, 8, "zipf"), (256, 2048, 256, "zipf"),
     (700, 33, 520, "few"), (1000, 151936, 16, "uniform"), (1023, 100, 72, "one"), (1025, 4097, 136, "zipf"), (3000, 2048, 256, "zipf"),
-    (4097, 300, 64, "falling"), (9001, 152064, 24, "zipf"), (20011, 17, 40, "zipf"), (16384, 70000, 8, "distinct"), (33000, 5000, 8, "one")])
+    (4097, 300, 64, "falling"), (9001, 152064, 24, "zipf"), (20011, 17, 40, "zipf"), (16384, 70000, 8, "distinct"), (33000, 5000, 8, "one"),
+    (4096, 500, 16, "zipf"), (65536, 152064, 8, "zipf"), (65537, 152064, 8, "zipf"), (70001, 300, 8, "one"), (100003, 600000, 8, "uniform"),
+    (131072, 3, 16, "falling")])
 @pytest.mark.parametrize("dtype,accumulate", [(torch.bfloat16, False), (torch.float32, False), (torch.bfloat16, True), (torch.float32, True)])
 def test_gradient(tik, T, V, H, kind, dtype, accumulate):
     ids = _i32(_ids(kind, T, V, np.random.default_rng(T)))
