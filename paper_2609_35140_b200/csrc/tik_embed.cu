@@ -1,6 +1,8 @@
 // Embedding lookup and its gradient by sorted tokens.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "tik_core.cuh"
 #include "tik_internal.h"
 #include "tik_ptx.cuh"
@@ -67,64 +69,74 @@ __global__ void __launch_bounds__(EMB_RANK_WARPS * 32) embed_rank_kernel(const E
     pdl_wait();
     pdl_launch_dependents();
     const int T = static_cast<int>(p.T), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.tickets[threadIdx.x] = 0;
     const int padded = (T + 4 * EMB_RANK_WARPS - 1) / (4 * EMB_RANK_WARPS) * (4 * EMB_RANK_WARPS);
-#pragma unroll 4
-    for (int i = threadIdx.x; i < padded; i += EMB_RANK_WARPS * 32) keys[i] = i < T ? emb_key(p, p.ids[i]) : 0x7fffffff;
+#pragma unroll                                               // (all in flight at once)
+    for (int j = 0; j < EMB_RANK_TOKENS / (EMB_RANK_WARPS * 32); ++j) {
+        const int i = threadIdx.x + j * EMB_RANK_WARPS * 32;
+        if (i < padded) keys[i] = i < T ? emb_key(p, p.ids[i]) : 0x7fffffff;
+    }
     __syncthreads();
-    const int t = blockIdx.x * 32 + lane, mine = t < T ? keys[t] : -1;
-    int less = 0, same = 0, same_before = 0;
-    const int per = padded / EMB_RANK_WARPS;
-#pragma unroll 4
-    for (int i = per * warp; i < per * (warp + 1); i += 4) {
+    const int t0 = blockIdx.x * 32, t = t0 + lane, mine = t < T ? keys[t] : -1;
+    // In front of the CTA's tokens an equal id comes earlier in the order, behind them it does not.
+    int place = 0, same = 0, same_before = 0;
+    const int per = padded / EMB_RANK_WARPS, begin = per * warp, end = begin + per;
+    auto four = [&](int i, auto before) {
         const int4 k4 = *reinterpret_cast<const int4*>(keys + i);
         const int k[4] = {k4.x, k4.y, k4.z, k4.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            less += k[j] < mine;
-            same += k[j] == mine;
-            same_before += k[j] == mine && i + j < t;
+            place += decltype(before)::value ? k[j] <= mine : k[j] < mine;
+            (decltype(before)::value ? same_before : same) += k[j] == mine;
         }
+    };
+    int i = begin;
+#pragma unroll 4
+    for (; i < min(end, t0); i += 4) four(i, std::true_type());
+    for (; i < min(end, t0 + 32); ++i) {
+        const bool equal = keys[i] == mine;
+        place += keys[i] < mine || (equal && i < t);
+        (i < t ? same_before : same) += equal;
     }
-    count[warp][0][lane] = less;
+#pragma unroll 4
+    for (; i < end; i += 4) four(i, std::false_type());
+    count[warp][0][lane] = place;
     count[warp][1][lane] = same;
     count[warp][2][lane] = same_before;
     __syncthreads();
     if (warp != 0 || t >= T) return;
-    less = same = same_before = 0;
+    place = same = same_before = 0;
 #pragma unroll
     for (int w = 0; w < EMB_RANK_WARPS; ++w) {
-        less += count[w][0][lane];
+        place += count[w][0][lane];
         same += count[w][1][lane];
         same_before += count[w][2][lane];
     }
-    const int at = less + same_before;
-    p.order[at] = t;
-    uint4 rec = emb_record(mine, same_before, same, t);
+    p.order[place] = t;
+    uint4 rec = emb_record(mine, same_before, same_before + same, t);
     if (mine == p.V) {
         atomicOr(p.dev_status, TIK_DEV_BAD_TOKEN);
         rec.y = 0;
     }
-    p.place[at] = rec;
+    p.place[place] = rec;
 }
 
 // Other calls: a stable radix sort by one cluster of eight CTAs, whose 256 warps own consecutive stretches of the list.  Per
 // digit: each warp counts its digits, the CTAs exchange their counts through distributed shared memory, and each
-// warp moves its elements, in order, to where the elements before them end.  ON_CHIP: the list stays in the CTAs' shared
-// memory between the passes (up to EMB_CHIP_TOKENS), which the zeros written meanwhile do not slow down; else in global memory.
+// warp moves its elements, in order, to where the elements before them end.  NW > 0: a stretch is NW windows of 32 elements,
+// held in registers, and the list stays in the CTAs' shared memory between the passes, which the zeros that are
+// written meanwhile do not slow down; 0 (more than EMB_CHIP_TOKENS): any number of windows, the list in global memory.
+// What a call costs are its few barriers across the cluster (~0.7 us each) and the chains between them.
 constexpr int EMB_CLUSTER = 8, EMB_SORT_THREADS = 1024, EMB_SORT_WARPS = EMB_SORT_THREADS / 32;
-constexpr int EMB_BINS = 512, EMB_CHIP_TOKENS = 65536;
+constexpr int EMB_BINS = 512, EMB_CHIP_TOKENS = 8 * 32 * EMB_SORT_WARPS * EMB_CLUSTER;
 struct EmbedSortSmem {
     int hist[EMB_SORT_WARPS][EMB_BINS];
     int total[EMB_BINS], base[EMB_BINS];
     int warp_sum[EMB_SORT_WARPS];
     int first_head[EMB_SORT_WARPS], last_head[EMB_SORT_WARPS];
     int cta_first_head, cta_last_head;
-    uint2 edge;                                              // the CTA's last element
 };
-// elements of a warp's stretch: whole windows of 32
-inline __host__ __device__ int emb_stretch(int T) {
-    return ((T + EMB_CLUSTER * EMB_SORT_WARPS - 1) / (EMB_CLUSTER * EMB_SORT_WARPS) + 31) / 32 * 32;
-}
+constexpr size_t emb_sort_smem(int nw) { return sizeof(EmbedSortSmem) + 2ull * nw * 32 * EMB_SORT_WARPS * sizeof(uint2); }
 
 __device__ __forceinline__ int ld_cluster_int(uint32_t addr) {
     int v;
@@ -135,40 +147,60 @@ __device__ __forceinline__ void st_cluster_uint2(uint32_t addr, uint2 v) {
     asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
 }
 
-template <bool ON_CHIP>
+template <int NW>
 __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const EmbedParams p, int passes, int digit_bits) {
+    constexpr bool ON_CHIP = NW > 0;
     extern __shared__ __align__(16) unsigned char emb_smem[];
     EmbedSortSmem& sm = *reinterpret_cast<EmbedSortSmem*>(emb_smem);
-    uint2* list = reinterpret_cast<uint2*>(emb_smem + sizeof(EmbedSortSmem));        // ON_CHIP: two buffers of a CTA's stretch
+    uint2* list = reinterpret_cast<uint2*>(emb_smem + sizeof(EmbedSortSmem));        // ON_CHIP: two buffers of the CTA's elements
     const int T = static_cast<int>(p.T), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_ctarank();
     pdl_wait();
     pdl_launch_dependents();
+    if (rank == 0 && tid < 2) p.tickets[tid] = 0;
     const int bins = 1 << digit_bits;
-    const int per = emb_stretch(T), chunk = per * EMB_SORT_WARPS;
+    const int per = ON_CHIP ? 32 * NW : ((T + EMB_CLUSTER * EMB_SORT_WARPS - 1) / (EMB_CLUSTER * EMB_SORT_WARPS) + 31) / 32 * 32;
+    const int chunk = per * EMB_SORT_WARPS;
     const long long cta_from = static_cast<long long>(chunk) * rank, from = cta_from + per * warp;
     const int first = static_cast<int>(from < T ? from : T), last = static_cast<int>(from + per < T ? from + per : T);
     int* mine = sm.hist[warp];
-    // elements of this CTA's stretch before pass `pass` (pass == passes: sorted)
+    // elements of this warp's stretch before pass `pass` (pass == passes: sorted)
     auto element = [&](int pass, int i) {
         if (pass == 0) return make_uint2(emb_key(p, p.ids[i]), i);
         if (ON_CHIP) return list[(pass & 1) * chunk + static_cast<int>(i - cta_from)];
         return __ldcg(&p.keys[pass & 1][i]);
     };
-    cluster_sync_all();                                      // every CTA runs before any writes to another's shared memory
+    // the element's place among those of its digit that this warp has seen; counts it
+    auto count = [&](bool valid, uint32_t key, int shift) {
+        int at = 0;
+        const unsigned here = __ballot_sync(0xffffffffu, valid);
+        if (valid) {
+            const int digit = (key >> shift) & (bins - 1);
+            const unsigned peers = __match_any_sync(here, digit);
+            at = mine[digit] + __popc(peers & ((1u << lane) - 1));
+            __syncwarp(here);
+            if (lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
+        }
+        __syncwarp();
+        return at;
+    };
+    uint2 held[ON_CHIP ? NW : 1];
+    int at[ON_CHIP ? NW : 1];
+    auto hold = [&](int pass) {
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            if (first + 32 * w + lane < last) held[w] = element(pass, first + 32 * w + lane);
+    };
+    if (ON_CHIP) hold(0);
     for (int pass = 0; pass < passes; ++pass) {
         const int shift = pass * digit_bits;
         for (int i = lane; i < bins; i += 32) mine[i] = 0;
         __syncwarp();
-        for (int i0 = first; i0 < last; i0 += 32) {
-            const int i = i0 + lane;
-            const unsigned here = __ballot_sync(0xffffffffu, i < last);
-            if (i < last) {
-                const int digit = (element(pass, i).x >> shift) & (bins - 1);
-                const unsigned peers = __match_any_sync(here, digit);
-                if (lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
-            }
-            __syncwarp();
+        if (ON_CHIP) {
+#pragma unroll
+            for (int w = 0; w < NW; ++w) at[w] = count(first + 32 * w + lane < last, held[w].x, shift);
+        } else {
+            for (int i = first + lane; i - lane < last; i += 32) count(i < last, i < last ? element(pass, i).x : 0, shift);
         }
         __syncthreads();
         int sum = 0;
@@ -200,51 +232,53 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
         }
         if (lane == 31) sm.warp_sum[warp] = scan;
         __syncthreads();
-        int below = lane < warp ? sm.warp_sum[lane] : 0;
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) below += __shfl_xor_sync(0xffffffffu, below, off);
+        const int below = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0);
         if (tid < bins) sm.base[tid] = scan - all + before + below;
         __syncthreads();
-        for (int i0 = first; i0 < last; i0 += 32) {
-            const int i = i0 + lane;
-            const unsigned here = __ballot_sync(0xffffffffu, i < last);
-            if (i < last) {
-                const uint2 e = element(pass, i);
-                const int digit = (e.x >> shift) & (bins - 1);
-                const unsigned peers = __match_any_sync(here, digit);
-                const int at = sm.base[digit] + mine[digit] + __popc(peers & ((1u << lane) - 1));
-                __syncwarp(here);
-                if (lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
-                if (ON_CHIP) {
-                    const uint32_t to = static_cast<uint32_t>(at) / static_cast<uint32_t>(chunk);
-                    st_cluster_uint2(mapa_cluster(smem_u32(list + ((pass + 1) & 1) * chunk + (at - static_cast<int>(to) * chunk)), to), e);
-                } else {
-                    __stcg(&p.keys[(pass + 1) & 1][at], e);
-                }
+        auto move = [&](uint2 e, int in_cta) {               // in_cta: the place among the CTA's elements of that digit
+            const int to = sm.base[(e.x >> shift) & (bins - 1)] + in_cta;
+            if (ON_CHIP) {
+                const uint32_t cta = static_cast<uint32_t>(to) / static_cast<uint32_t>(chunk);
+                st_cluster_uint2(mapa_cluster(smem_u32(list + ((pass + 1) & 1) * chunk + (to - static_cast<int>(cta) * chunk)), cta), e);
+            } else {
+                __stcg(&p.keys[(pass + 1) & 1][to], e);
             }
-            __syncwarp();
+        };
+        if (ON_CHIP) {
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                if (first + 32 * w + lane < last) move(held[w], at[w] + mine[(held[w].x >> shift) & (bins - 1)]);
+        } else {
+            for (int i = first + lane; i - lane < last; i += 32) {
+                const uint2 e = i < last ? element(pass, i) : make_uint2(0, 0);
+                const int in_cta = count(i < last, e.x, shift);
+                if (i < last) move(e, in_cta);
+            }
         }
+        __syncwarp();
         cluster_sync_all();
+        if (ON_CHIP) hold(pass + 1);
     }
     // Records need the ends of each run.  Heads (first places of runs) of a warp's windows, the first and the last of its stretch,
     // then of its CTA; what a stretch does not hold, the closest stretch before or after it does.
-    if (tid == 0 && cta_from < T) sm.edge = element(passes, static_cast<int>(cta_from + chunk < T ? cta_from + chunk : T) - 1);
-    cluster_sync_all();
     constexpr int NONE_BEFORE = -1, NONE_AFTER = 0x7fffffff;
-    auto heads_of = [&](int i0) {
+    auto window = [&](int i0) {                              // i0 + lane's element; past the end a key that no token has
         const int i = i0 + lane;
-        const uint32_t key = i < T ? element(passes, i).x : 0xffffffffu;
+        return i < T ? (ON_CHIP ? list[(passes & 1) * chunk + static_cast<int>(i - cta_from)] : __ldcg(&p.keys[passes & 1][i]))
+                     : make_uint2(0xffffffffu, 0);
+    };
+    auto heads_of = [&](int i0, uint32_t key) {
         uint32_t left = __shfl_up_sync(0xffffffffu, key, 1);
         if (lane == 0) {
             left = 0xfffffffeu;
-            if (i0 > cta_from) left = element(passes, i0 - 1).x;
-            else if (rank > 0) left = ld_cluster_int(mapa_cluster(smem_u32(&sm.edge), rank - 1));
+            if (i0 > cta_from || (!ON_CHIP && i0 > 0)) left = element(passes, i0 - 1).x;
+            else if (rank > 0) left = ld_cluster_int(mapa_cluster(smem_u32(list + (passes & 1) * chunk + chunk - 1), rank - 1));
         }
         return __ballot_sync(0xffffffffu, key != left);      // (places from T on: the first of them is a head)
     };
     int first_head = NONE_AFTER, last_head = NONE_BEFORE;
     for (int i0 = first; i0 < last; i0 += 32) {
-        const unsigned heads = heads_of(i0);
+        const unsigned heads = heads_of(i0, window(i0).x);
         if (heads == 0) continue;
         if (first_head == NONE_AFTER) first_head = i0 + __ffs(heads) - 1;
         last_head = i0 + 31 - __clz(heads);
@@ -254,24 +288,17 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
         sm.last_head[warp] = last_head;
     }
     __syncthreads();
-    int before = NONE_BEFORE, after = NONE_AFTER;            // closest heads outside the stretch
-    {
-        int cta_first = sm.first_head[lane], cta_last = sm.last_head[lane];
-        before = lane < warp ? cta_last : NONE_BEFORE;
-        after = lane > warp ? cta_first : NONE_AFTER;
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) {
-            before = max(before, __shfl_xor_sync(0xffffffffu, before, off));
-            after = min(after, __shfl_xor_sync(0xffffffffu, after, off));
-            cta_first = min(cta_first, __shfl_xor_sync(0xffffffffu, cta_first, off));
-            cta_last = max(cta_last, __shfl_xor_sync(0xffffffffu, cta_last, off));
-        }
-        if (tid == 0) {
+    const int first_w = sm.first_head[lane], last_w = sm.last_head[lane];
+    int before = __reduce_max_sync(0xffffffffu, lane < warp ? last_w : NONE_BEFORE);         // closest heads outside the stretch
+    int after = __reduce_min_sync(0xffffffffu, lane > warp ? first_w : NONE_AFTER);
+    if (warp == 0) {
+        const int cta_first = __reduce_min_sync(0xffffffffu, first_w), cta_last = __reduce_max_sync(0xffffffffu, last_w);
+        if (lane == 0) {
             sm.cta_first_head = cta_first;
             sm.cta_last_head = cta_last;
         }
+        __syncwarp();
     }
-    __syncwarp();
     cluster_sync_all();
     {
         int cta_first = NONE_AFTER, cta_last = NONE_BEFORE;
@@ -279,24 +306,20 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
             if (lane > static_cast<int>(rank)) cta_first = ld_cluster_int(mapa_cluster(smem_u32(&sm.cta_first_head), lane));
             if (lane < static_cast<int>(rank)) cta_last = ld_cluster_int(mapa_cluster(smem_u32(&sm.cta_last_head), lane));
         }
-#pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) {
-            cta_first = min(cta_first, __shfl_xor_sync(0xffffffffu, cta_first, off));
-            cta_last = max(cta_last, __shfl_xor_sync(0xffffffffu, cta_last, off));
-        }
-        before = max(before, cta_last);
-        after = min(min(after, cta_first), T);
+        before = max(before, __reduce_max_sync(0xffffffffu, cta_last));
+        after = min(min(after, __reduce_min_sync(0xffffffffu, cta_first)), T);
     }
     const uint32_t bad = p.V;
     int next = -1;                                           // the first head behind the window
     for (int i0 = first; i0 < last; i0 += 32) {
         const int i = i0 + lane;
-        const unsigned heads = heads_of(i0);
+        const uint2 e = window(i0);
+        const unsigned heads = heads_of(i0, e.x);
         const unsigned to_lane = 0xffffffffu >> (31 - lane);
         if (next < i0 + 32) {
             next = after;
             for (int j0 = i0 + 32; j0 < last; j0 += 32) {
-                const unsigned more = heads_of(j0);
+                const unsigned more = heads_of(j0, window(j0).x);
                 if (more) {
                     next = j0 + __ffs(more) - 1;
                     break;
@@ -304,7 +327,6 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
             }
         }
         if (i < last) {
-            const uint2 e = element(passes, i);
             const unsigned upto = heads & to_lane, behind = heads & ~to_lane;
             const int head = upto ? i0 + 31 - __clz(upto) : before;
             const int tail = behind ? i0 + __ffs(behind) - 1 : next;
@@ -318,6 +340,7 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
         }
         if (heads) before = i0 + 31 - __clz(heads);
     }
+    __syncwarp();
     cluster_sync_all();                                      // no CTA leaves while another may read its shared memory
 }
 
@@ -363,15 +386,49 @@ __device__ __forceinline__ void emb_add(float (&sum)[8], const uint4& v) {
 }
 
 // Zeros for the rows without a token, and the pieces' sums.  The zeros need the ids alone, so they start while the sort runs:
-// every CTA marks which of its share of the rows occur, and one warp copies zeros over the others by bulk stores,
-// which take no other warp's issue slots.  The sort releases its dependents behind its own wait, so whatever came
-// before it has completed when this grid starts, and it writes neither ids nor table.
+// every CTA marks which rows occur, and its first warp copies zeros over the others by bulk stores, which take no other
+// warp's issue slots.  The sort releases its dependents behind its own wait, so whatever came before it has completed when
+// this grid starts, and it writes neither ids nor table.  A first part of the rows is shared out evenly; the rest, and the
+// sums, are taken in small shares by whoever is free, from counters that the sort has cleared: SMs write at rates that differ by
+// a fifth, pieces differ in rows, and a CTA takes a whole SM, so that those on the sort's eight begin when it ends.
 constexpr int EMB_SUM_THREADS = 512, EMB_SUM_WARPS = EMB_SUM_THREADS / 32;
-constexpr int EMB_MARK_ROWS = 32768;                         // rows marked at a time
+constexpr int EMB_MARK_ROWS = 1 << 18;                       // rows marked at a time
 constexpr int EMB_ZEROS = 8192;                              // bytes of a bulk store
+constexpr int EMB_SHARE = 1 << 18;                           // bytes of a share of the zeros, about
+constexpr int EMB_PREFETCH = 64 << 20;                       // bytes brought to L2 ahead: half of it
+
+// zeros over rows [r, r + n)
+__device__ __forceinline__ void emb_fill(char* table, long long row_bytes, uint32_t zeros, long long r, int n) {
+    char* to = table + r * row_bytes;
+    for (long long left = n * row_bytes; left > 0;) {
+        const int bytes = left < EMB_ZEROS ? static_cast<int>(left) : EMB_ZEROS;
+        bulk_store(to, zeros, bytes);
+        to += bytes;
+        left -= bytes;
+    }
+}
+// ... over the absent ones of 32-row words [w0, w1) of the marks, by a whole warp
+__device__ __forceinline__ void emb_fill_words(char* table, long long row_bytes, uint32_t zeros, const uint32_t* present, long long row0,
+                                               int rows, int w0, int w1, int lane) {
+    if (w1 - w0 == 1) {                                      // long rows: one per lane
+        const int r = 32 * w0 + lane;
+        if (r < rows && !(present[w0] >> lane & 1)) emb_fill(table, row_bytes, zeros, row0 + r, 1);
+        return;
+    }
+    for (int w = w0 + lane; w < w1; w += 32) {
+        const int n = rows - 32 * w < 32 ? rows - 32 * w : 32;
+        uint32_t absent = ~present[w] & (0xffffffffu >> (32 - n));
+        while (absent) {                                     // stretches of rows without a token
+            const int r = __ffs(absent) - 1, end = __ffs(~(absent >> r)) - 1, len = end < 0 ? 32 - r : end;
+            emb_fill(table, row_bytes, zeros, row0 + 32 * w + r, len);
+            absent &= len == 32 ? 0u : ~(((1u << len) - 1) << r);
+        }
+    }
+}
+
 template <bool FP32, bool ACC>
-__global__ void __launch_bounds__(EMB_SUM_THREADS) embed_sum_kernel(const EmbedParams p) {
-    __shared__ uint32_t present[ACC ? 1 : EMB_MARK_ROWS / 32];
+__global__ void __launch_bounds__(EMB_SUM_THREADS) embed_sum_kernel(const EmbedParams p, int late) {
+    extern __shared__ uint32_t present[];                    // !ACC: a bit per row, at most EMB_MARK_ROWS
     __shared__ alignas(16) uint4 zeros[ACC ? 1 : EMB_ZEROS / 16];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, T = static_cast<int>(p.T);
     const int vpr = p.H / 8;
@@ -380,11 +437,11 @@ __global__ void __launch_bounds__(EMB_SUM_THREADS) embed_sum_kernel(const EmbedP
         for (int i = tid; i < EMB_ZEROS / 16; i += EMB_SUM_THREADS) zeros[i] = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
         const long long row_bytes = static_cast<long long>(p.H) * (FP32 ? 4 : 2);
-        const long long share = (p.V + gridDim.x - 1ll) / gridDim.x, begin = share * blockIdx.x;
-        const long long end = begin + share < p.V ? begin + share : p.V;
-        for (long long row0 = begin; row0 < end; row0 += EMB_MARK_ROWS) {
-            const int rows = static_cast<int>(end - row0 < EMB_MARK_ROWS ? end - row0 : EMB_MARK_ROWS);
-            for (int i = tid; i < (rows + 31) / 32; i += EMB_SUM_THREADS) present[i] = 0;
+        char* table = static_cast<char*>(p.d_table);
+        const int fillers = gridDim.x - late, me = blockIdx.x;           // (the last `late` CTAs begin late)
+        for (long long row0 = 0; row0 < p.V; row0 += EMB_MARK_ROWS) {
+            const int rows = static_cast<int>(p.V - row0 < EMB_MARK_ROWS ? p.V - row0 : EMB_MARK_ROWS), words = (rows + 31) / 32;
+            for (int i = tid; i < words; i += EMB_SUM_THREADS) present[i] = 0;
             __syncthreads();
 #pragma unroll 8
             for (int i = tid; i < T; i += EMB_SUM_THREADS) {
@@ -393,120 +450,139 @@ __global__ void __launch_bounds__(EMB_SUM_THREADS) embed_sum_kernel(const EmbedP
             }
             __syncthreads();
             if (warp == 0) {
-                auto fill = [&](int r, int n) {
-                    char* to = static_cast<char*>(p.d_table) + (row0 + r) * row_bytes;
-                    for (long long left = n * row_bytes; left > 0;) {
-                        const int bytes = left < EMB_ZEROS ? static_cast<int>(left) : EMB_ZEROS;
-                        bulk_store(to, smem_u32(zeros), bytes);
-                        to += bytes;
-                        left -= bytes;
-                    }
-                };
-                for (int w = lane; w < (rows + 31) / 32; w += 32) {
-                    const int n = rows - 32 * w < 32 ? rows - 32 * w : 32;
-                    uint32_t absent = ~present[w] & (0xffffffffu >> (32 - n));
-                    while (absent) {                         // stretches of rows without a token
-                        const int r = __ffs(absent) - 1, len = __ffs(~(absent >> r)) - 1;
-                        const int rows_here = len < 0 ? 32 - r : len;
-                        fill(32 * w + r, rows_here);
-                        absent &= rows_here == 32 ? 0u : ~(((1u << rows_here) - 1) << r);
+                // a third in even shares, or all of it where nothing has cleared the counters or they are taken
+                const bool last = row0 + EMB_MARK_ROWS >= p.V && p.T > 0;
+                const int even = last ? words / 3 : words;
+                const int w0 = me < fillers ? static_cast<int>(static_cast<long long>(even) * me / fillers) : 0;
+                const int w1 = me < fillers ? static_cast<int>(static_cast<long long>(even) * (me + 1) / fillers) : 0;
+                for (int w = w0; w < w1; ++w) emb_fill_words(table, row_bytes, smem_u32(zeros), present, row0, rows, w, w + 1, lane);
+                if (last) {
+                    pdl_wait();
+                    const int step = static_cast<int>(EMB_SHARE / (32 * row_bytes) > 1 ? EMB_SHARE / (32 * row_bytes) : 1);
+                    int ticket = 0;
+                    if (lane == 0) ticket = atomicAdd(&p.tickets[0], 1);
+                    for (;;) {
+                        const long long w = even + static_cast<long long>(step) * __shfl_sync(0xffffffffu, ticket, 0);
+                        if (w >= words) break;
+                        if (lane == 0) ticket = atomicAdd(&p.tickets[0], 1);         // (the next one, under this one's stores)
+                        const int to = w + step < words ? static_cast<int>(w) + step : words;
+                        emb_fill_words(table, row_bytes, smem_u32(zeros), present, row0, rows, static_cast<int>(w), to, lane);
                     }
                 }
                 tma_store_commit();
             }
-            if (row0 + EMB_MARK_ROWS < end) __syncthreads();
+            if (row0 + EMB_MARK_ROWS < p.V) __syncthreads();
+        }
+    }
+    if (ACC) {
+        // Nothing may be added before the sort is through, but what will be read can be brought to L2 meanwhile (two micro-batches
+        // of 6007 x 1536 in fp32, the second one accumulated: 180.2 us without, PREFETCHED with).
+        const int row = p.H * 2, old = p.H * (FP32 ? 4 : 2);
+        const long long most = EMB_PREFETCH / (row + old), n = p.T < most ? p.T : most;
+        for (long long t = blockIdx.x * EMB_SUM_THREADS + tid; t < n; t += gridDim.x * EMB_SUM_THREADS) {
+            const unsigned id = static_cast<unsigned>(__ldcg(&p.ids[t]));
+            bulk_prefetch_l2(p.d_y + t * p.H, row);
+            if (id < static_cast<unsigned>(p.V)) bulk_prefetch_l2(static_cast<char*>(p.d_table) + static_cast<long long>(id) * old, old);
         }
     }
     pdl_wait();
-    // A warp has the same NV * 256 columns of consecutive places.  It looks up 32 places at a time and goes through the rows of
+    // A warp takes `places` consecutive places and NV * 256 columns.  It looks the places up and goes through the rows of
     // the pieces that begin there, whichever piece they belong to, U at a time: most pieces are one row, and one
     // after the other they would leave a few hundred bytes per warp in flight.
     constexpr int NV = ACC ? 1 : 2, U = ACC && FP32 ? 6 : 8; // (16-byte vectors per lane: the old values need registers too)
+    constexpr int IDLE = ACC ? 0 : 1;                        // the first warp has the zeros
     struct Item {
         int place, key, len, start;
     };
     __shared__ Item list[EMB_SUM_WARPS][32];
-    const int slices = (vpr + 32 * NV - 1) / (32 * NV), warps = gridDim.x * EMB_SUM_WARPS, me = blockIdx.x * EMB_SUM_WARPS + warp;
-    const int groups = warps >= slices ? warps / slices : 1, group = warps >= slices ? me / slices : 0;
-    const int per = static_cast<int>((p.T + groups - 1) / groups);
-    const long long places_from = static_cast<long long>(per) * group;
-    const int places_to = static_cast<int>(group >= groups ? 0 : places_from + per < T ? places_from + per : T);
-    for (int slice = me % slices; slice < slices; slice += warps) {
-        const int c0 = slice * 32 * NV + lane;
+    const int slices = (vpr + 32 * NV - 1) / (32 * NV), warps = gridDim.x * (EMB_SUM_WARPS - IDLE);
+    // Two shares a warp of one place at least (a share costs three trips to L2 before its first row) and 16 at most (balance).
+    const long long each = p.T * slices / (2ll * warps);
+    const int places = each < 1 ? 1 : each > 16 ? 16 : static_cast<int>(each);
+    const long long shares = (p.T + places - 1) / places * slices;
+    auto look_up = [&](long long share) {
+        const long long at = share / slices * places + lane;
+        return share < shares && lane < places && at < T ? __ldcg(&p.place[at]) : make_uint4(0, 0, 0, 0);
+    };
+    // the first two shares are even; the one after the next is asked for, and the next one looked up, under this one's rows
+    long long share = warp < IDLE ? shares : static_cast<long long>(warp - IDLE) * gridDim.x + blockIdx.x, next = share + warps;
+    uint4 rec = look_up(share), next_rec;
+    int ticket = 0;
+    for (; share < shares; share = next, next = 2ll * warps + __shfl_sync(0xffffffffu, ticket, 0), rec = next_rec) {
+        next_rec = look_up(next);
+        if (lane == 0 && next < shares) ticket = atomicAdd(&p.tickets[1], 1);
+        const long long p0 = share / slices * places;
+        const int c0 = static_cast<int>(share % slices) * 32 * NV + lane;
         bool in[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) in[v] = c0 + 32 * v < vpr;
         const uint4* dy = reinterpret_cast<const uint4*>(p.d_y) + c0;
         float sum[NV][8] = {};
-        for (long long p0 = places_from; p0 < places_to; p0 += 32) {
-            uint4 rec = make_uint4(0, 0, 0, 0);
-            if (p0 + lane < places_to) rec = __ldcg(&p.place[p0 + lane]);
-            const int len = rec.y & EMB_LEN;
-            int end = len;
+        const int len = rec.y & EMB_LEN;
+        int end = len;
 #pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const int n = __shfl_up_sync(0xffffffffu, end, off);
-                if (lane >= off) end += n;
-            }
-            const int rows = __shfl_sync(0xffffffffu, end, 31), start = end - len;
-            const unsigned pieces = __ballot_sync(0xffffffffu, len > 0), before_lane = (1u << lane) - 1;
-            if (len > 0)
-                list[warp][__popc(pieces & before_lane)] = {static_cast<int>(p0) + lane, static_cast<int>(rec.x),
-                                                            static_cast<int>(rec.y & (EMB_LEN | EMB_MANY)), start};
-            __syncwarp();
-            for (int r0 = 0; r0 < rows; r0 += 32) {
-                // lane l: row r0 + l, its piece (the o-th) and its token
-                const unsigned starts = __reduce_or_sync(0xffffffffu, len > 0 && start >= r0 && start < r0 + 32 ? 1u << (start - r0) : 0u);
-                const int o = __popc(__ballot_sync(0xffffffffu, len > 0 && start < r0)) + __popc(starts & (before_lane * 2 + 1)) - 1;
-                int token = 0;
-                bool at_end = false;
-                if (r0 + lane < rows) {
-                    const Item& it = list[warp][o];
-                    const int r = r0 + lane - it.start;
-                    token = __ldcg(&p.order[it.place + r]);
-                    at_end = r + 1 == static_cast<int>(it.len & EMB_LEN);
-                }
-                const unsigned ends = __ballot_sync(0xffffffffu, at_end);
-                const int n = rows - r0 < 32 ? rows - r0 : 32;
-                for (int j = 0; j < n; j += U) {
-                    uint4 row[U][NV];
-                    EmbedOld<FP32> old[ACC ? U : 1][NV];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const uint4* from = dy + static_cast<long long>(__shfl_sync(0xffffffffu, token, (j + u) & 31)) * vpr;
-                        const int ou = __shfl_sync(0xffffffffu, o, (j + u) & 31);
-#pragma unroll
-                        for (int v = 0; v < NV; ++v)
-                            if (j + u < n && in[v]) {
-                                row[u][v] = __ldcg(from + 32 * v);
-                                if (ACC && (ends >> (j + u) & 1)) emb_old(p, static_cast<long long>(list[warp][ou].key) * vpr + c0 + 32 * v, old[ACC ? u : 0][v]);
-                            }
-                    }
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        if (j + u >= n) break;
-#pragma unroll
-                        for (int v = 0; v < NV; ++v) emb_add(sum[v], row[u][v]);
-                        const int ou = __shfl_sync(0xffffffffu, o, j + u);
-                        if (!(ends >> (j + u) & 1)) continue;
-                        const Item it = list[warp][ou];
-#pragma unroll
-                        for (int v = 0; v < NV; ++v) {
-                            if (in[v] && (it.len & EMB_MANY)) {
-                                float4* to = reinterpret_cast<float4*>(p.part + emb_slot(it.place, it.len & EMB_LEN) * p.H) + 2 * (c0 + 32 * v);
-                                to[0] = make_float4(sum[v][0], sum[v][1], sum[v][2], sum[v][3]);
-                                to[1] = make_float4(sum[v][4], sum[v][5], sum[v][6], sum[v][7]);
-                            } else if (in[v]) {
-                                emb_store<FP32, ACC>(p, static_cast<long long>(it.key) * vpr + c0 + 32 * v, sum[v], old[ACC ? u : 0][v]);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) sum[v][e] = 0.0f;
-                        }
-                    }
-                }
-            }
-            __syncwarp();
+        for (int off = 1; off < 32; off <<= 1) {
+            const int n = __shfl_up_sync(0xffffffffu, end, off);
+            if (lane >= off) end += n;
         }
+        const int rows = __shfl_sync(0xffffffffu, end, 31), start = end - len;
+        const unsigned pieces = __ballot_sync(0xffffffffu, len > 0), before_lane = (1u << lane) - 1;
+        if (len > 0)
+            list[warp][__popc(pieces & before_lane)] = {static_cast<int>(p0) + lane, static_cast<int>(rec.x),
+                                                        static_cast<int>(rec.y & (EMB_LEN | EMB_MANY)), start};
+        __syncwarp();
+        for (int r0 = 0; r0 < rows; r0 += 32) {
+            // lane l: row r0 + l, its piece (the o-th) and its token
+            const unsigned starts = __reduce_or_sync(0xffffffffu, len > 0 && start >= r0 && start < r0 + 32 ? 1u << (start - r0) : 0u);
+            const int o = __popc(__ballot_sync(0xffffffffu, len > 0 && start < r0)) + __popc(starts & (before_lane * 2 + 1)) - 1;
+            int token = 0;
+            bool at_end = false;
+            if (r0 + lane < rows) {
+                const Item& it = list[warp][o];
+                const int r = r0 + lane - it.start;
+                token = __ldcg(&p.order[it.place + r]);
+                at_end = r + 1 == static_cast<int>(it.len & EMB_LEN);
+            }
+            const unsigned ends = __ballot_sync(0xffffffffu, at_end);
+            const int n = rows - r0 < 32 ? rows - r0 : 32;
+            for (int j = 0; j < n; j += U) {
+                uint4 row[U][NV];
+                EmbedOld<FP32> old[ACC ? U : 1][NV];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const uint4* from = dy + static_cast<long long>(__shfl_sync(0xffffffffu, token, (j + u) & 31)) * vpr;
+                    const int ou = __shfl_sync(0xffffffffu, o, (j + u) & 31);
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+                        if (j + u < n && in[v]) {
+                            row[u][v] = __ldcg(from + 32 * v);
+                            if (ACC && (ends >> (j + u) & 1)) emb_old(p, static_cast<long long>(list[warp][ou].key) * vpr + c0 + 32 * v, old[ACC ? u : 0][v]);
+                        }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (j + u >= n) break;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) emb_add(sum[v], row[u][v]);
+                    const int ou = __shfl_sync(0xffffffffu, o, j + u);
+                    if (!(ends >> (j + u) & 1)) continue;
+                    const Item it = list[warp][ou];
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        if (in[v] && (it.len & EMB_MANY)) {
+                            float4* to = reinterpret_cast<float4*>(p.part + emb_slot(it.place, it.len & EMB_LEN) * p.H) + 2 * (c0 + 32 * v);
+                            to[0] = make_float4(sum[v][0], sum[v][1], sum[v][2], sum[v][3]);
+                            to[1] = make_float4(sum[v][4], sum[v][5], sum[v][6], sum[v][7]);
+                        } else if (in[v]) {
+                            emb_store<FP32, ACC>(p, static_cast<long long>(it.key) * vpr + c0 + 32 * v, sum[v], old[ACC ? u : 0][v]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[v][e] = 0.0f;
+                    }
+                }
+            }
+        }
+        __syncwarp();
     }
     if (!ACC && warp == 0) tma_store_wait_all();
     pdl_launch_dependents();
@@ -565,7 +641,7 @@ __global__ void __launch_bounds__(EMB_FOLD_WARPS * 32) embed_fold_kernel(const E
 static size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 size_t embed_bwd_bytes(int64_t T, int, int H) {
     const size_t n = static_cast<size_t>(T);
-    return align16(4 * n) + 16 * n + (T > EMB_CHIP_TOKENS ? 2 * 8 * n : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;
+    return align16(4 * n) + 16 * n + (T > EMB_CHIP_TOKENS ? 2 * 8 * n : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;      // (16: the counters)
 }
 
 cudaError_t launch_embed(const EmbedParams& p, cudaStream_t stream) {
@@ -575,7 +651,9 @@ cudaError_t launch_embed(const EmbedParams& p, cudaStream_t stream) {
 
 template <bool FP32, bool ACC>
 static cudaError_t launch_embed_sums(const EmbedParams& p, cudaStream_t stream) {
-    cudaError_t e = launch_pdl(embed_sum_kernel<FP32, ACC>, dim3(static_cast<unsigned>(p.sm_count)), EMB_SUM_THREADS, 0, stream, 1, p);
+    const int late = p.T > EMB_RANK_TOKENS && p.sm_count > 2 * EMB_CLUSTER ? EMB_CLUSTER : 0;
+    const size_t marks = ACC ? 0 : (std::min(p.V, EMB_MARK_ROWS) + 31) / 32 * sizeof(uint32_t);
+    cudaError_t e = launch_pdl(embed_sum_kernel<FP32, ACC>, dim3(static_cast<unsigned>(p.sm_count)), EMB_SUM_THREADS, marks, stream, 1, p, late);
     if (e != cudaSuccess || p.T <= EMB_PIECE) return e;
     const unsigned blocks = static_cast<unsigned>((p.T + EMB_FOLD_WARPS * 32 - 1) / (EMB_FOLD_WARPS * 32));
     return launch_pdl(embed_fold_kernel<FP32, ACC>, dim3(blocks, (p.H / 8 + 31) / 32), EMB_FOLD_WARPS * 32, 0, stream, 1, p);
@@ -583,6 +661,8 @@ static cudaError_t launch_embed_sums(const EmbedParams& p, cudaStream_t stream) 
 
 cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
     char* at = static_cast<char*>(ws);
+    p.tickets = reinterpret_cast<int*>(at);
+    at += 16;
     p.place = reinterpret_cast<uint4*>(at);
     at += 16 * p.T;
     const bool on_chip = p.T <= EMB_CHIP_TOKENS;
@@ -593,19 +673,28 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
     cudaError_t e = cudaSuccess;
     if (p.T > EMB_RANK_TOKENS) {
         static DeviceOnce configured;
-        const size_t base = sizeof(EmbedSortSmem), list = 2ull * sizeof(uint2) * EMB_SORT_WARPS;      // per element of a stretch
         e = configured.run([&]() {
-            const cudaError_t e1 = cudaFuncSetAttribute(embed_sort_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                        static_cast<int>(base + list * emb_stretch(EMB_CHIP_TOKENS)));
-            return e1 != cudaSuccess ? e1 : cudaFuncSetAttribute(embed_sort_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                                 static_cast<int>(base));
+            cudaError_t r = cudaSuccess;
+            auto allow = [&](auto kern, int nw) {
+                if (r == cudaSuccess)
+                    r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(emb_sort_smem(nw)));
+            };
+            allow(embed_sort_kernel<0>, 0);
+            allow(embed_sort_kernel<1>, 1);
+            allow(embed_sort_kernel<2>, 2);
+            allow(embed_sort_kernel<4>, 4);
+            allow(embed_sort_kernel<8>, 8);
+            return r;
         });
         if (e != cudaSuccess) return e;
         int bits = 1;
         while (p.V >> bits) ++bits;                          // keys are 0 .. V
         const int passes = (bits + 8) / 9, digit_bits = (bits + passes - 1) / passes;
-        e = launch_pdl(on_chip ? embed_sort_kernel<true> : embed_sort_kernel<false>, dim3(EMB_CLUSTER), EMB_SORT_THREADS,
-                       base + (on_chip ? list * emb_stretch(static_cast<int>(p.T)) : 0), stream, EMB_CLUSTER, p, passes, digit_bits);
+        const long long windows = (p.T + EMB_CHIP_TOKENS / 8 - 1) / (EMB_CHIP_TOKENS / 8);       // per warp
+        const int nw = !on_chip ? 0 : windows <= 1 ? 1 : windows <= 2 ? 2 : windows <= 4 ? 4 : 8;
+        auto kern = nw == 0 ? embed_sort_kernel<0> : nw == 1 ? embed_sort_kernel<1> : nw == 2 ? embed_sort_kernel<2>
+                  : nw == 4 ? embed_sort_kernel<4> : embed_sort_kernel<8>;
+        e = launch_pdl(kern, dim3(EMB_CLUSTER), EMB_SORT_THREADS, emb_sort_smem(nw), stream, EMB_CLUSTER, p, passes, digit_bits);
     } else if (p.T > 0) {
         e = launch_pdl(embed_rank_kernel, dim3(static_cast<unsigned>((p.T + 31) / 32)), EMB_RANK_WARPS * 32, 0, stream, 1, p);
     }

@@ -217,6 +217,7 @@ struct EmbedParams {
     int32_t* order;              // scratch [T]: tokens by id, equal ids by position
     uint4* place;                // scratch [T]: what begins at a place of that order (tik_embed.cu)
     uint2* keys[2];              // scratch [T] each: (id, token) between the passes of the sort
+    int* tickets;                // scratch [2]: shares of the zeros and of the sums taken so far
     float* part;                 // scratch [2 (T / 32 + 1)][H]: sums of a long run's pieces
     int sm_count;
     int* dev_status;
