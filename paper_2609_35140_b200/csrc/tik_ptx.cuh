@@ -203,6 +203,10 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, uint32_t src,
 __device__ __forceinline__ void bulk_store(void* dst, uint32_t src, int bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
 }
+// L2 prefetch of a stretch of memory; address and size are multiples of 16 bytes.
+__device__ __forceinline__ void bulk_prefetch_l2(const void* src, int bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
 // at most one bulk store group of this thread is still reading its shared-memory source
 __device__ __forceinline__ void tma_store_wait_read1() {
     asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
