@@ -885,6 +885,7 @@ tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, co
     p.d_post_weight = d_post_weight;
     p.d_gate = d_gate;
     p.part = static_cast<float*>(ws);
+    p.dev_status = ctx->dev_status;
     cudaError_t e = launch_block_norm_bwd(p, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_block_norm_bwd");
 }

@@ -246,7 +246,8 @@ struct BlockNormParams {
     __nv_bfloat16* d_x;          // [T][H] or null
     __nv_bfloat16* d_residual;   // [T][H]
     float *d_weight, *d_post_weight, *d_gate;
-    float* part;                 // scratch [CTAs][2][H]: sums over a CTA's tokens
+    float* part;                 // scratch [2][CTAs][H]: sums over a CTA's tokens
+    int* dev_status;
 };
 size_t block_norm_bwd_bytes(int64_t T, int H);
 cudaError_t launch_block_norm(const BlockNormParams& p, cudaStream_t stream);
