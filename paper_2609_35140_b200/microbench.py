@@ -10,6 +10,9 @@ median and minimum, the algorithmic work and the resulting rate.
   python -m paper_2609_35140_b200.microbench decode  --seqs 16 --len 16384 --hq 32 --hkv 8
   python -m paper_2609_35140_b200.microbench logprob --rows 64 --hidden 3584 --vocab 152064
   python -m paper_2609_35140_b200.microbench linear  --rows 64 --hidden 3584 --out 18944
+  python -m paper_2609_35140_b200.microbench embed_bwd --rows 16001 --hidden 3584 --vocab 152064      (also embed)
+  python -m paper_2609_35140_b200.microbench norm_bwd  --rows 16001 --hidden 3584                     (also norm)
+  python -m paper_2609_35140_b200.microbench clip      --rows 100000 --hidden 3584                    (rows x hidden elements)
 """
 from __future__ import annotations
 
@@ -144,6 +147,30 @@ def run(a) -> dict:
         out.update(shape={"rows": a.rows, "hidden": a.hidden, "out": n_out}, flops=fl, weight_bytes=byt,
                    tflops=fl / (med * 1e-3) / 1e12, weight_gbs=byt / (med * 1e-3) / 1e9,
                    weight_gbs_best=byt / (mn * 1e-3) / 1e9)
+    elif a.case in ("embed", "embed_bwd", "norm", "norm_bwd", "clip"):
+        gen = torch.Generator(device=dev).manual_seed(4321)
+        make = lambda *shape, std=1.0: synth._randn_bf16(shape, gen, dev, std=std, chunk_rows=1 << 14)
+        T, H, V = a.rows, a.hidden, a.vocab
+        if a.case in ("embed", "embed_bwd"):
+            ids = torch.randint(0, V, (T,), generator=gen, device=dev).to(torch.int32)
+            x, table = make(T, H), make(V, H, std=0.02) if a.case == "embed" else torch.empty(V, H, dtype=torch.bfloat16, device=dev)
+            fn = (lambda: tik.tik_embedding(ids, table, y=x)) if a.case == "embed" else (lambda: tik.tik_embedding_bwd(x, ids, V, d_table=table))
+            byt = 4.0 * T * H if a.case == "embed" else 2.0 * (T + V) * H
+        elif a.case == "clip":
+            grads = [make(T, H, std=1e-3)]
+            out_t = [torch.empty_like(g) for g in grads]
+            fn = lambda: tik.tik_grad_clip(grads, 1e-3, out=out_t)
+            byt = 6.0 * T * H
+        else:
+            x, s, dy, ds = (make(T, H) for _ in range(4))
+            w, post, gate = (make(1, H)[0] for _ in range(3))
+            if a.case == "norm":
+                fn = lambda: tik.tik_block_norm(x, s, w, 1e-6, post_weight=post, gate=gate, s=ds, y=dy)
+            else:
+                fn = lambda: tik.tik_block_norm_bwd(dy, ds, x, s, w, 1e-6, post_weight=post, gate=gate)
+            byt = (8.0 if a.case == "norm" else 12.0) * T * H
+        med, mn = _time(fn, a.reps, a.warmup, flush)
+        out.update(shape={"rows": T, "hidden": H, "vocab": V}, bytes=byt, gbs=byt / (med * 1e-3) / 1e9, gbs_best=byt / (mn * 1e-3) / 1e9)
     else:
         raise SystemExit("unknown case " + a.case)
     out.update(ms=med, ms_best=mn, reps=a.reps, device_flags=tik.device_status())
@@ -152,7 +179,8 @@ def run(a) -> dict:
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    ap.add_argument("case", choices=["train", "prefill", "decode", "logprob", "linear"])
+    ap.add_argument("case", choices=["train", "prefill", "decode", "logprob", "linear", "embed", "embed_bwd", "norm",
+                                     "norm_bwd", "clip"])
     ap.add_argument("--seqs", type=int, default=1)
     ap.add_argument("--len", type=int, default=4096)
     ap.add_argument("--lens", default="", help="comma-separated lengths (overrides --seqs/--len)")
