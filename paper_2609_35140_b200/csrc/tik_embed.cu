@@ -19,19 +19,36 @@ __device__ __forceinline__ uint4 scaled8(uint4 v, float scale) {
     return pack8(f);
 }
 
-// y[t] = scale * table[ids[t]]: one 16-byte vector per thread.
-__global__ void __launch_bounds__(EMB_THREADS) embed_kernel(const EmbedParams p) {
+// y[t] = scale * table[ids[t]]; 16-byte vectors, VPT per thread (a block covers 256 * VPT consecutive ones).  A vector is two
+// loads one behind the other, id and row, so large calls have four of each in flight per thread (8191 x 4096: 23.6 us with
+// one, MEASURED with four); small calls take one, which spreads them over more blocks.
+constexpr unsigned EMB_VEC_MAX = 0xfffff000u;                // vectors per launch: 32-bit indices
+template <int VPT>
+__global__ void __launch_bounds__(EMB_THREADS) embed_kernel(const EmbedParams p, unsigned nvec, unsigned vpr) {
+    const unsigned base = blockIdx.x * (EMB_THREADS * VPT) + threadIdx.x;
     pdl_wait();
     pdl_launch_dependents();
-    const int vpr = p.H / 8;
-    const long long i = static_cast<long long>(blockIdx.x) * EMB_THREADS + threadIdx.x;
-    if (i >= p.T * vpr) return;
-    const long long t = i / vpr;
-    const int c = static_cast<int>(i - t * vpr), id = p.ids[t];
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (id >= 0 && id < p.V) v = scaled8(reinterpret_cast<const uint4*>(p.table)[static_cast<long long>(id) * vpr + c], p.scale);
-    else if (c == 0) atomicOr(p.dev_status, TIK_DEV_BAD_TOKEN);
-    reinterpret_cast<uint4*>(p.y)[i] = v;
+    uint4 v[VPT];
+    int id[VPT];
+    unsigned c[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const unsigned i = base + EMB_THREADS * j, t = i / vpr;
+        c[j] = i - t * vpr;
+        id[j] = i < nvec ? p.ids[t] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        v[j] = make_uint4(0, 0, 0, 0);
+        if (id[j] >= 0 && id[j] < p.V) v[j] = reinterpret_cast<const uint4*>(p.table)[static_cast<size_t>(id[j]) * vpr + c[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const unsigned i = base + EMB_THREADS * j;
+        if (i >= nvec) break;
+        if (c[j] == 0 && (id[j] < 0 || id[j] >= p.V)) atomicOr(p.dev_status, TIK_DEV_BAD_TOKEN);
+        reinterpret_cast<uint4*>(p.y)[i] = scaled8(v[j], p.scale);
+    }
 }
 
 // ---- gradient --------------------------------------------------------------------------------
@@ -640,9 +657,19 @@ size_t embed_bwd_bytes(int64_t T, int, int H) {
     return align16(4 * n) + 16 * n + (T > EMB_CHIP_TOKENS ? 2 * 8 * n : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;      // (16: the counters)
 }
 
-cudaError_t launch_embed(const EmbedParams& p, cudaStream_t stream) {
-    const long long n = p.T * (p.H / 8);
-    return launch_pdl(embed_kernel, dim3(static_cast<unsigned>((n + EMB_THREADS - 1) / EMB_THREADS)), EMB_THREADS, 0, stream, 1, p);
+cudaError_t launch_embed(const EmbedParams& p0, cudaStream_t stream) {
+    EmbedParams p = p0;
+    const unsigned vpr = p.H / 8;
+    // a launch takes as many rows as 32-bit vector indices count
+    for (long long rows, left = p.T; left > 0; left -= rows, p.ids += rows, p.y += rows * p.H) {
+        rows = std::min<long long>(left, EMB_VEC_MAX / vpr);
+        const unsigned n = static_cast<unsigned>(rows * vpr);
+        const bool large = n >= (1u << 20);
+        const unsigned per = EMB_THREADS * (large ? 4 : 1);
+        const cudaError_t e = launch_pdl(large ? embed_kernel<4> : embed_kernel<1>, dim3((n - 1) / per + 1), EMB_THREADS, 0, stream, 1, p, n, vpr);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 template <bool FP32, bool ACC>

@@ -13,7 +13,10 @@ namespace tik {
 constexpr int GRAD_THREADS = 256;
 constexpr int GRAD_VEC = 8;                                  // 16-byte vectors per thread and chunk
 constexpr int GRAD_CHUNK = GRAD_THREADS * GRAD_VEC;          // vectors of a chunk: 32 KiB
+// Four CTAs on an SM, and shared memory that nothing uses to keep it at four: with the slots that registers leave, the CTAs of a call
+// that starts as its predecessor drains pile up, five on some SMs and three on others, and each has an even share of the list.
 constexpr int GRAD_CTAS = 592;
+constexpr size_t GRAD_SMEM = 46 * 1024;
 
 // The list travels as a kernel parameter: nothing to copy, and a captured graph holds it.
 struct GradEntry {
@@ -40,13 +43,16 @@ struct GradChunk {
     int fp32;
 };
 template <int CAP>
-__device__ __forceinline__ GradChunk grad_chunk(const GradList<CAP>& l, unsigned c) {
-    int lo = 0, hi = l.n;                                    // the last tensor with first <= c (empty ones take no chunk)
+__device__ __forceinline__ GradChunk grad_chunk(const GradList<CAP>& l, unsigned c, int& at) {
+    // the last tensor with first <= c (empty ones take no chunk): mostly the one of the CTA's chunk before, `at`
+    int lo = l.e[at].first <= c ? at : 0, hi = l.n;
+    if (lo + 1 < hi && l.e[lo + 1].first > c) hi = lo + 1;
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (l.e[mid].first <= c) lo = mid;
         else hi = mid;
     }
+    at = lo;
     const GradEntry& e = l.e[lo];
     GradChunk g;
     g.in = static_cast<const char*>(e.in);
@@ -126,8 +132,9 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_norm_kernel(const __grid_co
     pdl_wait();
     pdl_launch_dependents();
     double sum = 0.0;
+    int tensor = 0;
     for (unsigned c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-        const GradChunk g = grad_chunk(l, c);
+        const GradChunk g = grad_chunk(l, c, tensor);
         const uint4* src = reinterpret_cast<const uint4*>(g.in + g.head * (g.fp32 ? 4 : 2)) + g.first_vec;
         uint4 v[GRAD_VEC];
 #pragma unroll
@@ -159,7 +166,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_fold_kernel(const double* p
 
 template <int CAP>
 __global__ void __launch_bounds__(GRAD_THREADS) grad_clip_kernel(const __grid_constant__ GradList<CAP> l, const double* part, int nparts,
-                                                                 float* norm, float max_norm) {
+                                                                 float* norm, float max_norm, bool in_place) {
     __shared__ double buf[GRAD_THREADS / 32];
     const int tid = threadIdx.x;
     pdl_wait();
@@ -173,8 +180,11 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_clip_kernel(const __grid_co
     }
     const bool clip = v > max_norm && v <= 3.402823466e38f;
     const float coef = clip ? __fdiv_rn(max_norm, v) : 1.0f;
-    for (unsigned c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-        const GradChunk g = grad_chunk(l, c);
+    if (!clip && in_place) return;
+    // Back to front: what the norm read last may still be in L2.
+    int tensor = l.n - 1;
+    for (unsigned i = blockIdx.x; i < l.chunks; i += gridDim.x) {
+        const GradChunk g = grad_chunk(l, l.chunks - 1 - i, tensor);
         if (!clip && g.out == g.in) continue;
         const int size = g.fp32 ? 4 : 2;
         const uint4* src = reinterpret_cast<const uint4*>(g.in + g.head * size) + g.first_vec;
@@ -185,8 +195,8 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_clip_kernel(const __grid_co
         for (int j = 0; j < GRAD_VEC; ++j) if (tid + GRAD_THREADS * j < g.vecs) v[j] = src[tid + GRAD_THREADS * j];
 #pragma unroll
         for (int j = 0; j < GRAD_VEC; ++j) {
-            const int i = tid + GRAD_THREADS * j;
-            if (i >= g.vecs) break;
+            const int at = tid + GRAD_THREADS * j;
+            if (at >= g.vecs) break;
             unsigned w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
             if (clip) {
 #pragma unroll
@@ -194,7 +204,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_clip_kernel(const __grid_co
                     w[k] = g.fp32 ? __float_as_uint(__fmul_rn(__uint_as_float(w[k]), coef))
                                   : pack_bf16x2(__fmul_rn(__uint_as_float(w[k] << 16), coef), __fmul_rn(__uint_as_float(w[k] & 0xffff0000u), coef));
             }
-            char* to = dst + 16ll * i;
+            char* to = dst + 16ll * at;
             if (whole) {
                 *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
             } else if (g.fp32) {
@@ -205,11 +215,11 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_clip_kernel(const __grid_co
                 for (int k = 0; k < 8; ++k) reinterpret_cast<unsigned short*>(to)[k] = static_cast<unsigned short>(w[k / 2] >> (16 * (k & 1)));
             }
         }
-        const long long i = grad_end(g, tid);
-        if (i >= 0) {
-            const float f = grad_element(g, i), r = clip ? __fmul_rn(f, coef) : f;
-            if (g.fp32) reinterpret_cast<float*>(g.out)[i] = r;
-            else reinterpret_cast<__nv_bfloat16*>(g.out)[i] = __float2bfloat16_rn(r);
+        const long long end = grad_end(g, tid);
+        if (end >= 0) {
+            const float f = grad_element(g, end), r = clip ? __fmul_rn(f, coef) : f;
+            if (g.fp32) reinterpret_cast<float*>(g.out)[end] = r;
+            else reinterpret_cast<__nv_bfloat16*>(g.out)[end] = __float2bfloat16_rn(r);
         }
     }
 }
@@ -238,6 +248,7 @@ static cudaError_t for_lists(const void* const* grads, void* const* out, const i
     }
     return cudaSuccess;
 }
+static size_t grad_smem(int ctas) { return ctas < GRAD_CTAS ? 0 : GRAD_SMEM; }
 static GradList<GRAD_CAP_SMALL> small_list(const GradList<GRAD_CAP>& l) {
     GradList<GRAD_CAP_SMALL> s;
     std::copy(l.e, l.e + l.n, s.e);
@@ -252,8 +263,8 @@ static cudaError_t launch_squares(const void* const* grads, const int64_t* numel
     return for_lists(grads, nullptr, numel, dtypes, n, [&](const GradList<GRAD_CAP>& l, int ctas) {
         double* to = part + *parts;
         *parts += ctas;
-        return l.n <= GRAD_CAP_SMALL ? launch_pdl(grad_norm_kernel<GRAD_CAP_SMALL>, dim3(ctas), GRAD_THREADS, 0, stream, 1, small_list(l), to)
-                                     : launch_pdl(grad_norm_kernel<GRAD_CAP>, dim3(ctas), GRAD_THREADS, 0, stream, 1, l, to);
+        return l.n <= GRAD_CAP_SMALL ? launch_pdl(grad_norm_kernel<GRAD_CAP_SMALL>, dim3(ctas), GRAD_THREADS, grad_smem(ctas), stream, 1, small_list(l), to)
+                                     : launch_pdl(grad_norm_kernel<GRAD_CAP>, dim3(ctas), GRAD_THREADS, grad_smem(ctas), stream, 1, l, to);
     });
 }
 
@@ -276,8 +287,8 @@ cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const i
     const double* from = norm_known ? nullptr : part;
     return for_lists(grads, out, numel, dtypes, n, [&](const GradList<GRAD_CAP>& l, int ctas) {
         return l.n <= GRAD_CAP_SMALL
-                   ? launch_pdl(grad_clip_kernel<GRAD_CAP_SMALL>, dim3(ctas), GRAD_THREADS, 0, stream, 1, small_list(l), from, parts, norm, max_norm)
-                   : launch_pdl(grad_clip_kernel<GRAD_CAP>, dim3(ctas), GRAD_THREADS, 0, stream, 1, l, from, parts, norm, max_norm);
+                   ? launch_pdl(grad_clip_kernel<GRAD_CAP_SMALL>, dim3(ctas), GRAD_THREADS, grad_smem(ctas), stream, 1, small_list(l), from, parts, norm, max_norm, out == nullptr)
+                   : launch_pdl(grad_clip_kernel<GRAD_CAP>, dim3(ctas), GRAD_THREADS, grad_smem(ctas), stream, 1, l, from, parts, norm, max_norm, out == nullptr);
     });
 }
 
