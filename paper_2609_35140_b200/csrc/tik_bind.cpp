@@ -357,6 +357,15 @@ void want_sizes(const at::Tensor* t, at::IntArrayRef sizes, const char* what) {
     if (t) want_sizes(*t, sizes, what);
 }
 
+// A contiguous tensor over a part of another one's storage, `at` elements in (a view without the dispatcher: ~0.1 us of host
+// time where an allocation takes 0.8).
+at::Tensor part_of(const at::Tensor& whole, int64_t at, at::IntArrayRef sizes) {
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+    impl->set_storage_offset(whole.storage_offset() + at);
+    impl->set_sizes_contiguous(sizes);
+    return at::Tensor(std::move(impl));
+}
+
 PyObject* embedding(Args a) {
     const int dev = current_device();
     tik_ctx* ctx = context(dev);
@@ -474,9 +483,14 @@ PyObject* block_norm_bwd(Args a) {
     at::Tensor made[5];
     made[1] = empty({T, H}, at::kBFloat16, s);
     if (x) made[0] = empty({T, H}, at::kBFloat16, s);
-    if (w) made[2] = empty({H}, at::kFloat, s);
-    if (post) made[3] = empty({H}, at::kFloat, s);
-    if (gate) made[4] = empty(gate->sizes(), at::kFloat, s);
+    // the fp32 gradients are parts of one allocation, each at a multiple of 16 bytes
+    const int64_t need[3] = {w ? H : 0, post ? H : 0, gate ? gate->numel() : 0};
+    if (w || post || gate) {
+        const at::Tensor whole = empty({need[0] + need[1] + need[2]}, at::kFloat, s);
+        if (w) made[2] = part_of(whole, 0, {H});
+        if (post) made[3] = part_of(whole, need[0], {H});
+        if (gate) made[4] = part_of(whole, need[0] + need[1], gate->sizes());
+    }
     auto opt = [](const at::Tensor& t) { return t.defined() ? &t : nullptr; };
     void *dyp = bf(dy), *dsp = bf(ds), *xp = bf(x), *sp = bf(s), *wp = bf(w), *pp = bf(post), *gp = bf(gate), *dxp = bf(opt(made[0])),
          *drp = bf(made[1]), *st = stream();
@@ -517,30 +531,41 @@ struct GradArgs {
     }
 };
 
-// the norm's own tensor: given or made
-const at::Tensor& norm_of(const at::Tensor* given, at::Tensor& made, int device) {
-    if (given) {
-        want_sizes(*given, {1}, "norm");
-        return *given;
+// The norm's own tensor and the scratch of a gradient call, given or made; both made are parts of one allocation.
+struct GradNorm {
+    at::Tensor made;
+    float* norm = nullptr;
+    Scratch ws;
+    GradNorm(const at::Tensor* norm_in, const at::Tensor* ws_in, int n, int device, bool scratch) {
+        const size_t need = scratch ? tik_workspace_bytes(TIK_OP_GRAD_NORM, n, 0, 0, 0, 0, 0, 0) : 0;
+        if (ws_in) ws.use(*ws_in);
+        if (norm_in) {
+            want_sizes(*norm_in, {1}, "norm");
+            norm = f32(norm_in);
+            if (!ws_in && need > 0) ws.make(need, *norm_in);
+            return;
+        }
+        constexpr int64_t SKIP = 4;                          // floats, so that the scratch keeps its alignment
+        const at::Tensor whole = at::detail::empty_cuda({SKIP + (ws_in ? 0 : static_cast<int64_t>(need / sizeof(float)))}, at::kFloat,
+                                                        at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)), std::nullopt);
+        made = part_of(whole, 0, {1});
+        norm = f32(&made);
+        if (!ws_in) {
+            ws.p = norm + SKIP;
+            ws.bytes = need;
+        }
     }
-    return made = at::detail::empty_cuda({1}, at::kFloat, at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)), std::nullopt);
-}
-Scratch grad_ws(const at::Tensor* given, int n, const at::Tensor& like) {
-    return sized_ws(given, tik_workspace_bytes(TIK_OP_GRAD_NORM, n, 0, 0, 0, 0, 0, 0), like);
-}
+};
 
 PyObject* grad_norm(Args a) {
     const int dev = current_device();
     tik_ctx* ctx = context(dev);
     const GradArgs g(a.next(), dev);
     const at::Tensor *norm_in = on(dev, a.opt()), *ws_in = on(dev, a.opt());
-    at::Tensor made;
-    const at::Tensor& norm = norm_of(norm_in, made, dev);
-    const Scratch ws = grad_ws(ws_in, g.n, norm);
-    float* np = f32(&norm);
+    GradNorm n(norm_in, ws_in, g.n, dev, true);
     void* st = stream();
-    check(unlocked([&] { return tik_grad_norm(ctx, g.ptrs.data(), g.numel.data(), g.types.data(), g.n, np, ws.p, ws.bytes, st); }), ctx);
-    return wrap(norm_in, made);
+    check(unlocked([&] { return tik_grad_norm(ctx, g.ptrs.data(), g.numel.data(), g.types.data(), g.n, n.norm, n.ws.p, n.ws.bytes, st); }), ctx);
+    return wrap(norm_in, n.made);
 }
 
 PyObject* grad_clip(Args a) {
@@ -557,15 +582,11 @@ PyObject* grad_clip(Args a) {
         if (out.numel != g.numel || out.types != g.types) raise(PyExc_ValueError, "out has other types or sizes than grads");
         to.swap(out.ptrs);
     }
-    at::Tensor made;
-    const at::Tensor& norm = norm_of(norm_in, made, dev);
-    Scratch ws;
-    if (!norm_in || ws_in) ws = grad_ws(ws_in, g.n, norm);
-    float* np = f32(&norm);
+    GradNorm n(norm_in, ws_in, g.n, dev, norm_in == nullptr);
     void* st = stream();
     check(unlocked([&] { return tik_grad_clip(ctx, g.ptrs.data(), out_list != Py_None ? to.data() : nullptr, g.numel.data(), g.types.data(),
-                                              g.n, max_norm, np, norm_in != nullptr, ws.p, ws.bytes, st); }), ctx);
-    return wrap(norm_in, made);
+                                              g.n, max_norm, n.norm, norm_in != nullptr, n.ws.p, n.ws.bytes, st); }), ctx);
+    return wrap(norm_in, n.made);
 }
 
 PyObject* attn_prefill(Args a) {

@@ -21,7 +21,7 @@ __device__ __forceinline__ uint4 scaled8(uint4 v, float scale) {
 
 // y[t] = scale * table[ids[t]]; 16-byte vectors, VPT per thread (a block covers 256 * VPT consecutive ones).  A vector is two
 // loads one behind the other, id and row, so large calls have four of each in flight per thread (8191 x 4096: 23.6 us with
-// one, MEASURED with four); small calls take one, which spreads them over more blocks.
+// one, 17.8 with four); small calls take one, which spreads them over more blocks.
 constexpr unsigned EMB_VEC_MAX = 0xfffff000u;                // vectors per launch: 32-bit indices
 template <int VPT>
 __global__ void __launch_bounds__(EMB_THREADS) embed_kernel(const EmbedParams p, unsigned nvec, unsigned vpr) {
@@ -651,6 +651,132 @@ __global__ void __launch_bounds__(EMB_FOLD_WARPS * 32) embed_fold_kernel(const E
     }
 }
 
+// Calls of at most EMB_SMALL_TOKENS tokens whose zeros are little work: one launch and no sort.  A warp takes a token and 256
+// columns, finds the tokens of the same id by comparing, and, if its own is the first of them, adds up their rows.  A run of
+// several pieces waits until the CTA is through with the others and then gets a warp per piece; eight pieces at most are added
+// up in the order of embed_fold_kernel.  256 tokens x 256, vocabulary 2048: 8.9 us by the three kernels, 3.0 by this one.
+constexpr int EMB_SMALL_TOKENS = EMB_FOLD_WARPS * EMB_PIECE, EMB_SMALL_WORDS = EMB_SMALL_TOKENS / 32;
+constexpr long long EMB_SMALL_BYTES = 32 << 20;              // of the table, where it is written whole
+constexpr int EMB_SMALL_ROWS = 1 << 16;                      // rows of a CTA's share of the zeros
+constexpr int EMB_QUEUE = 32;
+template <bool FP32, bool ACC>
+__global__ void __launch_bounds__(EMB_SUM_THREADS) embed_small_kernel(const EmbedParams p) {
+    __shared__ int keys[EMB_SMALL_TOKENS];
+    __shared__ short runs[EMB_SUM_WARPS][EMB_SMALL_TOKENS];  // a warp's run: its tokens
+    __shared__ int queue[EMB_QUEUE], queued;                 // items with a long run
+    __shared__ float sums[EMB_FOLD_WARPS][8][32];
+    __shared__ uint32_t present[ACC ? 1 : EMB_SMALL_ROWS / 32];
+    __shared__ alignas(16) uint4 zeros[ACC ? 1 : EMB_ZEROS / 16];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, T = static_cast<int>(p.T), vpr = p.H / 8;
+    const long long row_bytes = static_cast<long long>(p.H) * (FP32 ? 4 : 2);
+    const int share = (p.V + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), row0 = share * blockIdx.x;
+    const int rows = ACC ? 0 : min(share, p.V - row0);
+    if (!ACC) {
+        for (int i = tid; i < (rows + 31) / 32; i += EMB_SUM_THREADS) present[i] = 0;
+        for (int i = tid; i < EMB_ZEROS / 16; i += EMB_SUM_THREADS) zeros[i] = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+    }
+    if (tid == 0) queued = 0;
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
+    if (tid < EMB_SMALL_TOKENS) {
+        const int key = tid < T ? emb_key(p, p.ids[tid]) : -1;
+        keys[tid] = key;
+        if (!ACC && key >= row0 && key - row0 < rows) atomicOr(&present[(key - row0) >> 5], 1u << ((key - row0) & 31));
+        if (key == p.V && blockIdx.x == 0) atomicOr(p.dev_status, TIK_DEV_BAD_TOKEN);
+    }
+    __syncthreads();
+    if (!ACC && warp == EMB_SUM_WARPS - 1) {
+        emb_fill_words(static_cast<char*>(p.d_table), row_bytes, smem_u32(zeros), present, row0, rows, 0, (rows + 31) / 32, lane);
+        tma_store_commit();
+    }
+    constexpr int U = 16;                                    // rows in flight
+    const int slices = (vpr + 31) / 32;
+    // the tokens of `token`'s run into runs[warp]; their number, 0 unless it is the first of them
+    auto find = [&](int token) {
+        const int mine = keys[token];
+        int n = 0;
+        bool first = mine != p.V;
+#pragma unroll
+        for (int w = 0; w < EMB_SMALL_WORDS; ++w) {
+            const int i = 32 * w + lane;
+            const unsigned same = __ballot_sync(0xffffffffu, keys[i] == mine);
+            if (i < token && (same >> lane & 1)) first = false;
+            if (same >> lane & 1) runs[warp][n + __popc(same & ((1u << lane) - 1))] = static_cast<short>(i);
+            n += __popc(same);
+        }
+        first = __all_sync(0xffffffffu, first);
+        __syncwarp();
+        return first ? n : 0;
+    };
+    // rows [from, to), 32 at most, of the run
+    auto add_rows = [&](int from, int to, const uint4* column, float (&sum)[8]) {
+        const int token = from + lane < to ? runs[warp][from + lane] : 0;
+        for (int r0 = 0; r0 < to - from; r0 += U) {
+            uint4 row[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const unsigned t = __shfl_sync(0xffffffffu, token, r0 + u);
+                if (column && r0 + u < to - from) row[u] = __ldcg(column + static_cast<size_t>(t) * vpr);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (r0 + u < to - from) emb_add(sum, row[u]);
+        }
+    };
+    auto column_of = [&](int c) { return c < vpr ? reinterpret_cast<const uint4*>(p.d_y) + c : nullptr; };
+    for (int item = warp * gridDim.x + blockIdx.x; item < T * slices; item += EMB_SUM_WARPS * gridDim.x) {
+        const int token = item / slices, c = (item - token * slices) * 32 + lane, n = find(token);
+        if (n > EMB_PIECE) {
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&queued, 1);
+            at = __shfl_sync(0xffffffffu, at, 0);
+            if (at < EMB_QUEUE) {
+                if (lane == 0) queue[at] = item;
+                continue;
+            }
+        }
+        const long long at = static_cast<long long>(keys[token]) * vpr + c;
+        EmbedOld<FP32> old;
+        if (ACC && n > 0 && c < vpr) emb_old(p, at, old);
+        float sum[8];
+        for (int r = 0; r < n; r += EMB_PIECE) {             // (more than one piece: the queue was full)
+            float piece[8] = {};
+            add_rows(r, min(n, r + EMB_PIECE), column_of(c), piece);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = r == 0 ? piece[e] : __fadd_rn(sum[e], piece[e]);
+        }
+        if (n > 0 && c < vpr) emb_store<FP32, ACC>(p, at, sum, old);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int q = 0; q < min(queued, EMB_QUEUE); ++q) {
+        const int item = queue[q], token = item / slices, c = (item - token * slices) * 32 + lane, n = find(token);
+        const int pieces = (n + EMB_PIECE - 1) / EMB_PIECE;
+        float sum[8] = {};
+        if (warp < pieces) add_rows(warp * EMB_PIECE, min(n, (warp + 1) * EMB_PIECE), column_of(c), sum);
+        if (warp < EMB_FOLD_WARPS) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sums[warp][e][lane] = sum[e];
+        }
+        __syncthreads();
+        if (warp == 0 && c < vpr) {
+            const long long at = static_cast<long long>(keys[token]) * vpr + c;
+            EmbedOld<FP32> old;
+            if (ACC) emb_old(p, at, old);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int w = 1; w < EMB_FOLD_WARPS; ++w) sum[e] = __fadd_rn(sum[e], sums[w][e][lane]);
+            }
+            emb_store<FP32, ACC>(p, at, sum, old);
+        }
+        __syncthreads();
+    }
+    if (!ACC && warp == EMB_SUM_WARPS - 1) tma_store_wait_all();
+}
+
 static size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 size_t embed_bwd_bytes(int64_t T, int, int H) {
     const size_t n = static_cast<size_t>(T);
@@ -673,6 +799,10 @@ cudaError_t launch_embed(const EmbedParams& p0, cudaStream_t stream) {
 }
 
 template <bool FP32, bool ACC>
+static cudaError_t launch_embed_small(const EmbedParams& p, cudaStream_t stream) {
+    return launch_pdl(embed_small_kernel<FP32, ACC>, dim3(static_cast<unsigned>(p.sm_count)), EMB_SUM_THREADS, 0, stream, 1, p);
+}
+template <bool FP32, bool ACC>
 static cudaError_t launch_embed_sums(const EmbedParams& p, cudaStream_t stream) {
     const int late = p.T > EMB_RANK_TOKENS && p.sm_count > 2 * EMB_CLUSTER ? EMB_CLUSTER : 0;
     const size_t marks = ACC ? 0 : (std::min(p.V, EMB_MARK_ROWS) + 31) / 32 * sizeof(uint32_t);
@@ -694,6 +824,11 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
     p.order = reinterpret_cast<int32_t*>(at);
     p.part = reinterpret_cast<float*>(at + align16(4 * p.T));
     cudaError_t e = cudaSuccess;
+    const long long table_bytes = static_cast<long long>(p.V) * p.H * (p.fp32 ? 4 : 2);
+    if (p.T > 0 && p.T <= EMB_SMALL_TOKENS && (p.accumulate || (table_bytes <= EMB_SMALL_BYTES && p.V / p.sm_count < EMB_SMALL_ROWS)) &&
+        p.H < (1 << 24))
+        return p.fp32 ? (p.accumulate ? launch_embed_small<true, true>(p, stream) : launch_embed_small<true, false>(p, stream))
+                      : (p.accumulate ? launch_embed_small<false, true>(p, stream) : launch_embed_small<false, false>(p, stream));
     if (p.T > EMB_RANK_TOKENS) {
         static DeviceOnce configured;
         e = configured.run([&]() {
