@@ -2,6 +2,8 @@
 // and its gradient.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "tik_core.cuh"
 #include "tik_internal.h"
 #include "tik_ptx.cuh"
@@ -12,7 +14,11 @@ constexpr int BN_THREADS = 128;
 
 // One CTA per row with the reduction shape of rmsnorm_kernel (NV 16-byte vectors per thread): without post norm and gate
 // and with a scale of 1 the results are those of its residual form, bit for bit.
-template <int NV>
+// FEW (calls of up to BN_FEW_ROWS rows): weights and gate are requested with the row, not when they are needed -- a chain of
+// trips to L2 that many resident rows hide, and that a decode step waits for (call after call on the device, us: 64 x 3584 4.2 without
+// and 2.4 with FEW; 1024 x 3584 5.4 and 5.8; 9001 x 5120 58 and 92: its registers halve the rows on an SM).
+constexpr long long BN_FEW_ROWS = 512;
+template <int NV, bool FEW>
 __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormParams p) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long row = blockIdx.x;
@@ -23,76 +29,95 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
     const uint4* wn = reinterpret_cast<const uint4*>(p.weight);
     __shared__ float tot_x[4], tot_s[4];
     pdl_wait();
-    pdl_launch_dependents();
-    uint4 xv[NV], rv[NV];
+    if (gridDim.x <= 2048 || p.H >= 1536) pdl_launch_dependents();       // (many short rows go without: the rule in tik_ffn.cu)
+    uint4 xv[NV], rv[NV], wpv[FEW ? NV : 1], gv[FEW ? NV : 1], wnv[FEW ? NV : 1];
+    const uint4* gc = p.gate_kind == GATE_CHANNEL ? reinterpret_cast<const uint4*>(p.gate) : nullptr;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int v = tid + BN_THREADS * j;
         if (v < nvec) {
             xv[j] = x[v];
             rv[j] = res[v];
+            if (FEW) {
+                if (wp) wpv[j] = wp[v];
+                if (gc) gv[j] = gc[v];
+                if (wn) wnv[j] = wn[v];
+            }
         }
     }
     const float inv_h = 1.0f / static_cast<float>(p.H);
-    const float gt = p.gate_kind == GATE_TOKEN ? __bfloat162float(p.gate[row]) : 1.0f;
-    float inv_x = 1.0f;
-    if (p.post_weight) {
-        float part = 0.0f;
+    float c = p.branch_scale;                                // what all channels have in common
+    if (p.gate_kind == GATE_TOKEN) c = __fmul_rn(c, __bfloat162float(p.gate[row]));
+    if (wp) {
+        F2 part = f2(0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (tid + BN_THREADS * j < nvec) {
-                float f[8];
-                unpack8(xv[j], f);
+                const uint32_t xw[4] = {xv[j].x, xv[j].y, xv[j].z, xv[j].w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) part = __fmaf_rn(f[e], f[e], part);
+                for (int e = 0; e < 4; ++e) {
+                    const F2 f = f2_bf16(xw[e]);
+                    part = f2_fma(f, f, part);
+                }
             }
-        part = hn_warp_total(part);
-        if (lane == 0) tot_x[warp] = part;
+        const float sum = hn_warp_total(f2_sum(part));
+        if (lane == 0) tot_x[warp] = sum;
         __syncthreads();
-        inv_x = prep_inv_rms(hn_block_total(tot_x), inv_h, p.eps);
+        c = __fmul_rn(c, prep_inv_rms(hn_block_total(tot_x), inv_h, p.eps));
     }
-    float s[NV][8], part = 0.0f;
+    const F2 c2 = f2(c);
+    uint32_t s[NV][4];
+    float part = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int v = tid + BN_THREADS * j;
         if (v >= nvec) continue;
-        float f[8], r[8];
-        unpack8(xv[j], f);
-        unpack8(rv[j], r);
-        if (p.post_weight) {
-            float w[8];
-            unpack8(wp[v], w);
+        const uint32_t xw[4] = {xv[j].x, xv[j].y, xv[j].z, xv[j].w}, rw[4] = {rv[j].x, rv[j].y, rv[j].z, rv[j].w};
+        F2 f[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = prep_norm(f[e], inv_x, w[e]);
+        for (int e = 0; e < 4; ++e) f[e] = f2_mul(f2_bf16(xw[e]), c2);
+        if (wp) {
+            const uint4 w4 = FEW ? wpv[FEW ? j : 0] : wp[v];
+            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = f2_mul(f[e], f2_bf16(w[e]));
         }
-        if (p.gate_kind == GATE_CHANNEL) {
-            float g[8];
-            unpack8(reinterpret_cast<const uint4*>(p.gate)[v], g);
+        if (gc) {
+            const uint4 g4 = FEW ? gv[FEW ? j : 0] : gc[v];
+            const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = __fmul_rn(f[e], g[e]);
+            for (int e = 0; e < 4; ++e) f[e] = f2_mul(f[e], f2_bf16(g[e]));
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[j][e] = __fadd_rn(r[e], __fmul_rn(__fmul_rn(f[e], gt), p.branch_scale));
-        const uint4 packed = pack8(s[j]);
-        reinterpret_cast<uint4*>(p.s)[row * nvec + v] = packed;
-        unpack8(packed, s[j]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part = __fmaf_rn(s[j][e], s[j][e], part);
+        for (int e = 0; e < 4; ++e) {
+            float lo, hi;
+            f2_get(f2_add(f2_bf16(rw[e]), f[e]), lo, hi);
+            s[j][e] = pack_bf16x2(lo, hi);
+            // (one chain in the order of the elements, as rmsnorm_kernel's)
+            f2_get(f2_bf16(s[j][e]), lo, hi);
+            part = __fmaf_rn(hi, hi, __fmaf_rn(lo, lo, part));
+        }
+        reinterpret_cast<uint4*>(p.s)[row * nvec + v] = make_uint4(s[j][0], s[j][1], s[j][2], s[j][3]);
     }
-    if (!p.weight) return;
+    if (!wn) return;
     part = hn_warp_total(part);
     if (lane == 0) tot_s[warp] = part;
     __syncthreads();
-    const float inv_s = prep_inv_rms(hn_block_total(tot_s), inv_h, p.eps);
+    const F2 inv = f2(prep_inv_rms(hn_block_total(tot_s), inv_h, p.eps));
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int v = tid + BN_THREADS * j;
         if (v >= nvec) continue;
-        float w[8], o[8];
-        unpack8(wn[v], w);
+        const uint4 w4 = FEW ? wnv[FEW ? j : 0] : wn[v];
+        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+        uint32_t o[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = prep_norm(s[j][e], inv_s, w[e]);
-        reinterpret_cast<uint4*>(p.y)[row * nvec + v] = pack8(o);
+        for (int e = 0; e < 4; ++e) {
+            float lo, hi;
+            f2_get(f2_mul(f2_mul(f2_bf16(s[j][e]), inv), f2_bf16(w[e])), lo, hi);
+            o[e] = pack_bf16x2(lo, hi);
+        }
+        reinterpret_cast<uint4*>(p.y)[row * nvec + v] = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
@@ -395,8 +420,11 @@ size_t block_norm_bwd_bytes(int64_t T, int H) { return static_cast<size_t>(bwd_s
 
 cudaError_t launch_block_norm(const BlockNormParams& p, cudaStream_t stream) {
     const int nv = (p.H / 8 + BN_THREADS - 1) / BN_THREADS;
-    auto kern = nv <= 1 ? block_norm_kernel<1> : nv <= 2 ? block_norm_kernel<2> : nv <= 4 ? block_norm_kernel<4> : block_norm_kernel<8>;
-    return launch_pdl(kern, dim3(static_cast<unsigned>(p.T)), BN_THREADS, 0, stream, 1, p);
+    auto pick = [&](auto few) {
+        constexpr bool FEW = decltype(few)::value;
+        return nv <= 1 ? block_norm_kernel<1, FEW> : nv <= 2 ? block_norm_kernel<2, FEW> : nv <= 4 ? block_norm_kernel<4, FEW> : block_norm_kernel<8, FEW>;
+    };
+    return launch_pdl(p.T <= BN_FEW_ROWS ? pick(std::true_type()) : pick(std::false_type()), dim3(static_cast<unsigned>(p.T)), BN_THREADS, 0, stream, 1, p);
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream) {
