@@ -299,7 +299,8 @@ tik_status tik_embedding(tik_ctx* ctx, const int32_t* ids, const void* table, vo
  * equal ids by position, and a row's tokens are summed in fp32 in that order in a shape that depends on their
  * number only: no atomics on values, the same bits on every call, whatever other ids the batch holds.  One rounding of
  * g (accumulate: of d_table + g).  Ids outside [0, V) have no gradient and raise TIK_DEV_BAD_TOKEN.
- * T == 0 with accumulate == 0 writes zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes. */
+ * T == 0 with accumulate == 0 writes zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes; concurrent
+ * calls (and captured graphs that may run at the same time) need buffers of their own.  One to three kernels on `stream`. */
 tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, void* d_table, int table_dtype,
                              int accumulate, float scale, int64_t T, int V, int H, void* ws, size_t ws_bytes,
                              void* stream);
@@ -328,7 +329,8 @@ tik_status tik_block_norm(tik_ctx* ctx, const void* x, const void* residual, con
  * (d_x NULL exactly when x is), each may be one of d_y, d_s, x, s; d_weight, d_post_weight fp32 [H], d_gate fp32 [H] or
  * [T]: each exactly when its factor is given, overwritten (zeros for T == 0).  fp32 arithmetic; sums over tokens in one fixed
  * order without atomics: the same inputs give the same bits on every call.
- * ws: tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, ..., H, 0) bytes. */
+ * ws: tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, ..., H, 0) bytes, as above.  Two kernels on `stream`, one where no
+ * sum over tokens is asked for. */
 tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, const void* x, const void* s,
                               const void* post_weight, const void* gate, int gate_kind, float branch_scale,
                               const void* weight, float eps, void* d_x, void* d_residual, float* d_weight,
@@ -341,7 +343,7 @@ tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, co
  *   be 0 (then grads[i] may be NULL).  norm: device fp32 [1].
  * Squares of 64 elements or fewer are summed in fp32 (in fp64 where they leave its range), everything above in fp64 in one fixed
  * order: the same list gives the same bits on every call and every device.  Infinities and NaN pass into the norm.
- * ws: tik_workspace_bytes(TIK_OP_GRAD_NORM, n, ...) bytes. */
+ * ws: tik_workspace_bytes(TIK_OP_GRAD_NORM, n, ...) bytes, as above.  A kernel per thousand tensors and one more. */
 tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* numel, const int* dtypes, int n,
                          float* norm, void* ws, size_t ws_bytes, void* stream);
 
@@ -351,7 +353,8 @@ tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* 
  * grads[i]).  The factor is the fp32 quotient; products in fp32, one rounding.
  * norm: device fp32 [1].  norm_given == 0: computed first, as by tik_grad_norm, and stored there; else read, e.g. after a
  * sharded trainer has combined its ranks' norms.  max_norm must be finite and > 0.  Tensors that are written may not overlap
- * each other or another input (TIK_ERR_INVALID_ARG).  ws as for tik_grad_norm (norm_given: may be NULL). */
+ * each other or another input (TIK_ERR_INVALID_ARG).  ws as for tik_grad_norm (norm_given: may be NULL).  A kernel per
+ * thousand tensors, as many again where the norm is computed. */
 tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* out, const int64_t* numel,
                          const int* dtypes, int n, float max_norm, float* norm, int norm_given, void* ws,
                          size_t ws_bytes, void* stream);

@@ -53,7 +53,7 @@ def _forward(tik, t, a, rows=slice(None), **out):
                               gate=gate, branch_scale=a, **out)
 
 
-@pytest.mark.parametrize("T,H", SIZES)
+@pytest.mark.parametrize("T,H", SIZES + [(512, 264), (513, 264), (2100, 72), (600, 1032), (530, 3584), (521, 5120)])
 @pytest.mark.parametrize("form", FORMS)
 def test_forward(tik, T, H, form):
     a = form["a"]
@@ -212,6 +212,26 @@ def test_captured_and_replayed(tik):
         g.replay()
         for got, want in zip(out, step()):
             assert count_diff(got, want) == 0
+
+
+@pytest.mark.parametrize("T,H", [(300, 256), (150, 3584), (5, 8192)])
+def test_gradients_over_their_inputs(tik, T, H):
+    """Through the C interface: d_residual over d_s or d_y, d_x over x, s or d_y."""
+    a = 0.7
+    t = _inputs(T, H, True, "channel", True, a, seed=70)
+    s, dy, ds = _randn((T, H), 71, 4.0), _randn((T, H), 72), _randn((T, H), 73)
+    want = tik.tik_block_norm_bwd(dy, ds, t["x"], s, t["weight"], 1e-6, post_weight=t["post"], gate=t["gate"], branch_scale=a)
+    ws = torch.empty(tik.workspace_bytes(tik.OP_BLOCK_NORM_BWD, T, H=H), dtype=torch.uint8, device="cuda")
+    f32 = [torch.empty(H, device="cuda") for _ in range(3)]
+    for over_x, over_r in (("x", "ds"), ("s", "dy"), ("dy", "ds"), ("ds", "x")):
+        v = {"x": t["x"].clone(), "s": s.clone(), "dy": dy.clone(), "ds": ds.clone()}
+        ptr = lambda k: v[k].data_ptr()
+        rc = tik.load().tik_block_norm_bwd(tik.context(), ptr("dy"), ptr("ds"), ptr("x"), ptr("s"), t["post"].data_ptr(), t["gate"].data_ptr(), 1, a,
+                                           t["weight"].data_ptr(), 1e-6, ptr(over_x), ptr(over_r), *[f.data_ptr() for f in f32], T, H,
+                                           ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        for got, ref in zip([v[over_x], v[over_r]] + f32, want):
+            assert count_diff(got, ref) == 0, (over_x, over_r)
 
 
 def test_refused_tensors(tik):
