@@ -127,19 +127,18 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
 // (four hundred a row and thread) and the waits between them leave room: the first sums of a row are taken beside the second
 // of the row before it, so that a row costs one barrier and one reduction of four values.  One persistent CTA per SM,
 // made of groups that each take a row at a time; rows arrive by bulk copies into a ring that the groups share.  A thread has the
-// same BN_NV x 8 columns of every row, so that the sums over tokens stay in its registers until the end;
+// same NV x 8 columns of every row, so that the sums over tokens stay in its registers until the end;
 // block_norm_fold_kernel adds up the CTAs'.
-constexpr int BN_NV = 2;                                     // 16-byte vectors per thread
-constexpr int BN_THREADS_MOST = 512;                         // at 128 registers
+constexpr int BN_THREADS_MOST = 512, BN_THREADS_WIDE = 640;  // at 128 and at 96 registers
 
 struct BlockNormBwdShape {
-    int group, groups, ctas, slots, slot_bytes, factor_bytes;            // threads of a group
+    int nv, group, groups, ctas, slots, slot_bytes, factor_bytes;        // 16-byte vectors per thread, threads of a group
     size_t smem;
 };
 constexpr int BN_SLOTS = 64;
 struct BlockNormBwdSmem {
     unsigned long long full[BN_SLOTS];
-    float4 sums[2][16];                                      // [turn][warp of the CTA]
+    float4 sums[2][BN_THREADS_WIDE / 32];                    // [turn][warp of the CTA]
     int abort_word;
 };
 constexpr int BN_RING = (sizeof(BlockNormBwdSmem) + 127) / 128 * 128;
@@ -163,7 +162,8 @@ __device__ __forceinline__ float bn_rsqrt(float x) {
     return r;
 }
 
-__global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(const BlockNormParams p, const BlockNormBwdShape shape) {
+template <int NV, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockNormParams p, const BlockNormBwdShape shape) {
     extern __shared__ __align__(128) unsigned char bn_smem[];
     BlockNormBwdSmem& sm = *reinterpret_cast<BlockNormBwdSmem*>(bn_smem);
     // branch_scale * post_weight * gate (per channel) of the columns in fp32; then the ring
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
     unsigned char* const ring = bn_smem + BN_RING + shape.factor_bytes;
     const int width = shape.group, group = threadIdx.x / width, tid = threadIdx.x - group * width;       // threads of a group
     const int lane = threadIdx.x & 31, warps = width >> 5, warp = tid >> 5;
-    const int nvec = p.H / 8, row_vecs = BN_NV * width;      // (a row in the ring is as wide as the threads' vectors)
+    const int nvec = p.H / 8, row_vecs = NV * width;      // (a row in the ring is as wide as the threads' vectors)
     const float inv_h = 1.0f / static_cast<float>(p.H);
     const bool norm = p.weight != nullptr, post = p.post_weight != nullptr, branch = p.x != nullptr;
     // What is absent reads as zeros: planes that are not there, vectors behind the row.
@@ -200,10 +200,10 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
     if (threadIdx.x == 0)
         for (int n = 0; n < shape.slots; ++n) request(blockIdx.x + n * gridDim.x, n);
     // [half vector][thread]: 16 bytes a thread and instruction; every group writes the same values and reads what it wrote itself
-    uint32_t w[BN_NV][4];
-    F2 sum_w[BN_NV][4], sum_c[BN_NV][4];
+    uint32_t w[NV][4];
+    F2 sum_w[NV][4], sum_c[NV][4];
 #pragma unroll
-    for (int j = 0; j < BN_NV; ++j) {
+    for (int j = 0; j < NV; ++j) {
         const int v = tid + width * j;
         auto column = [&](const __nv_bfloat16* base, bool there, float (&to)[8]) {
             unpack8(there && v < nvec ? reinterpret_cast<const uint4*>(base)[v] : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), to);
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
         const uint4* at = row_at(s);
         F2 sx = f2(0.0f), ss = f2(0.0f), sq = f2(0.0f);
 #pragma unroll
-        for (int j = 0; j < BN_NV; ++j) {
+        for (int j = 0; j < NV; ++j) {
             uint32_t x[4], s4[4], dy[4];
             take(at, 1, j, x);
             take(at, 2, j, s4);
@@ -257,11 +257,12 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
         if ((lane & 7) == 0) mine[4 * warp + lane / 8] = part;
         if (warps > 1) named_bar_sync(1 + group, width);
         else __syncwarp();
+        constexpr int WARPS = NV == 1 ? 32 : 16;             // of a group, at most
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if ((lane & 15) < warps) v = sm.sums[turn][group * warps + (lane & 15)];
-        const float t = bn_sums4<8>(v.x, v.y, v.z, v.w, lane);
+        if ((lane & (WARPS - 1)) < warps) v = sm.sums[turn][group * warps + (lane & (WARPS - 1))];
+        const float t = bn_sums4<WARPS / 2>(v.x, v.y, v.z, v.w, lane);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xffffffffu, t, 4 * i);
+        for (int i = 0; i < 4; ++i) to[i] = __shfl_sync(0xffffffffu, t, WARPS / 4 * i);
         turn ^= 1;
     };
     float sums[4];
@@ -274,11 +275,11 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
         const float rs = norm ? bn_rsqrt(fmaf(sums[1], inv_h, p.eps)) : 0.0f, rx = post ? bn_rsqrt(fmaf(sums[0], inv_h, p.eps)) : 1.0f;
         const F2 rs2 = f2(rs), ks2 = f2(-(rs * rs * rs * (sums[2] * inv_h))), c2 = f2(gt * rx);
         const size_t out_at = static_cast<size_t>(row) * nvec + tid;
-        uint32_t x[BN_NV][4];
-        F2 Gf[BN_NV][4], td = f2(0.0f);                      // G times its factor
+        uint32_t x[NV][4];
+        F2 Gf[NV][4], td = f2(0.0f);                      // G times its factor
         const uint4* at = row_at(slot);
 #pragma unroll
-        for (int j = 0; j < BN_NV; ++j) {
+        for (int j = 0; j < NV; ++j) {
             const float4 f0 = factors[2 * j * width + tid], f1 = factors[(2 * j + 1) * width + tid];
             const F2 f[4] = {f2(f0.x, f0.y), f2(f0.z, f0.w), f2(f1.x, f1.y), f2(f1.z, f1.w)};
             uint32_t ds[4], s[4], dy[4], out[4];
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
         if (p.gate_kind == GATE_TOKEN && tid == 0) p.d_gate[row] = rx * sums[3];
         const F2 kx2 = f2(post ? -(gt * rx * rx * rx * (sums[3] * inv_h)) : 0.0f);
 #pragma unroll
-        for (int j = 0; j < BN_NV; ++j) {
+        for (int j = 0; j < NV; ++j) {
             uint32_t out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -333,16 +334,16 @@ __global__ void __launch_bounds__(BN_THREADS_MOST, 1) block_norm_bwd_kernel(cons
     F2* const all = reinterpret_cast<F2*>(ring);             // [plane][half vector][group][thread] of two F2
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < BN_NV; ++j)
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int i = (2 * j + e / 2) * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x);
             all[2 * i + e % 2] = sum_w[j][e];
-            all[2 * (2 * BN_NV * static_cast<int>(blockDim.x) + i) + e % 2] = sum_c[j][e];
+            all[2 * (2 * NV * static_cast<int>(blockDim.x) + i) + e % 2] = sum_c[j][e];
         }
     __syncthreads();
-    for (int i = threadIdx.x; i < 4 * BN_NV * width; i += blockDim.x) {
-        const int part = i / width, t = i - part * width, plane = part / (2 * BN_NV), half = part % (2 * BN_NV);
+    for (int i = threadIdx.x; i < 4 * NV * width; i += blockDim.x) {
+        const int part = i / width, t = i - part * width, plane = part / (2 * NV), half = part % (2 * NV);
         if (plane == 0 ? !norm : !column) continue;
         const int c = 2 * (t + width * (half / 2)) + half % 2;               // 4 columns
         if (4 * c >= p.H) continue;
@@ -398,20 +399,21 @@ __global__ void __launch_bounds__(BN_FOLD_WARPS * 32) block_norm_fold_kernel(con
     }
 }
 
-// Threads for BN_NV vectors each; as many groups as 512 threads hold and as leave a row ahead in the ring, which fills shared
+// Threads for NV vectors each; as many groups as 512 threads hold and as leave a row ahead in the ring, which fills shared
 // memory.  (148 SMs: the number of CTAs and groups decides the order of the sums over tokens, so it does not follow the device.)
 static BlockNormBwdShape bwd_shape(int64_t T, int H) {
     BlockNormBwdShape s;
-    s.group = (H / 8 + 32 * BN_NV - 1) / (32 * BN_NV) * 32;
-    s.slot_bytes = 4 * 16 * BN_NV * s.group;
-    s.factor_bytes = 32 * BN_NV * s.group;
+    s.nv = H > 4096 && H <= 8 * BN_THREADS_WIDE ? 1 : 2;
+    s.group = (H / 8 + 32 * s.nv - 1) / (32 * s.nv) * 32;
+    s.slot_bytes = 4 * 16 * s.nv * s.group;
+    s.factor_bytes = 32 * s.nv * s.group;
     s.slots = std::min(BN_SLOTS, (227 * 1024 - BN_RING - s.factor_bytes) / s.slot_bytes);
     s.ctas = static_cast<int>(std::min<int64_t>(T, 148));
     const int64_t rows = (T + 147) / 148;                    // of a CTA
-    s.groups = static_cast<int>(std::min<int64_t>(BN_THREADS_MOST / s.group, rows));
+    s.groups = static_cast<int>(std::min<int64_t>(std::max(1, BN_THREADS_MOST / s.group), rows));
     while (s.groups > 1 && 2 * s.groups >= s.slots) --s.groups;
     // (a short call's ring holds its rows; the groups' sums need 64 bytes a thread and vector of it at the end)
-    const int sums = (64 * BN_NV * s.groups * s.group + s.slot_bytes - 1) / s.slot_bytes;
+    const int sums = (64 * s.nv * s.groups * s.group + s.slot_bytes - 1) / s.slot_bytes;
     s.slots = static_cast<int>(std::min<int64_t>(s.slots, std::max<int64_t>({rows, sums, s.groups + 1})));
     s.smem = BN_RING + s.factor_bytes + static_cast<size_t>(s.slots) * s.slot_bytes;
     return s;
@@ -432,10 +434,12 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream)
     if (shape.ctas > 0) {
         static DeviceOnce configured;
         cudaError_t e = configured.run([&]() {
-            return cudaFuncSetAttribute(block_norm_bwd_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+            const cudaError_t r = cudaFuncSetAttribute(block_norm_bwd_kernel<2, BN_THREADS_MOST>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+            return r != cudaSuccess ? r : cudaFuncSetAttribute(block_norm_bwd_kernel<1, BN_THREADS_WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
         });
         if (e != cudaSuccess) return e;
-        e = launch_pdl(block_norm_bwd_kernel, dim3(shape.ctas), shape.group * shape.groups, shape.smem, stream, 1, p, shape);
+        e = launch_pdl(shape.nv == 2 ? block_norm_bwd_kernel<2, BN_THREADS_MOST> : block_norm_bwd_kernel<1, BN_THREADS_WIDE>, dim3(shape.ctas),
+                       shape.group * shape.groups, shape.smem, stream, 1, p, shape);
         if (e != cudaSuccess) return e;
     }
     if (!p.d_weight && !p.d_post_weight && p.gate_kind != GATE_CHANNEL) return cudaSuccess;
