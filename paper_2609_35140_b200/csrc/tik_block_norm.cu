@@ -399,18 +399,20 @@ __global__ void __launch_bounds__(BN_FOLD_WARPS * 32) block_norm_fold_kernel(con
     }
 }
 
-// Threads for NV vectors each; as many groups as 512 threads hold and as leave a row ahead in the ring, which fills shared
-// memory.  (148 SMs: the number of CTAs and groups decides the order of the sums over tokens, so it does not follow the device.)
+// Threads for NV vectors each: two, which halves what a row costs beside its columns (28 warps of one vector at 3584 channels 126 us,
+// 14 of two 121), but one where two would leave lanes idle or too few warps on an SM (9001 x 5120: 111 us with one, 130 with two).  As
+// many groups as the threads hold and as leave a row ahead in the ring, which fills shared memory.  (148 SMs: the number of CTAs
+// and groups decides the order of the sums over tokens, so it does not follow the device.)
 static BlockNormBwdShape bwd_shape(int64_t T, int H) {
     BlockNormBwdShape s;
-    s.nv = H > 4096 && H <= 8 * BN_THREADS_WIDE ? 1 : 2;
+    s.nv = H <= 256 || (H > 4096 && H <= 8 * BN_THREADS_WIDE) ? 1 : 2;
     s.group = (H / 8 + 32 * s.nv - 1) / (32 * s.nv) * 32;
     s.slot_bytes = 4 * 16 * s.nv * s.group;
     s.factor_bytes = 32 * s.nv * s.group;
     s.slots = std::min(BN_SLOTS, (227 * 1024 - BN_RING - s.factor_bytes) / s.slot_bytes);
     s.ctas = static_cast<int>(std::min<int64_t>(T, 148));
     const int64_t rows = (T + 147) / 148;                    // of a CTA
-    s.groups = static_cast<int>(std::min<int64_t>(std::max(1, BN_THREADS_MOST / s.group), rows));
+    s.groups = static_cast<int>(std::min<int64_t>(std::max(1, (s.nv == 1 ? BN_THREADS_WIDE : BN_THREADS_MOST) / s.group), rows));
     while (s.groups > 1 && 2 * s.groups >= s.slots) --s.groups;
     // (a short call's ring holds its rows; the groups' sums need 64 bytes a thread and vector of it at the end)
     const int sums = (64 * s.nv * s.groups * s.group + s.slot_bytes - 1) / s.slot_bytes;
