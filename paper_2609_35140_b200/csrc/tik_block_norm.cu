@@ -129,6 +129,18 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
 // made of groups that each take a row at a time; rows arrive by bulk copies into a ring that the groups share.  A thread has the
 // same NV x 8 columns of every row, so that the sums over tokens stay in its registers until the end;
 // block_norm_fold_kernel adds up the CTAs'.
+// Two fp32 values.  (The two-wide instructions of block_norm_kernel make this kernel slower: 12 % fewer instructions, but warps wait
+// for them longer than fourteen warps on an SM hide; 16001 x 3584 121.9 us with them, 119.3 without.)
+struct S2 {
+    float lo, hi;
+};
+__device__ __forceinline__ S2 s2(float both) { return {both, both}; }
+__device__ __forceinline__ S2 s2(float lo, float hi) { return {lo, hi}; }
+__device__ __forceinline__ S2 s2_bf16(uint32_t w) { return {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
+__device__ __forceinline__ S2 s2_fma(S2 a, S2 b, S2 c) { return {__fmaf_rn(a.lo, b.lo, c.lo), __fmaf_rn(a.hi, b.hi, c.hi)}; }
+__device__ __forceinline__ S2 s2_mul(S2 a, S2 b) { return {__fmul_rn(a.lo, b.lo), __fmul_rn(a.hi, b.hi)}; }
+__device__ __forceinline__ float s2_sum(S2 a) { return __fadd_rn(a.lo, a.hi); }
+
 constexpr int BN_THREADS_MOST = 512, BN_THREADS_WIDE = 640;  // at 128 and at 96 registers
 
 struct BlockNormBwdShape {
@@ -201,7 +213,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         for (int n = 0; n < shape.slots; ++n) request(blockIdx.x + n * gridDim.x, n);
     // [half vector][thread]: 16 bytes a thread and instruction; every group writes the same values and reads what it wrote itself
     uint32_t w[NV][4];
-    F2 sum_w[NV][4], sum_c[NV][4];
+    S2 sum_w[NV][4], sum_c[NV][4];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int v = tid + width * j;
@@ -218,7 +230,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         const uint4 wv = norm && v < nvec ? reinterpret_cast<const uint4*>(p.weight)[v] : make_uint4(0, 0, 0, 0);
         w[j][0] = wv.x, w[j][1] = wv.y, w[j][2] = wv.z, w[j][3] = wv.w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum_w[j][e] = sum_c[j][e] = f2(0.0f);
+        for (int e = 0; e < 4; ++e) sum_w[j][e] = sum_c[j][e] = s2(0.0f);
     }
     int slot = group, turn = 0;                              // (there are more slots than groups)
     uint32_t parity = 0;
@@ -233,7 +245,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     auto first_sums = [&](int s, uint32_t par) {
         mbar_wait(smem_u32(&sm.full[s]), par, &sm.abort_word, p.dev_status);
         const uint4* at = row_at(s);
-        F2 sx = f2(0.0f), ss = f2(0.0f), sq = f2(0.0f);
+        S2 sx = s2(0.0f), ss = s2(0.0f), sq = s2(0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             uint32_t x[4], s4[4], dy[4];
@@ -242,13 +254,13 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
             take(at, 3, j, dy);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const F2 xe = f2_bf16(x[e]), se = f2_bf16(s4[e]);
-                sx = f2_fma(xe, xe, sx);
-                ss = f2_fma(se, se, ss);
-                sq = f2_fma(f2_mul(f2_bf16(dy[e]), f2_bf16(w[j][e])), se, sq);
+                const S2 xe = s2_bf16(x[e]), se = s2_bf16(s4[e]);
+                sx = s2_fma(xe, xe, sx);
+                ss = s2_fma(se, se, ss);
+                sq = s2_fma(s2_mul(s2_bf16(dy[e]), s2_bf16(w[j][e])), se, sq);
             }
         }
-        tx = f2_sum(sx), ts = f2_sum(ss), tq = f2_sum(sq);
+        tx = s2_sum(sx), ts = s2_sum(ss), tq = s2_sum(sq);
     };
     // (tx, ts, tq, td) of the group
     auto total = [&](float td, float (&to)[4]) {
@@ -273,15 +285,15 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     for (; row < T; row += step) {
         const float gt = p.gate_kind == GATE_TOKEN ? __bfloat162float(p.gate[row]) : 1.0f;
         const float rs = norm ? bn_rsqrt(fmaf(sums[1], inv_h, p.eps)) : 0.0f, rx = post ? bn_rsqrt(fmaf(sums[0], inv_h, p.eps)) : 1.0f;
-        const F2 rs2 = f2(rs), ks2 = f2(-(rs * rs * rs * (sums[2] * inv_h))), c2 = f2(gt * rx);
+        const S2 rs2 = s2(rs), ks2 = s2(-(rs * rs * rs * (sums[2] * inv_h))), c2 = s2(gt * rx);
         const size_t out_at = static_cast<size_t>(row) * nvec + tid;
         uint32_t x[NV][4];
-        F2 Gf[NV][4], td = f2(0.0f);                      // G times its factor
+        S2 Gf[NV][4], td = s2(0.0f);                      // G times its factor
         const uint4* at = row_at(slot);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const float4 f0 = factors[2 * j * width + tid], f1 = factors[(2 * j + 1) * width + tid];
-            const F2 f[4] = {f2(f0.x, f0.y), f2(f0.z, f0.w), f2(f1.x, f1.y), f2(f1.z, f1.w)};
+            const S2 f[4] = {s2(f0.x, f0.y), s2(f0.z, f0.w), s2(f1.x, f1.y), s2(f1.z, f1.w)};
             uint32_t ds[4], s[4], dy[4], out[4];
             take(at, 0, j, ds);
             take(at, 1, j, x[j]);
@@ -289,15 +301,14 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
             take(at, 3, j, dy);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const F2 xe = f2_bf16(x[j][e]), se = f2_bf16(s[e]), rdy = f2_mul(rs2, f2_bf16(dy[e]));
-                const F2 G = f2_fma(ks2, se, f2_fma(rdy, f2_bf16(w[j][e]), f2_bf16(ds[e])));
-                sum_w[j][e] = f2_fma(rdy, se, sum_w[j][e]);
-                sum_c[j][e] = f2_fma(f2_mul(G, xe), c2, sum_c[j][e]);
-                Gf[j][e] = f2_mul(G, f[e]);
-                td = f2_fma(Gf[j][e], xe, td);
-                float lo, hi;
-                f2_get(G, lo, hi);
-                out[e] = pack_bf16x2(lo, hi);
+                const S2 xe = s2_bf16(x[j][e]), se = s2_bf16(s[e]), rdy = s2_mul(rs2, s2_bf16(dy[e]));
+                const S2 G = s2_fma(ks2, se, s2_fma(rdy, s2_bf16(w[j][e]), s2_bf16(ds[e])));
+                sum_w[j][e] = s2_fma(rdy, se, sum_w[j][e]);
+                sum_c[j][e] = s2_fma(s2_mul(G, xe), c2, sum_c[j][e]);
+                Gf[j][e] = s2_mul(G, f[e]);
+                td = s2_fma(Gf[j][e], xe, td);
+                const S2 v = G;
+                out[e] = pack_bf16x2(v.lo, v.hi);
             }
             if (tid + width * j < nvec) reinterpret_cast<uint4*>(p.d_residual)[out_at + width * j] = make_uint4(out[0], out[1], out[2], out[3]);
         }
@@ -309,29 +320,28 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         }
         tx = ts = tq = 0.0f;
         if (row + step < T) first_sums(next, next_parity);
-        total(f2_sum(td), sums);
+        total(s2_sum(td), sums);
         // everybody in the group is through with the row: a later one takes its slot
         if (tid == 0) request(row + shape.slots * gridDim.x, slot);
         slot = next;
         parity = next_parity;
         if (!branch) continue;
         if (p.gate_kind == GATE_TOKEN && tid == 0) p.d_gate[row] = rx * sums[3];
-        const F2 kx2 = f2(post ? -(gt * rx * rx * rx * (sums[3] * inv_h)) : 0.0f);
+        const S2 kx2 = s2(post ? -(gt * rx * rx * rx * (sums[3] * inv_h)) : 0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             uint32_t out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float lo, hi;
-                f2_get(f2_fma(c2, Gf[j][e], f2_mul(kx2, f2_bf16(x[j][e]))), lo, hi);
-                out[e] = pack_bf16x2(lo, hi);
+                const S2 v = s2_fma(c2, Gf[j][e], s2_mul(kx2, s2_bf16(x[j][e])));
+                out[e] = pack_bf16x2(v.lo, v.hi);
             }
             if (tid + width * j < nvec) reinterpret_cast<uint4*>(p.d_x)[out_at + width * j] = make_uint4(out[0], out[1], out[2], out[3]);
         }
     }
     // The groups' sums, in their order, through the ring (nothing is on its way there any more).
     const bool column = post || p.gate_kind == GATE_CHANNEL;
-    F2* const all = reinterpret_cast<F2*>(ring);             // [plane][half vector][group][thread] of two F2
+    S2* const all = reinterpret_cast<S2*>(ring);             // [plane][half vector][group][thread] of two S2
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < NV; ++j)
