@@ -78,18 +78,19 @@ __device__ __forceinline__ int emb_key(const EmbedParams& p, int id) { return id
 // Calls of few tokens: a token's place is the number of tokens before it in the order, counted by comparing all pairs.
 // Lanes are tokens; the warps of a CTA share the tokens that they are compared with, from shared memory (out of L2 every
 // load of the chain waits behind the zeros that are being written meanwhile).
-constexpr int EMB_RANK_TOKENS = 4096;
-constexpr int EMB_RANK_WARPS = 8;
+constexpr int EMB_RANK_TOKENS = 4608;                        // (one wave of CTAs; 4097 tokens x 256, added, us: 13.4 so, 18.4 by sorting)
+constexpr int EMB_RANK_WARPS = 32;                           // (4000 tokens: 14 us with eight, 9 with 32)
 __global__ void __launch_bounds__(EMB_RANK_WARPS * 32) embed_rank_kernel(const EmbedParams p) {
     __shared__ alignas(16) int keys[EMB_RANK_TOKENS];
-    __shared__ int count[EMB_RANK_WARPS][3][32];
+    __shared__ int count[3][32];
+    if (threadIdx.x < 96) (&count[0][0])[threadIdx.x] = 0;
     pdl_wait();
     pdl_launch_dependents();
     const int T = static_cast<int>(p.T), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (blockIdx.x == 0 && threadIdx.x < 2) p.tickets[threadIdx.x] = 0;
     const int padded = (T + 4 * EMB_RANK_WARPS - 1) / (4 * EMB_RANK_WARPS) * (4 * EMB_RANK_WARPS);
 #pragma unroll                                               // (all in flight at once)
-    for (int j = 0; j < EMB_RANK_TOKENS / (EMB_RANK_WARPS * 32); ++j) {
+    for (int j = 0; j < (EMB_RANK_TOKENS + EMB_RANK_WARPS * 32 - 1) / (EMB_RANK_WARPS * 32); ++j) {
         const int i = threadIdx.x + j * EMB_RANK_WARPS * 32;
         if (i < padded) keys[i] = i < T ? emb_key(p, p.ids[i]) : 0x7fffffff;
     }
@@ -117,18 +118,14 @@ __global__ void __launch_bounds__(EMB_RANK_WARPS * 32) embed_rank_kernel(const E
     }
 #pragma unroll 4
     for (; i < end; i += 4) four(i, std::false_type());
-    count[warp][0][lane] = place;
-    count[warp][1][lane] = same;
-    count[warp][2][lane] = same_before;
+    atomicAdd(&count[0][lane], place);
+    atomicAdd(&count[1][lane], same);
+    atomicAdd(&count[2][lane], same_before);
     __syncthreads();
     if (warp != 0 || t >= T) return;
-    place = same = same_before = 0;
-#pragma unroll
-    for (int w = 0; w < EMB_RANK_WARPS; ++w) {
-        place += count[w][0][lane];
-        same += count[w][1][lane];
-        same_before += count[w][2][lane];
-    }
+    place = count[0][lane];
+    same = count[1][lane];
+    same_before = count[2][lane];
     p.order[place] = t;
     uint4 rec = emb_record(mine, same_before, same_before + same, t);
     if (mine == p.V) {

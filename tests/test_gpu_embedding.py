@@ -97,7 +97,7 @@ def _ids(kind, T, V, rng):
     (700, 33, 520, "few"), (1000, 151936, 16, "uniform"), (1023, 100, 72, "one"), (1025, 4097, 136, "zipf"), (3000, 2048, 256, "zipf"),
     (4097, 300, 64, "falling"), (9001, 152064, 24, "zipf"), (20011, 17, 40, "zipf"), (16384, 70000, 8, "distinct"), (33000, 5000, 8, "one"),
     (255, 40, 264, "few"), (256, 700, 3584, "one"), (256, 3, 64, "uniform"), (257, 3, 64, "uniform"), (200, 5, 75776, "uniform"), (90, 4, 20000, "one"),
-    (4096, 500, 16, "zipf"), (65536, 152064, 8, "zipf"), (65537, 152064, 8, "zipf"), (70001, 300, 8, "one"), (100003, 600000, 8, "uniform"),
+    (4096, 500, 16, "zipf"), (4608, 151936, 16, "zipf"), (4609, 151936, 16, "zipf"), (8193, 2000, 16, "uniform"), (65536, 152064, 8, "zipf"), (65537, 152064, 8, "zipf"), (70001, 300, 8, "one"), (100003, 600000, 8, "uniform"),
     (131072, 3, 16, "falling")])
 @pytest.mark.parametrize("dtype,accumulate", [(torch.bfloat16, False), (torch.float32, False), (torch.bfloat16, True), (torch.float32, True)])
 def test_gradient(tik, T, V, H, kind, dtype, accumulate):
