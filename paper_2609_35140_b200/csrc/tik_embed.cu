@@ -137,10 +137,9 @@ __global__ void __launch_bounds__(EMB_RANK_WARPS * 32) embed_rank_kernel(const E
 
 // Other calls: a stable radix sort by one cluster of eight CTAs, whose 256 warps own consecutive stretches of the list.  Per
 // digit: each warp counts its digits, the CTAs exchange their counts through distributed shared memory, and each
-// warp moves its elements, in order, to where the elements before them end.  NW > 0: a stretch is NW windows of 32 elements,
-// held in registers, and the list stays in the CTAs' shared memory between the passes, which the zeros that are
-// written meanwhile do not slow down; 0 (more than EMB_CHIP_TOKENS): any number of windows, the list in global memory.
-// What a call costs are its few barriers across the cluster (~0.7 us each) and the chains between them.
+// warp moves its elements, in order, to where the elements before them end.  A stretch is NW windows of 32 elements, held in
+// registers, and the list stays in the CTAs' shared memory between the passes, which the zeros that are written meanwhile
+// do not slow down.  What a call costs are its few barriers across the cluster (~0.7 us each) and the chains between them.
 constexpr int EMB_CLUSTER = 8, EMB_SORT_THREADS = 1024, EMB_SORT_WARPS = EMB_SORT_THREADS / 32;
 constexpr int EMB_BINS = 512, EMB_CHIP_TOKENS = 8 * 32 * EMB_SORT_WARPS * EMB_CLUSTER;
 struct EmbedSortSmem {
@@ -161,61 +160,67 @@ __device__ __forceinline__ void st_cluster_uint2(uint32_t addr, uint2 v) {
     asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
 }
 
+// A digit's place among those of its kind that this warp has seen; counts it.
+__device__ __forceinline__ int emb_count(int* counts, bool valid, int digit, int lane) {
+    int at = 0;
+    const unsigned here = __ballot_sync(0xffffffffu, valid);
+    if (valid) {
+        const unsigned peers = __match_any_sync(here, digit);
+        at = counts[digit] + __popc(peers & ((1u << lane) - 1));
+        __syncwarp(here);
+        if (lane == __ffs(peers) - 1) counts[digit] += __popc(peers);
+    }
+    __syncwarp();
+    return at;
+}
+// The record of place i of 32 that a warp holds, element e; heads: first places of runs among them, before / next: the closest ones
+// outside.
+__device__ __forceinline__ void emb_write_record(const EmbedParams& p, int i0, uint2 e, unsigned heads, int before, int next, int lane) {
+    const unsigned to_lane = 0xffffffffu >> (31 - lane), upto = heads & to_lane, behind = heads & ~to_lane;
+    const int i = i0 + lane, head = upto ? i0 + 31 - __clz(upto) : before, tail = behind ? i0 + __ffs(behind) - 1 : next;
+    uint4 rec = emb_record(e.x, i - head, tail - head, e.y);
+    if (e.x == static_cast<uint32_t>(p.V)) {
+        rec.y = 0;
+        if (i == head) atomicOr(p.dev_status, TIK_DEV_BAD_TOKEN);
+    }
+    p.order[i] = e.y;
+    p.place[i] = rec;
+}
+
 template <int NW>
 __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const EmbedParams p, int passes, int digit_bits) {
-    constexpr bool ON_CHIP = NW > 0;
     extern __shared__ __align__(16) unsigned char emb_smem[];
     EmbedSortSmem& sm = *reinterpret_cast<EmbedSortSmem*>(emb_smem);
-    uint2* list = reinterpret_cast<uint2*>(emb_smem + sizeof(EmbedSortSmem));        // ON_CHIP: two buffers of the CTA's elements
+    uint2* list = reinterpret_cast<uint2*>(emb_smem + sizeof(EmbedSortSmem));        // two buffers of the CTA's elements
     const int T = static_cast<int>(p.T), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_ctarank();
     pdl_wait();
     pdl_launch_dependents();
     if (rank == 0 && tid < 2) p.tickets[tid] = 0;
     const int bins = 1 << digit_bits;
-    const int per = ON_CHIP ? 32 * NW : ((T + EMB_CLUSTER * EMB_SORT_WARPS - 1) / (EMB_CLUSTER * EMB_SORT_WARPS) + 31) / 32 * 32;
-    const int chunk = per * EMB_SORT_WARPS;
+    constexpr int per = 32 * NW, chunk = per * EMB_SORT_WARPS;
     const long long cta_from = static_cast<long long>(chunk) * rank, from = cta_from + per * warp;
     const int first = static_cast<int>(from < T ? from : T), last = static_cast<int>(from + per < T ? from + per : T);
     int* mine = sm.hist[warp];
     // elements of this warp's stretch before pass `pass` (pass == passes: sorted)
     auto element = [&](int pass, int i) {
         if (pass == 0) return make_uint2(emb_key(p, p.ids[i]), i);
-        if (ON_CHIP) return list[(pass & 1) * chunk + static_cast<int>(i - cta_from)];
-        return __ldcg(&p.keys[pass & 1][i]);
+        return list[(pass & 1) * chunk + static_cast<int>(i - cta_from)];
     };
-    // the element's place among those of its digit that this warp has seen; counts it
-    auto count = [&](bool valid, uint32_t key, int shift) {
-        int at = 0;
-        const unsigned here = __ballot_sync(0xffffffffu, valid);
-        if (valid) {
-            const int digit = (key >> shift) & (bins - 1);
-            const unsigned peers = __match_any_sync(here, digit);
-            at = mine[digit] + __popc(peers & ((1u << lane) - 1));
-            __syncwarp(here);
-            if (lane == __ffs(peers) - 1) mine[digit] += __popc(peers);
-        }
-        __syncwarp();
-        return at;
-    };
-    uint2 held[ON_CHIP ? NW : 1];
-    int at[ON_CHIP ? NW : 1];
+    uint2 held[NW];
+    int at[NW];
     auto hold = [&](int pass) {
 #pragma unroll
         for (int w = 0; w < NW; ++w)
             if (first + 32 * w + lane < last) held[w] = element(pass, first + 32 * w + lane);
     };
-    if (ON_CHIP) hold(0);
+    hold(0);
     for (int pass = 0; pass < passes; ++pass) {
         const int shift = pass * digit_bits;
         for (int i = lane; i < bins; i += 32) mine[i] = 0;
         __syncwarp();
-        if (ON_CHIP) {
 #pragma unroll
-            for (int w = 0; w < NW; ++w) at[w] = count(first + 32 * w + lane < last, held[w].x, shift);
-        } else {
-            for (int i = first + lane; i - lane < last; i += 32) count(i < last, i < last ? element(pass, i).x : 0, shift);
-        }
+        for (int w = 0; w < NW; ++w) at[w] = emb_count(mine, first + 32 * w + lane < last, held[w].x >> shift & (bins - 1), lane);
         __syncthreads();
         int sum = 0;
         if (tid < bins) {                                    // a bin's counts -> counts of the warps before
@@ -249,43 +254,28 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
         const int below = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0);
         if (tid < bins) sm.base[tid] = scan - all + before + below;
         __syncthreads();
-        auto move = [&](uint2 e, int in_cta) {               // in_cta: the place among the CTA's elements of that digit
-            const int to = sm.base[(e.x >> shift) & (bins - 1)] + in_cta;
-            if (ON_CHIP) {
-                const uint32_t cta = static_cast<uint32_t>(to) / static_cast<uint32_t>(chunk);
-                st_cluster_uint2(mapa_cluster(smem_u32(list + ((pass + 1) & 1) * chunk + (to - static_cast<int>(cta) * chunk)), cta), e);
-            } else {
-                __stcg(&p.keys[(pass + 1) & 1][to], e);
-            }
-        };
-        if (ON_CHIP) {
 #pragma unroll
-            for (int w = 0; w < NW; ++w)
-                if (first + 32 * w + lane < last) move(held[w], at[w] + mine[(held[w].x >> shift) & (bins - 1)]);
-        } else {
-            for (int i = first + lane; i - lane < last; i += 32) {
-                const uint2 e = i < last ? element(pass, i) : make_uint2(0, 0);
-                const int in_cta = count(i < last, e.x, shift);
-                if (i < last) move(e, in_cta);
-            }
+        for (int w = 0; w < NW; ++w) {
+            if (first + 32 * w + lane >= last) continue;
+            const int digit = held[w].x >> shift & (bins - 1), to = sm.base[digit] + mine[digit] + at[w], cta = to / chunk;
+            st_cluster_uint2(mapa_cluster(smem_u32(list + ((pass + 1) & 1) * chunk + (to - cta * chunk)), cta), held[w]);
         }
         __syncwarp();
         cluster_sync_all();
-        if (ON_CHIP) hold(pass + 1);
+        hold(pass + 1);
     }
     // Records need the ends of each run.  Heads (first places of runs) of a warp's windows, the first and the last of its stretch,
     // then of its CTA; what a stretch does not hold, the closest stretch before or after it does.
     constexpr int NONE_BEFORE = -1, NONE_AFTER = 0x7fffffff;
     auto window = [&](int i0) {                              // i0 + lane's element; past the end a key that no token has
         const int i = i0 + lane;
-        return i < T ? (ON_CHIP ? list[(passes & 1) * chunk + static_cast<int>(i - cta_from)] : __ldcg(&p.keys[passes & 1][i]))
-                     : make_uint2(0xffffffffu, 0);
+        return i < T ? list[(passes & 1) * chunk + static_cast<int>(i - cta_from)] : make_uint2(0xffffffffu, 0);
     };
     auto heads_of = [&](int i0, uint32_t key) {
         uint32_t left = __shfl_up_sync(0xffffffffu, key, 1);
         if (lane == 0) {
             left = 0xfffffffeu;
-            if (i0 > cta_from || (!ON_CHIP && i0 > 0)) left = element(passes, i0 - 1).x;
+            if (i0 > cta_from) left = element(passes, i0 - 1).x;
             else if (rank > 0) left = ld_cluster_int(mapa_cluster(smem_u32(list + (passes & 1) * chunk + chunk - 1), rank - 1));
         }
         return __ballot_sync(0xffffffffu, key != left);      // (places from T on: the first of them is a head)
@@ -323,13 +313,10 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
         before = max(before, __reduce_max_sync(0xffffffffu, cta_last));
         after = min(min(after, __reduce_min_sync(0xffffffffu, cta_first)), T);
     }
-    const uint32_t bad = p.V;
     int next = -1;                                           // the first head behind the window
     for (int i0 = first; i0 < last; i0 += 32) {
-        const int i = i0 + lane;
         const uint2 e = window(i0);
         const unsigned heads = heads_of(i0, e.x);
-        const unsigned to_lane = 0xffffffffu >> (31 - lane);
         if (next < i0 + 32) {
             next = after;
             for (int j0 = i0 + 32; j0 < last; j0 += 32) {
@@ -340,22 +327,136 @@ __global__ void __launch_bounds__(EMB_SORT_THREADS) embed_sort_kernel(const Embe
                 }
             }
         }
-        if (i < last) {
-            const unsigned upto = heads & to_lane, behind = heads & ~to_lane;
-            const int head = upto ? i0 + 31 - __clz(upto) : before;
-            const int tail = behind ? i0 + __ffs(behind) - 1 : next;
-            uint4 rec = emb_record(e.x, i - head, tail - head, e.y);
-            if (e.x == bad) {
-                rec.y = 0;
-                if (i == head) atomicOr(p.dev_status, TIK_DEV_BAD_TOKEN);
-            }
-            p.order[i] = e.y;
-            p.place[i] = rec;
-        }
+        if (i0 + lane < last) emb_write_record(p, i0, e, heads, before, next, lane);
         if (heads) before = i0 + 31 - __clz(heads);
     }
     __syncwarp();
     cluster_sync_all();                                      // no CTA leaves while another may read its shared memory
+}
+
+// More than EMB_CHIP_TOKENS: the list in global memory, EMB_WIDE_CTAS CTAs, two launches a digit -- counts of every CTA, then each
+// CTA adds up the counts before it, counts once more and moves its elements -- and one for the records.  (By the cluster above
+// out of global memory, for which eight SMs have too few loads in flight, 65 537 tokens took 94 us with the sums of 256 columns and
+// 262 144 299; so 54 and 105.  65 536 by the cluster on chip: 60, under the zeros where those are written.)
+constexpr int EMB_WIDE_CTAS = 128, EMB_WIDE_AHEAD = 4;       // windows of a warp in flight
+struct EmbedWideSmem {
+    int hist[EMB_SORT_WARPS][EMB_BINS];
+    int base[EMB_BINS], half[2][EMB_BINS], all[2][EMB_BINS], warp_sum[EMB_SORT_WARPS];
+};
+// f(index, element) for the warp's stretch in order, every lane taking part; index >= last: there is none
+template <class F>
+__device__ __forceinline__ void emb_wide_elements(const EmbedParams& p, int pass, int lane, F&& f) {
+    const int T = static_cast<int>(p.T), warp = blockIdx.x * EMB_SORT_WARPS + (threadIdx.x >> 5);
+    const int per = ((T + EMB_WIDE_CTAS * EMB_SORT_WARPS - 1) / (EMB_WIDE_CTAS * EMB_SORT_WARPS) + 31) / 32 * 32;
+    const long long from = static_cast<long long>(per) * warp;
+    const int first = static_cast<int>(from < T ? from : T), last = static_cast<int>(from + per < T ? from + per : T);
+    for (int i0 = first; i0 < last; i0 += 32 * EMB_WIDE_AHEAD) {
+        uint2 e[EMB_WIDE_AHEAD];
+#pragma unroll
+        for (int u = 0; u < EMB_WIDE_AHEAD; ++u) {
+            const int i = i0 + 32 * u + lane;
+            if (i < last) e[u] = pass == 0 ? make_uint2(emb_key(p, p.ids[i]), i) : __ldcg(&p.keys[pass & 1][i]);
+        }
+#pragma unroll
+        for (int u = 0; u < EMB_WIDE_AHEAD; ++u) f(i0 + 32 * u + lane < last, e[u]);
+    }
+}
+__global__ void __launch_bounds__(EMB_SORT_THREADS) embed_wide_count_kernel(const EmbedParams p, int pass, int digit_bits) {
+    extern __shared__ __align__(16) unsigned char emb_smem[];
+    EmbedWideSmem& sm = *reinterpret_cast<EmbedWideSmem*>(emb_smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bins = 1 << digit_bits, shift = pass * digit_bits;
+    for (int i = lane; i < bins; i += 32) sm.hist[warp][i] = 0;
+    __syncwarp();
+    pdl_wait();
+    pdl_launch_dependents();
+    emb_wide_elements(p, pass, lane, [&](bool there, uint2 e) { emb_count(sm.hist[warp], there, e.x >> shift & (bins - 1), lane); });
+    __syncthreads();
+    if (tid >= bins) return;
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < EMB_SORT_WARPS; ++w) sum += sm.hist[w][tid];
+    p.counts[blockIdx.x * EMB_BINS + tid] = sum;
+}
+__global__ void __launch_bounds__(EMB_SORT_THREADS) embed_wide_move_kernel(const EmbedParams p, int pass, int digit_bits) {
+    extern __shared__ __align__(16) unsigned char emb_smem[];
+    EmbedWideSmem& sm = *reinterpret_cast<EmbedWideSmem*>(emb_smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, bins = 1 << digit_bits, shift = pass * digit_bits;
+    for (int i = lane; i < bins; i += 32) sm.hist[warp][i] = 0;
+    __syncwarp();
+    pdl_wait();
+    pdl_launch_dependents();
+    emb_wide_elements(p, pass, lane, [&](bool there, uint2 e) { emb_count(sm.hist[warp], there, e.x >> shift & (bins - 1), lane); });
+    {
+        const int bin = tid % EMB_BINS, part = tid / EMB_BINS;           // two threads a bin, half of the CTAs each
+        int before = 0, all = 0;
+        if (bin < bins) {
+#pragma unroll 16
+            for (int c = part * (EMB_WIDE_CTAS / 2); c < (part + 1) * (EMB_WIDE_CTAS / 2); ++c) {
+                const int n = __ldcg(&p.counts[c * EMB_BINS + bin]);
+                before += c < static_cast<int>(blockIdx.x) ? n : 0;
+                all += n;
+            }
+        }
+        sm.half[part][bin] = before;
+        sm.all[part][bin] = all;
+    }
+    __syncthreads();
+    int all = 0, scan = 0;
+    if (tid < bins) {
+        int sum = sm.half[0][tid] + sm.half[1][tid];                     // of the CTAs before, then of the warps before
+#pragma unroll
+        for (int w = 0; w < EMB_SORT_WARPS; ++w) {
+            const int n = sm.hist[w][tid];
+            sm.hist[w][tid] = sum;
+            sum += n;
+        }
+        scan = all = sm.all[0][tid] + sm.all[1][tid];
+    }
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int n = __shfl_up_sync(0xffffffffu, scan, off);
+        if (lane >= off) scan += n;
+    }
+    if (lane == 31) sm.warp_sum[warp] = scan;
+    __syncthreads();
+    const int below = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0);
+    if (tid < bins) sm.base[tid] = scan - all + below;
+    __syncthreads();
+    emb_wide_elements(p, pass, lane, [&](bool there, uint2 e) {
+        const int digit = e.x >> shift & (bins - 1), at = emb_count(sm.hist[warp], there, digit, lane);
+        if (there) __stcg(&p.keys[(pass + 1) & 1][sm.base[digit] + at], e);
+    });
+}
+// first place of [0, n) whose key is >= key, found by a whole warp (keys ascending)
+__device__ __forceinline__ int emb_lower_bound(const uint2* keys, int n, uint32_t key, int lane) {
+    int lo = 0, hi = n;                      // keys before lo are < key, keys from hi on are not
+    while (lo < hi) {
+        const int step = (hi - lo + 31) / 32, probe = lo + step * (lane + 1) - 1;
+        const unsigned below = __ballot_sync(0xffffffffu, probe < hi && __ldcg(&keys[probe]).x < key);
+        const int c = __popc(below);
+        hi = min(hi, lo + step * (c + 1) - 1);
+        lo += step * c;
+    }
+    return lo;
+}
+// a window of 32 places per warp
+constexpr int EMB_RECORD_WARPS = 8;
+__global__ void __launch_bounds__(EMB_RECORD_WARPS * 32) embed_wide_record_kernel(const EmbedParams p, int passes) {
+    pdl_wait();
+    pdl_launch_dependents();
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.tickets[threadIdx.x] = 0;
+    const int T = static_cast<int>(p.T), lane = threadIdx.x & 31, i0 = (blockIdx.x * EMB_RECORD_WARPS + (threadIdx.x >> 5)) * 32, i = i0 + lane;
+    if (i0 >= T) return;
+    const uint2* keys = p.keys[passes & 1];
+    const uint2 e = i < T ? __ldcg(&keys[i]) : make_uint2(0xffffffffu, 0);
+    uint32_t left = __shfl_up_sync(0xffffffffu, e.x, 1);
+    if (lane == 0) left = i0 > 0 ? __ldcg(&keys[i0 - 1]).x : 0xfffffffeu;
+    const uint32_t right = i0 + 32 < T ? __ldcg(&keys[i0 + 32]).x : 0xfffffffeu;
+    const unsigned heads = __ballot_sync(0xffffffffu, e.x != left);
+    const uint32_t k0 = __shfl_sync(0xffffffffu, e.x, 0), k31 = __shfl_sync(0xffffffffu, e.x, 31);
+    const int before = heads & 1 ? i0 : emb_lower_bound(keys, T, k0, lane);
+    const int next = k31 == right ? emb_lower_bound(keys, T, k31 + 1, lane) : min(i0 + 32, T);
+    if (i < T) emb_write_record(p, i0, e, heads, before, next, lane);
 }
 
 // eight columns of a table row: what is there, and the new value
@@ -506,7 +607,8 @@ __global__ void __launch_bounds__(EMB_SUM_THREADS) embed_sum_kernel(const EmbedP
     };
     __shared__ Item list[EMB_SUM_WARPS][32];
     const int slices = (vpr + 32 * NV - 1) / (32 * NV), warps = gridDim.x * (EMB_SUM_WARPS - IDLE);
-    // Two shares a warp of one place at least (a share costs three trips to L2 before its first row) and 16 at most (balance).
+    // Two shares a warp of one place at least (a share costs three trips to L2 before its first row; six a warp: 203 us instead of 180 for
+    // two micro-batches of 6007 x 1536, fp32) and 16 places at most (32: 97 us instead of 86 for 16 001 x 3584, fp32, added).
     const long long each = p.T * slices / (2ll * warps);
     const int places = each < 1 ? 1 : each > 16 ? 16 : static_cast<int>(each);
     const long long shares = (p.T + places - 1) / places * slices;
@@ -653,7 +755,8 @@ __global__ void __launch_bounds__(EMB_FOLD_WARPS * 32) embed_fold_kernel(const E
 // several pieces waits until the CTA is through with the others and then gets a warp per piece; eight pieces at most are added
 // up in the order of embed_fold_kernel.  256 tokens x 256, vocabulary 2048: 8.9 us by the three kernels, 3.0 by this one.
 constexpr int EMB_SMALL_TOKENS = EMB_FOLD_WARPS * EMB_PIECE, EMB_SMALL_WORDS = EMB_SMALL_TOKENS / 32;
-constexpr long long EMB_SMALL_BYTES = 32 << 20;              // of the table, where it is written whole
+constexpr long long EMB_SMALL_BYTES = 128 << 20;             // of the table, where it is written whole: beyond, even shares of the zeros cost more
+                                                             // (256 tokens, us: 134 MB 23.1 so and 24.6 by the three kernels, 268 MB 45.7 and 42.5)
 constexpr int EMB_SMALL_ROWS = 1 << 16;                      // rows of a CTA's share of the zeros
 constexpr int EMB_QUEUE = 32;
 template <bool FP32, bool ACC>
@@ -777,7 +880,7 @@ __global__ void __launch_bounds__(EMB_SUM_THREADS) embed_small_kernel(const Embe
 static size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 size_t embed_bwd_bytes(int64_t T, int, int H) {
     const size_t n = static_cast<size_t>(T);
-    return align16(4 * n) + 16 * n + (T > EMB_CHIP_TOKENS ? 2 * 8 * n : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;      // (16: the counters)
+    return align16(4 * n) + 16 * n + (T > EMB_CHIP_TOKENS ? 2 * 8 * n + 4 * EMB_WIDE_CTAS * EMB_BINS : 0) + (T > EMB_PIECE ? 2 * (n / EMB_PIECE + 1) * 4 * H : 0) + 16;      // (16: the counters)
 }
 
 cudaError_t launch_embed(const EmbedParams& p0, cudaStream_t stream) {
@@ -801,7 +904,7 @@ static cudaError_t launch_embed_small(const EmbedParams& p, cudaStream_t stream)
 }
 template <bool FP32, bool ACC>
 static cudaError_t launch_embed_sums(const EmbedParams& p, cudaStream_t stream) {
-    const int late = p.T > EMB_RANK_TOKENS && p.sm_count > 2 * EMB_CLUSTER ? EMB_CLUSTER : 0;
+    const int late = p.T > EMB_RANK_TOKENS && p.T <= EMB_CHIP_TOKENS && p.sm_count > 2 * EMB_CLUSTER ? EMB_CLUSTER : 0;
     const size_t marks = ACC ? 0 : (std::min(p.V, EMB_MARK_ROWS) + 31) / 32 * sizeof(uint32_t);
     cudaError_t e = launch_pdl(embed_sum_kernel<FP32, ACC>, dim3(static_cast<unsigned>(p.sm_count)), EMB_SUM_THREADS, marks, stream, 1, p, late);
     if (e != cudaSuccess || p.T <= EMB_PIECE) return e;
@@ -815,9 +918,12 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
     at += 16;
     p.place = reinterpret_cast<uint4*>(at);
     at += 16 * p.T;
-    const bool on_chip = p.T <= EMB_CHIP_TOKENS;
-    if (!on_chip)
+    const bool wide = p.T > EMB_CHIP_TOKENS;
+    if (wide) {
+        p.counts = reinterpret_cast<int*>(at);
+        at += 4 * EMB_WIDE_CTAS * EMB_BINS;
         for (int i = 0; i < 2; ++i, at += 8 * p.T) p.keys[i] = reinterpret_cast<uint2*>(at);
+    }
     p.order = reinterpret_cast<int32_t*>(at);
     p.part = reinterpret_cast<float*>(at + align16(4 * p.T));
     cudaError_t e = cudaSuccess;
@@ -834,7 +940,8 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
                 if (r == cudaSuccess)
                     r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(emb_sort_smem(nw)));
             };
-            allow(embed_sort_kernel<0>, 0);
+            if (r == cudaSuccess) r = cudaFuncSetAttribute(embed_wide_count_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(EmbedWideSmem));
+            if (r == cudaSuccess) r = cudaFuncSetAttribute(embed_wide_move_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(EmbedWideSmem));
             allow(embed_sort_kernel<1>, 1);
             allow(embed_sort_kernel<2>, 2);
             allow(embed_sort_kernel<4>, 4);
@@ -845,11 +952,21 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
         int bits = 1;
         while (p.V >> bits) ++bits;                          // keys are 0 .. V
         const int passes = (bits + 8) / 9, digit_bits = (bits + passes - 1) / passes;
-        const long long windows = (p.T + EMB_CHIP_TOKENS / 8 - 1) / (EMB_CHIP_TOKENS / 8);       // per warp
-        const int nw = !on_chip ? 0 : windows <= 1 ? 1 : windows <= 2 ? 2 : windows <= 4 ? 4 : 8;
-        auto kern = nw == 0 ? embed_sort_kernel<0> : nw == 1 ? embed_sort_kernel<1> : nw == 2 ? embed_sort_kernel<2>
-                  : nw == 4 ? embed_sort_kernel<4> : embed_sort_kernel<8>;
-        e = launch_pdl(kern, dim3(EMB_CLUSTER), EMB_SORT_THREADS, emb_sort_smem(nw), stream, EMB_CLUSTER, p, passes, digit_bits);
+        if (wide) {
+            for (int pass = 0; pass < passes && e == cudaSuccess; ++pass) {
+                e = launch_pdl(embed_wide_count_kernel, dim3(EMB_WIDE_CTAS), EMB_SORT_THREADS, sizeof(EmbedWideSmem), stream, 1, p, pass, digit_bits);
+                if (e == cudaSuccess)
+                    e = launch_pdl(embed_wide_move_kernel, dim3(EMB_WIDE_CTAS), EMB_SORT_THREADS, sizeof(EmbedWideSmem), stream, 1, p, pass, digit_bits);
+            }
+            if (e != cudaSuccess) return e;
+            const unsigned grid = static_cast<unsigned>((p.T + 32 * EMB_RECORD_WARPS - 1) / (32 * EMB_RECORD_WARPS));
+            e = launch_pdl(embed_wide_record_kernel, dim3(grid), EMB_RECORD_WARPS * 32, 0, stream, 1, p, passes);
+        } else {
+            const long long windows = (p.T + EMB_CHIP_TOKENS / 8 - 1) / (EMB_CHIP_TOKENS / 8);       // per warp
+            const int nw = windows <= 1 ? 1 : windows <= 2 ? 2 : windows <= 4 ? 4 : 8;
+            auto kern = nw == 1 ? embed_sort_kernel<1> : nw == 2 ? embed_sort_kernel<2> : nw == 4 ? embed_sort_kernel<4> : embed_sort_kernel<8>;
+            e = launch_pdl(kern, dim3(EMB_CLUSTER), EMB_SORT_THREADS, emb_sort_smem(nw), stream, EMB_CLUSTER, p, passes, digit_bits);
+        }
     } else if (p.T > 0) {
         e = launch_pdl(embed_rank_kernel, dim3(static_cast<unsigned>((p.T + 31) / 32)), EMB_RANK_WARPS * 32, 0, stream, 1, p);
     }

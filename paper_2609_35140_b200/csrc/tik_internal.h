@@ -216,7 +216,8 @@ struct EmbedParams {
     int V, H;
     int32_t* order;              // scratch [T]: tokens by id, equal ids by position
     uint4* place;                // scratch [T]: what begins at a place of that order (tik_embed.cu)
-    uint2* keys[2];              // scratch [T] each: (id, token) between the passes of the sort
+    uint2* keys[2];              // scratch [T] each: (id, token) between the passes of a long list's sort
+    int* counts;                 // scratch: its digits per CTA
     int* tickets;                // scratch [2]: shares of the zeros and of the sums taken so far
     float* part;                 // scratch [2 (T / 32 + 1)][H]: sums of a long run's pieces
     int sm_count;
