@@ -295,30 +295,33 @@ cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const i
 bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, bool* no_memory) {
     struct Range {
         uintptr_t from, to;
-        bool written;
     };
     *no_memory = false;
     if (n <= 0) return false;
-    Range* r = static_cast<Range*>(malloc(2ull * n * sizeof(Range)));
-    if (!r) return *no_memory = true;
-    size_t count = 0;
+    Range* const written = static_cast<Range*>(malloc(2ull * n * sizeof(Range)));
+    if (!written) return *no_memory = true;
+    Range* const read = written + n;                         // inputs that are not written in place
+    int nw = 0, nr = 0;
     for (int i = 0; i < n; ++i) {
         if (numel[i] == 0) continue;
         const uintptr_t bytes = static_cast<uintptr_t>(numel[i]) * (dtypes[i] == 1 ? 4 : 2);
         const uintptr_t in = reinterpret_cast<uintptr_t>(grads[i]), to = out ? reinterpret_cast<uintptr_t>(out[i]) : in;
-        r[count++] = {to, to + bytes, true};
-        if (to != in) r[count++] = {in, in + bytes, false};
+        written[nw++] = {to, to + bytes};
+        if (to != in) read[nr++] = {in, in + bytes};
     }
     auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
-    if (!std::is_sorted(r, r + count, before)) std::sort(r, r + count, before);
-    uintptr_t end_written = 0, end_any = 0;
+    auto ascending = [&](Range* r, int count) {              // (lists of a flat buffer's views are already)
+        if (!std::is_sorted(r, r + count, before)) std::sort(r, r + count, before);
+    };
+    ascending(written, nw);
+    ascending(read, nr);
     bool overlap = false;
-    for (size_t i = 0; i < count && !overlap; ++i) {
-        overlap = r[i].from < (r[i].written ? end_any : end_written);
-        end_any = std::max(end_any, r[i].to);
-        if (r[i].written) end_written = std::max(end_written, r[i].to);
+    for (int i = 1; i < nw && !overlap; ++i) overlap = written[i].from < written[i - 1].to;
+    for (int i = 0, j = 0; i < nr && !overlap; ++i) {
+        while (j < nw && written[j].to <= read[i].from) ++j;
+        overlap = j < nw && written[j].from < read[i].to;
     }
-    free(r);
+    free(written);
     return overlap;
 }
 

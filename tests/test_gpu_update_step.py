@@ -145,6 +145,38 @@ def test_steps_of_threads_on_streams_of_their_own(tik):
             assert count_diff(a[k], w[k]) == 0, k
 
 
+def test_calls_through_buffers_that_are_written_again(tik):
+    """Chains without a synchronisation, each call's inputs written by the one before it: whatever runs under its predecessor's tail
+    sees what a synchronised chain sees."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    W, K = 20_000, 1024
+    tables = [_randn((W, K), g) for _ in range(2)]
+    sizes = [200, 3000, 6000, 20_000, 257, 66_000, 4608]
+    ids = [torch.randint(0, W, (n,), generator=g, device="cuda").to(torch.int32) for n in sizes]
+    w = _randn((K,), g, 0.1, 1.0)
+
+    def chain(sync):
+        a, b = (t.clone() for t in tables)
+        seen = []
+        for i, n in enumerate(sizes * 2):
+            step = (lambda: torch.cuda.synchronize()) if sync else (lambda: None)
+            idx = ids[i % len(sizes)]
+            if i % 3 == 1:
+                idx = torch.roll(idx, i)                       # written just before the call that reads it
+            y = tik.tik_embedding(idx, a, 0.5); step()
+            y, s = tik.tik_block_norm(y, y, w, EPS, post_weight=w); step()
+            dx, dr, dw, dp, _ = tik.tik_block_norm_bwd(y, s, y, s, w, EPS, post_weight=w); step()
+            tik.tik_embedding_bwd(dx, idx, W, 1.0, d_table=b, accumulate=i % 4 == 3); step()
+            seen.append(tik.tik_grad_clip([b, dw, dp], 100.0 + i)); step()
+            tik.tik_embedding_bwd(dr, idx, W, 1.0, d_table=b, accumulate=True); step()
+            a, b = b, a                                        # the next lookup reads what was just added up
+        torch.cuda.synchronize()
+        return seen + [a, b]
+
+    for x, y in zip(chain(False), chain(True)):
+        assert count_diff(x, y) == 0
+
+
 def test_launch_counts(tik):
     """Kernels per call: the ones that the header states."""
     def launches(f):
@@ -156,6 +188,8 @@ def test_launch_counts(tik):
     table, dy = _randn((V, H), g), _randn((5000, H), g)
     assert launches(lambda: tik.tik_embedding(ids, table)) == 1
     assert launches(lambda: tik.tik_embedding_bwd(dy, ids, V)) == 3
+    many, long_ids = _randn((65_537, H), g), torch.randint(0, V, (65_537,), generator=g, device="cuda").to(torch.int32)
+    assert launches(lambda: tik.tik_embedding_bwd(many, long_ids, V)) == 5            # one digit of nine bits
     assert launches(lambda: tik.tik_embedding_bwd(dy[:200].contiguous(), ids[:200].contiguous(), V)) == 1
     w = _randn((H,), g)
     assert launches(lambda: tik.tik_block_norm(dy, dy, w, EPS, post_weight=w, gate=w)) == 1

@@ -2,6 +2,7 @@
 every refusal comes before anything is queued, so none of this needs a GPU (and with one it is left out: were a check
 lost, the call would reach it with made-up addresses)."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -129,6 +130,22 @@ def test_written_tensors_may_not_overlap(ctx):
     assert refused([C, D], [4, 4], [0, 0], out=[D, E])                        # a result over another input
     assert refused([C], [4], [0], out=[C + 2])                                # a shifted copy of itself
     assert refused([C, D], [4, 4], [1, 0], out=[C, C + 14])                   # fp32: 16 bytes
+
+
+def test_overlap_rule_against_all_pairs(ctx):
+    """Random lists: refused exactly where a written range meets another written one or an input that is not written."""
+    rng = random.Random(3)
+    for _ in range(3000):
+        n = rng.randint(1, 6)
+        ins, numel = [16 * rng.randint(1, 60) for _ in range(n)], [rng.choice([0, 4, 8, 16, 40]) for _ in range(n)]
+        outs = None if rng.random() < 0.4 else [i if rng.random() < 0.3 else 16 * rng.randint(1, 60) for i in ins]
+        to = outs or ins
+        W = [(to[k], to[k] + 2 * numel[k]) for k in range(n) if numel[k]]
+        R = [(ins[k], ins[k] + 2 * numel[k]) for k in range(n) if numel[k] and ins[k] != to[k]]
+        meet = lambda a, b: a[0] < b[1] and b[0] < a[1]
+        overlap = any(meet(W[i], W[j]) for i in range(len(W)) for j in range(i)) or any(meet(a, b) for a in W for b in R)
+        # without scratch a list that passes is refused for that
+        assert _clip(ctx, ins, numel, [0] * n, out=outs, ws=None, ws_bytes=0) == (INVALID if overlap else WORKSPACE)
 
 
 def test_scratch_sizes():
