@@ -12,17 +12,28 @@ namespace tik {
 
 constexpr int BN_THREADS = 128;
 
+// a row's sum from its warps' totals
+template <int ROWS>
+__device__ __forceinline__ float bn_row_total(const float* w4, int mine) {
+    return ROWS == 4 ? w4[mine] : ROWS == 2 ? __fadd_rn(w4[2 * mine], w4[2 * mine + 1]) : hn_block_total(w4);
+}
+
 // One CTA per row with the reduction shape of rmsnorm_kernel (NV 16-byte vectors per thread): without post norm and gate
 // and with a scale of 1 the results are those of its residual form, bit for bit.
 // FEW (calls of up to BN_FEW_ROWS rows): weights and gate are requested with the row, not when they are needed -- a chain of
 // trips to L2 that many resident rows hide, and that a decode step waits for (call after call on the device, us: 64 x 3584 4.2 without
 // and 2.4 with FEW; 1024 x 3584 5.4 and 5.8; 9001 x 5120 58 and 92: its registers halve the rows on an SM).
+// ROWS: rows of a CTA.  Of up to 256 (512) channels a row's data sit in one (two) of the four warps of that shape, whose totals are then
+// the whole sum, so four (two) rows take a CTA and a CTA per row does not wait for its turn to start (60 000 x 256: 50.4 us
+// with one row, ROWSUS with four).
 constexpr long long BN_FEW_ROWS = 512;
-template <int NV, bool FEW>
+template <int NV, bool FEW, int ROWS>
 __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormParams p) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long row = blockIdx.x;
-    const int nvec = p.H / 8;
+    constexpr int WIDTH = BN_THREADS / ROWS;
+    const int mine = threadIdx.x / WIDTH, tid = threadIdx.x % WIDTH, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long row = blockIdx.x * static_cast<long long>(ROWS) + mine;
+    const bool there = ROWS == 1 || row < p.T;
+    const int nvec = there ? p.H / 8 : 0;
     const uint4* x = reinterpret_cast<const uint4*>(p.x) + row * nvec;
     const uint4* res = reinterpret_cast<const uint4*>(p.residual) + row * nvec;
     const uint4* wp = reinterpret_cast<const uint4*>(p.post_weight);
@@ -34,7 +45,7 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
     const uint4* gc = p.gate_kind == GATE_CHANNEL ? reinterpret_cast<const uint4*>(p.gate) : nullptr;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int v = tid + BN_THREADS * j;
+        const int v = tid + WIDTH * j;
         if (v < nvec) {
             xv[j] = x[v];
             rv[j] = res[v];
@@ -47,12 +58,12 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
     }
     const float inv_h = 1.0f / static_cast<float>(p.H);
     float c = p.branch_scale;                                // what all channels have in common
-    if (p.gate_kind == GATE_TOKEN) c = __fmul_rn(c, __bfloat162float(p.gate[row]));
+    if (p.gate_kind == GATE_TOKEN) c = __fmul_rn(c, there ? __bfloat162float(p.gate[row]) : 0.0f);
     if (wp) {
         F2 part = f2(0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (tid + BN_THREADS * j < nvec) {
+            if (tid + WIDTH * j < nvec) {
                 const uint32_t xw[4] = {xv[j].x, xv[j].y, xv[j].z, xv[j].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -63,14 +74,14 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
         const float sum = hn_warp_total(f2_sum(part));
         if (lane == 0) tot_x[warp] = sum;
         __syncthreads();
-        c = __fmul_rn(c, prep_inv_rms(hn_block_total(tot_x), inv_h, p.eps));
+        c = __fmul_rn(c, prep_inv_rms(bn_row_total<ROWS>(tot_x, mine), inv_h, p.eps));
     }
     const F2 c2 = f2(c);
     uint32_t s[NV][4];
     float part = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int v = tid + BN_THREADS * j;
+        const int v = tid + WIDTH * j;
         if (v >= nvec) continue;
         const uint32_t xw[4] = {xv[j].x, xv[j].y, xv[j].z, xv[j].w}, rw[4] = {rv[j].x, rv[j].y, rv[j].z, rv[j].w};
         F2 f[4];
@@ -103,10 +114,10 @@ __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormP
     part = hn_warp_total(part);
     if (lane == 0) tot_s[warp] = part;
     __syncthreads();
-    const F2 inv = f2(prep_inv_rms(hn_block_total(tot_s), inv_h, p.eps));
+    const F2 inv = f2(prep_inv_rms(bn_row_total<ROWS>(tot_s, mine), inv_h, p.eps));
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int v = tid + BN_THREADS * j;
+        const int v = tid + WIDTH * j;
         if (v >= nvec) continue;
         const uint4 w4 = FEW ? wnv[FEW ? j : 0] : wn[v];
         const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
@@ -174,7 +185,8 @@ __device__ __forceinline__ float bn_rsqrt(float x) {
     return r;
 }
 
-template <int NV, int THREADS>
+// X: something of x is needed -- it has a norm or a gate.  Without either d_x is G times a number, and x is not read.
+template <int NV, int THREADS, bool X>
 __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockNormParams p, const BlockNormBwdShape shape) {
     extern __shared__ __align__(128) unsigned char bn_smem[];
     BlockNormBwdSmem& sm = *reinterpret_cast<BlockNormBwdSmem*>(bn_smem);
@@ -185,7 +197,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     const int lane = threadIdx.x & 31, warps = width >> 5, warp = tid >> 5;
     const int nvec = p.H / 8, row_vecs = NV * width;      // (a row in the ring is as wide as the threads' vectors)
     const float inv_h = 1.0f / static_cast<float>(p.H);
-    const bool norm = p.weight != nullptr, post = p.post_weight != nullptr, branch = p.x != nullptr;
+    const bool norm = p.weight != nullptr, post = X && p.post_weight != nullptr, branch = p.d_x != nullptr;
     // What is absent reads as zeros: planes that are not there, vectors behind the row.
     for (int i = threadIdx.x; i < shape.slots * 4 * row_vecs; i += blockDim.x) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
@@ -197,14 +209,14 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     __syncthreads();
     pdl_wait();
     pdl_launch_dependents();
-    const int planes = (norm ? 2 : 0) + (branch ? 1 : 0) + (p.d_s ? 1 : 0);
+    const int planes = (norm ? 2 : 0) + (X ? 1 : 0) + (p.d_s ? 1 : 0);
     // The CTA's n-th row, which group n % groups takes, is row blockIdx.x + n * gridDim.x; planes of a slot: d_s, x, s, d_y.
     const unsigned T = static_cast<unsigned>(p.T);           // (below 2^31: a row behind the last one does not wrap)
     auto request = [&](unsigned row, int slot) {
         if (row >= T) return;
         const uint32_t bar = smem_u32(&sm.full[slot]), to = smem_u32(ring + slot * shape.slot_bytes);
         mbar_expect_tx(bar, planes * p.H * 2);
-        const __nv_bfloat16* src[4] = {p.d_s, p.x, norm ? p.s : nullptr, norm ? p.d_y : nullptr};
+        const __nv_bfloat16* src[4] = {p.d_s, X ? p.x : nullptr, norm ? p.s : nullptr, norm ? p.d_y : nullptr};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (src[i]) bulk_load(to + i * 16 * row_vecs, src[i] + static_cast<size_t>(row) * p.H, p.H * 2, bar);
@@ -249,13 +261,13 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             uint32_t x[4], s4[4], dy[4];
-            take(at, 1, j, x);
+            if (X) take(at, 1, j, x);
             take(at, 2, j, s4);
             take(at, 3, j, dy);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const S2 xe = s2_bf16(x[e]), se = s2_bf16(s4[e]);
-                sx = s2_fma(xe, xe, sx);
+                const S2 se = s2_bf16(s4[e]);
+                if (X) sx = s2_fma(s2_bf16(x[e]), s2_bf16(x[e]), sx);
                 ss = s2_fma(se, se, ss);
                 sq = s2_fma(s2_mul(s2_bf16(dy[e]), s2_bf16(w[j][e])), se, sq);
             }
@@ -296,17 +308,20 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
             const S2 f[4] = {s2(f0.x, f0.y), s2(f0.z, f0.w), s2(f1.x, f1.y), s2(f1.z, f1.w)};
             uint32_t ds[4], s[4], dy[4], out[4];
             take(at, 0, j, ds);
-            take(at, 1, j, x[j]);
+            if (X) take(at, 1, j, x[j]);
             take(at, 2, j, s);
             take(at, 3, j, dy);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const S2 xe = s2_bf16(x[j][e]), se = s2_bf16(s[e]), rdy = s2_mul(rs2, s2_bf16(dy[e]));
+                const S2 se = s2_bf16(s[e]), rdy = s2_mul(rs2, s2_bf16(dy[e]));
                 const S2 G = s2_fma(ks2, se, s2_fma(rdy, s2_bf16(w[j][e]), s2_bf16(ds[e])));
                 sum_w[j][e] = s2_fma(rdy, se, sum_w[j][e]);
-                sum_c[j][e] = s2_fma(s2_mul(G, xe), c2, sum_c[j][e]);
                 Gf[j][e] = s2_mul(G, f[e]);
-                td = s2_fma(Gf[j][e], xe, td);
+                if (X) {
+                    const S2 xe = s2_bf16(x[j][e]);
+                    sum_c[j][e] = s2_fma(s2_mul(G, xe), c2, sum_c[j][e]);
+                    td = s2_fma(Gf[j][e], xe, td);
+                }
                 const S2 v = G;
                 out[e] = pack_bf16x2(v.lo, v.hi);
             }
@@ -333,7 +348,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
             uint32_t out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const S2 v = s2_fma(c2, Gf[j][e], s2_mul(kx2, s2_bf16(x[j][e])));
+                const S2 v = X ? s2_fma(c2, Gf[j][e], s2_mul(kx2, s2_bf16(x[j][e]))) : s2_mul(c2, Gf[j][e]);
                 out[e] = pack_bf16x2(v.lo, v.hi);
             }
             if (tid + width * j < nvec) reinterpret_cast<uint4*>(p.d_x)[out_at + width * j] = make_uint4(out[0], out[1], out[2], out[3]);
@@ -436,9 +451,12 @@ cudaError_t launch_block_norm(const BlockNormParams& p, cudaStream_t stream) {
     const int nv = (p.H / 8 + BN_THREADS - 1) / BN_THREADS;
     auto pick = [&](auto few) {
         constexpr bool FEW = decltype(few)::value;
-        return nv <= 1 ? block_norm_kernel<1, FEW> : nv <= 2 ? block_norm_kernel<2, FEW> : nv <= 4 ? block_norm_kernel<4, FEW> : block_norm_kernel<8, FEW>;
+        return p.H <= 256 ? block_norm_kernel<1, FEW, 4> : p.H <= 512 ? block_norm_kernel<1, FEW, 2> : nv <= 1 ? block_norm_kernel<1, FEW, 1>
+             : nv <= 2 ? block_norm_kernel<2, FEW, 1> : nv <= 4 ? block_norm_kernel<4, FEW, 1> : block_norm_kernel<8, FEW, 1>;
     };
-    return launch_pdl(p.T <= BN_FEW_ROWS ? pick(std::true_type()) : pick(std::false_type()), dim3(static_cast<unsigned>(p.T)), BN_THREADS, 0, stream, 1, p);
+    const long long rows = p.H <= 256 ? 4 : p.H <= 512 ? 2 : 1;
+    return launch_pdl(p.T <= BN_FEW_ROWS ? pick(std::true_type()) : pick(std::false_type()), dim3(static_cast<unsigned>((p.T + rows - 1) / rows)),
+                      BN_THREADS, 0, stream, 1, p);
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream) {
@@ -446,12 +464,21 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream)
     if (shape.ctas > 0) {
         static DeviceOnce configured;
         cudaError_t e = configured.run([&]() {
-            const cudaError_t r = cudaFuncSetAttribute(block_norm_bwd_kernel<2, BN_THREADS_MOST>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-            return r != cudaSuccess ? r : cudaFuncSetAttribute(block_norm_bwd_kernel<1, BN_THREADS_WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+            cudaError_t r = cudaSuccess;
+            auto allow = [&](auto kern) {
+                if (r == cudaSuccess) r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+            };
+            allow(block_norm_bwd_kernel<2, BN_THREADS_MOST, true>);
+            allow(block_norm_bwd_kernel<2, BN_THREADS_MOST, false>);
+            allow(block_norm_bwd_kernel<1, BN_THREADS_WIDE, true>);
+            allow(block_norm_bwd_kernel<1, BN_THREADS_WIDE, false>);
+            return r;
         });
         if (e != cudaSuccess) return e;
-        e = launch_pdl(shape.nv == 2 ? block_norm_bwd_kernel<2, BN_THREADS_MOST> : block_norm_bwd_kernel<1, BN_THREADS_WIDE>, dim3(shape.ctas),
-                       shape.group * shape.groups, shape.smem, stream, 1, p, shape);
+        const bool x = p.post_weight || p.gate;
+        auto kern = shape.nv == 2 ? (x ? block_norm_bwd_kernel<2, BN_THREADS_MOST, true> : block_norm_bwd_kernel<2, BN_THREADS_MOST, false>)
+                                  : (x ? block_norm_bwd_kernel<1, BN_THREADS_WIDE, true> : block_norm_bwd_kernel<1, BN_THREADS_WIDE, false>);
+        e = launch_pdl(kern, dim3(shape.ctas), shape.group * shape.groups, shape.smem, stream, 1, p, shape);
         if (e != cudaSuccess) return e;
     }
     if (!p.d_weight && !p.d_post_weight && p.gate_kind != GATE_CHANNEL) return cudaSuccess;

@@ -53,7 +53,7 @@ def _forward(tik, t, a, rows=slice(None), **out):
                               gate=gate, branch_scale=a, **out)
 
 
-@pytest.mark.parametrize("T,H", SIZES + [(512, 264), (513, 264), (2100, 72), (600, 1032), (530, 3584), (521, 5120)])
+@pytest.mark.parametrize("T,H", SIZES + [(512, 264), (513, 264), (2100, 72), (2, 256), (5, 512), (701, 256), (703, 512), (515, 520), (2051, 8), (600, 1032), (530, 3584), (521, 5120)])
 @pytest.mark.parametrize("form", FORMS)
 def test_forward(tik, T, H, form):
     a = form["a"]
