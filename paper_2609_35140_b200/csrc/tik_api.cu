@@ -258,7 +258,7 @@ size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d
         return static_cast<size_t>(rows_or_batch) * Hq * sizeof(float);
     }
     if (op == TIK_OP_EMBEDDING_BWD) return rows_or_batch > 0 && H > 0 && V > 0 ? embed_bwd_bytes(rows_or_batch, V, H) : 0;
-    if (op == TIK_OP_BLOCK_NORM_BWD) return rows_or_batch > 0 && H > 0 ? block_norm_bwd_bytes(rows_or_batch, H) : 0;
+    if (op == TIK_OP_BLOCK_NORM_BWD) return rows_or_batch > 0 && H > 0 && H <= 8192 ? block_norm_bwd_bytes(rows_or_batch, H) : 0;
     if (op == TIK_OP_GRAD_NORM) return rows_or_batch > 0 ? grad_norm_bytes(rows_or_batch) : 0;
     return 0;
 }

@@ -25,7 +25,7 @@ __device__ __forceinline__ float bn_row_total(const float* w4, int mine) {
 // and 2.4 with FEW; 1024 x 3584 5.4 and 5.8; 9001 x 5120 58 and 92: its registers halve the rows on an SM).
 // ROWS: rows of a CTA.  Of up to 256 (512) channels a row's data sit in one (two) of the four warps of that shape, whose totals are then
 // the whole sum, so four (two) rows take a CTA and a CTA per row does not wait for its turn to start (60 000 x 256: 50.4 us
-// with one row, ROWSUS with four).
+// with one row, 24.6 with four).
 constexpr long long BN_FEW_ROWS = 512;
 template <int NV, bool FEW, int ROWS>
 __global__ void __launch_bounds__(BN_THREADS) block_norm_kernel(const BlockNormParams p) {
@@ -185,7 +185,8 @@ __device__ __forceinline__ float bn_rsqrt(float x) {
     return r;
 }
 
-// X: something of x is needed -- it has a norm or a gate.  Without either d_x is G times a number, and x is not read.
+// X: something of x is needed -- it has a norm or a gate.  Without either d_x is G times a number, and x is not read (gradient of
+// the norm before a block alone, 16 001 x 3584: 99 us with x, 81 without; 40 000 x 1024 70 and 58).
 template <int NV, int THREADS, bool X>
 __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockNormParams p, const BlockNormBwdShape shape) {
     extern __shared__ __align__(128) unsigned char bn_smem[];
@@ -290,14 +291,18 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         turn ^= 1;
     };
     float sums[4];
-    if (row < T) {
-        first_sums(slot, parity);
-        total(0.0f, sums);
-    }
+    if (row < T) first_sums(slot, parity);
+    // A barrier's parity tells a phase from the next one only, so whoever waits for a slot's row has to know that the row before it
+    // in that slot has arrived.  Of later rows it does: a row is requested by a group that has seen the row that many groups
+    // behind the old one of that slot.  For the first rows that replace another, which are waited for beside rows of the first
+    // fill, it is the groups' first rows that have to be there.
+    __syncthreads();
+    if (row < T) total(0.0f, sums);
     for (; row < T; row += step) {
         const float gt = p.gate_kind == GATE_TOKEN ? __bfloat162float(p.gate[row]) : 1.0f;
         const float rs = norm ? bn_rsqrt(fmaf(sums[1], inv_h, p.eps)) : 0.0f, rx = post ? bn_rsqrt(fmaf(sums[0], inv_h, p.eps)) : 1.0f;
-        const S2 rs2 = s2(rs), ks2 = s2(-(rs * rs * rs * (sums[2] * inv_h))), c2 = s2(gt * rx);
+        // (products in this order stay in range where the sum is small because s is: r^3 alone would not)
+        const S2 rs2 = s2(rs), ks2 = s2(-(rs * (rs * (rs * (sums[2] * inv_h))))), c2 = s2(gt * rx);
         const size_t out_at = static_cast<size_t>(row) * nvec + tid;
         uint32_t x[NV][4];
         S2 Gf[NV][4], td = s2(0.0f);                      // G times its factor
@@ -342,7 +347,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         parity = next_parity;
         if (!branch) continue;
         if (p.gate_kind == GATE_TOKEN && tid == 0) p.d_gate[row] = rx * sums[3];
-        const S2 kx2 = s2(post ? -(gt * rx * rx * rx * (sums[3] * inv_h)) : 0.0f);
+        const S2 kx2 = s2(post ? -(gt * (rx * (rx * (rx * (sums[3] * inv_h))))) : 0.0f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             uint32_t out[4];
@@ -425,8 +430,8 @@ __global__ void __launch_bounds__(BN_FOLD_WARPS * 32) block_norm_fold_kernel(con
 }
 
 // Threads for NV vectors each: two, which halves what a row costs beside its columns (28 warps of one vector at 3584 channels 126 us,
-// 14 of two 121), but one where two would leave lanes idle or too few warps on an SM (9001 x 5120: 111 us with one, 130 with two).  As
-// many groups as the threads hold and as leave a row ahead in the ring, which fills shared memory.  (148 SMs: the number of CTAs
+// 14 of two 121), but one where two would leave lanes idle (up to 256 channels) or too few warps on an SM (above 4096 channels one
+// group is all that fits; 9001 x 5120: 107 us by 20 warps of one, 112 by 10 of two).  As many groups as the threads hold and as leave a row ahead in the ring, which fills shared memory.  (148 SMs: the number of CTAs
 // and groups decides the order of the sums over tokens, so it does not follow the device.)
 static BlockNormBwdShape bwd_shape(int64_t T, int H) {
     BlockNormBwdShape s;

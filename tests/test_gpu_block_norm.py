@@ -249,3 +249,24 @@ def test_refused_tensors(tik):
                 lambda: tik.tik_block_norm_bwd(x[:3], r, x, s, w, 1e-6)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("std_x,std_s,eps,zero_rows", [(1.0, 1e-14, 0.0, False), (1e-14, 1.0, 0.0, False), (1.0, 1.0, 1e-28, True), (1e-12, 1e-12, 1e-30, True)])
+def test_backward_of_tiny_rows(tik, std_x, std_s, eps, zero_rows):
+    """Rows so small that the cube of their norm's factor is beyond fp32, and rows of zeros beside them."""
+    T, H = 9, 264
+    t = _inputs(T, H, True, "channel", True, 1.0)
+    x, s, dy, ds = _randn((T, H), 21, std_x), _randn((T, H), 22, std_s), _randn((T, H), 23), _randn((T, H), 24)
+    if zero_rows:
+        for z in (x, s):
+            z[2] = 0
+            z[7] = 0
+    got = tik.tik_block_norm_bwd(dy, ds, x, s, t["weight"], eps, post_weight=t["post"], gate=t["gate"])
+    ref, mag = oracle.block_norm_bwd(_np(dy), _np(ds), _np(x), _np(s), _np(t["weight"]), float(np.float32(eps)), _np(t["post"]), _np(t["gate"]), 1.0)
+    for name, g in zip(NAMES, got):
+        # steps as in _check_backward
+        steps = 256 + (T + 300 if g.dtype == torch.float32 else 0)
+        e = steps * U32 * mag[name]
+        half = UBF if g.dtype == torch.bfloat16 else U32
+        assert np.all(np.isfinite(ref[name]) == np.isfinite(_np(g)))
+        assert np.all(np.abs(_np(g) - ref[name]) <= half * (np.abs(ref[name]) + e) + e), name

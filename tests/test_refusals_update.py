@@ -152,5 +152,7 @@ def test_scratch_sizes():
     assert tik.workspace_bytes(tik.OP_BLOCK_NORM_BWD, 5, H=64) == 5 * 2 * 64 * 4
     assert tik.workspace_bytes(tik.OP_EMBEDDING_BWD, 5, H=64, V=10) >= 40
     assert tik.workspace_bytes(tik.OP_GRAD_NORM, 1) > 8
+    for H in (8200, 1 << 20, 1 << 29, (1 << 31) - 8):        # (sizes that the gradient refuses)
+        assert tik.workspace_bytes(tik.OP_BLOCK_NORM_BWD, 5, H=H) == 0
     for op in (tik.OP_BLOCK_NORM_BWD, tik.OP_EMBEDDING_BWD, tik.OP_GRAD_NORM):
         assert tik.workspace_bytes(op, 0, H=64, V=10) == 0
