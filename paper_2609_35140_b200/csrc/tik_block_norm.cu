@@ -155,7 +155,7 @@ __device__ __forceinline__ float s2_sum(S2 a) { return __fadd_rn(a.lo, a.hi); }
 constexpr int BN_THREADS_MOST = 512, BN_THREADS_WIDE = 640;  // at 128 and at 96 registers
 
 struct BlockNormBwdShape {
-    int nv, group, groups, ctas, slots, slot_bytes, factor_bytes;        // 16-byte vectors per thread, threads of a group
+    int nv, most, group, groups, ctas, slots, slot_bytes, factor_bytes;  // 16-byte vectors per thread, threads at most, threads of a group
     size_t smem;
 };
 constexpr int BN_SLOTS = 64;
@@ -186,9 +186,10 @@ __device__ __forceinline__ float bn_rsqrt(float x) {
 }
 
 // X: something of x is needed -- it has a norm or a gate.  Without either d_x is G times a number, and x is not read (gradient of
-// the norm before a block alone, 16 001 x 3584: 99 us with x, 81 without; 40 000 x 1024 70 and 58).
+// the norm before a block alone, 16 001 x 3584: 99 us with x, 82 without).
 template <int NV, int THREADS, bool X>
 __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockNormParams p, const BlockNormBwdShape shape) {
+    constexpr int PLANES = X ? 4 : 3;                        // of a slot: d_s, x, s, d_y
     extern __shared__ __align__(128) unsigned char bn_smem[];
     BlockNormBwdSmem& sm = *reinterpret_cast<BlockNormBwdSmem*>(bn_smem);
     // branch_scale * post_weight * gate (per channel) of the columns in fp32; then the ring
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     const float inv_h = 1.0f / static_cast<float>(p.H);
     const bool norm = p.weight != nullptr, post = X && p.post_weight != nullptr, branch = p.d_x != nullptr;
     // What is absent reads as zeros: planes that are not there, vectors behind the row.
-    for (int i = threadIdx.x; i < shape.slots * 4 * row_vecs; i += blockDim.x) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < shape.slots * PLANES * row_vecs; i += blockDim.x) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
     if (threadIdx.x == 0) {
         for (int i = 0; i < shape.slots; ++i) mbar_init(smem_u32(&sm.full[i]), 1);
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     pdl_wait();
     pdl_launch_dependents();
     const int planes = (norm ? 2 : 0) + (X ? 1 : 0) + (p.d_s ? 1 : 0);
-    // The CTA's n-th row, which group n % groups takes, is row blockIdx.x + n * gridDim.x; planes of a slot: d_s, x, s, d_y.
+    // The CTA's n-th row, which group n % groups takes, is row blockIdx.x + n * gridDim.x.
     const unsigned T = static_cast<unsigned>(p.T);           // (below 2^31: a row behind the last one does not wrap)
     auto request = [&](unsigned row, int slot) {
         if (row >= T) return;
@@ -220,7 +221,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         const __nv_bfloat16* src[4] = {p.d_s, X ? p.x : nullptr, norm ? p.s : nullptr, norm ? p.d_y : nullptr};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (src[i]) bulk_load(to + i * 16 * row_vecs, src[i] + static_cast<size_t>(row) * p.H, p.H * 2, bar);
+            if (src[i]) bulk_load(to + (X || i == 0 ? i : i - 1) * 16 * row_vecs, src[i] + static_cast<size_t>(row) * p.H, p.H * 2, bar);
     };
     if (threadIdx.x == 0)
         for (int n = 0; n < shape.slots; ++n) request(blockIdx.x + n * gridDim.x, n);
@@ -263,8 +264,8 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         for (int j = 0; j < NV; ++j) {
             uint32_t x[4], s4[4], dy[4];
             if (X) take(at, 1, j, x);
-            take(at, 2, j, s4);
-            take(at, 3, j, dy);
+            take(at, PLANES - 2, j, s4);
+            take(at, PLANES - 1, j, dy);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const S2 se = s2_bf16(s4[e]);
@@ -314,8 +315,8 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
             uint32_t ds[4], s[4], dy[4], out[4];
             take(at, 0, j, ds);
             if (X) take(at, 1, j, x[j]);
-            take(at, 2, j, s);
-            take(at, 3, j, dy);
+            take(at, PLANES - 2, j, s);
+            take(at, PLANES - 1, j, dy);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const S2 se = s2_bf16(s[e]), rdy = s2_mul(rs2, s2_bf16(dy[e]));
@@ -430,27 +431,37 @@ __global__ void __launch_bounds__(BN_FOLD_WARPS * 32) block_norm_fold_kernel(con
 }
 
 // Threads for NV vectors each: two, which halves what a row costs beside its columns (28 warps of one vector at 3584 channels 126 us,
-// 14 of two 121), but one where two would leave lanes idle (up to 256 channels) or too few warps on an SM (above 4096 channels one
-// group is all that fits; 9001 x 5120: 107 us by 20 warps of one, 112 by 10 of two).  As many groups as the threads hold and as leave a row ahead in the ring, which fills shared memory.  (148 SMs: the number of CTAs
-// and groups decides the order of the sums over tokens, so it does not follow the device.)
-static BlockNormBwdShape bwd_shape(int64_t T, int H) {
+// 14 of two 121), but one where two would leave lanes idle (up to 256 channels) or, with x, too few warps on an SM (above 4096
+// channels one group is all that fits at 128 registers; 9001 x 5120: 107 us by 20 warps of one, 112 by 10 of two, 134 by two groups
+// of 10 at 96 registers, which spill).  Without x 96 registers are enough for the second group there (9001 x 5120 85 -> 66 us; at
+// 3584 and 6144 channels, where they would gain no group, 128 are faster, 88 -> 84 and 86 -> 81).  As many groups as the threads
+// hold.  The ring: for one group all of shared memory; for two an odd number of slots, which the groups then take in turns (14 000 x
+// 4096: six 119 us, five 113; 16 001 x 3584: seven 113, six 115, five 116); for more 164 KB, since rows that are asked for earlier
+// only get in the way of the writes (20 000 x 2048: 87 us with 227 KB, 83 with 164, 86 with 140; 32 000 x 1536 104, 98, 102).
+// (148 SMs: the number of CTAs and groups decides the order of the sums over tokens, so it does not follow the device.)
+constexpr int BN_RING_MANY = 164 * 1024;
+static BlockNormBwdShape bwd_shape(int64_t T, int H, bool x) {
     BlockNormBwdShape s;
-    s.nv = H <= 256 || (H > 4096 && H <= 8 * BN_THREADS_WIDE) ? 1 : 2;
+    s.nv = H <= 256 || (x && H > 4096 && H <= 8 * BN_THREADS_WIDE) ? 1 : 2;
     s.group = (H / 8 + 32 * s.nv - 1) / (32 * s.nv) * 32;
-    s.slot_bytes = 4 * 16 * s.nv * s.group;
+    const bool two = s.group > BN_THREADS_MOST / 2 && s.group <= BN_THREADS_WIDE / 2;
+    s.most = s.nv == 1 || (!x && two) ? BN_THREADS_WIDE : BN_THREADS_MOST;
+    s.slot_bytes = (x ? 4 : 3) * 16 * s.nv * s.group;
     s.factor_bytes = 32 * s.nv * s.group;
     s.slots = std::min(BN_SLOTS, (227 * 1024 - BN_RING - s.factor_bytes) / s.slot_bytes);
     s.ctas = static_cast<int>(std::min<int64_t>(T, 148));
     const int64_t rows = (T + 147) / 148;                    // of a CTA
-    s.groups = static_cast<int>(std::min<int64_t>(std::max(1, (s.nv == 1 ? BN_THREADS_WIDE : BN_THREADS_MOST) / s.group), rows));
+    s.groups = static_cast<int>(std::min<int64_t>(std::max(1, s.most / s.group), rows));
     while (s.groups > 1 && 2 * s.groups >= s.slots) --s.groups;
+    if (s.groups > 2) s.slots = std::min(s.slots, BN_RING_MANY / s.slot_bytes);
+    if (s.groups == 2) s.slots -= s.slots % 2 == 0;
     // (a short call's ring holds its rows; the groups' sums need 64 bytes a thread and vector of it at the end)
     const int sums = (64 * s.nv * s.groups * s.group + s.slot_bytes - 1) / s.slot_bytes;
     s.slots = static_cast<int>(std::min<int64_t>(s.slots, std::max<int64_t>({rows, sums, s.groups + 1})));
     s.smem = BN_RING + s.factor_bytes + static_cast<size_t>(s.slots) * s.slot_bytes;
     return s;
 }
-size_t block_norm_bwd_bytes(int64_t T, int H) { return static_cast<size_t>(bwd_shape(T, H).ctas) * 2 * H * sizeof(float); }
+size_t block_norm_bwd_bytes(int64_t T, int H) { return static_cast<size_t>(bwd_shape(T, H, true).ctas) * 2 * H * sizeof(float); }
 
 cudaError_t launch_block_norm(const BlockNormParams& p, cudaStream_t stream) {
     const int nv = (p.H / 8 + BN_THREADS - 1) / BN_THREADS;
@@ -465,7 +476,8 @@ cudaError_t launch_block_norm(const BlockNormParams& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream) {
-    const BlockNormBwdShape shape = bwd_shape(p.T, p.H);
+    const bool x = p.post_weight || p.gate;
+    const BlockNormBwdShape shape = bwd_shape(p.T, p.H, x);
     if (shape.ctas > 0) {
         static DeviceOnce configured;
         cudaError_t e = configured.run([&]() {
@@ -475,14 +487,17 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, cudaStream_t stream)
             };
             allow(block_norm_bwd_kernel<2, BN_THREADS_MOST, true>);
             allow(block_norm_bwd_kernel<2, BN_THREADS_MOST, false>);
+            allow(block_norm_bwd_kernel<2, BN_THREADS_WIDE, false>);
             allow(block_norm_bwd_kernel<1, BN_THREADS_WIDE, true>);
             allow(block_norm_bwd_kernel<1, BN_THREADS_WIDE, false>);
             return r;
         });
         if (e != cudaSuccess) return e;
-        const bool x = p.post_weight || p.gate;
-        auto kern = shape.nv == 2 ? (x ? block_norm_bwd_kernel<2, BN_THREADS_MOST, true> : block_norm_bwd_kernel<2, BN_THREADS_MOST, false>)
-                                  : (x ? block_norm_bwd_kernel<1, BN_THREADS_WIDE, true> : block_norm_bwd_kernel<1, BN_THREADS_WIDE, false>);
+        const bool wide = shape.most == BN_THREADS_WIDE;
+        auto kern = shape.nv == 1 ? (x ? block_norm_bwd_kernel<1, BN_THREADS_WIDE, true> : block_norm_bwd_kernel<1, BN_THREADS_WIDE, false>)
+                    : x           ? block_norm_bwd_kernel<2, BN_THREADS_MOST, true>
+                    : wide        ? block_norm_bwd_kernel<2, BN_THREADS_WIDE, false>
+                                  : block_norm_bwd_kernel<2, BN_THREADS_MOST, false>;
         e = launch_pdl(kern, dim3(shape.ctas), shape.group * shape.groups, shape.smem, stream, 1, p, shape);
         if (e != cudaSuccess) return e;
     }
