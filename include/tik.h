@@ -299,7 +299,7 @@ tik_status tik_embedding(tik_ctx* ctx, const int32_t* ids, const void* table, vo
  * equal ids by position, and a row's tokens are summed in fp32 in that order in a shape that depends on their
  * number only: no atomics on values, the same bits on every call, whatever other ids the batch holds.  One rounding of
  * g (accumulate: of d_table + g).  Ids outside [0, V) have no gradient and raise TIK_DEV_BAD_TOKEN.
- * T == 0 with accumulate == 0 writes zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes; concurrent
+ * H must be a multiple of 8 and <= 2^23.  T == 0 with accumulate == 0 writes zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes; concurrent
  * calls (and captured graphs that may run at the same time) need buffers of their own.  One to three kernels on `stream`, more
  * (seven for V < 2^18) above 65536 tokens. */
 tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, void* d_table, int table_dtype,

@@ -779,6 +779,7 @@ tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, 
     if (!std::isfinite(scale)) return fail(ctx, TIK_ERR_INVALID_ARG, "scale must be finite");
     if (table_dtype != TIK_DTYPE_BF16 && table_dtype != TIK_DTYPE_FP32) return fail(ctx, TIK_ERR_INVALID_ARG, "unknown element type");
     if (H % 8 != 0) return fail(ctx, TIK_ERR_UNSUPPORTED, "H must be a multiple of 8");
+    if (H > (1 << 23)) return fail(ctx, TIK_ERR_UNSUPPORTED, "H must be <= 2^23");
     if (T == 0 && accumulate) return TIK_OK;
     if (!d_table || (T > 0 && (!d_y || !ids))) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
     if (!aligned16(d_y) || !aligned16(d_table) || !aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");

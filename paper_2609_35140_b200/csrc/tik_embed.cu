@@ -928,8 +928,7 @@ cudaError_t launch_embed_bwd(EmbedParams& p, void* ws, cudaStream_t stream) {
     p.part = reinterpret_cast<float*>(at + align16(4 * p.T));
     cudaError_t e = cudaSuccess;
     const long long table_bytes = static_cast<long long>(p.V) * p.H * (p.fp32 ? 4 : 2);
-    if (p.T > 0 && p.T <= EMB_SMALL_TOKENS && (p.accumulate || (table_bytes <= EMB_SMALL_BYTES && p.V / p.sm_count < EMB_SMALL_ROWS)) &&
-        p.H < (1 << 24))
+    if (p.T > 0 && p.T <= EMB_SMALL_TOKENS && (p.accumulate || (table_bytes <= EMB_SMALL_BYTES && p.V / p.sm_count < EMB_SMALL_ROWS)))
         return p.fp32 ? (p.accumulate ? launch_embed_small<true, true>(p, stream) : launch_embed_small<true, false>(p, stream))
                       : (p.accumulate ? launch_embed_small<false, true>(p, stream) : launch_embed_small<false, false>(p, stream));
     if (p.T > EMB_RANK_TOKENS) {

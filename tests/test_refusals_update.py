@@ -47,7 +47,7 @@ EMBED_BWD = dict(d_y=A, ids=B, d_table=C, type=0, accumulate=0, scale=1.0, T=5, 
 
 @pytest.mark.parametrize("changed,code", [
     (dict(T=-1), INVALID), (dict(V=0), INVALID), (dict(H=-8), INVALID), (dict(scale=NAN), INVALID), (dict(type=2), INVALID),
-    (dict(H=4), UNSUPPORTED), (dict(d_y=None), INVALID), (dict(ids=None), INVALID), (dict(d_table=None), INVALID),
+    (dict(H=4), UNSUPPORTED), (dict(H=(1 << 23) + 8, ws_bytes=1 << 62), UNSUPPORTED), (dict(d_y=None), INVALID), (dict(ids=None), INVALID), (dict(d_table=None), INVALID),
     (dict(T=0, d_table=None), INVALID), (dict(d_y=A + 4), UNSUPPORTED), (dict(d_table=C + 8), UNSUPPORTED), (dict(ws=D + 4), UNSUPPORTED),
     (dict(T=1 << 30, ws_bytes=1 << 62), UNSUPPORTED), (dict(V=1 << 30), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(ws_bytes=39), WORKSPACE),
     (dict(T=0, accumulate=1, d_y=None, ids=None), OK)])
