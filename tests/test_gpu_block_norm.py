@@ -270,3 +270,29 @@ def test_backward_of_tiny_rows(tik, std_x, std_s, eps, zero_rows):
         half = UBF if g.dtype == torch.bfloat16 else U32
         assert np.all(np.isfinite(ref[name]) == np.isfinite(_np(g)))
         assert np.all(np.abs(_np(g) - ref[name]) <= half * (np.abs(ref[name]) + e) + e), name
+
+
+@pytest.mark.parametrize("T,H", [(3, 8), (64, 264), (300, 3584)])
+def test_results_have_memory_of_their_own(tik, T, H):
+    """Small calls make their results in one allocation: the parts are aligned, apart from each other, and usable one by one."""
+    t = _inputs(T, H, True, "channel", True, 1.0)
+    y, s = _forward(tik, t, 1.0)
+    got = tik.tik_block_norm_bwd(y, s, t["x"], s, t["weight"], 1e-6, post_weight=t["post"], gate=t["gate"])
+    for group in ((y, s), got):
+        spans = sorted((r.data_ptr(), r.data_ptr() + r.numel() * r.element_size()) for r in group)
+        assert all(a % 16 == 0 for a, _ in spans) and all(e <= b for (_, e), (b, _) in zip(spans, spans[1:]))
+        assert all(r.is_contiguous() for r in group)
+    keep = [r.clone() for r in got]
+    for i in range(5):
+        got[i].add_(1)
+        for j in range(i + 1, 5):
+            assert count_diff(got[j], keep[j]) == 0
+    d_w = got[2]
+    want = d_w.clone()
+    del got, y, s
+    torch.empty(1 << 20, dtype=torch.uint8, device="cuda").fill_(255)
+    assert count_diff(d_w, want) == 0
+    ds = tik.tik_block_norm_bwd(None, t["x"], None, t["residual"], None, 1e-6)[1]              # one result alone
+    assert count_diff(ds, t["x"]) == 0
+    empty = tik.tik_block_norm(t["x"][:0], t["residual"][:0], t["weight"], 1e-6)
+    assert [tuple(r.shape) for r in empty] == [(0, H), (0, H)]
