@@ -235,7 +235,7 @@ def tik_block_norm(x, residual, weight, eps: float, post_weight=None, gate=None,
                    s: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
     """The step between two blocks: s = residual + branch_scale * gate * norm(x; post_weight), y = norm(s; weight), all [T,H]
     bf16.  post_weight, gate ([H] per channel or [T,1] per token) and weight may be None (no norm of x, no gate, no y).
-    Returns (y, s); s may be residual itself (in place)."""
+    Returns (y, s); s may be residual itself (in place).  Results that are small (1 MiB together) share an allocation."""
     return (_native or _load_native()).block_norm(x, residual, weight, eps, post_weight, gate, branch_scale, s, y)
 
 

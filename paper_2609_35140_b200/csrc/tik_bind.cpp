@@ -374,7 +374,7 @@ struct Pool {
     int64_t used = 0;
     static int64_t room(int64_t bytes) { return (bytes + 127) / 128 * 128; }
     Pool(int64_t total, const at::Tensor& like) {
-        if (total <= MOST) whole = empty({total}, at::kByte, like);
+        if (total > 0 && total <= MOST) whole = empty({total}, at::kByte, like);
     }
     at::Tensor take(at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& like) {
         if (!whole.defined()) return empty(sizes, type, like);
