@@ -296,3 +296,12 @@ def test_results_have_memory_of_their_own(tik, T, H):
     assert count_diff(ds, t["x"]) == 0
     empty = tik.tik_block_norm(t["x"][:0], t["residual"][:0], t["weight"], 1e-6)
     assert [tuple(r.shape) for r in empty] == [(0, H), (0, H)]
+
+
+@pytest.mark.parametrize("T,H", [(9001, 264), (4500, 1032), (3001, 1536), (2401, 2560), (2100, 3584), (1700, 4096), (1501, 5120), (901, 6144), (701, 8192)])
+@pytest.mark.parametrize("form", [FORMS[0], FORMS[1], FORMS[6]])
+def test_backward_of_many_rows(tik, T, H, form):
+    """Rows enough for every slot of the ring to be used again, by other groups than before."""
+    t = _inputs(T, H, **form, seed=50)
+    s, dy, ds = _randn((T, H), 51, 4.0), _randn((T, H), 52), _randn((T, H), 53)
+    _check_backward(tik, t, s, dy, ds, form["a"], T, H)
