@@ -863,6 +863,8 @@ tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, co
         if (!x && (post_weight || gate)) return fail(ctx, TIK_ERR_INVALID_ARG, "post_weight and gate need x");
         if (!gate != !d_gate) return fail(ctx, TIK_ERR_INVALID_ARG, "gate and d_gate go together");
     }
+    // (without rows a token gate has no elements and need not have an address; a channel gate's gradient is written all the same)
+    if (gate_kind == TIK_GATE_CHANNEL && (!gate || !d_gate)) return fail(ctx, TIK_ERR_INVALID_ARG, "a channel gate and d_gate go together");
     if (!aligned16(d_y) || !aligned16(d_s) || !aligned16(x) || !aligned16(s) || !aligned16(d_x) || !aligned16(d_residual) || !aligned16(ws))
         return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
     const size_t need = tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, 0, 0, 0, 0, H, 0);

@@ -156,3 +156,16 @@ def test_scratch_sizes():
         assert tik.workspace_bytes(tik.OP_BLOCK_NORM_BWD, 5, H=H) == 0
     for op in (tik.OP_BLOCK_NORM_BWD, tik.OP_EMBEDDING_BWD, tik.OP_GRAD_NORM):
         assert tik.workspace_bytes(op, 0, H=64, V=10) == 0
+
+
+@pytest.mark.parametrize("changed", [dict(kind=1), dict(kind=1, d_gate=E), dict(kind=1, gate=E), dict(kind=1, gate=E, post=E, d_post=E)])
+@pytest.mark.parametrize("T", [0, 5])
+def test_block_norm_bwd_wants_a_channel_gate_and_its_gradient_for_any_number_of_rows(ctx, changed, T):
+    """d_gate [H] is written (zeros) where there are no rows, too."""
+    assert _call("tik_block_norm_bwd", ["ctx", *NORM_BWD], NORM_BWD, ctx=ctx, T=T, ws=None, **changed) == INVALID
+
+
+def test_block_norm_bwd_of_no_rows_needs_no_token_gate(ctx):
+    """Its [0] elements have no address.  (Without weights nothing is to be written: no launch.)"""
+    none = dict(d_y=None, d_s=None, x=None, s=None, weight=None, d_x=None, d_residual=None, d_weight=None)
+    assert _call("tik_block_norm_bwd", ["ctx", *NORM_BWD], NORM_BWD, ctx=ctx, T=0, ws=None, kind=2, **none) == OK
