@@ -188,8 +188,14 @@ __device__ __forceinline__ float bn_sums4(float a, float b, float c, float d, in
     for (int off = FIRST / 4; off >= 1; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
     return t;
 }
-// (approximate to two units in the last place, of arguments that are normal numbers where eps is)
+
+// Root of a mean square: it may be subnormal, when eps is 0 or smaller than that, and the forward's root takes it as it is.  rsqrtf's
+// scaling of such arguments costs the rows of one vector a thread more than of two (9001 x 5120 107 us, 60 000 x 256 51.6), so there the
+// instruction without it comes first and rsqrtf behind a branch that hardly any row takes (104 and 50.8; with two vectors
+// 16 001 x 3584 takes 111 us by rsqrtf and 115 so).
+template <int NV>
 __device__ __forceinline__ float bn_rsqrt(float x) {
+    if (NV > 1) return rsqrtf(x);
     float r;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
@@ -311,9 +317,15 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
     if (row < T) total(0.0f, sums);
     for (; row < T; row += step) {
         const float gt = p.gate_kind == GATE_TOKEN ? __bfloat162float(p.gate[row]) : 1.0f;
-        const float rs = norm ? bn_rsqrt(fmaf(sums[1], inv_h, p.eps)) : 0.0f, rx = post ? bn_rsqrt(fmaf(sums[0], inv_h, p.eps)) : 1.0f;
-        // (products in this order stay in range where the sum is small because s is: r^3 alone would not)
-        const S2 rs2 = s2(rs), ks2 = s2(-(rs * (rs * (rs * (sums[2] * inv_h))))), c2 = s2(gt * rx);
+        const float ms = fmaf(sums[1], inv_h, p.eps), mx = fmaf(sums[0], inv_h, p.eps);
+        float rs = norm ? bn_rsqrt<NV>(ms) : 0.0f, rx = post ? bn_rsqrt<NV>(mx) : 1.0f;
+        if (NV == 1 && (ms < 0x1p-126f || (X && mx < 0x1p-126f))) {
+            if (norm) rs = rsqrtf(ms);
+            if (post) rx = rsqrtf(mx);
+        }
+        // G = d_s + r (q - k s): k = r^2 mean(q s), by products in this order, is no larger than r times the rms of q, which is in
+        // range where G is.  r^3 is not for rows below 1e-13, nor r^3 mean(q s) below 1e-19.
+        const S2 rs2 = s2(rs), ks2 = s2(-(rs * (rs * (sums[2] * inv_h)))), c2 = s2(gt * rx);
         const size_t out_at = static_cast<size_t>(row) * nvec + tid;
         uint32_t x[NV][4];
         S2 Gf[NV][4], td = s2(0.0f);                      // G times its factor
@@ -330,7 +342,7 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const S2 q = s2_fma_bf16(dy[e], w[j][e], s2(0.0f));
-                const S2 G = s2_fma(ks2, s2_bf16(s[e]), s2_fma(rs2, q, s2_bf16(ds[e])));
+                const S2 G = s2_fma(rs2, s2_fma(ks2, s2_bf16(s[e]), q), s2_bf16(ds[e]));
                 sum_w[j][e] = s2_fma(rs2, s2_fma_bf16(dy[e], s[e], s2(0.0f)), sum_w[j][e]);
                 Gf[j][e] = s2_mul(G, f[e]);
                 if (X) {
@@ -358,13 +370,13 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         parity = next_parity;
         if (!branch) continue;
         if (p.gate_kind == GATE_TOKEN && tid == 0) p.d_gate[row] = rx * sums[3];
-        const S2 kx2 = s2(post ? -(gt * (rx * (rx * (rx * (sums[3] * inv_h))))) : 0.0f);
+        const S2 kx2 = s2(post ? -(rx * (rx * (sums[3] * inv_h))) : 0.0f);       // d_x likewise
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             uint32_t out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const S2 v = X ? s2_fma(c2, Gf[j][e], s2_mul(kx2, s2_bf16(x[j][e]))) : s2_mul(c2, Gf[j][e]);
+                const S2 v = s2_mul(c2, X ? s2_fma(kx2, s2_bf16(x[j][e]), Gf[j][e]) : Gf[j][e]);
                 out[e] = pack_bf16x2(v.lo, v.hi);
             }
             if (tid + width * j < nvec) reinterpret_cast<uint4*>(p.d_x)[out_at + width * j] = make_uint4(out[0], out[1], out[2], out[3]);

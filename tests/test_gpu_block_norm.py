@@ -305,3 +305,36 @@ def test_backward_of_many_rows(tik, T, H, form):
     t = _inputs(T, H, **form, seed=50)
     s, dy, ds = _randn((T, H), 51, 4.0), _randn((T, H), 52), _randn((T, H), 53)
     _check_backward(tik, t, s, dy, ds, form["a"], T, H)
+
+
+@pytest.mark.parametrize("H", [72, 264, 3584, 4104])
+@pytest.mark.parametrize("std_x,std_s,eps,zeros", [(1.0, 1e-20, 0.0, ""), (1e-20, 1.0, 0.0, ""), (1e-20, 1e-15, 0.0, ""), (1e-15, 1e-20, 0.0, ""),
+                                                   (1.0, 1e-21, 0.0, ""), (1e-21, 1.0, 0.0, ""), (1.0, 1e-20, 1e-40, "s"), (1e-20, 1.0, 1e-40, "x")])
+@pytest.mark.parametrize("plain", [False, True])
+def test_backward_of_rows_whose_mean_square_is_subnormal(tik, std_x, std_s, eps, zeros, H, plain):
+    """The forward's factor of such rows is finite, and so are the gradients.  What their mean squares lose: every addition is off by
+    2^-150 at most, half a step of fp32's subnormal numbers, so the mean (H additions of squares and under 40 of parts, over
+    H; one rounding more) by (2 + 40 / H) 2^-150.  The root halves that relative error, and a gradient's terms hold the root three
+    times at most: 1.8 times the mean's relative error of the sum of magnitudes, with a fifth to spare for second order."""
+    T = 9
+    t = _inputs(T, H, True, "channel", True, 1.0)
+    x, s, dy, ds = _randn((T, H), 21, std_x), _randn((T, H), 22, std_s), _randn((T, H), 23), _randn((T, H), 24)
+    for z in zeros:
+        {"x": x, "s": s}[z][2:5:2] = 0
+    eps32 = float(np.float32(eps))
+    lost = lambda v: (2 + 40 / H) * 2.0 ** -150 / ((_np(v) ** 2).mean(axis=1).min() + eps32)
+    post, gate = (None, None) if plain else (t["post"], t["gate"])
+    if plain:
+        x = None
+    got = tik.tik_block_norm_bwd(dy, ds, x, s, t["weight"], eps, post_weight=post, gate=gate)
+    ref, mag = oracle.block_norm_bwd(_np(dy), _np(ds), _np(x), _np(s), _np(t["weight"]), eps32, _np(post), _np(gate), 1.0)
+    for name, g in zip(NAMES, got):
+        if g is None:
+            continue
+        # steps as in _check_backward
+        steps = 256 + (T + 300 if g.dtype == torch.float32 else 0)
+        more = 1.8 * lost(s) + (1.8 * lost(x) if name not in ("d_residual", "d_weight") else 0.0)
+        e = (steps * U32 + more) * mag[name]
+        half = UBF if g.dtype == torch.bfloat16 else U32
+        assert np.all(np.isfinite(ref[name])) and bool(torch.isfinite(g).all()), name
+        assert np.all(np.abs(_np(g) - ref[name]) <= half * (np.abs(ref[name]) + e) + e), name
