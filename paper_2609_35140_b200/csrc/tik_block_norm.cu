@@ -370,17 +370,22 @@ __global__ void __launch_bounds__(THREADS, 1) block_norm_bwd_kernel(const BlockN
         parity = next_parity;
         if (!branch) continue;
         if (p.gate_kind == GATE_TOKEN && tid == 0) p.d_gate[row] = rx * sums[3];
-        const S2 kx2 = s2(post ? -(rx * (rx * (sums[3] * inv_h))) : 0.0f);       // d_x likewise
+        const S2 kx2 = s2(-(rx * (rx * (sums[3] * inv_h))));               // d_x likewise
+        auto write_dx = [&](auto norm_of_x) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            uint32_t out[4];
+            for (int j = 0; j < NV; ++j) {
+                uint32_t out[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const S2 v = s2_mul(c2, X ? s2_fma(kx2, s2_bf16(x[j][e]), Gf[j][e]) : Gf[j][e]);
-                out[e] = pack_bf16x2(v.lo, v.hi);
+                for (int e = 0; e < 4; ++e) {
+                    const S2 v = s2_mul(c2, decltype(norm_of_x)::value ? s2_fma(kx2, s2_bf16(x[j][e]), Gf[j][e]) : Gf[j][e]);
+                    out[e] = pack_bf16x2(v.lo, v.hi);
+                }
+                if (tid + width * j < nvec) reinterpret_cast<uint4*>(p.d_x)[out_at + width * j] = make_uint4(out[0], out[1], out[2], out[3]);
             }
-            if (tid + width * j < nvec) reinterpret_cast<uint4*>(p.d_x)[out_at + width * j] = make_uint4(out[0], out[1], out[2], out[3]);
-        }
+        };
+        // (without a norm of x its values are in no term of d_x: zero times an infinity would be one)
+        if (post) write_dx(std::bool_constant<X>());
+        else write_dx(std::false_type());
     }
     // The groups' sums, in their order, through the ring (nothing is on its way there any more).
     const bool column = post || p.gate_kind == GATE_CHANNEL;

@@ -338,3 +338,22 @@ def test_backward_of_rows_whose_mean_square_is_subnormal(tik, std_x, std_s, eps,
         half = UBF if g.dtype == torch.bfloat16 else U32
         assert np.all(np.isfinite(ref[name])) and bool(torch.isfinite(g).all()), name
         assert np.all(np.abs(_np(g) - ref[name]) <= half * (np.abs(ref[name]) + e) + e), name
+
+
+@pytest.mark.parametrize("T,H", [(40, 256), (40, 3584), (3, 5120)])
+@pytest.mark.parametrize("gate", ["channel", "token"])
+def test_without_a_post_norm_d_x_does_not_depend_on_x(tik, T, H, gate):
+    """d_x = branch_scale * gate * G then: infinities and NaN in x reach the gate's gradient alone."""
+    t = _inputs(T, H, False, gate, True, 1.0)
+    s, dy, ds = _randn((T, H), 2, 4.0), _randn((T, H), 3), _randn((T, H), 4)
+    bad = t["x"].clone()
+    bad[0, 5], bad[T - 1, H - 1], bad[T // 2] = float("inf"), float("nan"), -float("inf")
+    want, got = (tik.tik_block_norm_bwd(dy, ds, x, s, t["weight"], 1e-6, gate=t["gate"], branch_scale=0.5) for x in (t["x"], bad))
+    for i in range(3):
+        assert count_diff(got[i], want[i]) == 0, NAMES[i]
+    clean = torch.ones(got[4].numel(), dtype=torch.bool, device="cuda")
+    if gate == "token":
+        clean[[0, T - 1, T // 2]] = False
+    else:
+        clean[:] = False
+    assert count_diff(got[4].flatten()[clean], want[4].flatten()[clean]) == 0 and not bool(torch.isfinite(got[4].flatten()[~clean]).any())
