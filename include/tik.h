@@ -355,8 +355,9 @@ tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* 
  * caller to see.  out NULL: in place; else a HOST array of device pointers of the same types and sizes (out[i] may be
  * grads[i]).  The factor is the fp32 quotient; products in fp32, one rounding.
  * norm: device fp32 [1].  norm_given == 0: computed first, as by tik_grad_norm, and stored there; else read, e.g. after a
- * sharded trainer has combined its ranks' norms.  max_norm must be finite and > 0.  Tensors that are written may not overlap
- * each other or another input (TIK_ERR_INVALID_ARG).  ws as for tik_grad_norm (norm_given: may be NULL).  A kernel per
+ * sharded trainer has combined its ranks' norms.  max_norm must be finite and > 0.  Tensors that are written, the norm
+ * among them where it is computed, may not overlap each other or another input, the norm among those where it is given
+ * (TIK_ERR_INVALID_ARG).  ws as for tik_grad_norm (norm_given: may be NULL).  A kernel per
  * thousand tensors, as many again where the norm is computed. */
 tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* out, const int64_t* numel,
                          const int* dtypes, int n, float max_norm, float* norm, int norm_given, void* ws,

@@ -935,7 +935,7 @@ tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* ou
             return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
     }
     bool no_memory = false;
-    if (grad_ranges_overlap(grads, out, numel, dtypes, n, &no_memory))
+    if (grad_ranges_overlap(grads, out, numel, dtypes, n, norm, norm_given != 0, &no_memory))
         return fail(ctx, TIK_ERR_INVALID_ARG, no_memory ? "out of host memory" : "tensors to be written overlap");
     if (!aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
     const size_t need = norm_given ? 0 : tik_workspace_bytes(TIK_OP_GRAD_NORM, n, 0, 0, 0, 0, 0, 0);

@@ -292,15 +292,16 @@ cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const i
     });
 }
 
-bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, bool* no_memory) {
+bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, const float* norm,
+                         bool norm_known, bool* no_memory) {
     struct Range {
         uintptr_t from, to;
     };
     *no_memory = false;
     if (n <= 0) return false;
-    Range* const written = static_cast<Range*>(malloc(2ull * n * sizeof(Range)));
+    Range* const written = static_cast<Range*>(malloc(2ull * (n + 1ull) * sizeof(Range)));
     if (!written) return *no_memory = true;
-    Range* const read = written + n;                         // inputs that are not written in place
+    Range* const read = written + n + 1;                     // inputs that are not written in place
     int nw = 0, nr = 0;
     for (int i = 0; i < n; ++i) {
         if (numel[i] == 0) continue;
@@ -309,6 +310,9 @@ bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64
         written[nw++] = {to, to + bytes};
         if (to != in) read[nr++] = {in, in + bytes};
     }
+    const Range of_norm = {reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm + 1)};
+    if (norm_known) read[nr++] = of_norm;
+    else written[nw++] = of_norm;
     auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
     auto ascending = [&](Range* r, int count) {              // (lists of a flat buffer's views are already)
         if (!std::is_sorted(r, r + count, before)) std::sort(r, r + count, before);

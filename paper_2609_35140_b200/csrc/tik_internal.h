@@ -260,8 +260,10 @@ cudaError_t launch_grad_norm(const void* const* grads, const int64_t* numel, con
                              cudaStream_t stream);
 cudaError_t launch_grad_clip(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, float max_norm,
                              float* norm, bool norm_known, double* part, cudaStream_t stream);
-// whether two of the ranges that a clip writes, or one of them and another range that it reads, share a byte (or no memory)
-bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, bool* no_memory);
+// whether two of the ranges that a clip writes, or one of them and another range that it reads, share a byte (or no memory); the norm
+// is one or the other
+bool grad_ranges_overlap(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int n, const float* norm,
+                         bool norm_known, bool* no_memory);
 
 struct LinearParams {
     __nv_bfloat16* y;            // [T][N]

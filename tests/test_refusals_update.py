@@ -169,3 +169,20 @@ def test_block_norm_bwd_of_no_rows_needs_no_token_gate(ctx):
     """Its [0] elements have no address.  (Without weights nothing is to be written: no launch.)"""
     none = dict(d_y=None, d_s=None, x=None, s=None, weight=None, d_x=None, d_residual=None, d_weight=None)
     assert _call("tik_block_norm_bwd", ["ctx", *NORM_BWD], NORM_BWD, ctx=ctx, T=0, ws=None, kind=2, **none) == OK
+
+
+def test_the_norm_of_a_clip_is_no_gradient(ctx):
+    """The norm is written beside the gradients' reads where it is computed, and read beside their writes where it is given."""
+    def refused(*a, **k):
+        # (without scratch a list that passes is refused for that, or goes on to a launch where the norm is given)
+        return _clip(ctx, *a, **k) == INVALID and b"overlap" in tik.load().tik_last_error(ctx)
+    none = dict(ws=None, ws_bytes=0)
+    for given in (0, 1):
+        assert refused([C, D], [4, 4], [1, 1], norm=C + 12, given=given, **none)                  # an element of a tensor clipped in place
+        assert refused([C], [4], [0], norm=C + 4, given=given, **none)                            # bf16: two of them
+        assert refused([C, D], [4, 4], [1, 1], out=[C, E], norm=E, given=given, **none)           # an element of a result
+    assert refused([C], [4], [1], out=[D], norm=C, **none)                                        # computed, over an input
+    assert _clip(ctx, [C], [4], [1], norm=C + 16, **none) == WORKSPACE                            # next to it
+    assert _clip(ctx, [C], [4], [0], norm=C - 4, **none) == WORKSPACE
+    assert _clip(ctx, [C, D], [0, 4], [1, 1], norm=C, **none) == WORKSPACE                        # a tensor of no elements
+    assert _clip(ctx, [], [], [], given=1, **none) == OK
