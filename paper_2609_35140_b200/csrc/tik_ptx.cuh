@@ -104,12 +104,15 @@ __device__ __forceinline__ int warp_find_sequence(const int32_t* cu, int S, long
 // call run under the tail of the call before it.  The rules that keep a chain of such kernels
 // ordered like a plain stream:
 //   * before pdl_wait() a CTA touches no global memory except kernel parameters and L2 prefetches
-//     (writes land in L2, so a prefetched line cannot go stale);
+//     (writes land in L2, so a prefetched line cannot go stale), but for the three grids of the next point;
 //   * every CTA executes pdl_wait() on every path, early exits included, so a grid completes after
-//     its predecessor.  Two grids overlap their predecessor on purpose, which writes nothing that they read: the dQ
-//     grid of the backward and the persistent grid behind the single-tile grid.  They wait at their end (one
-//     block of dQ, every CTA of the other), never release dependents early, and read what earlier calls may have
-//     left in L1 around it (__ldcg);
+//     its predecessor.  Three grids overlap their predecessor on purpose, which writes nothing that they read and touches nothing
+//     that they write meanwhile: the dQ grid of the backward and the persistent grid behind the single-tile grid, which wait at
+//     their end (one block of dQ, every CTA of the other), and the sums of a table gradient, embed_sum_kernel, which reads the ids
+//     and writes zeros into the table beside the sort and waits before it reads what the sort wrote.  They never release
+//     dependents before that wait, and read what earlier calls may have left in L1 around it (__ldcg).  What such a grid
+//     shares with calls before its predecessor is in order by the next point, which its predecessor therefore has to keep
+//     (of a table gradient embed_rank_kernel, embed_sort_kernel or embed_wide_record_kernel): everything older has completed;
 //   * pdl_launch_dependents() comes after pdl_wait(): when a kernel starts, everything before its
 //     immediate predecessor has completed;
 //   * ... and after the CTA's tensor memory is allocated (behind the barrier that publishes its address): a dependent
