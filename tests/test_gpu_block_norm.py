@@ -357,3 +357,17 @@ def test_without_a_post_norm_d_x_does_not_depend_on_x(tik, T, H, gate):
     else:
         clean[:] = False
     assert count_diff(got[4].flatten()[clean], want[4].flatten()[clean]) == 0 and not bool(torch.isfinite(got[4].flatten()[~clean]).any())
+
+
+@pytest.mark.parametrize("T,H", [(20011, 256), (30000, 72), (9473, 8)])
+@pytest.mark.parametrize("form", [FORMS[0], FORMS[1], FORMS[6], None])
+def test_backward_of_many_narrow_rows(tik, T, H, form):
+    """Groups of one warp: 20 groups share a ring of 64 slots per CTA, which 9472 rows fill for the first time.  (None: the plain norm.)"""
+    t = _inputs(T, H, **(form or FORMS[6]), seed=50)
+    if form is None:
+        t["x"] = None
+    s, dy, ds = _randn((T, H), 51, 4.0), _randn((T, H), 52), _randn((T, H), 53)
+    got = _check_backward(tik, t, s, dy, ds, form["a"] if form else 1.0, T, H)
+    again = tik.tik_block_norm_bwd(dy, ds, t["x"], s, t["weight"], 1e-6, post_weight=t["post"], gate=t["gate"], branch_scale=form["a"] if form else 1.0)
+    for g, h in zip(got, again):
+        assert g is None or count_diff(g, h) == 0

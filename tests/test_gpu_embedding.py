@@ -200,3 +200,34 @@ def test_refused_tensors(tik):
                 lambda: tik.tik_embedding_bwd(d_y, ids, 0), lambda: tik.tik_embedding_bwd(d_y, ids, 4, accumulate=True)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("n", [1, 33, 200, 5000, 66000])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_a_rows_bits_among_more_tokens_than_one_cluster_sorts(tik, n, accumulate):
+    """As above, for lists that many CTAs sort, against the call on the row's own gradients by whichever path takes those."""
+    H, V, T = 72, 3000, 70_001
+    rng = np.random.default_rng(n)
+    d_y, old = _randn((T, H), 12), _randn((V, H), 13, 2.0, torch.float32)
+    at = np.sort(rng.permutation(T)[:n])
+    ids = rng.integers(0, V - 1, T)
+    ids[ids >= 1234] += 1
+    ids[at] = 1234
+    alone, among = old.clone(), old.clone()
+    tik.tik_embedding_bwd(d_y[torch.from_numpy(at).cuda()].contiguous(), _i32(np.full(n, 1234)), V, 0.9, d_table=alone, accumulate=accumulate)
+    tik.tik_embedding_bwd(d_y, _i32(ids), V, 0.9, d_table=among, accumulate=accumulate)
+    assert count_diff(alone[1234], among[1234]) == 0 and count_diff(alone[1234], old[1234]) > 0
+
+
+@pytest.mark.parametrize("dtype,accumulate", [(torch.bfloat16, False), (torch.float32, True)])
+def test_more_long_runs_than_a_cta_sets_aside(tik, dtype, accumulate):
+    """Seven runs of 36 tokens in 782 slices of columns: about 37 items of several pieces for each of 148 CTAs, which set 32 aside for all
+    of their warps and add up the others warp by warp.  The same bits as by columns in parts, where none is left over."""
+    V, H, step = 8, 200_000, 8000
+    ids = _i32(np.random.default_rng(6).permutation(np.concatenate([np.repeat(np.arange(7), 36), np.full(4, 7)])))
+    d_y, old = _randn((256, H), 1), _randn((V, H), 2, 2.0, dtype)
+    got = tik.tik_embedding_bwd(d_y, ids, V, -1.7, d_table=old.clone(), accumulate=accumulate)
+    for c in range(0, H, step):
+        part = tik.tik_embedding_bwd(d_y[:, c:c + step].contiguous(), ids, V, -1.7, d_table=old[:, c:c + step].contiguous(), accumulate=accumulate)
+        assert count_diff(got[:, c:c + step].contiguous(), part) == 0, c
+    _check_bwd(tik, d_y[:, :step].contiguous(), ids, V, -1.7, dtype, accumulate, 5)
