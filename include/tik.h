@@ -286,7 +286,7 @@ tik_status tik_linear(tik_ctx* ctx, const void* x, const void* weight, void* y, 
  * forward and every rollout step): y[t] = scale * table[ids[t]].
  *   ids int32 [T], table bf16 [V][H] -> y bf16 [T][H]; the product in fp32, one rounding (scale 1: an
  *   exact copy).  An id outside [0, V) gives a row of zeros and raises TIK_DEV_BAD_TOKEN.
- * H must be a multiple of 8.  Needs no workspace. */
+ * y does not overlap the table.  H must be a multiple of 8, T < 2^31.  Needs no workspace. */
 tik_status tik_embedding(tik_ctx* ctx, const int32_t* ids, const void* table, void* y, float scale, int64_t T,
                          int V, int H, void* stream);
 
@@ -299,9 +299,10 @@ tik_status tik_embedding(tik_ctx* ctx, const int32_t* ids, const void* table, vo
  * equal ids by position, and a row's tokens are summed in fp32 in that order in a shape that depends on their
  * number only: no atomics on values, the same bits on every call, whatever other ids the batch holds.  One rounding of
  * g (accumulate: of d_table + g).  Ids outside [0, V) have no gradient and raise TIK_DEV_BAD_TOKEN.
- * H must be a multiple of 8 and <= 2^23.  T == 0 with accumulate == 0 writes zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes; concurrent
- * calls (and captured graphs that may run at the same time) need buffers of their own.  One to three kernels on `stream`, more
- * (seven for V < 2^18) above 65536 tokens. */
+ * H must be a multiple of 8 and <= 2^23, T and V below 2^30; d_table overlaps no input.  T == 0 with accumulate == 0 writes
+ * zeros.  ws: tik_workspace_bytes(TIK_OP_EMBEDDING_BWD, T, ..., H, V) bytes; concurrent calls (and captured graphs that may run
+ * at the same time) need buffers of their own.  One to three kernels on `stream`; above 65536 tokens three and two for
+ * every nine bits of V, or part of nine: five for V < 2^9, seven for V < 2^18. */
 tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, void* d_table, int table_dtype,
                              int accumulate, float scale, int64_t T, int V, int H, void* ws, size_t ws_bytes,
                              void* stream);
@@ -317,21 +318,23 @@ tik_status tik_embedding_bwd(tik_ctx* ctx, const void* d_y, const int32_t* ids, 
  * from the rounded s, which the next layer reads).  A row's result depends on that row only, not on T.
  * Means of squares are fp32 numbers, here and in the gradient: with an eps of 0 they are accurate for rows of root mean
  * square from 2^-63 (1.1e-19) to 2^57, lose bits below that and are zero, as of a row of zeros, below 2^-75.
- * H must be a multiple of 8 and <= 8192. */
+ * H must be a multiple of 8 and <= 8192, T < 2^31. */
 tik_status tik_block_norm(tik_ctx* ctx, const void* x, const void* residual, const void* post_weight,
                           const void* gate, int gate_kind, float branch_scale, const void* weight, void* s, void* y,
                           float eps, int64_t T, int H, void* stream);
 
 /* Backward of tik_block_norm; with x NULL of the plain norm y = tik_rmsnorm(s, weight).  Given d_y = dL/dy and d_s =
- * dL/ds (what reaches the residual stream from further on; either may be NULL for zeros, d_y exactly when weight is):
+ * dL/ds (what reaches the residual stream from further on; either may be NULL for zeros, d_y exactly when weight is), for the
+ * same H and T:
  *   r = rsqrt(mean s^2 + eps), q = d_y * weight:  G = d_s + r * (q - s r^2 mean(q s)),  d_weight = sum_t d_y s r
  *   d_residual = G;  d_n = branch_scale * gate * G;  d_gate = branch_scale * sum G n  (over t, or per token over the channels)
  *   rx = rsqrt(mean x^2 + eps), p = d_n * post_weight:  d_x = rx * (p - x rx^2 mean(p x)),  d_post_weight = sum_t d_n x rx
  *   (post_weight NULL: d_x = d_n)
  * x and s are the forward's input and output (the rounding of s counts as the identity).  d_residual, d_x bf16 [T][H]
- * (d_x NULL exactly when x is), each may be one of d_y, d_s, x, s; d_weight, d_post_weight fp32 [H], d_gate fp32 [H] or
- * [T]: each exactly when its factor is given, overwritten (zeros for T == 0).  fp32 arithmetic; sums over tokens in one fixed
- * order without atomics: the same inputs give the same bits on every call.
+ * (d_x NULL exactly when x is), each may be one of d_y, d_s, x, s, but both not the same; d_weight, d_post_weight fp32 [H],
+ * d_gate fp32 [H] or [T]: each exactly when its factor is given (a channel gate and its gradient for T == 0, too), overwritten
+ * (zeros for T == 0).  fp32 arithmetic; sums over tokens in one fixed order without atomics: the same inputs give the same
+ * bits on every call.
  * ws: tik_workspace_bytes(TIK_OP_BLOCK_NORM_BWD, T, ..., H, 0) bytes, as above.  Two kernels on `stream`, one where no
  * sum over tokens is asked for. */
 tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, const void* x, const void* s,
@@ -345,7 +348,8 @@ tik_status tik_block_norm_bwd(tik_ctx* ctx, const void* d_y, const void* d_s, co
  *   tensor's elements are contiguous, its base aligned to its element; no further alignment is asked for, and numel[i] may
  *   be 0 (then grads[i] may be NULL).  norm: device fp32 [1].
  * Squares of 64 elements or fewer are summed in fp32 (in fp64 where they leave its range), everything above in fp64 in one fixed
- * order: the same list gives the same bits on every call and every device.  Infinities and NaN pass into the norm.
+ * order: the same list (values, sizes, bases as far from a 16-byte boundary) gives the same bits on every call and every
+ * device.  Infinities and NaN pass into the norm.
  * ws: tik_workspace_bytes(TIK_OP_GRAD_NORM, n, ...) bytes, as above.  A kernel per thousand tensors and one more. */
 tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* numel, const int* dtypes, int n,
                          float* norm, void* ws, size_t ws_bytes, void* stream);

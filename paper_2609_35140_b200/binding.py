@@ -235,7 +235,8 @@ def tik_block_norm(x, residual, weight, eps: float, post_weight=None, gate=None,
                    s: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
     """The step between two blocks: s = residual + branch_scale * gate * norm(x; post_weight), y = norm(s; weight), all [T,H]
     bf16.  post_weight, gate ([H] per channel or [T,1] per token) and weight may be None (no norm of x, no gate, no y).
-    Returns (y, s); s may be residual itself (in place).  Results that are small (1 MiB together) share an allocation."""
+    Returns (y, s); s may be residual itself (in place).  Results that are small (1 MiB together) are parts of one storage:
+    saving one or resizing its storage to free it takes the other along; pass s and y to have them apart."""
     return (_native or _load_native()).block_norm(x, residual, weight, eps, post_weight, gate, branch_scale, s, y)
 
 
@@ -243,19 +244,21 @@ def tik_block_norm_bwd(d_y, d_s, x, s, weight, eps: float, post_weight=None, gat
                        ws: Optional[torch.Tensor] = None):
     """Backward of tik_block_norm (x, s: its input and output; x None: of tik_rmsnorm(s, weight)).  d_s None: zeros; d_y None
     where weight is.  Returns (d_x, d_residual, d_weight, d_post_weight, d_gate), fp32 for the last three, None for
-    what is absent.  Deterministic."""
+    what is absent.  Deterministic.  The last three always are parts of one storage, all results where they and the
+    scratch are small (1 MiB together): saving one or resizing its storage to free it takes the others along; clone it for that."""
     return (_native or _load_native()).block_norm_bwd(d_y, d_s, x, s, weight, eps, post_weight, gate, branch_scale, ws)
 
 
 def tik_grad_norm(grads, norm: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
-    """sqrt of the sum of squares over a list of contiguous bf16 / fp32 tensors -> norm fp32 [1] (device)."""
+    """sqrt of the sum of squares over a list of contiguous bf16 / fp32 tensors -> norm fp32 [1] (device; one that is made here
+    shares its storage with the call's scratch, 5 KB per thousand tensors, unless ws is passed)."""
     return (_native or _load_native()).grad_norm(grads, norm, ws)
 
 
 def tik_grad_clip(grads, max_norm: float, norm: Optional[torch.Tensor] = None, out=None,
                   ws: Optional[torch.Tensor] = None):
     """grads *= max_norm / norm where max_norm < norm < inf, in place or into the tensors of `out`; returns norm.  norm: None =
-    computed here; a tensor fp32 [1] = taken from there (a sharded trainer's combined norm)."""
+    computed here, in a storage as tik_grad_norm's; a tensor fp32 [1] = taken from there (a sharded trainer's combined norm)."""
     return (_native or _load_native()).grad_clip(grads, max_norm, norm, out, ws)
 
 
