@@ -59,10 +59,18 @@ typedef int tik_status;
 #define TIK_OP_EMBEDDING_BWD 5
 #define TIK_OP_BLOCK_NORM_BWD 6
 #define TIK_OP_GRAD_NORM 7
+#define TIK_OP_TOKEN_LOGPROB_BWD 8
+#define TIK_OP_POLICY_LOSS 9
 
 /* element types of tensors that may have either */
 #define TIK_DTYPE_BF16 0
 #define TIK_DTYPE_FP32 1
+#define TIK_DTYPE_E4M3 2           /* 8-bit moments of tik_adamw */
+
+/* how tik_policy_loss reduces over tokens */
+#define TIK_LOSS_SUM 0
+#define TIK_LOSS_TOKEN_MEAN 1
+#define TIK_LOSS_SEQUENCE_MEAN 2
 
 /* the gate of tik_block_norm */
 #define TIK_GATE_NONE 0
@@ -109,10 +117,10 @@ int tik_selftest_bwd_dq(int64_t S, int64_t total_tokens, int max_seqlen, int Hq,
 unsigned long long tik_kernel_launches(void);
 
 /* Scratch bytes an operator needs.  rows_or_batch: decode batch B, log-prob rows T, or the number
- * of sequences S for train forward / prefill, tokens T for the embedding and block-norm gradients, the
- * number of tensors for the gradient norm.  max_ctx: the host's bound on a context length
- * (decode, prefill) or sequence length (train forward).  H for the log-prob op and the embedding and
- * block-norm gradients, V for the log-prob op and the embedding gradient.  Returns 0
+ * of sequences S for train forward / prefill, tokens T for the embedding, block-norm and log-prob gradients and the policy
+ * loss, the number of tensors for the gradient norm.  max_ctx: the host's bound on a context length
+ * (decode, prefill) or sequence length (train forward), the number of sequences S for the policy loss.  H for the log-prob op,
+ * its gradient and the embedding and block-norm gradients, V for the log-prob op, its gradient and the embedding gradient.  Returns 0
  * when no scratch is needed or usable (train forward / prefill outside the range that the
  * persistent schedule handles: they then run without scratch). */
 size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d,
@@ -257,6 +265,50 @@ tik_status tik_token_logprob(tik_ctx* ctx, const void* hidden, const void* lm_he
                              int H, int V, float inv_temperature, void* ws, size_t ws_bytes,
                              void* stream);
 
+/* Gradient of tik_token_logprob (no paper counterpart: the policy update's way back into the model).  With f = inv_temperature,
+ * z[t][v] = f hidden[t] . lm_head[v] and p[t][v] = exp(z[t][v] - lse[t]):
+ *   d_z[t][v] = f d_logprob[t] ([v == target_ids[t]] - p[t][v])
+ *   d_hidden[t] = sum_v d_z[t][v] lm_head[v],     d_lm_head[v] = sum_t d_z[t][v] hidden[t]
+ * hidden, lm_head, target_ids, inv_temperature as in the forward, lse fp32 [T] its output; d_logprob fp32 [T].
+ * d_hidden bf16 [T][H], d_lm_head bf16 or fp32 [V][H] by lm_head_dtype (TIK_DTYPE_*): either may be NULL (not both).
+ * accumulate != 0 (fp32 only): d_lm_head is added to, as by the later micro-batches of a step; else every row is written,
+ * with zeros for T == 0.  Logits are computed again, d_z is rounded to bf16 and is the operand of both products, sums are fp32:
+ * each term of a sum is off by 2^-8 of itself at most.  A token with d_logprob 0 (masked) gives no gradient whatever its lse, and
+ * one whose target is outside [0, V) gives none and raises TIK_DEV_BAD_TARGET; hidden rows must be finite all the same.
+ * Deterministic: fixed orders, no atomics on values.  Outputs overlap neither inputs nor each other.
+ * H must be a multiple of 64, V <= 2^30, T < 2^31 - 256.  ws: tik_workspace_bytes(TIK_OP_TOKEN_LOGPROB_BWD, T, ..., H, V) bytes (d_z
+ * of a vocabulary chunk, 2 GiB at most up to T = 2^22, and fp32 sums); concurrent calls (and captured graphs that may run at the same time) need
+ * buffers of their own.  Per vocabulary chunk one kernel and one more for each gradient, and one at the end for d_hidden. */
+tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const void* hidden, const void* lm_head,
+                                 const int32_t* target_ids, const float* lse, void* d_hidden, void* d_lm_head, int lm_head_dtype,
+                                 int accumulate, int64_t T, int H, int V, float inv_temperature, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* Clipped policy loss with a KL term, and its gradient with respect to the log-probabilities (the policy update's objective; the
+ * paper takes it from its trainer and gives no formula).  Per token, with x = logprob - old_logprob, r = exp(x), advantage A, y = ref_logprob - logprob:
+ *   policy = max(-A r, -A clamp(r, 1 - clip_low, 1 + clip_high));  clip_dual != 0 and A < 0: at most -A clip_dual
+ *   l = policy + kl_coef (exp(y) - y - 1),        g = dl/dlogprob = (cut ? 0 : -A r) - kl_coef (exp(y) - 1)
+ * where a token is cut when r is beyond the threshold that its advantage's sign asks for, strictly, decided on x in 64 bits.  Over
+ * the tokens that count, those whose weight w is not 0 (weight NULL: all, with w = 1):
+ *   loss = sum_t f_t l_t,  d_logprob[t] = f_t g_t (0 for the others),  f_t = scale w_t / n, n by reduction (TIK_LOSS_*):
+ *   SUM 1;  TOKEN_MEAN the number of tokens that count;  SEQUENCE_MEAN the number of those in t's sequence (scale 1 / S: the
+ *   mean over sequences of their means)
+ * What a token that does not count holds (infinities, NaN) goes nowhere; others pass theirs on.
+ *   logprob, old_logprob, weight (or NULL), ref_logprob (or NULL: no KL term, kl_coef 0): fp32 [T]
+ *   advantage: fp32 [T], or [S] with advantage_per_sequence
+ *   cu_seqlens: int32 [S+1] or NULL; needed per sequence.  Where given, tokens before cu_seqlens[0] or from cu_seqlens[S] on
+ *   (a padded batch) do not count.
+ *   loss: fp32 [1];  d_logprob: fp32 [T] or NULL, each element written, may be one of the inputs [T];
+ *   stats: fp32 [5] or NULL: sum f policy, sum f (exp(y) - y - 1), and over the tokens that count the share that is cut, the mean
+ *   of r - 1 - x, and their number.
+ * fp32 per token, sums over tokens in fp64 in one fixed order: the same inputs give the same bits on every call.  T < 2^31; tensors
+ * aligned to their elements.  ws: tik_workspace_bytes(TIK_OP_POLICY_LOSS, T, ..., S as max_ctx, ...) bytes, as above.  One kernel up
+ * to 32768 tokens (with weights and per-sequence means also at most 8192 sequences), else two. */
+tik_status tik_policy_loss(tik_ctx* ctx, const float* logprob, const float* old_logprob, const float* advantage,
+                           int advantage_per_sequence, const float* weight, const float* ref_logprob, const int32_t* cu_seqlens, int S,
+                           int64_t T, float clip_low, float clip_high, float clip_dual, float kl_coef, int reduction, float scale,
+                           float* loss, float* d_logprob, float* stats, void* ws, size_t ws_bytes, void* stream);
+
 /* Hidden RMSNorm, optionally fused with the residual add (the paper's operator table, Sec. 6:
  * "Hidden RMSNorm", "Fused residual + RMSNorm"; no formulas are given, the textbook ones apply).
  *   residual == NULL:  y[t] = x[t] * rsqrt(mean_j x[t][j]^2 + eps) * weight
@@ -366,6 +418,33 @@ tik_status tik_grad_norm(tik_ctx* ctx, const void* const* grads, const int64_t* 
 tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* out, const int64_t* numel,
                          const int* dtypes, int n, float max_norm, float* norm, int norm_given, void* ws,
                          size_t ws_bytes, void* stream);
+
+/* AdamW step over n tensors, in place:
+ *   g = c grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = (1 - lr weight_decay) p - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ *   params, grads, master, exp_avg (m), exp_avg_sq (v), exp_avg_scale, exp_avg_sq_scale: HOST arrays of n device pointers,
+ *   param_dtypes, grad_dtypes (TIK_DTYPE_*, bf16 or fp32 each) and numel: HOST arrays, read during the call.  A tensor's elements
+ *   are contiguous, its base aligned to its element; numel[i] may be 0.
+ *   master: NULL, or fp32 copies of the weights ([i] NULL for fp32 weights): p is the copy then, and the weight its rounding.
+ *   state_dtype TIK_DTYPE_FP32: m, v fp32.  TIK_DTYPE_E4M3: 8 bits.  Of every 32 consecutive elements (the last block may
+ *   be shorter), exp_avg holds m / 2^k and exp_avg_sq holds sqrt(v) / 2^k' in e4m3, and a byte of exp_avg_scale / exp_avg_sq_scale
+ *   ([ceil(numel / 32)]) holds k + 127 / k' + 127: k >= -127 is the smallest with which the block's largest is at most 448.  A
+ *   root that is not 0 is stored as 2^-9 at least.  What is not finite is stored as NaN and does not count for k.  All zeros is the state
+ *   before the first step.
+ *   step: this step's number, from 1 on.  lr_device, step_device: device fp32 [1], int32 [1], or NULL; read in place of lr and step
+ *   when the kernel runs, so that a captured step follows them.
+ *   norm: device fp32 [1] or NULL (c = 1): the gradients' norm, as tik_grad_norm leaves it.  c = max_norm / norm where max_norm < norm
+ *   < infinity, else 1, and a norm that is not finite skips the step: nothing is written.
+ *   stochastic != 0: 8-bit moments and bf16 weights without a master copy are rounded to one of their two neighbours, up with
+ *   the probability of the distance from the lower one: 16 bits of a hash of the element's place in the call (elements of the tensors before it
+ *   counted), seed and step decide.  Else to the nearest.
+ * fp32 arithmetic.  Tensors that are written overlap neither each other nor an input (TIK_ERR_INVALID_ARG).  No workspace.  A kernel
+ * per four hundred tensors. */
+tik_status tik_adamw(tik_ctx* ctx, void* const* params, const int* param_dtypes, const void* const* grads, const int* grad_dtypes,
+                     float* const* master, void* const* exp_avg, void* const* exp_avg_sq, uint8_t* const* exp_avg_scale,
+                     uint8_t* const* exp_avg_sq_scale, int state_dtype, const int64_t* numel, int n, double lr, double beta1, double beta2,
+                     double eps, double weight_decay, int64_t step, const float* lr_device, const int32_t* step_device, const float* norm,
+                     float max_norm, int stochastic, uint32_t seed, void* stream);
 
 /* Decode attention without any allocation (the paper has no counterpart; this variant
  * exists for deployments of this library).  Same arguments, kernels and output bits as

@@ -19,7 +19,8 @@ from . import build as _build
 
 OK = 0
 OP_ATTN_TRAIN_FWD, OP_ATTN_PREFILL, OP_ATTN_DECODE, OP_TOKEN_LOGPROB, OP_ATTN_TRAIN_BWD = 0, 1, 2, 3, 4
-OP_EMBEDDING_BWD, OP_BLOCK_NORM_BWD, OP_GRAD_NORM = 5, 6, 7
+OP_EMBEDDING_BWD, OP_BLOCK_NORM_BWD, OP_GRAD_NORM, OP_TOKEN_LOGPROB_BWD, OP_POLICY_LOSS = 5, 6, 7, 8, 9
+LOSS_REDUCTIONS = {"sum": 0, "token": 1, "sequence": 2}
 DEV_BAD_BLOCK, DEV_BAD_TARGET, DEV_WAIT_EXPIRED, DEV_BAD_POSITION, DEV_BAD_CONTEXT, DEV_BAD_TOKEN = 1, 2, 4, 8, 16, 32
 
 _lib = None
@@ -79,6 +80,10 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     lib.tik_block_norm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, f32, vp, f32, vp, vp, vp, vp, vp, i64, i32, vp, sz, vp]
     lib.tik_grad_norm.argtypes = [vp, vp, vp, vp, i32, vp, vp, sz, vp]
     lib.tik_grad_clip.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp, i32, vp, sz, vp]
+    f64, u32 = c.c_double, c.c_uint32
+    lib.tik_token_logprob_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i64, i32, i32, f32, vp, sz, vp]
+    lib.tik_policy_loss.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, i64, f32, f32, f32, f32, i32, f32, vp, vp, vp, vp, sz, vp]
+    lib.tik_adamw.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, f64, f64, f64, f64, f64, i64, vp, vp, vp, f32, i32, u32, vp]
     lib.tik_attn_decode_static.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                            i32, f32, vp, vp]
     lib.tik_attn_decode_static.restype = i32
@@ -86,7 +91,7 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
                  "tik_kv_cache_write", "tik_attn_prefill", "tik_attn_decode", "tik_token_logprob",
                  "tik_qk_norm_rope_kv_write", "tik_rmsnorm", "tik_swiglu", "tik_linear",
                  "tik_attn_train_bwd", "tik_embedding", "tik_embedding_bwd", "tik_block_norm", "tik_block_norm_bwd",
-                 "tik_grad_norm", "tik_grad_clip"):
+                 "tik_grad_norm", "tik_grad_clip", "tik_token_logprob_bwd", "tik_policy_loss", "tik_adamw"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -219,6 +224,30 @@ def tik_token_logprob(hidden, lm_head, target_ids, inv_temperature: float = 1.0,
     return (_native or _load_native()).token_logprob(hidden, lm_head, target_ids, inv_temperature, ws, logprob, lse)
 
 
+def tik_token_logprob_bwd(d_logprob, hidden, lm_head, target_ids, lse, inv_temperature: float = 1.0, need_hidden: bool = True,
+                          need_lm_head: bool = True, d_hidden: Optional[torch.Tensor] = None,
+                          d_lm_head: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None):
+    """Gradient of tik_token_logprob: d_logprob fp32 [T] and the forward's inputs and lse [T] -> (d_hidden [T,H] bf16, d_lm_head
+    [V,H]: bf16, or the bf16 or fp32 tensor passed), None for what is not needed.  accumulate: added to d_lm_head (fp32).  Tokens with
+    d_logprob 0 give no gradient.  Deterministic.  Scratch is d_z of a vocabulary chunk in bf16, up to 2 GiB."""
+    return (_native or _load_native()).token_logprob_bwd(d_logprob, hidden, lm_head, target_ids, lse, inv_temperature, bool(need_hidden),
+                                                         bool(need_lm_head), d_hidden, d_lm_head, bool(accumulate), ws)
+
+
+def tik_policy_loss(logprob, old_logprob, advantage, weight=None, ref_logprob=None, cu_seqlens=None, clip_low: float = 0.2,
+                    clip_high: float = 0.2, clip_dual: float = 0.0, kl_coef: float = 0.0, reduction: str = "token", scale: float = 1.0,
+                    grad: bool = True, d_logprob: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """Clipped policy loss with a KL term over packed tokens, fp32 [T]; advantage [T], or [S,1] per sequence; weight: 0 masks a token,
+    anything else is its factor; cu_seqlens int32 [S+1].  reduction: "sum", "token" (mean over the tokens that count) or "sequence"
+    (scale times the sum over sequences of their means).  Returns (loss [1], d_logprob [T] (None without grad), stats [5]: policy
+    part, KL part, share of tokens cut, mean of r - 1 - log r, tokens that count).  loss and stats always are parts of one storage,
+    d_logprob and the scratch too where all is small (1 MiB together)."""
+    if reduction not in LOSS_REDUCTIONS:
+        raise ValueError("reduction must be one of %s" % ", ".join(LOSS_REDUCTIONS))
+    return (_native or _load_native()).policy_loss(logprob, old_logprob, advantage, weight, ref_logprob, cu_seqlens, clip_low, clip_high,
+                                                   clip_dual, kl_coef, LOSS_REDUCTIONS[reduction], scale, bool(grad), d_logprob, ws)
+
+
 def tik_embedding(ids, table, scale: float = 1.0, y: Optional[torch.Tensor] = None):
     """scale * table[ids]: ids int32 [T], table [V,H] bf16 -> y [T,H].  Ids outside [0,V): zeros and DEV_BAD_TOKEN."""
     return (_native or _load_native()).embedding(ids, table, scale, y)
@@ -260,6 +289,18 @@ def tik_grad_clip(grads, max_norm: float, norm: Optional[torch.Tensor] = None, o
     """grads *= max_norm / norm where max_norm < norm < inf, in place or into the tensors of `out`; returns norm.  norm: None =
     computed here, in a storage as tik_grad_norm's; a tensor fp32 [1] = taken from there (a sharded trainer's combined norm)."""
     return (_native or _load_native()).grad_clip(grads, max_norm, norm, out, ws)
+
+
+def tik_adamw(params, grads, exp_avg, exp_avg_sq, lr, step, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+              weight_decay: float = 0.0, master=None, exp_avg_scale=None, exp_avg_sq_scale=None,
+              norm: Optional[torch.Tensor] = None, max_norm: float = 1.0, seed: Optional[int] = None):
+    """AdamW step over lists of contiguous tensors, in place.  params, grads: bf16 or fp32 each; master: list of fp32 copies of bf16
+    weights (None for fp32 ones).  exp_avg, exp_avg_sq: fp32, or with the scales (float8_e8m0fnu or uint8, one per 32 elements of the
+    flattened tensor) float8_e4m3fn, exp_avg_sq then holding the root.  lr and step (from 1 on): numbers, or device tensors fp32 [1] and
+    int32 [1] that are read when the kernel runs.  norm: fp32 [1] as tik_grad_norm leaves it; gradients count clipped to max_norm, and a norm
+    that is not finite skips the step.  seed: stochastic rounding of 8-bit moments and of bf16 weights without a master copy."""
+    (_native or _load_native()).adamw(params, grads, exp_avg, exp_avg_sq, lr, step, beta1, beta2, eps, weight_decay, master, exp_avg_scale,
+                                      exp_avg_sq_scale, norm, max_norm, seed)
 
 
 STATIC_SCRATCH_BYTES = 8 << 20

@@ -17,8 +17,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
-bool make_tmap_bf16(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
-                    const uint64_t* strides_bytes, const uint32_t* box, std::string* err, bool swizzle64) {
+static bool make_tmap(tik_ctx* ctx, CUtensorMap* out, CUtensorMapDataType type, const void* base, int rank, const uint64_t* dims,
+                      const uint64_t* strides_bytes, const uint32_t* box, std::string* err, bool swizzle64) {
     cuuint64_t gdim[5], gstr[4];
     cuuint32_t bdim[5], estr[5];
     for (int i = 0; i < rank; ++i) {
@@ -28,7 +28,7 @@ bool make_tmap_bf16(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank, 
         if (i > 0) gstr[i - 1] = strides_bytes[i - 1];
     }
     CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
-        out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(base), gdim,
+        out, type, static_cast<cuuint32_t>(rank), const_cast<void*>(base), gdim,
         gstr, bdim, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
@@ -40,6 +40,14 @@ bool make_tmap_bf16(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank, 
         return false;
     }
     return true;
+}
+bool make_tmap_bf16(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank, const uint64_t* dims,
+                    const uint64_t* strides_bytes, const uint32_t* box, std::string* err, bool swizzle64) {
+    return make_tmap(ctx, out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, rank, dims, strides_bytes, box, err, swizzle64);
+}
+bool make_tmap_f32(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                   const uint32_t* box, std::string* err) {
+    return make_tmap(ctx, out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, base, rank, dims, strides_bytes, box, err, false);
 }
 
 static tik_status fail(tik_ctx* ctx, tik_status s, const char* msg) {
@@ -260,6 +268,12 @@ size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d
     if (op == TIK_OP_EMBEDDING_BWD) return rows_or_batch > 0 && H > 0 && V > 0 ? embed_bwd_bytes(rows_or_batch, V, H) : 0;
     if (op == TIK_OP_BLOCK_NORM_BWD) return rows_or_batch > 0 && H > 0 && H <= 8192 ? block_norm_bwd_bytes(rows_or_batch, H) : 0;
     if (op == TIK_OP_GRAD_NORM) return rows_or_batch > 0 ? grad_norm_bytes(rows_or_batch) : 0;
+    if (op == TIK_OP_TOKEN_LOGPROB_BWD) {
+        if (rows_or_batch <= 0 || rows_or_batch >= (1ll << 31) - 256 || H <= 0 || V <= 0 || V > (1 << 30)) return 0;
+        const LogprobBwdPlan g = logprob_bwd_plan(rows_or_batch, H, V);
+        return g.dz_bytes + g.sum_bytes + g.part_bytes;
+    }
+    if (op == TIK_OP_POLICY_LOSS) return policy_loss_bytes(max_ctx > 0 ? max_ctx : 0);
     return 0;
 }
 
@@ -632,6 +646,131 @@ tik_status tik_token_logprob(tik_ctx* ctx, const void* hidden, const void* lm_he
     return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_token_logprob");
 }
 
+tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const void* hidden, const void* lm_head,
+                                 const int32_t* target_ids, const float* lse, void* d_hidden, void* d_lm_head, int lm_head_dtype,
+                                 int accumulate, int64_t T, int H, int V, float inv_temperature, void* ws, size_t ws_bytes,
+                                 void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    if (T < 0 || H <= 0 || V <= 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative or zero size");
+    if (!(inv_temperature > 0.0f) || !std::isfinite(inv_temperature))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "inv_temperature must be finite and > 0");
+    if (lm_head_dtype != TIK_DTYPE_BF16 && lm_head_dtype != TIK_DTYPE_FP32) return fail(ctx, TIK_ERR_INVALID_ARG, "unknown element type");
+    if (accumulate && (!d_lm_head || lm_head_dtype != TIK_DTYPE_FP32))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "accumulate needs d_lm_head in fp32");
+    if (!d_hidden && !d_lm_head) return T == 0 ? TIK_OK : fail(ctx, TIK_ERR_INVALID_ARG, "neither d_hidden nor d_lm_head");
+    if (H % 64 != 0) return fail(ctx, TIK_ERR_UNSUPPORTED, "H must be a multiple of 64");
+    if (V > (1 << 30)) return fail(ctx, TIK_ERR_UNSUPPORTED, "V must be <= 2^30");
+    if (!aligned16(hidden) || !aligned16(lm_head) || !aligned16(d_hidden) || !aligned16(d_lm_head) || !aligned16(ws))
+        return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (!d_lm_head || accumulate) return TIK_OK;
+        const size_t bytes = static_cast<size_t>(V) * H * (lm_head_dtype == TIK_DTYPE_FP32 ? 4 : 2);
+        cudaError_t e = cudaMemsetAsync(d_lm_head, 0, bytes, st);
+        return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_token_logprob_bwd");
+    }
+    if (!d_logprob || !hidden || !lm_head || !target_ids || !lse) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (T >= (1ll << 31) - 256) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31 - 256");
+    const LogprobBwdPlan g = logprob_bwd_plan(T, H, V);
+    const size_t need = g.dz_bytes + g.sum_bytes + g.part_bytes;
+    if (!ws || ws_bytes < need) return fail(ctx, TIK_ERR_WORKSPACE, "log-prob gradient workspace too small");
+
+    LogprobBwdParams p{};
+    p.target = target_ids;
+    p.lse = lse;
+    p.d_logprob = d_logprob;
+    p.T = T;
+    p.H = H;
+    p.V = V;
+    p.inv_temperature = inv_temperature;
+    p.d_hidden = static_cast<__nv_bfloat16*>(d_hidden);
+    p.want_table = d_lm_head != nullptr;
+    p.table_fp32 = lm_head_dtype == TIK_DTYPE_FP32;
+    p.sm_count = ctx->sm_count;
+    p.dev_status = ctx->dev_status;
+    char* at = static_cast<char*>(ws);
+    void* dz = at;
+    p.sum = reinterpret_cast<float*>(at + g.dz_bytes);
+    p.part = reinterpret_cast<float*>(at + g.dz_bytes + g.sum_bytes);
+
+    const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.chunk);
+    const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, uT}, rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2};
+    const uint32_t rows[2] = {64, 128}, slab[2] = {64, 64}, rows4[2] = {32, 128};    // K-major operands and bf16 output, MN-major, fp32 output
+    LogprobBwdMaps m;
+    std::string err;
+    bool ok = make_tmap_bf16(ctx, &m.hidden_k, hidden, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
+              make_tmap_bf16(ctx, &m.hidden_mn, hidden, 2, xd, rowH, slab, &err) && make_tmap_bf16(ctx, &m.head_mn, lm_head, 2, wd, rowH, slab, &err) &&
+              make_tmap_bf16(ctx, &m.dz_out, dz, 2, zd, rowZ, rows, &err) && make_tmap_bf16(ctx, &m.dz_mn, dz, 2, zd, rowZ, slab, &err);
+    if (ok && d_lm_head)
+        ok = p.table_fp32 ? make_tmap_f32(ctx, &m.table_out, d_lm_head, 2, wd, rowH4, rows4, &err)
+                          : make_tmap_bf16(ctx, &m.table_out, d_lm_head, 2, wd, rowH, rows, &err);
+    if (ok && d_hidden) {
+        const uint64_t tiles = ((uT + 255) / 256) * ((uH + 255) / 256);
+        const uint64_t parts = (tiles - static_cast<uint64_t>(g.whole)) * g.split;
+        const uint64_t pd[2] = {256, parts * 256}, rowP[1] = {1024};
+        // (a call has whole tiles, split ones, or both; the map of what it has not is not used)
+        if (g.whole > 0) ok = make_tmap_f32(ctx, &m.sum_out, p.sum, 2, xd, rowH4, rows4, &err);
+        if (ok && parts > 0) ok = make_tmap_f32(ctx, &m.part_out, p.part, 2, pd, rowP, rows4, &err);
+        if (g.whole == 0) m.sum_out = m.part_out;
+        if (parts == 0) m.part_out = m.sum_out;
+    }
+    if (!ok) return fail(ctx, TIK_ERR_CUDA, err.c_str());
+    cudaError_t e = launch_logprob_bwd(m, p, g, accumulate != 0, st);
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_token_logprob_bwd");
+}
+
+tik_status tik_policy_loss(tik_ctx* ctx, const float* logprob, const float* old_logprob, const float* advantage,
+                           int advantage_per_sequence, const float* weight, const float* ref_logprob, const int32_t* cu_seqlens, int S,
+                           int64_t T, float clip_low, float clip_high, float clip_dual, float kl_coef, int reduction, float scale,
+                           float* loss, float* d_logprob, float* stats, void* ws, size_t ws_bytes, void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    if (T < 0 || S < 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative size");
+    if (!(clip_low >= 0.0f) || !(clip_low < 1.0f)) return fail(ctx, TIK_ERR_INVALID_ARG, "clip_low must be in [0, 1)");
+    if (!(clip_high >= 0.0f) || !std::isfinite(clip_high)) return fail(ctx, TIK_ERR_INVALID_ARG, "clip_high must be finite and >= 0");
+    if (clip_dual != 0.0f && (!(clip_dual > 1.0f) || !std::isfinite(clip_dual)))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "clip_dual must be 0 or finite and > 1");
+    if (!std::isfinite(kl_coef) || !std::isfinite(scale)) return fail(ctx, TIK_ERR_INVALID_ARG, "kl_coef and scale must be finite");
+    if (reduction != TIK_LOSS_SUM && reduction != TIK_LOSS_TOKEN_MEAN && reduction != TIK_LOSS_SEQUENCE_MEAN)
+        return fail(ctx, TIK_ERR_INVALID_ARG, "unknown reduction");
+    if (!loss) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (T > 0 && (!logprob || !old_logprob || !advantage)) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    if (T > 0 && (reduction == TIK_LOSS_SEQUENCE_MEAN || advantage_per_sequence) && (!cu_seqlens || S == 0))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "advantages or means per sequence need cu_seqlens");
+    if (kl_coef != 0.0f && T > 0 && !ref_logprob) return fail(ctx, TIK_ERR_INVALID_ARG, "kl_coef needs ref_logprob");
+    if (T >= (1ll << 31)) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31");
+    for (const void* q : {static_cast<const void*>(logprob), static_cast<const void*>(old_logprob), static_cast<const void*>(advantage),
+                          static_cast<const void*>(weight), static_cast<const void*>(ref_logprob), static_cast<const void*>(cu_seqlens),
+                          static_cast<const void*>(loss), static_cast<const void*>(d_logprob), static_cast<const void*>(stats)})
+        if (reinterpret_cast<uintptr_t>(q) & 3u) return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
+    if (!aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    const size_t need = tik_workspace_bytes(TIK_OP_POLICY_LOSS, T, 0, 0, 0, S, 0, 0);
+    if (!ws || ws_bytes < need) return fail(ctx, TIK_ERR_WORKSPACE, "policy loss workspace too small");
+    PolicyLossParams p{};
+    p.logprob = logprob;
+    p.old_logprob = old_logprob;
+    p.advantage = advantage;
+    p.weight = weight;
+    p.ref = ref_logprob;
+    p.cu = S > 0 && T > 0 ? cu_seqlens : nullptr;
+    p.S = S;
+    p.adv_per_seq = advantage_per_sequence != 0 && T > 0;
+    p.reduction = T > 0 ? reduction : TIK_LOSS_SUM;
+    p.T = T;
+    p.log_low = std::log1p(-static_cast<double>(clip_low));
+    p.log_high = std::log1p(static_cast<double>(clip_high));
+    p.log_dual = clip_dual != 0.0f ? std::log(static_cast<double>(clip_dual)) : INFINITY;
+    p.bound_low = 1.0f - clip_low;
+    p.bound_high = 1.0f + clip_high;
+    p.bound_dual = clip_dual;
+    p.kl_coef = kl_coef;
+    p.scale = scale;
+    p.loss = loss;
+    p.d_logprob = d_logprob;
+    p.stats = stats;
+    cudaError_t e = launch_policy_loss(p, ws, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_policy_loss");
+}
+
 tik_status tik_rmsnorm(tik_ctx* ctx, const void* x, void* residual, const void* weight, void* y, float eps,
                        int64_t T, int H, void* stream) {
     if (!ctx) return TIK_ERR_INVALID_ARG;
@@ -943,6 +1082,66 @@ tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* ou
     cudaError_t e = launch_grad_clip(grads, out, numel, dtypes, n, max_norm, norm, norm_given != 0, static_cast<double*>(ws),
                                      static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_grad_clip");
+}
+
+tik_status tik_adamw(tik_ctx* ctx, void* const* params, const int* param_dtypes, const void* const* grads, const int* grad_dtypes,
+                     float* const* master, void* const* exp_avg, void* const* exp_avg_sq, uint8_t* const* exp_avg_scale,
+                     uint8_t* const* exp_avg_sq_scale, int state_dtype, const int64_t* numel, int n, double lr, double beta1, double beta2,
+                     double eps, double weight_decay, int64_t step, const float* lr_device, const int32_t* step_device, const float* norm,
+                     float max_norm, int stochastic, uint32_t seed, void* stream) {
+    if (!ctx) return TIK_ERR_INVALID_ARG;
+    if (n < 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative size");
+    if (state_dtype != TIK_DTYPE_FP32 && state_dtype != TIK_DTYPE_E4M3) return fail(ctx, TIK_ERR_INVALID_ARG, "unknown element type");
+    const bool state8 = state_dtype == TIK_DTYPE_E4M3;
+    if (!(lr >= 0.0) || !std::isfinite(static_cast<float>(lr))) return fail(ctx, TIK_ERR_INVALID_ARG, "lr must be finite and >= 0");
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(ctx, TIK_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
+    if (!(static_cast<float>(eps) > 0.0f) || !std::isfinite(static_cast<float>(eps))) return fail(ctx, TIK_ERR_INVALID_ARG, "eps must be finite and > 0");
+    if (!(weight_decay >= 0.0) || !std::isfinite(static_cast<float>(weight_decay)))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "weight_decay must be finite and >= 0");
+    if (step < 1 && !step_device) return fail(ctx, TIK_ERR_INVALID_ARG, "step must be >= 1");
+    if (norm && (!(max_norm > 0.0f) || !std::isfinite(max_norm))) return fail(ctx, TIK_ERR_INVALID_ARG, "max_norm must be finite and > 0");
+    if (n > 0 && (!params || !param_dtypes || !grads || !grad_dtypes || !exp_avg || !exp_avg_sq || !numel || (state8 && (!exp_avg_scale || !exp_avg_sq_scale))))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+    auto odd = [](const void* q, uintptr_t size) { return (reinterpret_cast<uintptr_t>(q) & (size - 1)) != 0; };
+    int64_t total = 0;
+    for (int i = 0; i < n; ++i) {
+        if (numel[i] < 0) return fail(ctx, TIK_ERR_INVALID_ARG, "negative size");
+        for (int type : {param_dtypes[i], grad_dtypes[i]})
+            if (type != TIK_DTYPE_BF16 && type != TIK_DTYPE_FP32) return fail(ctx, TIK_ERR_INVALID_ARG, "unknown element type");
+        if (numel[i] == 0) continue;
+        if (!params[i] || !grads[i] || !exp_avg[i] || !exp_avg_sq[i] || (state8 && (!exp_avg_scale[i] || !exp_avg_sq_scale[i])) || (master && !master[i] && param_dtypes[i] == TIK_DTYPE_BF16))
+            return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
+        if (master && master[i] && param_dtypes[i] == TIK_DTYPE_FP32) return fail(ctx, TIK_ERR_INVALID_ARG, "fp32 weights have no master copy");
+        if (numel[i] >= (1ll << 40) || (total += numel[i]) >= (1ll << 40))
+            return fail(ctx, TIK_ERR_UNSUPPORTED, "the tensors must have less than 2^40 elements");
+        const uintptr_t size = state8 ? 1 : 4;
+        if (odd(params[i], param_dtypes[i] == TIK_DTYPE_FP32 ? 4 : 2) || odd(grads[i], grad_dtypes[i] == TIK_DTYPE_FP32 ? 4 : 2) ||
+            (master && odd(master[i], 4)) || odd(exp_avg[i], size) || odd(exp_avg_sq[i], size))
+            return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
+    }
+    if (odd(lr_device, 4) || odd(step_device, 4) || odd(norm, 4)) return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
+    const AdamTensors t = {params, param_dtypes, grads, grad_dtypes, master, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, numel, n};
+    AdamParams p{};
+    p.lr = lr;
+    p.weight_decay = weight_decay;
+    p.log_beta1 = std::log(beta1);
+    p.log_beta2 = std::log(beta2);
+    p.step = step;
+    p.lr_device = lr_device;
+    p.step_device = step_device;
+    p.norm = norm;
+    p.max_norm = max_norm;
+    p.beta1 = static_cast<float>(beta1);
+    p.beta2 = static_cast<float>(beta2);
+    p.one_minus_beta1 = static_cast<float>(1.0 - beta1);
+    p.one_minus_beta2 = static_cast<float>(1.0 - beta2);
+    p.eps = static_cast<float>(eps);
+    p.seed = seed;
+    bool no_memory = false;
+    if (adamw_ranges_overlap(t, p, state8, &no_memory))
+        return fail(ctx, TIK_ERR_INVALID_ARG, no_memory ? "out of host memory" : "tensors to be written overlap");
+    cudaError_t e = launch_adamw(t, p, state8, stochastic != 0, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_adamw");
 }
 
 tik_status tik_attn_train_bwd(tik_ctx* ctx, const void* q, const void* k, const void* v, const void* o,

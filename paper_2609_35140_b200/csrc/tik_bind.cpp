@@ -90,11 +90,12 @@ struct Args {
         if (v < INT32_MIN || v > INT32_MAX) raise(PyExc_OverflowError, "integer argument out of range");
         return static_cast<int>(v);
     }
-    float real() {
+    double dbl() {
         const double v = PyFloat_AsDouble(next());
         if (v == -1.0 && PyErr_Occurred()) throw PyError{};
-        return static_cast<float>(v);
+        return v;
     }
+    float real() { return static_cast<float>(dbl()); }
 };
 
 void* ptr(const at::Tensor& t) {
@@ -728,6 +729,186 @@ PyObject* token_logprob(Args a) {
     return wrap(lp_in, made);
 }
 
+PyObject* token_logprob_bwd(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const at::Tensor &g = on(dev, a.tensor()), &x = on(dev, a.tensor()), &w = on(dev, a.tensor()), &ids = on(dev, a.tensor()),
+                     &lse = on(dev, a.tensor());
+    const float inv_temperature = a.real();
+    const int need_hidden = a.int32(), need_table = a.int32();
+    const at::Tensor *dx_in = on(dev, a.opt()), *dw_in = on(dev, a.opt());
+    const int accumulate = a.int32();
+    const at::Tensor* ws_in = on(dev, a.opt());
+    want_rank(x, 2);
+    want_rank(w, 2);
+    const int64_t T = x.size(0);
+    const int H = dim(x, 1), V = dim(w, 0);
+    want_sizes(w, {V, H}, "lm_head");
+    want_sizes(g, {T}, "d_logprob");
+    want_sizes(ids, {T}, "target_ids");
+    want_sizes(lse, {T}, "lse");
+    want_sizes(dx_in, {T, H}, "d_hidden");
+    want_sizes(dw_in, {V, H}, "d_lm_head");
+    if ((dx_in && !need_hidden) || (dw_in && !need_table)) raise(PyExc_ValueError, "an output that is not needed is given");
+    if (!need_hidden && !need_table) raise(PyExc_ValueError, "neither d_hidden nor d_lm_head");
+    if (accumulate && !dw_in) raise(PyExc_ValueError, "accumulate needs d_lm_head");
+    at::Tensor made_x, made_w;
+    const at::Tensor *dx = need_hidden ? &out_or(dx_in, made_x, {T, H}, at::kBFloat16, x) : nullptr;
+    const at::Tensor *dw = need_table ? &out_or(dw_in, made_w, {V, H}, at::kBFloat16, x) : nullptr;
+    const Scratch ws = sized_ws(ws_in, tik_workspace_bytes(TIK_OP_TOKEN_LOGPROB_BWD, T, 0, 0, 0, 0, H, V), x);
+    const int type = dw ? element_type(*dw) : TIK_DTYPE_BF16;
+    void *xp = bf(x), *wp = bf(w), *dxp = bf(dx), *dwp = dw ? ptr(*dw) : nullptr, *st = stream();
+    const float *gp = f32(&g), *lp = f32(&lse);
+    const int32_t* ip = i32(ids);
+    check(unlocked([&] { return tik_token_logprob_bwd(ctx, gp, xp, wp, ip, lp, dxp, dwp, type, accumulate, T, H, V, inv_temperature, ws.p,
+                                                      ws.bytes, st); }), ctx);
+    PyObject *a0 = Py_None, *a1 = Py_None;
+    if (dx) a0 = wrap(dx_in, made_x);
+    else Py_INCREF(Py_None);
+    if (dw) a1 = wrap(dw_in, made_w);
+    else Py_INCREF(Py_None);
+    return Py_BuildValue("(NN)", a0, a1);
+}
+
+PyObject* policy_loss(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const at::Tensor &lp = on(dev, a.tensor()), &old = on(dev, a.tensor()), &adv = on(dev, a.tensor());
+    const at::Tensor *weight = on(dev, a.opt()), *ref = on(dev, a.opt()), *cu = on(dev, a.opt());
+    const float low = a.real(), high = a.real(), dual = a.real(), kl = a.real();
+    const int reduction = a.int32();
+    const float scale = a.real();
+    const int grad = a.int32();
+    const at::Tensor *d_in = on(dev, a.opt()), *ws_in = on(dev, a.opt());
+    want_rank(lp, 1);
+    const int64_t T = lp.size(0);
+    int S = 0;
+    if (cu) {
+        want_rank(*cu, 1);
+        S = dim(*cu, 0) - 1;
+        if (S < 0) raise(PyExc_ValueError, "cu_seqlens needs an element at least");
+    }
+    const bool per_sequence = adv.dim() == 2;
+    want_sizes(old, {T}, "old_logprob");
+    if (per_sequence) want_sizes(adv, {S, 1}, "advantage");
+    else want_sizes(adv, {T}, "advantage");
+    want_sizes(weight, {T}, "weight");
+    want_sizes(ref, {T}, "ref_logprob");
+    want_sizes(d_in, {T}, "d_logprob");
+    if (d_in && !grad) raise(PyExc_ValueError, "an output that is not needed is given");
+    const size_t need = tik_workspace_bytes(TIK_OP_POLICY_LOSS, T, 0, 0, 0, S, 0, 0);
+    // loss and stats are parts of one storage, with the gradient and the scratch where those are small
+    constexpr int64_t STATS = 5, SKIP = 4;                   // floats
+    const int64_t rows = Pool::room(4 * T), small = Pool::room(4 * (SKIP + STATS)), scratch = ws_in ? 0 : Pool::room(static_cast<int64_t>(need));
+    Pool pool((grad && !d_in ? rows : 0) + small + scratch, lp);
+    const at::Tensor both = pool.take({SKIP + STATS}, at::kFloat, lp);
+    const at::Tensor loss = part_of(both, both.storage_offset(), {1}, at::kFloat);
+    const at::Tensor stats = part_of(both, both.storage_offset() + SKIP, {STATS}, at::kFloat);
+    at::Tensor made;
+    if (grad && !d_in) made = pool.take({T}, at::kFloat, lp);
+    const at::Tensor* d = !grad ? nullptr : d_in ? d_in : &made;
+    Scratch ws;
+    if (ws_in) {
+        ws.use(*ws_in);
+    } else {
+        ws.own = pool.take({static_cast<int64_t>(need)}, at::kByte, lp);
+        ws.p = ws.own.data_ptr();
+        ws.bytes = need;
+    }
+    const float *lpp = f32(&lp), *op = f32(&old), *ap = f32(&adv), *wp = f32(weight), *rp = f32(ref);
+    float *lossp = f32(&loss), *dp = f32(d), *sp = f32(&stats);
+    const int32_t* cp = i32(cu);
+    void* st = stream();
+    check(unlocked([&] { return tik_policy_loss(ctx, lpp, op, ap, per_sequence, wp, rp, cp, S, T, low, high, dual, kl, reduction, scale, lossp,
+                                                dp, sp, ws.p, ws.bytes, st); }), ctx);
+    PyObject *a0 = THPVariable_Wrap(loss), *a1 = Py_None, *a2 = THPVariable_Wrap(stats);
+    if (d) a1 = wrap(d_in, made);
+    else Py_INCREF(Py_None);
+    return Py_BuildValue("(NNN)", a0, a1, a2);
+}
+
+// A Python list or tuple of tensors of one of some types, as a C array of their addresses.
+struct ListArgs {
+    std::vector<void*> ptrs;
+    ListArgs(PyObject* list, int device, const char* name, const std::vector<int64_t>& numel, std::initializer_list<at::ScalarType> types,
+             int64_t per, bool may_lack) {
+        if (!PyList_Check(list) && !PyTuple_Check(list)) raise(PyExc_TypeError, std::string(name) + ": expected a list or tuple of tensors");
+        if (PySequence_Fast_GET_SIZE(list) != static_cast<Py_ssize_t>(numel.size()))
+            raise(PyExc_ValueError, std::string(name) + " has another length than params");
+        ptrs.reserve(numel.size());
+        for (size_t i = 0; i < numel.size(); ++i) {
+            PyObject* o = PySequence_Fast_GET_ITEM(list, static_cast<Py_ssize_t>(i));
+            if (may_lack && o == Py_None) {
+                ptrs.push_back(nullptr);
+                continue;
+            }
+            if (!THPVariable_Check(o)) raise(PyExc_TypeError, std::string("expected a tensor, got ") + Py_TYPE(o)->tp_name);
+            const at::Tensor& t = on(device, THPVariable_Unpack(o));
+            bool known = false;
+            for (const at::ScalarType type : types) known = known || t.scalar_type() == type;
+            if (!known) raise_tik(std::string(name) + ": unexpected dtype " + at::toString(t.scalar_type()));
+            if (t.numel() != (numel[i] + per - 1) / per) raise(PyExc_ValueError, std::string(name) + " has other sizes than params");
+            ptrs.push_back(ptr(t));
+        }
+    }
+};
+
+PyObject* adamw(Args a) {
+    const int dev = current_device();
+    tik_ctx* ctx = context(dev);
+    const GradArgs p(a.next(), dev), g(a.next(), dev);
+    if (p.numel != g.numel) raise(PyExc_ValueError, "grads has other sizes than params");
+    PyObject *m_list = a.next(), *v_list = a.next();
+    auto number = [&](double& value, const at::Tensor*& tensor, at::ScalarType type, const char* name) {
+        PyObject* o = a.next();
+        if (THPVariable_Check(o)) {
+            tensor = &on(dev, THPVariable_Unpack(o));
+            want_sizes(*tensor, {1}, name);
+            ptr(*tensor, type);
+            return;
+        }
+        value = PyFloat_AsDouble(o);
+        if (value == -1.0 && PyErr_Occurred()) throw PyError{};
+    };
+    double lr = 0.0, step = 1.0;
+    const at::Tensor *lr_t = nullptr, *step_t = nullptr;
+    number(lr, lr_t, at::kFloat, "lr");
+    number(step, step_t, at::kInt, "step");
+    if (!(step >= 0.0 && step < 9.0e15) || step != static_cast<double>(static_cast<int64_t>(step))) raise(PyExc_ValueError, "step must be a whole number");
+    const double beta1 = a.dbl(), beta2 = a.dbl(), eps = a.dbl(), decay = a.dbl();
+    PyObject *master_list = a.next(), *ms_list = a.next(), *vs_list = a.next();
+    const at::Tensor* norm = on(dev, a.opt());
+    want_sizes(norm, {1}, "norm");
+    const float max_norm = a.real();
+    PyObject* seed_in = a.next();
+    uint32_t seed = 0;
+    const bool stochastic = seed_in != Py_None;
+    if (stochastic) {
+        seed = static_cast<uint32_t>(PyLong_AsUnsignedLongLongMask(seed_in));
+        if (PyErr_Occurred()) throw PyError{};
+    }
+    if ((ms_list == Py_None) != (vs_list == Py_None)) raise(PyExc_ValueError, "the moments' scales go together");
+    const bool state8 = ms_list != Py_None;
+    const at::ScalarType state = state8 ? at::kFloat8_e4m3fn : at::kFloat;
+    const std::vector<int64_t>& n = p.numel;
+    const ListArgs m(m_list, dev, "exp_avg", n, {state}, 1, false), v(v_list, dev, "exp_avg_sq", n, {state}, 1, false);
+    std::vector<void*> master, ms, vs;
+    if (master_list != Py_None) master = ListArgs(master_list, dev, "master", n, {at::kFloat}, 1, true).ptrs;
+    if (state8) {
+        ms = ListArgs(ms_list, dev, "exp_avg_scale", n, {at::kFloat8_e8m0fnu, at::kByte}, 32, false).ptrs;
+        vs = ListArgs(vs_list, dev, "exp_avg_sq_scale", n, {at::kFloat8_e8m0fnu, at::kByte}, 32, false).ptrs;
+    }
+    auto floats = [](const std::vector<void*>& l) { return l.empty() ? nullptr : reinterpret_cast<float* const*>(l.data()); };
+    auto bytes = [](const std::vector<void*>& l) { return l.empty() ? nullptr : reinterpret_cast<uint8_t* const*>(l.data()); };
+    const float *lrp = f32(lr_t), *np = f32(norm);
+    const int32_t* stp = i32(step_t);
+    void* st = stream();
+    check(unlocked([&] { return tik_adamw(ctx, p.ptrs.data(), p.types.data(), g.ptrs.data(), g.types.data(), floats(master), m.ptrs.data(),
+                                          v.ptrs.data(), bytes(ms), bytes(vs), state8 ? TIK_DTYPE_E4M3 : TIK_DTYPE_FP32, n.data(), p.n, lr, beta1,
+                                          beta2, eps, decay, static_cast<int64_t>(step), lrp, stp, np, max_norm, stochastic, seed, st); }), ctx);
+    Py_RETURN_NONE;
+}
+
 PyObject* context_handle(Args a) {           // device ordinal (or None: the current device) -> the context's address
     PyObject* o = a.next();
     int device = current_device();
@@ -762,6 +943,7 @@ PyMethodDef methods[] = {
     TIK_DEF(qk_norm_rope_kv_write), TIK_DEF(rmsnorm), TIK_DEF(swiglu), TIK_DEF(linear), TIK_DEF(attn_prefill),
     TIK_DEF(attn_prefill_kv), TIK_DEF(attn_decode), TIK_DEF(attn_decode_static), TIK_DEF(token_logprob), TIK_DEF(embedding),
     TIK_DEF(embedding_bwd), TIK_DEF(block_norm), TIK_DEF(block_norm_bwd), TIK_DEF(grad_norm), TIK_DEF(grad_clip),
+    TIK_DEF(token_logprob_bwd), TIK_DEF(policy_loss), TIK_DEF(adamw),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_tikbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -83,6 +83,9 @@ struct DeviceOnce {
 bool make_tmap_bf16(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank,
                     const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box,
                     std::string* err, bool swizzle64 = false);
+// The same of an fp32 tensor.
+bool make_tmap_f32(tik_ctx* ctx, CUtensorMap* out, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                   const uint32_t* box, std::string* err);
 
 struct AttnParams {
     alignas(64) CUtensorMap tmO; // train / prefill: tiled map of the output (same shape and box as Q)
@@ -191,6 +194,89 @@ struct LogprobParams {
 };
 cudaError_t launch_logprob(const CUtensorMap& tmA, const CUtensorMap& tmB, const LogprobParams& p, bool pair,
                            cudaStream_t stream);
+
+// Gradient of the log-probabilities (tik_logprob_bwd.cu).
+struct LogprobBwdParams {
+    const int32_t* target;       // [T]
+    const float* lse;            // [T], natural log, from the forward
+    const float* d_logprob;      // [T]
+    int64_t T;
+    int H, V;
+    float inv_temperature;
+    __nv_bfloat16* d_hidden;     // [T][H] or null
+    int want_table, table_fp32;
+    float* sum;                  // scratch [T][H]: d_hidden's whole tiles
+    float* part;                 // scratch [parts][split tiles][256][256]
+    int sm_count;
+    int* dev_status;
+    // of one launch
+    int v0, nv;                  // the vocabulary's columns of this chunk
+    int ldz;                     // columns of d_z
+    int row_tiles, col_tiles, nunit;     // 256 x 256 tiles, units
+    int whole, split;            // gradient of the hidden rows: tiles done whole, parts of the others
+    int add;                     // the output is added to
+};
+struct LogprobBwdPlan {
+    int chunks, chunk;           // of the vocabulary, columns of one (a multiple of 256)
+    int whole, split;
+    size_t dz_bytes, sum_bytes, part_bytes;
+};
+struct LogprobBwdMaps {
+    alignas(64) CUtensorMap hidden_k, head_k, hidden_mn, head_mn, dz_out, dz_mn, table_out, sum_out, part_out;
+};
+LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V);
+cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, bool add_table, cudaStream_t stream);
+
+// Policy loss (tik_loss.cu).
+constexpr int LOSS_SUM = 0, LOSS_TOKEN_MEAN = 1, LOSS_SEQUENCE_MEAN = 2;
+struct PolicyLossParams {
+    const float *logprob, *old_logprob;  // [T]
+    const float* advantage;      // [T], or [S] (adv_per_seq)
+    const float* weight;         // [T] or null
+    const float* ref;            // [T] or null
+    const int32_t* cu;           // [S + 1] or null
+    int S, adv_per_seq, reduction;
+    int64_t T;
+    double log_low, log_high, log_dual;
+    float bound_low, bound_high, bound_dual;
+    float kl_coef, scale;
+    float* loss;
+    float* d_logprob;            // [T] or null
+    float* stats;                // [5] or null
+    int* ticket;                 // scratch: CTAs that are done
+    double* part;                // scratch [CTAs][5]
+    int* count;                  // scratch [max(S, CTAs)]: tokens that count
+};
+size_t policy_loss_bytes(int64_t S);
+cudaError_t launch_policy_loss(PolicyLossParams& p, void* ws, cudaStream_t stream);     // fills in the scratch
+
+// AdamW over host lists of n tensors (tik_adamw.cu).
+struct AdamTensors {
+    void* const* params;
+    const int* param_dtypes;
+    const void* const* grads;
+    const int* grad_dtypes;
+    float* const* master;        // or null
+    void* const* m;
+    void* const* v;
+    uint8_t* const* m_scale;     // 8-bit moments only
+    uint8_t* const* v_scale;
+    const int64_t* numel;
+    int n;
+};
+struct AdamParams {
+    double lr, weight_decay, log_beta1, log_beta2;
+    long long step;
+    const float* lr_device;      // or null: lr
+    const int32_t* step_device;  // or null: step
+    const float* norm;           // or null
+    float max_norm;
+    float beta1, beta2, one_minus_beta1, one_minus_beta2, eps;
+    unsigned seed;
+};
+cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, cudaStream_t stream);
+// whether a range that the step writes meets another of its ranges (or no memory)
+bool adamw_ranges_overlap(const AdamTensors& t, const AdamParams& p, bool state8, bool* no_memory);
 
 struct NormParams {
     const __nv_bfloat16* x;      // [T][H]

@@ -1,0 +1,431 @@
+// Clipped policy loss with a KL term over packed tokens, and its gradient with respect to the log-probabilities.
+//
+// Per token, with x = logprob - old_logprob, r = exp(x), advantage A and y = ref_logprob - logprob:
+//   policy = max(-A r, -A clamp(r, 1 - clip_low, 1 + clip_high)),  for A < 0 and clip_dual: at most -A clip_dual
+//   kl     = exp(y) - y - 1
+//   l      = policy + kl_coef kl,      dl/dlogprob = (cut ? 0 : -A r) - kl_coef (exp(y) - 1)
+// and over the tokens whose weight w is not 0:  loss = sum_t f_t l_t,  d_logprob = f_t dl_t, with f_t = scale w_t, divided by the
+// number of such tokens (of the whole call, or of the token's sequence).
+//
+// Whether a token is cut is decided on x in 64 bits against the logarithms of the thresholds: r in 32 bits would put tokens on
+// the wrong side of a border where the gradient jumps.  Sums over tokens are fp64 in one fixed order, counts are integers.
+// 20 bytes in and 4 out per token: a call of less than some 100 000 tokens is all latency, and one cluster of up to eight CTAs takes
+// it in one launch, tokens in registers, counts and sums through distributed shared memory.  Longer calls, whose reads need all
+// SMs, take two: one counts, the other computes, and its last CTA folds the sums.
+#include <cstdlib>
+
+#include "tik_core.cuh"
+#include "tik_internal.h"
+#include "tik_ptx.cuh"
+
+namespace tik {
+
+namespace loss {
+constexpr int MAX_CLUSTER = 8;
+constexpr int SEQ_CAP = 8192;                // sequences' counts that a CTA of a cluster holds
+constexpr int STEPS = 8;                     // tokens of a thread, one per 32 tokens of its warp's stretch
+constexpr int CLUSTER_THREADS = 512;
+constexpr int GRID_THREADS = 256;
+constexpr int MAX_CTAS = 592;                // of the two-launch form
+constexpr int SUMS = 5;                      // policy, kl, cut, k3, tokens
+}  // namespace loss
+
+// exp(d) - d - 1 without cancellation: the series where d is small (eight terms: 2e-8 of the value at |d| = 1/2).
+__device__ __forceinline__ float exp_minus_tangent(float d) {
+    if (fabsf(d) > 0.5f) return expm1f(d) - d;
+    float p = 1.0f / 362880.0f;
+    p = fmaf(p, d, 1.0f / 40320.0f);
+    p = fmaf(p, d, 1.0f / 5040.0f);
+    p = fmaf(p, d, 1.0f / 720.0f);
+    p = fmaf(p, d, 1.0f / 120.0f);
+    p = fmaf(p, d, 1.0f / 24.0f);
+    p = fmaf(p, d, 1.0f / 6.0f);
+    p = fmaf(p, d, 0.5f);
+    return p * d * d;
+}
+
+// tokens that a sequence may hold
+__device__ __forceinline__ void loss_range(const PolicyLossParams& p, long long& from, long long& to) {
+    from = 0;
+    to = p.T;
+    if (p.cu) {
+        from = max(p.cu[0], 0);
+        to = min(static_cast<long long>(p.cu[p.S]), to);
+    }
+}
+
+struct LossToken {
+    float policy, kl, grad, k3;
+    bool cut;
+};
+__device__ __forceinline__ LossToken loss_token(const PolicyLossParams& p, float lp, float old, float adv, float ref) {
+    LossToken o;
+    const double x = static_cast<double>(lp) - static_cast<double>(old);
+    const float xf = static_cast<float>(x), r = expf(xf);
+    bool cut = false;
+    float at = r;
+    if (adv > 0.0f && x > p.log_high) {
+        cut = true;
+        at = p.bound_high;
+    } else if (adv < 0.0f && x < p.log_low) {
+        cut = true;
+        at = p.bound_low;
+    } else if (adv < 0.0f && x > p.log_dual) {             // (+infinity without a third threshold)
+        cut = true;
+        at = p.bound_dual;
+    }
+    o.cut = cut;
+    o.policy = -adv * at;
+    o.grad = cut ? 0.0f : o.policy;
+    o.k3 = exp_minus_tangent(xf);
+    o.kl = 0.0f;
+    if (p.ref) {
+        const float y = ref - lp;
+        o.kl = exp_minus_tangent(y);
+        o.grad -= p.kl_coef * expm1f(y);
+    }
+    return o;
+}
+
+// The sequences of a warp's ascending tokens.  `near`: cu[s0 + 1 + lane], the ends of the sequences from s0 on.
+struct LossSeq {
+    int s0, near;
+    __device__ __forceinline__ void load(const PolicyLossParams& p, int lane) { near = p.cu[min(s0 + 1 + lane, p.S)]; }
+    __device__ __forceinline__ void begin(const PolicyLossParams& p, long long token, int lane) {
+        s0 = warp_find_sequence(p.cu, p.S, token, lane);
+        load(p, lane);
+    }
+    // The sequence of each lane's token (whole warp, tokens ascending over the lanes and from call to call); some
+    // sequence for a token that none holds.
+    __device__ __forceinline__ int of(const PolicyLossParams& p, long long token, int lane) {
+        int n = 0;                                         // ends that the token has reached: a prefix of the 32
+#pragma unroll
+        for (int w = 16; w >= 1; w >>= 1)
+            if (__shfl_sync(0xffffffffu, near, n + w - 1) <= token) n += w;
+        if (__shfl_sync(0xffffffffu, near, 31) <= token) n = 32;
+        int s = s0 + n;
+        if (n == 32) {
+            int hi = p.S;                                  // cu[s] <= token; the last such s
+            while (hi - s > 1) {
+                const int mid = s + (hi - s) / 2;
+                if (p.cu[mid] <= token) s = mid;
+                else hi = mid;
+            }
+        }
+        s = min(s, p.S - 1);
+        const int last = __shfl_sync(0xffffffffu, s, 31);
+        if (last > s0) {
+            s0 = last;
+            load(p, lane);
+        }
+        return s;
+    }
+};
+
+template <class V>
+__device__ __forceinline__ V warp_total(V v) {
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
+}
+
+__device__ __forceinline__ double dsmem_read(uint32_t addr) {
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ int dsmem_read_int(uint32_t addr) {
+    int v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void dsmem_add(uint32_t addr, int v) {
+    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+__device__ __forceinline__ void loss_results(const PolicyLossParams& p, const double (&sum)[loss::SUMS]) {
+    const double n = sum[4] > 1.0 ? sum[4] : 1.0;
+    *p.loss = static_cast<float>(sum[0] + static_cast<double>(p.kl_coef) * sum[1]);
+    if (p.stats) {
+        p.stats[0] = static_cast<float>(sum[0]);
+        p.stats[1] = static_cast<float>(sum[1]);
+        p.stats[2] = static_cast<float>(sum[2] / n);
+        p.stats[3] = static_cast<float>(sum[3] / n);
+        p.stats[4] = static_cast<float>(sum[4]);
+    }
+}
+// Sums of a block's threads: thread 0 gets the totals, warps in ascending order.
+template <int THREADS>
+__device__ __forceinline__ void loss_block_sums(double (&v)[loss::SUMS], double (*buf)[loss::SUMS], int warps) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < loss::SUMS; ++i) {
+        v[i] = warp_total(v[i]);
+        if (lane == 0) buf[warp][i] = v[i];
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int i = 0; i < loss::SUMS; ++i) {
+            v[i] = 0.0;
+            for (int w = 0; w < warps; ++w) v[i] += buf[w][i];
+        }
+}
+
+// One cluster.  A thread holds `steps` tokens (at most STEPS): those of its lane in each 32 of its warp's stretch.
+__global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(const PolicyLossParams p, int steps) {
+    using namespace loss;
+    extern __shared__ int seq_count[];                     // [per]: tokens of the sequences rank * per ...
+    __shared__ double sums[CLUSTER_THREADS / 32][SUMS];
+    __shared__ double cta_sums[SUMS];
+    __shared__ int cta_count;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
+    const int ctas = static_cast<int>(gridDim.x), rank = static_cast<int>(blockIdx.x);
+    const bool per_sequence = p.reduction == LOSS_SEQUENCE_MEAN, count_seq = per_sequence && p.weight;
+    const int per = (p.S + ctas - 1) / ctas;
+    const bool find = p.adv_per_seq || per_sequence;
+    if (count_seq)
+        for (int i = tid; i < per; i += blockDim.x) seq_count[i] = 0;
+    if (tid == 0) cta_count = 0;
+    pdl_wait();
+    pdl_launch_dependents();
+    const long long t0 = (static_cast<long long>(rank) * warps + warp) * 32 * steps + lane;
+    long long from, to;
+    loss_range(p, from, to);
+    float lp[STEPS], old[STEPS], adv[STEPS], w[STEPS], ref[STEPS];
+    int seq[STEPS];
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+        const long long t = t0 + 32 * j;
+        const bool in = j < steps && t >= from && t < to;
+        w[j] = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f;
+        lp[j] = in ? p.logprob[t] : 0.0f;
+        old[j] = in ? p.old_logprob[t] : 0.0f;
+        adv[j] = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
+        ref[j] = in && p.ref ? p.ref[t] : 0.0f;
+    }
+    if (find) {
+        LossSeq q;
+        q.begin(p, t0 - lane, lane);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            if (j < steps) seq[j] = q.of(p, t0 + 32 * j, lane);
+            if (j < steps && p.adv_per_seq && w[j] != 0.0f) adv[j] = p.advantage[seq[j]];
+        }
+    }
+    if (ctas > 1) cluster_sync_all();                      // zeroed counts, and every CTA of the cluster has begun
+    else __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+        const unsigned on = __ballot_sync(0xffffffffu, w[j] != 0.0f);
+        total += __popc(on);
+        if (count_seq && j < steps) {
+            // a warp's tokens are mostly of one sequence: one addition for each run of equal ones
+            const int before = __shfl_up_sync(0xffffffffu, seq[j], 1);
+            const unsigned heads = __ballot_sync(0xffffffffu, lane == 0 || before != seq[j]);
+            if (heads >> lane & 1u) {
+                const unsigned later = lane == 31 ? 0u : heads & (0xffffffffu << (lane + 1));
+                const unsigned run = (later ? (1u << (__ffs(later) - 1)) - 1u : 0xffffffffu) & (0xffffffffu << lane);
+                const int n = __popc(on & run), owner = seq[j] / per;
+                if (n > 0) dsmem_add(mapa_cluster(smem_u32(&seq_count[seq[j] - owner * per]), owner), n);
+            }
+        }
+    }
+    if (lane == 0 && total > 0) atomicAdd(&cta_count, total);
+    if (ctas > 1) cluster_sync_all();
+    else __syncthreads();
+    int all = 0;
+    for (int c = 0; c < ctas; ++c) all += dsmem_read_int(mapa_cluster(smem_u32(&cta_count), c));
+    float f = p.scale;
+    if (p.reduction == LOSS_TOKEN_MEAN) f = static_cast<float>(static_cast<double>(p.scale) / (all > 1 ? all : 1));
+    double sum[SUMS] = {};
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+        const long long t = t0 + 32 * j;
+        if (j >= steps || t >= p.T) break;
+        float d = 0.0f;
+        if (w[j] != 0.0f) {
+            float fj = f;
+            if (per_sequence) {
+                const int s = seq[j], owner = s / per;
+                const int n = count_seq ? dsmem_read_int(mapa_cluster(smem_u32(&seq_count[s - owner * per]), owner)) : p.cu[s + 1] - p.cu[s];
+                fj = __fdiv_rn(f, static_cast<float>(n > 1 ? n : 1));
+            }
+            fj *= w[j];
+            const LossToken o = loss_token(p, lp[j], old[j], adv[j], ref[j]);
+            d = fj * o.grad;
+            sum[0] += static_cast<double>(fj) * o.policy;
+            sum[1] += static_cast<double>(fj) * o.kl;
+            sum[2] += o.cut ? 1.0 : 0.0;
+            sum[3] += o.k3;
+        }
+        if (p.d_logprob) p.d_logprob[t] = d;
+    }
+    loss_block_sums<CLUSTER_THREADS>(sum, sums, warps);
+    if (ctas == 1) {
+        if (tid == 0) {
+            sum[4] = all;
+            loss_results(p, sum);
+        }
+        return;
+    }
+    if (tid == 0)
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) cta_sums[i] = sum[i];
+    cluster_sync_all();
+    if (rank == 0 && tid == 0) {
+        for (int c = 1; c < ctas; ++c)
+#pragma unroll
+            for (int i = 0; i < SUMS; ++i) sum[i] += dsmem_read(mapa_cluster(smem_u32(&cta_sums[i]), c));
+        sum[4] = all;
+        loss_results(p, sum);
+    }
+    cluster_sync_all();                                    // nobody leaves while its sums may still be read
+}
+
+// Tokens per sequence (a CTA each, `count` has S entries), or of the CTAs' shares of the call; the ticket of the next kernel.
+__global__ void __launch_bounds__(loss::GRID_THREADS) loss_count_kernel(const PolicyLossParams p) {
+    using namespace loss;
+    __shared__ int buf[GRID_THREADS / 32];
+    const int tid = threadIdx.x;
+    pdl_wait();
+    pdl_launch_dependents();
+    if (blockIdx.x == 0 && tid == 0) *p.ticket = 0;
+    if (!p.weight) return;
+    long long lo, hi;
+    loss_range(p, lo, hi);
+    long long from = lo + static_cast<long long>(blockIdx.x) * GRID_THREADS, to = hi, step = static_cast<long long>(gridDim.x) * GRID_THREADS;
+    if (p.reduction == LOSS_SEQUENCE_MEAN) {
+        from = max(lo, static_cast<long long>(p.cu[blockIdx.x]));
+        to = min(hi, static_cast<long long>(p.cu[blockIdx.x + 1]));
+        step = GRID_THREADS;
+    }
+    int n = 0;
+#pragma unroll 8
+    for (long long t = from + tid; t < to; t += step) n += p.weight[t] != 0.0f;
+    n = warp_total(n);
+    if ((tid & 31) == 0) buf[tid >> 5] = n;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < GRID_THREADS / 32; ++w) n += buf[w];
+        p.count[blockIdx.x] = n;
+    }
+}
+
+__global__ void __launch_bounds__(loss::GRID_THREADS) loss_grid_kernel(const PolicyLossParams p, int counts) {
+    using namespace loss;
+    constexpr int WARPS = GRID_THREADS / 32;
+    __shared__ double sums[WARPS][SUMS];
+    __shared__ int buf[WARPS];
+    __shared__ bool last;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool per_sequence = p.reduction == LOSS_SEQUENCE_MEAN, find = p.adv_per_seq || per_sequence;
+    pdl_wait();
+    pdl_launch_dependents();
+    long long lo, hi;
+    loss_range(p, lo, hi);
+    float f = p.scale;
+    if (p.reduction == LOSS_TOKEN_MEAN) {
+        long long all = hi - lo;
+        if (p.weight) {
+            int n = 0;
+            for (int i = tid; i < counts; i += GRID_THREADS) n += p.count[i];
+            n = warp_total(n);
+            if (lane == 0) buf[warp] = n;
+            __syncthreads();
+            all = 0;
+            for (int w = 0; w < WARPS; ++w) all += buf[w];
+        }
+        f = static_cast<float>(static_cast<double>(p.scale) / (all > 1 ? all : 1));
+    }
+    double sum[SUMS] = {};
+    const long long stretch = 32 * STEPS, step = static_cast<long long>(gridDim.x) * WARPS * stretch;
+    for (long long base = (static_cast<long long>(blockIdx.x) * WARPS + warp) * stretch; base < p.T; base += step) {
+        float lp[STEPS], old[STEPS], adv[STEPS], w[STEPS], ref[STEPS];
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            const long long t = base + 32 * j + lane;
+            const bool in = t >= lo && t < hi;
+            w[j] = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f;
+            lp[j] = in ? p.logprob[t] : 0.0f;
+            old[j] = in ? p.old_logprob[t] : 0.0f;
+            adv[j] = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
+            ref[j] = in && p.ref ? p.ref[t] : 0.0f;
+        }
+        LossSeq q;
+        if (find) q.begin(p, base, lane);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            const long long t = base + 32 * j + lane;
+            const int s = find ? q.of(p, t, lane) : 0;
+            float d = 0.0f;
+            if (w[j] != 0.0f) {
+                float fj = f;
+                if (per_sequence) {
+                    const int n = p.weight ? p.count[s] : p.cu[s + 1] - p.cu[s];
+                    fj = __fdiv_rn(f, static_cast<float>(n > 1 ? n : 1));
+                }
+                fj *= w[j];
+                const LossToken o = loss_token(p, lp[j], old[j], p.adv_per_seq ? p.advantage[s] : adv[j], ref[j]);
+                d = fj * o.grad;
+                sum[0] += static_cast<double>(fj) * o.policy;
+                sum[1] += static_cast<double>(fj) * o.kl;
+                sum[2] += o.cut ? 1.0 : 0.0;
+                sum[3] += o.k3;
+                sum[4] += 1.0;
+            }
+            if (p.d_logprob && t < p.T) p.d_logprob[t] = d;
+        }
+    }
+    loss_block_sums<GRID_THREADS>(sum, sums, WARPS);
+    if (tid == 0) {
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) p.part[blockIdx.x * SUMS + i] = sum[i];
+        __threadfence();
+        last = atomicAdd(p.ticket, 1) == static_cast<int>(gridDim.x) - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    // the CTAs' sums in one order, whichever CTA is the last
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) sum[i] = 0.0;
+    for (int c = tid; c < static_cast<int>(gridDim.x); c += GRID_THREADS)
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) sum[i] += __ldcg(&p.part[c * SUMS + i]);
+    loss_block_sums<GRID_THREADS>(sum, sums, WARPS);
+    if (tid == 0) loss_results(p, sum);
+}
+
+// Scratch: the ticket (16 bytes), the CTAs' sums, and counts of sequences or CTAs.
+size_t policy_loss_bytes(int64_t S) {
+    const size_t counts = static_cast<size_t>(S > loss::MAX_CTAS ? S : loss::MAX_CTAS);
+    return 16 + sizeof(double) * loss::SUMS * loss::MAX_CTAS + (counts * sizeof(int) + 15) / 16 * 16;
+}
+
+cudaError_t launch_policy_loss(PolicyLossParams& p, void* ws, cudaStream_t stream) {
+    using namespace loss;
+    const bool counts_seq = p.reduction == LOSS_SEQUENCE_MEAN && p.weight;
+    const int64_t most = static_cast<int64_t>(MAX_CLUSTER) * CLUSTER_THREADS * STEPS;
+    if (p.T <= most && (!counts_seq || p.S <= SEQ_CAP)) {
+        // as many CTAs as leave a thread two tokens, and then as many tokens as it takes
+        int ctas = 1;
+        while (ctas < MAX_CLUSTER && p.T > 2ll * ctas * CLUSTER_THREADS) ctas *= 2;
+        const int threads = p.T > CLUSTER_THREADS ? CLUSTER_THREADS : p.T > 32 ? static_cast<int>((p.T + 31) / 32 * 32) : 32;
+        const int steps = static_cast<int>((p.T + static_cast<int64_t>(ctas) * threads - 1) / (static_cast<int64_t>(ctas) * threads));
+        const size_t smem = counts_seq ? static_cast<size_t>((p.S + ctas - 1) / ctas) * sizeof(int) : 0;
+        return launch_pdl(loss_cluster_kernel, dim3(ctas), static_cast<unsigned>(threads), smem, stream, static_cast<unsigned>(ctas), p, steps);
+    }
+    p.ticket = static_cast<int*>(ws);
+    p.part = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);
+    p.count = reinterpret_cast<int*>(p.part + SUMS * MAX_CTAS);
+    const int64_t stretches = (p.T + GRID_THREADS * STEPS - 1) / (GRID_THREADS * STEPS);
+    const int ctas = static_cast<int>(stretches < MAX_CTAS ? stretches : MAX_CTAS);
+    const int counts = !p.weight ? 1 : p.reduction == LOSS_SEQUENCE_MEAN ? p.S : ctas;
+    cudaError_t e = launch_pdl(loss_count_kernel, dim3(static_cast<unsigned>(counts)), GRID_THREADS, 0, stream, 1, p);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(loss_grid_kernel, dim3(static_cast<unsigned>(ctas)), GRID_THREADS, 0, stream, 1, p, counts);
+}
+
+}  // namespace tik

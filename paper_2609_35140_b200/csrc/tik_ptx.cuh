@@ -299,9 +299,9 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t lbo
     d |= 2ull << 61;   // SWIZZLE_128B
     return d;
 }
-// Instruction descriptor: D fp32, A/B bf16, A K-major; B K-major or MN-major.
-__host__ __device__ constexpr uint32_t mma_idesc_bf16(int M, int N, bool b_mn_major) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn_major ? 1u : 0u) << 16) |
+// Instruction descriptor: D fp32, A/B bf16, each K-major or MN-major.
+__host__ __device__ constexpr uint32_t mma_idesc_bf16(int M, int N, bool b_mn_major, bool a_mn_major = false) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
            (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 // Named barriers (ids 1..15; 0 is __syncthreads): producer side arrives, consumer side syncs.
