@@ -65,6 +65,13 @@ __device__ __forceinline__ void mma_ss_chain4_pair_steps(uint32_t d_tmem, uint64
         : "memory");
 }
 
+// One warp of both CTAs: all of tensor memory, two 256-column accumulators.  Before the CTA's dependents are released.
+constexpr uint32_t LPB_TMEM_COLS = 512;
+__device__ __forceinline__ void lpb_take_tensor_memory(volatile uint32_t* slot) {
+    tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(slot)), LPB_TMEM_COLS);
+    tmem_relinquish_pair();
+}
+
 struct LpbUnit {
     int row, col;                // of the output tile
     int k0, k1;                  // slices of 64 of the contracted axis
@@ -109,7 +116,6 @@ __global__ void __launch_bounds__(lpb::THREADS, 1)
 lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
            const __grid_constant__ CUtensorMap tmPart, const LogprobBwdParams p) {
     using namespace lpb;
-    constexpr uint32_t TMEM_COLS = 512;      // two 256-column accumulators
     constexpr bool A_MN = KIND == TABLE, B_MN = KIND != DZ;
     constexpr uint32_t IDESC = mma_idesc_bf16(256, TILE, B_MN, A_MN);
     const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
@@ -143,10 +149,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         tma_prefetch_desc(&tmOut);
         if (KIND == HIDDEN) tma_prefetch_desc(&tmPart);
     }
-    if (warp == 1) {
-        tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), TMEM_COLS);
-        tmem_relinquish_pair();
-    }
+    if (warp == 1) lpb_take_tensor_memory(tmem_slot);
     pdl_wait();
     if (tid == 0) *abort_word = (*reinterpret_cast<volatile int*>(p.dev_status) & TIK_DEV_WAIT_EXPIRED) ? 1 : 0;
     tc_fence_before();
@@ -330,7 +333,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();            // neither CTA leaves while the other may still touch it
-    if (warp == 1) tmem_dealloc_pair(tmem, TMEM_COLS);
+    if (warp == 1) tmem_dealloc_pair(tmem, LPB_TMEM_COLS);
 }
 
 // d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order.  Thread per eight channels.
