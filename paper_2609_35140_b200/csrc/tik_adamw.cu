@@ -14,7 +14,7 @@
 // below, from 16 bits of a hash of the element's place, the seed and the step), and so are bf16 weights without a master copy.
 //
 // HBM-bound: 12 bytes of bf16 weights, gradient and 8-bit moments to 28 with a master copy.  The list travels as a kernel parameter;
-// chunks of 8192 elements on 592 CTAs, four per SM.
+// chunks of 8192 elements on as many CTAs as the SMs hold.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -28,7 +28,6 @@ namespace tik {
 
 constexpr int ADAM_THREADS = 256;
 constexpr int ADAM_CHUNK = 8192;
-constexpr int ADAM_CTAS = 592;
 constexpr int ADAM_BLOCK = 32;                               // elements that share a scale
 
 struct AdamEntry {
@@ -42,7 +41,7 @@ struct AdamEntry {
     unsigned first;              // chunk of the launch with which the tensor begins
     int flags;
 };
-constexpr int ADAM_PARAM_FP32 = 1, ADAM_GRAD_FP32 = 2, ADAM_VECTORS = 4;
+constexpr int ADAM_PARAM_FP32 = 1, ADAM_GRAD_FP32 = 2;
 template <int CAP>
 struct AdamList {
     AdamEntry e[CAP];
@@ -75,85 +74,90 @@ __device__ __forceinline__ uint32_t adam_random(long long place, uint32_t key) {
     return adam_mix(static_cast<uint32_t>(place) * 0x632BE5ABu + key + static_cast<uint32_t>(place >> 32) * 0x85157AF5u);
 }
 
-// N elements from `at` on; what lies at or past n is 0
-template <int N>
-__device__ __forceinline__ void adam_load(float (&x)[N], const void* src, bool fp32, long long at, long long n) {
-    if (N == 8 && at + 8 <= n) {
-        if (fp32) {
-            const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(src) + at);
-            const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(src) + at + 4);
-            x[0] = a.x, x[1 % N] = a.y, x[2 % N] = a.z, x[3 % N] = a.w, x[4 % N] = b.x, x[5 % N] = b.y, x[6 % N] = b.z, x[7 % N] = b.w;
+// A thread's eight elements, in groups of W neighbours, a group of every thread after the other: W = 4 where a tensor lies at multiples of
+// 16 bytes (a warp's access is one run of 128 bytes or more, whole sectors), else W = 1.  A block of 32 is a group of 32 / W lanes.
+constexpr int ADAM_N = 8;
+template <int W>
+__device__ __forceinline__ long long adam_place(long long at, int i) { return at + i % W + (i / W) * (W * ADAM_THREADS); }
+
+// What lies at or past n is 0.
+template <int W>
+__device__ __forceinline__ void adam_load(float (&x)[ADAM_N], const void* src, bool fp32, long long at, long long n) {
+#pragma unroll
+    for (int i = 0; i < ADAM_N; i += W) {
+        const long long e = adam_place<W>(at, i);
+        if (W == 4 && e + W <= n) {
+            if (fp32) {
+                const float4 a = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(src) + e));
+                x[i] = a.x, x[i + 1 % W] = a.y, x[i + 2 % W] = a.z, x[i + 3 % W] = a.w;
+            } else {
+                const uint2 a = __ldcs(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(src) + e));
+                x[i] = __uint_as_float(a.x << 16), x[i + 1 % W] = __uint_as_float(a.x & 0xffff0000u);
+                x[i + 2 % W] = __uint_as_float(a.y << 16), x[i + 3 % W] = __uint_as_float(a.y & 0xffff0000u);
+            }
         } else {
-            const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(src) + at);
-            const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+            for (int j = 0; j < W; ++j) {
+                x[i + j] = 0.0f;
+                if (e + j < n) x[i + j] = fp32 ? static_cast<const float*>(src)[e + j] : __bfloat162float(static_cast<const __nv_bfloat16*>(src)[e + j]);
+            }
         }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        x[i] = 0.0f;
-        if (at + i < n) x[i] = fp32 ? static_cast<const float*>(src)[at + i] : __bfloat162float(static_cast<const __nv_bfloat16*>(src)[at + i]);
     }
 }
-template <int N>
-__device__ __forceinline__ void adam_store(const float (&x)[N], void* dst, bool fp32, long long at, long long n) {
-    if (N == 8 && at + 8 <= n) {
-        if (fp32) {
-            *reinterpret_cast<float4*>(static_cast<float*>(dst) + at) = make_float4(x[0], x[1 % N], x[2 % N], x[3 % N]);
-            *reinterpret_cast<float4*>(static_cast<float*>(dst) + at + 4) = make_float4(x[4 % N], x[5 % N], x[6 % N], x[7 % N]);
-        } else {
-            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(dst) + at) =
-                make_uint4(pack_bf16x2(x[0], x[1 % N]), pack_bf16x2(x[2 % N], x[3 % N]), pack_bf16x2(x[4 % N], x[5 % N]), pack_bf16x2(x[6 % N], x[7 % N]));
-        }
-        return;
-    }
+template <int W>
+__device__ __forceinline__ void adam_store(const float (&x)[ADAM_N], void* dst, bool fp32, long long at, long long n) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (at + i < n) {
-            if (fp32) static_cast<float*>(dst)[at + i] = x[i];
-            else static_cast<__nv_bfloat16*>(dst)[at + i] = __float2bfloat16_rn(x[i]);
+    for (int i = 0; i < ADAM_N; i += W) {
+        const long long e = adam_place<W>(at, i);
+        if (W == 4 && e + W <= n) {
+            if (fp32)
+                __stcs(reinterpret_cast<float4*>(static_cast<float*>(dst) + e), make_float4(x[i], x[i + 1 % W], x[i + 2 % W], x[i + 3 % W]));
+            else
+                __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(dst) + e),
+                       make_uint2(pack_bf16x2(x[i], x[i + 1 % W]), pack_bf16x2(x[i + 2 % W], x[i + 3 % W])));
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (e + j < n) {
+                    if (fp32) static_cast<float*>(dst)[e + j] = x[i + j];
+                    else static_cast<__nv_bfloat16*>(dst)[e + j] = __float2bfloat16_rn(x[i + j]);
+                }
         }
+    }
 }
 
 __device__ __forceinline__ float adam_scale_value(unsigned byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
-// N stored 8-bit values times their block's scale
-template <int N>
-__device__ __forceinline__ void adam_load8(float (&x)[N], const void* src, const uint8_t* scale, long long at, long long n) {
-    const uint8_t* q = static_cast<const uint8_t*>(src) + at;
-    const float s = at < n ? adam_scale_value(scale[at / ADAM_BLOCK]) : 0.0f;
-    unsigned w[2] = {0u, 0u};
-    if (N == 8 && at + 8 <= n) {
-        const uint2 a = *reinterpret_cast<const uint2*>(q);
-        w[0] = a.x;
-        w[1] = a.y;
-    } else {
+// Stored 8-bit values times their block's scale
+template <int W>
+__device__ __forceinline__ void adam_load8(float (&x)[ADAM_N], const void* src, const uint8_t* scale, long long at, long long n) {
+    const uint8_t* q = static_cast<const uint8_t*>(src);
+    unsigned w[2] = {0u, 0u}, byte[ADAM_N / W];
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < n) w[i / 4] |= static_cast<unsigned>(q[i]) << (8 * (i & 3));
+    for (int i = 0; i < ADAM_N; i += W) {
+        const long long e = adam_place<W>(at, i);
+        byte[i / W] = e < n ? scale[e / ADAM_BLOCK] : 0u;
+        if (W == 4 && e + W <= n) {
+            w[i / 4] = __ldcs(reinterpret_cast<const unsigned*>(q + e));
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (e + j < n) w[i / 4] |= static_cast<unsigned>(q[e + j]) << (8 * ((i + j) & 3));
+        }
     }
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
+    for (int i = 0; i < ADAM_N; i += 2) {
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[i / 4] >> (8 * (i & 2))), __NV_E4M3);
         const float2 f = __half22float2(__half2(h));
-        x[i] = f.x * s;
-        if (N > 1) x[(i + 1) % N] = f.y * s;
+        x[i] = f.x * adam_scale_value(byte[i / W]);
+        x[i + 1] = f.y * adam_scale_value(byte[(i + 1) / W]);
     }
 }
-// Largest magnitude of a block: `lanes` neighbouring lanes hold it.  What is not finite does not count.
-template <int N>
-__device__ __forceinline__ float adam_block_max(const float (&x)[N]) {
-    float a = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float f = fabsf(x[i]);
-        a = fmaxf(a, f <= 3.402823466e38f ? f : 0.0f);
-    }
-#pragma unroll
-    for (int off = 1; off < ADAM_BLOCK / N; off <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, off));
-    return a;
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
 }
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.402823466e38f; }
 // The power of two, as its biased exponent, with which a block whose largest magnitude is `a` fits 448 = 1.75 * 2^8.
 __device__ __forceinline__ unsigned adam_scale_of(float a) {
     const unsigned b = __float_as_uint(a);
@@ -167,85 +171,125 @@ __device__ __forceinline__ float adam_round_e4m3(float y, unsigned random16) {
     const float t = floorf(__fadd_rn(fabsf(y) * per_place, static_cast<float>(random16) * 0x1p-16f));
     return copysignf(t * place, y);
 }
-// Stores N values of a block and, from its first lane, the scale.  POSITIVE: no value above 0 becomes 0.
-template <int N, bool STOCHASTIC, bool POSITIVE>
-__device__ __forceinline__ void adam_store8(const float (&x)[N], const uint32_t (&random)[N], void* dst, uint8_t* scale, long long at, long long n) {
-    const unsigned byte = adam_scale_of(adam_block_max(x));
-    const float inv = __uint_as_float((254u - byte) << 23);
-    unsigned w[2] = {0u, 0u};
+// Stores values and, from each block's first lane, its scale.  POSITIVE: the second moment's roots, of which none above 0 becomes 0.
+template <int W, bool STOCHASTIC, bool POSITIVE>
+__device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint32_t (&random)[ADAM_N], void* dst, uint8_t* scale, long long at,
+                                            long long n) {
+    unsigned byte[ADAM_N / W], w[2] = {0u, 0u};
+    float y[ADAM_N];
+    bool plain = true;                                       // every value is finite, and 0 or in e4m3's normal range
 #pragma unroll
-    for (int i = 0; i < N; i += 2) {
-        float y[2];
+    for (int k = 0; k < ADAM_N / W; ++k) {
+        float a = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float f = i + j < N ? x[(i + j) % N] : 0.0f;
-            y[j] = f * inv;
-            if (STOCHASTIC) y[j] = adam_round_e4m3(y[j], POSITIVE ? random[(i + j) % N] >> 16 : random[(i + j) % N] & 0xffffu);
-            if (!(fabsf(f) <= 3.402823466e38f)) y[j] = CUDART_NAN_F;
+        for (int j = 0; j < W; ++j) a = max_or_nan(a, fabsf(x[W * k + j]));
+        if (!finite(a)) {                                    // what is not finite does not count
+            plain = false;
+            a = 0.0f;
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (finite(x[W * k + j])) a = fmaxf(a, fabsf(x[W * k + j]));
         }
-        unsigned q = __nv_cvt_float2_to_fp8x2(make_float2(y[0], y[1]), __NV_SATFINITE, __NV_E4M3);
-        if (POSITIVE) {
-            if ((q & 0xffu) == 0u && x[i] > 0.0f) q |= 1u;
-            if (N > 1 && (q & 0xff00u) == 0u && x[(i + 1) % N] > 0.0f) q |= 0x100u;
-        }
-        w[i / 4] |= q << (8 * (i & 2));
+#pragma unroll
+        for (int off = 1; off < ADAM_BLOCK / W; off <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, off));
+        byte[k] = adam_scale_of(a);
     }
-    uint8_t* to = static_cast<uint8_t*>(dst) + at;
-    if (N == 8 && at + 8 <= n) {
-        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+#pragma unroll
+    for (int i = 0; i < ADAM_N; ++i) {
+        y[i] = x[i] * __uint_as_float((254u - byte[i / W]) << 23);
+        plain = plain && (__float_as_uint(fabsf(y[i])) - 1u >= 0x3c800000u - 1u);
+    }
+    if (plain) {
+        if (STOCHASTIC)
+#pragma unroll
+            for (int i = 0; i < ADAM_N; ++i) {
+                // 20 of 23 places are cut off: the number is added below them.  (The same as below in the normal range.)
+                const unsigned r = POSITIVE ? random[i] >> 12 & 0xffff0u : (random[i] & 0xffffu) << 4;
+                y[i] = __uint_as_float((__float_as_uint(y[i]) + r) & 0xfff00000u);
+            }
+#pragma unroll
+        for (int i = 0; i < ADAM_N; i += 2)
+            w[i / 4] |= static_cast<unsigned>(__nv_cvt_float2_to_fp8x2(make_float2(y[i], y[i + 1]), __NV_SATFINITE, __NV_E4M3)) << (8 * (i & 2));
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < n) to[i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i & 3)));
+        for (int i = 0; i < ADAM_N; ++i) {
+            float f = y[i];
+            if (STOCHASTIC) f = adam_round_e4m3(f, POSITIVE ? random[i] >> 16 : random[i] & 0xffffu);
+            if (!finite(x[i])) f = CUDART_NAN_F;
+            unsigned q = __nv_cvt_float_to_fp8(f, __NV_SATFINITE, __NV_E4M3);
+            if (POSITIVE && q == 0u && x[i] > 0.0f) q = 1u;
+            w[i / 4] |= q << (8 * (i & 3));
+        }
     }
-    if (at < n && at % ADAM_BLOCK == 0) scale[at / ADAM_BLOCK] = static_cast<uint8_t>(byte);
+    uint8_t* to = static_cast<uint8_t*>(dst);
+#pragma unroll
+    for (int i = 0; i < ADAM_N; i += W) {
+        const long long e = adam_place<W>(at, i);
+        if (W == 4 && e + W <= n) {
+            __stcs(reinterpret_cast<unsigned*>(to + e), w[i / 4]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (e + j < n) to[e + j] = static_cast<uint8_t>(w[i / 4] >> (8 * ((i + j) & 3)));
+        }
+        if (e < n && e % ADAM_BLOCK == 0) scale[e / ADAM_BLOCK] = static_cast<uint8_t>(byte[i / W]);
+    }
 }
 
-// N elements of a tensor, the same N for all lanes of a warp, whose elements are neighbours.
-template <int N, bool STATE8, bool STOCHASTIC>
+// Eight elements of each of a warp's lanes.
+template <int W, bool STATE8, bool STOCHASTIC>
 __device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, const AdamParams& p, const AdamStep& s, float clip) {
     const long long n = e.n;
-    float w[N], g[N], m[N], v[N];
+    float x[ADAM_N], g[ADAM_N], m[ADAM_N], v[ADAM_N];
     const bool p32 = e.flags & ADAM_PARAM_FP32;
-    adam_load(g, e.grad, e.flags & ADAM_GRAD_FP32, at, n);
+    adam_load<W>(g, e.grad, e.flags & ADAM_GRAD_FP32, at, n);
     if (STATE8) {
-        adam_load8(m, e.m, e.m_scale, at, n);
-        adam_load8(v, e.v, e.v_scale, at, n);
+        adam_load8<W>(m, e.m, e.m_scale, at, n);
+        adam_load8<W>(v, e.v, e.v_scale, at, n);
     } else {
-        adam_load(m, e.m, true, at, n);
-        adam_load(v, e.v, true, at, n);
+        adam_load<W>(m, e.m, true, at, n);
+        adam_load<W>(v, e.v, true, at, n);
     }
-    adam_load(w, e.master ? static_cast<const void*>(e.master) : e.param, e.master ? true : p32, at, n);
-    uint32_t random[N];
+    adam_load<W>(x, e.master ? static_cast<const void*>(e.master) : e.param, e.master ? true : p32, at, n);
+    uint32_t random[ADAM_N];
+    const float to_m = p.one_minus_beta1 * clip, to_v = p.one_minus_beta2 * clip * clip;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < ADAM_N; ++i) {
         if (STATE8) v[i] = v[i] * v[i];
-        const float gi = g[i] * clip;
-        m[i] = fmaf(p.beta1, m[i], p.one_minus_beta1 * gi);
-        v[i] = fmaf(p.beta2, v[i], p.one_minus_beta2 * gi * gi);
-        const float root = sqrtf(v[i]);
-        w[i] = fmaf(s.decay, w[i], -s.size * __fdividef(m[i], fmaf(root, s.root, p.eps)));
+        m[i] = fmaf(p.beta1, m[i], to_m * g[i]);
+        v[i] = fmaf(p.beta2, v[i], to_v * g[i] * g[i]);
+        float root;
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[i]));
+        float inverse;                                       // (root <= 2^64 and eps >= 2^-126: far inside the range)
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaf(root, s.root, p.eps)));
+        x[i] = fmaf(s.decay, x[i], -s.size * m[i] * inverse);
         if (STATE8) v[i] = root;
-        random[i] = STOCHASTIC ? adam_random(e.place + at + i, s.key) : 0u;
+        random[i] = STOCHASTIC ? adam_random(e.place + adam_place<W>(at, i), s.key) : 0u;
     }
     if (STATE8) {
-        adam_store8<N, STOCHASTIC, false>(m, random, e.m, e.m_scale, at, n);
-        adam_store8<N, STOCHASTIC, true>(v, random, e.v, e.v_scale, at, n);
+        adam_store8<W, STOCHASTIC, false>(m, random, e.m, e.m_scale, at, n);
+        adam_store8<W, STOCHASTIC, true>(v, random, e.v, e.v_scale, at, n);
     } else {
-        adam_store(m, e.m, true, at, n);
-        adam_store(v, e.v, true, at, n);
+        adam_store<W>(m, e.m, true, at, n);
+        adam_store<W>(v, e.v, true, at, n);
     }
-    if (e.master) adam_store(w, e.master, true, at, n);
+    if (e.master) adam_store<W>(x, e.master, true, at, n);
     if (STOCHASTIC && !e.master && !p32) {
+        float top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (fabsf(w[i]) <= 3.402823466e38f) w[i] = __uint_as_float((__float_as_uint(w[i]) + (adam_mix(random[i]) & 0xffffu)) & 0xffff0000u);
+        for (int i = 0; i < ADAM_N; ++i) top = max_or_nan(top, fabsf(x[i]));
+        const bool all = finite(top);
+#pragma unroll
+        for (int i = 0; i < ADAM_N; ++i)
+            if (all || finite(x[i])) x[i] = __uint_as_float((__float_as_uint(x[i]) + (adam_mix(random[i]) & 0xffffu)) & 0xffff0000u);
     }
-    adam_store(w, e.param, p32, at, n);
+    adam_store<W>(x, e.param, p32, at, n);
 }
 
-template <int CAP, bool STATE8, bool STOCHASTIC>
-__global__ void __launch_bounds__(ADAM_THREADS) adam_kernel(const __grid_constant__ AdamList<CAP> l, const __grid_constant__ AdamParams p,
+// CTAs that an SM holds, and the grid has for it: with more of them than it holds, a second wave of a few would have the chip to itself.
+constexpr int adam_ctas_per_sm(int w, bool state8) { return state8 ? (w == 4 ? 3 : 2) : 4; }
+template <int CAP, int W, bool STATE8, bool STOCHASTIC>
+__global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) adam_kernel(const __grid_constant__ AdamList<CAP> l, const __grid_constant__ AdamParams p,
                                                             const AdamStep given) {
     __shared__ AdamStep from_device;
     const int tid = threadIdx.x;
@@ -275,36 +319,25 @@ __global__ void __launch_bounds__(ADAM_THREADS) adam_kernel(const __grid_constan
         at = lo;
         const AdamEntry& e = l.e[lo];
         const long long base = static_cast<long long>(c - e.first) * ADAM_CHUNK;
-        if (e.flags & ADAM_VECTORS) {
+        // a trip of a CTA is eight elements of every thread
 #pragma unroll 1
-            for (int i = 0; i < ADAM_CHUNK; i += 8 * ADAM_THREADS) {
-                if (base + i >= e.n) break;
-                adam_elements<8, STATE8, STOCHASTIC>(e, base + i + 8 * tid, p, s, clip);
-            }
-        } else {
-            // Tensors that lie at odd addresses: an element per lane, a block of 32 per warp.
-#pragma unroll 4
-            for (int i = 0; i < ADAM_CHUNK; i += ADAM_THREADS) {
-                if (base + i >= e.n) break;
-                adam_elements<1, STATE8, STOCHASTIC>(e, base + i + tid, p, s, clip);
-            }
-        }
+        for (int i = 0; i < ADAM_CHUNK && base + i < e.n; i += ADAM_N * ADAM_THREADS)
+            adam_elements<W, STATE8, STOCHASTIC>(e, base + i + W * tid, p, s, clip);
     }
 }
 
-template <bool STATE8, bool STOCHASTIC>
+template <int W, bool STATE8, bool STOCHASTIC>
 static cudaError_t launch_adam_list(const AdamList<ADAM_CAP>& l, const AdamParams& p, const AdamStep& s, cudaStream_t stream) {
-    const dim3 ctas(std::min<unsigned>(l.chunks, ADAM_CTAS));
-    if (l.n > ADAM_CAP_SMALL) return launch_pdl(adam_kernel<ADAM_CAP, STATE8, STOCHASTIC>, ctas, ADAM_THREADS, 0, stream, 1, l, p, s);
+    const dim3 ctas(std::min<unsigned>(l.chunks, static_cast<unsigned>(p.sm_count * adam_ctas_per_sm(W, STATE8))));
+    if (l.n > ADAM_CAP_SMALL) return launch_pdl(adam_kernel<ADAM_CAP, W, STATE8, STOCHASTIC>, ctas, ADAM_THREADS, 0, stream, 1, l, p, s);
     AdamList<ADAM_CAP_SMALL> few;
     std::copy(l.e, l.e + l.n, few.e);
     few.n = l.n;
     few.chunks = l.chunks;
-    return launch_pdl(adam_kernel<ADAM_CAP_SMALL, STATE8, STOCHASTIC>, ctas, ADAM_THREADS, 0, stream, 1, few, p, s);
+    return launch_pdl(adam_kernel<ADAM_CAP_SMALL, W, STATE8, STOCHASTIC>, ctas, ADAM_THREADS, 0, stream, 1, few, p, s);
 }
-
-cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, cudaStream_t stream) {
-    const AdamStep s = adam_step(p, p.lr, p.step);
+template <int W>
+static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, const AdamStep& s, cudaStream_t stream) {
     long long place = 0;
     for (int at = 0; at < t.n;) {
         AdamList<ADAM_CAP> l;
@@ -313,7 +346,7 @@ cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8,
         for (; at < t.n && l.n < ADAM_CAP; ++at) {
             const long long n = t.numel[at];
             if (n == 0) continue;
-            AdamEntry& e = l.e[l.n++];
+            AdamEntry e;
             e.grad = t.grads[at];
             e.param = t.params[at];
             e.master = t.master ? t.master[at] : nullptr;
@@ -325,19 +358,28 @@ cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8,
             e.place = place;
             e.first = static_cast<unsigned>(chunks);
             e.flags = (t.param_dtypes[at] == 1 ? ADAM_PARAM_FP32 : 0) | (t.grad_dtypes[at] == 1 ? ADAM_GRAD_FP32 : 0);
+            place += n;
             auto bits = [](const void* q) { return reinterpret_cast<uintptr_t>(q); };
             const uintptr_t state = bits(e.m) | bits(e.v);
-            if (((bits(e.grad) | bits(e.param) | bits(e.master)) & 15) == 0 && (state & (state8 ? 7 : 15)) == 0) e.flags |= ADAM_VECTORS;
-            place += n;
+            const bool vectors = ((bits(e.grad) | bits(e.param) | bits(e.master)) & 15) == 0 && (state & (state8 ? 3 : 15)) == 0;
+            if (vectors != (W == 4)) continue;
+            l.e[l.n++] = e;
             chunks += (n + ADAM_CHUNK - 1) / ADAM_CHUNK;
         }
         l.chunks = static_cast<unsigned>(chunks);
         if (l.n == 0) continue;
-        const cudaError_t err = state8 ? (stochastic ? launch_adam_list<true, true>(l, p, s, stream) : launch_adam_list<true, false>(l, p, s, stream))
-                                       : (stochastic ? launch_adam_list<false, true>(l, p, s, stream) : launch_adam_list<false, false>(l, p, s, stream));
+        const cudaError_t err = state8 ? (stochastic ? launch_adam_list<W, true, true>(l, p, s, stream) : launch_adam_list<W, true, false>(l, p, s, stream))
+                                       : (stochastic ? launch_adam_list<W, false, true>(l, p, s, stream) : launch_adam_list<W, false, false>(l, p, s, stream));
         if (err != cudaSuccess) return err;
     }
     return cudaSuccess;
+}
+
+// Tensors that lie at odd addresses take launches of their own, behind the others'.
+cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, cudaStream_t stream) {
+    const AdamStep s = adam_step(p, p.lr, p.step);
+    const cudaError_t e = launch_adam_lists<4>(t, p, state8, stochastic, s, stream);
+    return e == cudaSuccess ? launch_adam_lists<1>(t, p, state8, stochastic, s, stream) : e;
 }
 
 bool adamw_ranges_overlap(const AdamTensors& t, const AdamParams& p, bool state8, bool* no_memory) {

@@ -1095,7 +1095,8 @@ tik_status tik_adamw(tik_ctx* ctx, void* const* params, const int* param_dtypes,
     const bool state8 = state_dtype == TIK_DTYPE_E4M3;
     if (!(lr >= 0.0) || !std::isfinite(static_cast<float>(lr))) return fail(ctx, TIK_ERR_INVALID_ARG, "lr must be finite and >= 0");
     if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(ctx, TIK_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
-    if (!(static_cast<float>(eps) > 0.0f) || !std::isfinite(static_cast<float>(eps))) return fail(ctx, TIK_ERR_INVALID_ARG, "eps must be finite and > 0");
+    if (!(static_cast<float>(eps) >= 1.17549435e-38f) || !std::isfinite(static_cast<float>(eps)))
+        return fail(ctx, TIK_ERR_INVALID_ARG, "eps must be finite and at least 2^-126");
     if (!(weight_decay >= 0.0) || !std::isfinite(static_cast<float>(weight_decay)))
         return fail(ctx, TIK_ERR_INVALID_ARG, "weight_decay must be finite and >= 0");
     if (step < 1 && !step_device) return fail(ctx, TIK_ERR_INVALID_ARG, "step must be >= 1");
@@ -1137,6 +1138,7 @@ tik_status tik_adamw(tik_ctx* ctx, void* const* params, const int* param_dtypes,
     p.one_minus_beta2 = static_cast<float>(1.0 - beta2);
     p.eps = static_cast<float>(eps);
     p.seed = seed;
+    p.sm_count = ctx->sm_count;
     bool no_memory = false;
     if (adamw_ranges_overlap(t, p, state8, &no_memory))
         return fail(ctx, TIK_ERR_INVALID_ARG, no_memory ? "out of host memory" : "tensors to be written overlap");
