@@ -14,7 +14,7 @@
 // below, from 16 bits of a hash of the element's place, the seed and the step), and so are bf16 weights without a master copy.
 //
 // HBM-bound: 12 bytes of bf16 weights, gradient and 8-bit moments to 28 with a master copy.  The list travels as a kernel parameter;
-// chunks of 8192 elements on as many CTAs as the SMs hold.
+// a ring of bulk copies in each of as many CTAs as the SMs hold keeps 150 KB and more an SM on their way.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -27,7 +27,6 @@
 namespace tik {
 
 constexpr int ADAM_THREADS = 256;
-constexpr int ADAM_CHUNK = 8192;
 constexpr int ADAM_BLOCK = 32;                               // elements that share a scale
 
 struct AdamEntry {
@@ -38,7 +37,7 @@ struct AdamEntry {
     uint8_t *m_scale, *v_scale;
     long long n;
     long long place;             // of the first element among all of the call's
-    unsigned first;              // chunk of the launch with which the tensor begins
+    unsigned first;              // trip of the launch with which the tensor begins
     int flags;
 };
 constexpr int ADAM_PARAM_FP32 = 1, ADAM_GRAD_FP32 = 2;
@@ -46,7 +45,7 @@ template <int CAP>
 struct AdamList {
     AdamEntry e[CAP];
     int n;
-    unsigned chunks;
+    unsigned trips;
 };
 constexpr int ADAM_CAP_SMALL = 32, ADAM_CAP = 400;           // (parameters may take 32764 bytes)
 
@@ -80,18 +79,20 @@ constexpr int ADAM_N = 8;
 template <int W>
 __device__ __forceinline__ long long adam_place(long long at, int i) { return at + i % W + (i / W) * (W * ADAM_THREADS); }
 
-// What lies at or past n is 0.
-template <int W>
+// From global memory, where what lies at or past n is 0, or from a stage of the ring, which is whole.
+template <int W, bool STAGED>
 __device__ __forceinline__ void adam_load(float (&x)[ADAM_N], const void* src, bool fp32, long long at, long long n) {
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && e + W <= n) {
+        if (W == 4 && (STAGED || e + W <= n)) {
             if (fp32) {
-                const float4 a = __ldcs(reinterpret_cast<const float4*>(static_cast<const float*>(src) + e));
+                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(src) + e);
+                const float4 a = STAGED ? *p : __ldcs(p);
                 x[i] = a.x, x[i + 1 % W] = a.y, x[i + 2 % W] = a.z, x[i + 3 % W] = a.w;
             } else {
-                const uint2 a = __ldcs(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(src) + e));
+                const uint2* p = reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(src) + e);
+                const uint2 a = STAGED ? *p : __ldcs(p);
                 x[i] = __uint_as_float(a.x << 16), x[i + 1 % W] = __uint_as_float(a.x & 0xffff0000u);
                 x[i + 2 % W] = __uint_as_float(a.y << 16), x[i + 3 % W] = __uint_as_float(a.y & 0xffff0000u);
             }
@@ -99,7 +100,7 @@ __device__ __forceinline__ void adam_load(float (&x)[ADAM_N], const void* src, b
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 x[i + j] = 0.0f;
-                if (e + j < n) x[i + j] = fp32 ? static_cast<const float*>(src)[e + j] : __bfloat162float(static_cast<const __nv_bfloat16*>(src)[e + j]);
+                if (STAGED || e + j < n) x[i + j] = fp32 ? static_cast<const float*>(src)[e + j] : __bfloat162float(static_cast<const __nv_bfloat16*>(src)[e + j]);
             }
         }
     }
@@ -127,21 +128,30 @@ __device__ __forceinline__ void adam_store(const float (&x)[ADAM_N], void* dst, 
 }
 
 __device__ __forceinline__ float adam_scale_value(unsigned byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
-// Stored 8-bit values times their block's scale
+// The scales' bytes of a thread's groups
 template <int W>
-__device__ __forceinline__ void adam_load8(float (&x)[ADAM_N], const void* src, const uint8_t* scale, long long at, long long n) {
+__device__ __forceinline__ void adam_load_scales(unsigned (&byte)[ADAM_N / W], const uint8_t* scale, long long at, long long n) {
+#pragma unroll
+    for (int k = 0; k < ADAM_N / W; ++k) {
+        const long long e = adam_place<W>(at, W * k);
+        byte[k] = e < n ? scale[e / ADAM_BLOCK] : 0u;
+    }
+}
+// Stored 8-bit values times their block's scale
+template <int W, bool STAGED>
+__device__ __forceinline__ void adam_load8(float (&x)[ADAM_N], const void* src, const unsigned (&byte)[ADAM_N / W], long long at, long long n) {
     const uint8_t* q = static_cast<const uint8_t*>(src);
-    unsigned w[2] = {0u, 0u}, byte[ADAM_N / W];
+    unsigned w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        byte[i / W] = e < n ? scale[e / ADAM_BLOCK] : 0u;
-        if (W == 4 && e + W <= n) {
-            w[i / 4] = __ldcs(reinterpret_cast<const unsigned*>(q + e));
+        if (W == 4 && (STAGED || e + W <= n)) {
+            const unsigned* p = reinterpret_cast<const unsigned*>(q + e);
+            w[i / 4] = STAGED ? *p : __ldcs(p);
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                if (e + j < n) w[i / 4] |= static_cast<unsigned>(q[e + j]) << (8 * ((i + j) & 3));
+                if (STAGED || e + j < n) w[i / 4] |= static_cast<unsigned>(q[e + j]) << (8 * ((i + j) & 3));
         }
     }
 #pragma unroll
@@ -236,22 +246,42 @@ __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint
     }
 }
 
-// Eight elements of each of a warp's lanes.
-template <int W, bool STATE8, bool STOCHASTIC>
-__device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, const AdamParams& p, const AdamStep& s, float clip) {
+// Where a trip's inputs are: the tensor's own arrays, or a stage of the ring whose first elements are the trip's.
+struct AdamInputs {
+    const void *grad, *weight, *m, *v;
+};
+// Random numbers of W neighbours: the places differ in their low words alone unless those wrap.
+template <int W>
+__device__ __forceinline__ void adam_randoms(uint32_t (&random)[ADAM_N], long long place, uint32_t key) {
+#pragma unroll
+    for (int i = 0; i < ADAM_N; i += W) {
+        const long long first = adam_place<W>(place, i);
+        const uint32_t low = static_cast<uint32_t>(first), x = low * 0x632BE5ABu + key + static_cast<uint32_t>(first >> 32) * 0x85157AF5u;
+#pragma unroll
+        for (int j = 0; j < W; ++j) random[i + j] = adam_mix(x + static_cast<uint32_t>(j) * 0x632BE5ABu);
+        if (W > 1 && low > 0xffffffffu - W)
+#pragma unroll
+            for (int j = 1; j < W; ++j) random[i + j] = adam_random(first + j, key);
+    }
+}
+// Eight elements of each of a warp's lanes: at `at` of the tensor, and `in` of the inputs.
+template <int W, bool STATE8, bool STOCHASTIC, bool STAGED>
+__device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, const AdamInputs& src, long long in, const unsigned (&m_byte)[ADAM_N / W],
+                                              const unsigned (&v_byte)[ADAM_N / W], const AdamParams& p, const AdamStep& s, float clip) {
     const long long n = e.n;
     float x[ADAM_N], g[ADAM_N], m[ADAM_N], v[ADAM_N];
     const bool p32 = e.flags & ADAM_PARAM_FP32;
-    adam_load<W>(g, e.grad, e.flags & ADAM_GRAD_FP32, at, n);
+    adam_load<W, STAGED>(g, src.grad, e.flags & ADAM_GRAD_FP32, in, n);
     if (STATE8) {
-        adam_load8<W>(m, e.m, e.m_scale, at, n);
-        adam_load8<W>(v, e.v, e.v_scale, at, n);
+        adam_load8<W, STAGED>(m, src.m, m_byte, in, n);
+        adam_load8<W, STAGED>(v, src.v, v_byte, in, n);
     } else {
-        adam_load<W>(m, e.m, true, at, n);
-        adam_load<W>(v, e.v, true, at, n);
+        adam_load<W, STAGED>(m, src.m, true, in, n);
+        adam_load<W, STAGED>(v, src.v, true, in, n);
     }
-    adam_load<W>(x, e.master ? static_cast<const void*>(e.master) : e.param, e.master ? true : p32, at, n);
-    uint32_t random[ADAM_N];
+    adam_load<W, STAGED>(x, src.weight, e.master || p32, in, n);
+    uint32_t random[ADAM_N] = {};
+    if (STOCHASTIC) adam_randoms<W>(random, e.place + at, s.key);
     const float to_m = p.one_minus_beta1 * clip, to_v = p.one_minus_beta2 * clip * clip;
 #pragma unroll
     for (int i = 0; i < ADAM_N; ++i) {
@@ -264,7 +294,6 @@ __device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, 
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaf(root, s.root, p.eps)));
         x[i] = fmaf(s.decay, x[i], -s.size * m[i] * inverse);
         if (STATE8) v[i] = root;
-        random[i] = STOCHASTIC ? adam_random(e.place + adam_place<W>(at, i), s.key) : 0u;
     }
     if (STATE8) {
         adam_store8<W, STOCHASTIC, false>(m, random, e.m, e.m_scale, at, n);
@@ -286,13 +315,50 @@ __device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, 
     adam_store<W>(x, e.param, p32, at, n);
 }
 
+// A trip is ADAM_TRIP elements of one tensor, eight of every thread.  A CTA's trips come through a ring of stages that one
+// thread fills by bulk copies: loads into registers kept too few bytes in flight (466 M elements with 8-bit moments 2435 us).  Bulk
+// copies want multiples of 16 bytes: an array that lies otherwise is copied from the 16 bytes around its ends, which are the
+// tensor's own unless the trip is its first or last; those trips, and ones that are not whole, are read without a stage.
+constexpr int ADAM_TRIP = ADAM_N * ADAM_THREADS;
+constexpr int ADAM_STAGES = 8;                               // at most
+struct AdamRing {
+    int stages, stage_bytes;
+    int weight_at, m_at, v_at;                               // of a stage; the gradient is at 0
+};
+struct AdamTrip {
+    long long base;
+    int entry;                                               // -1: the CTA's last trip is over
+    int staged;
+};
+__device__ __forceinline__ unsigned adam_skew(const void* array, long long bytes) {
+    return static_cast<unsigned>((reinterpret_cast<uintptr_t>(array) + bytes) & 15u);
+}
+// Copies from byte `from` of an array, less what it lies past a multiple of 16, `all` bytes.
+__device__ __forceinline__ void adam_fetch(uint32_t dst, const void* array, long long from, unsigned all, uint32_t bar) {
+    bulk_load(dst, static_cast<const char*>(array) + from - adam_skew(array, from), static_cast<int>(all), bar);
+}
+
 // CTAs that an SM holds, and the grid has for it: with more of them than it holds, a second wave of a few would have the chip to itself.
-constexpr int adam_ctas_per_sm(int w, bool state8) { return state8 ? (w == 4 ? 3 : 2) : 4; }
+constexpr int adam_ctas_per_sm(int w, bool state8) { return state8 && w == 1 ? 2 : 3; }
 template <int CAP, int W, bool STATE8, bool STOCHASTIC>
 __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) adam_kernel(const __grid_constant__ AdamList<CAP> l, const __grid_constant__ AdamParams p,
-                                                            const AdamStep given) {
+                                                                                         const AdamStep given, const AdamRing ring) {
+    extern __shared__ __align__(128) char adam_smem[];
     __shared__ AdamStep from_device;
+    __shared__ AdamTrip trips[ADAM_STAGES];
+    __shared__ __align__(8) unsigned long long bars[ADAM_STAGES];
+    __shared__ int left[ADAM_STAGES];                        // warps that are done with a stage's trip
+    __shared__ int abort_word;
     const int tid = threadIdx.x;
+    const uint32_t full = smem_u32(bars), stage0 = smem_u32(adam_smem);
+    if (tid == 0) {
+        for (int i = 0; i < ring.stages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            left[i] = 0;
+        }
+        fence_barrier_init();
+        abort_word = 0;
+    }
     pdl_wait();
     pdl_launch_dependents();
     float clip = 1.0f;
@@ -301,40 +367,121 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
         if (!(norm <= 3.402823466e38f)) return;
         if (norm > p.max_norm) clip = __fdiv_rn(p.max_norm, norm);
     }
-    AdamStep s = given;
-    if (p.lr_device || p.step_device) {
-        if (tid == 0) from_device = adam_step(p, p.lr_device ? static_cast<double>(*p.lr_device) : p.lr, p.step_device ? *p.step_device : p.step);
-        __syncthreads();
-        s = from_device;
-    }
-    int at = 0;                                              // tensor of the CTA's last chunk
-    for (unsigned c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-        int lo = l.e[at].first <= c ? at : 0, hi = l.n;      // the last tensor with first <= c
-        if (lo + 1 < hi && l.e[lo + 1].first > c) hi = lo + 1;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (l.e[mid].first <= c) lo = mid;
-            else hi = mid;
+    if ((p.lr_device || p.step_device) && tid == 0)
+        from_device = adam_step(p, p.lr_device ? static_cast<double>(*p.lr_device) : p.lr, p.step_device ? *p.step_device : p.step);
+    __syncthreads();
+    const AdamStep s = p.lr_device || p.step_device ? from_device : given;
+
+    auto fill = [&](int i, int entry) {                      // trip i of this CTA; entry: tensor of an earlier one
+        const int stage = i % ring.stages;
+        const unsigned c = blockIdx.x + static_cast<unsigned>(i) * gridDim.x;
+        const uint32_t bar = full + 8 * stage;
+        AdamTrip t = {0, -1, 0};
+        if (c < l.trips) {
+            int lo = entry, hi = l.n;                        // the last tensor with first <= c
+            if (lo + 1 < hi && l.e[lo + 1].first > c) hi = lo + 1;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (l.e[mid].first <= c) lo = mid;
+                else hi = mid;
+            }
+            const AdamEntry& e = l.e[lo];
+            t.entry = lo;
+            t.base = static_cast<long long>(c - e.first) * ADAM_TRIP;
+            t.staged = W == 4 ? t.base + ADAM_TRIP <= e.n : t.base > 0 && t.base + ADAM_TRIP + 16 <= e.n;
         }
-        at = lo;
-        const AdamEntry& e = l.e[lo];
-        const long long base = static_cast<long long>(c - e.first) * ADAM_CHUNK;
-        // a trip of a CTA is eight elements of every thread
-#pragma unroll 1
-        for (int i = 0; i < ADAM_CHUNK && base + i < e.n; i += ADAM_N * ADAM_THREADS)
-            adam_elements<W, STATE8, STOCHASTIC>(e, base + i + W * tid, p, s, clip);
+        trips[stage] = t;
+        if (!t.staged) {
+            mbar_arrive(bar);
+            return;
+        }
+        const AdamEntry& e = l.e[t.entry];
+        const uint32_t dst = stage0 + stage * ring.stage_bytes;
+        const int g = e.flags & ADAM_GRAD_FP32 ? 4 : 2, w = e.master || (e.flags & ADAM_PARAM_FP32) ? 4 : 2, st = STATE8 ? 1 : 4;
+        const void* weight = e.master ? static_cast<const void*>(e.master) : e.param;
+        auto size = [&](const void* a, int k) { return (adam_skew(a, t.base * k) + static_cast<unsigned>(ADAM_TRIP * k) + 15u) & ~15u; };
+        mbar_expect_tx(bar, size(e.grad, g) + size(weight, w) + size(e.m, st) + size(e.v, st));
+        adam_fetch(dst, e.grad, t.base * g, size(e.grad, g), bar);
+        adam_fetch(dst + ring.weight_at, weight, t.base * w, size(weight, w), bar);
+        adam_fetch(dst + ring.m_at, e.m, t.base * st, size(e.m, st), bar);
+        adam_fetch(dst + ring.v_at, e.v, t.base * st, size(e.v, st), bar);
+    };
+    if (tid == 0)
+        for (int i = 0; i < ring.stages; ++i) fill(i, 0);
+
+    for (int i = 0;; ++i) {
+        const int stage = i % ring.stages, use = i / ring.stages;
+        mbar_wait(full + 8 * stage, use & 1, &abort_word, p.dev_status);
+        if (*static_cast<volatile int*>(&abort_word)) break;
+        const AdamTrip t = trips[stage];
+        if (t.entry < 0) break;
+        const AdamEntry& e = l.e[t.entry];
+        const long long at = t.base + W * tid;
+        unsigned m_byte[ADAM_N / W] = {}, v_byte[ADAM_N / W] = {};
+        if (STATE8) {
+            adam_load_scales<W>(m_byte, e.m_scale, at, e.n);
+            adam_load_scales<W>(v_byte, e.v_scale, at, e.n);
+        }
+        if (t.staged) {
+            const char* src = adam_smem + stage * ring.stage_bytes;
+            const int g = e.flags & ADAM_GRAD_FP32 ? 4 : 2, w = e.master || (e.flags & ADAM_PARAM_FP32) ? 4 : 2, st = STATE8 ? 1 : 4;
+            const void* weight = e.master ? static_cast<const void*>(e.master) : e.param;
+            const AdamInputs in = W == 4 ? AdamInputs{src, src + ring.weight_at, src + ring.m_at, src + ring.v_at}
+                                         : AdamInputs{src + adam_skew(e.grad, t.base * g), src + ring.weight_at + adam_skew(weight, t.base * w),
+                                                      src + ring.m_at + adam_skew(e.m, t.base * st), src + ring.v_at + adam_skew(e.v, t.base * st)};
+            adam_elements<W, STATE8, STOCHASTIC, true>(e, at, in, W * tid, m_byte, v_byte, p, s, clip);
+        } else {
+            adam_elements<W, STATE8, STOCHASTIC, false>(e, at, {e.grad, e.master ? static_cast<const void*>(e.master) : e.param, e.m, e.v}, at, m_byte, v_byte, p, s, clip);
+        }
+        // the last warp to leave a stage fills it again
+        __syncwarp();
+        if ((tid & 31) == 0) {
+            __threadfence_block();
+            if (atomicAdd(&left[stage], 1) == ADAM_THREADS / 32 - 1) {
+                left[stage] = 0;
+                __threadfence_block();
+                fill(i + ring.stages, t.entry);
+            }
+        }
+        __syncwarp();
     }
 }
 
 template <int W, bool STATE8, bool STOCHASTIC>
 static cudaError_t launch_adam_list(const AdamList<ADAM_CAP>& l, const AdamParams& p, const AdamStep& s, cudaStream_t stream) {
-    const dim3 ctas(std::min<unsigned>(l.chunks, static_cast<unsigned>(p.sm_count * adam_ctas_per_sm(W, STATE8))));
-    if (l.n > ADAM_CAP_SMALL) return launch_pdl(adam_kernel<ADAM_CAP, W, STATE8, STOCHASTIC>, ctas, ADAM_THREADS, 0, stream, 1, l, p, s);
+    // a stage has room for the list's widest tensors; as many stages as an SM's shared memory has room for
+    constexpr int per_sm = adam_ctas_per_sm(W, STATE8), most = 216 * 1024 / per_sm;
+    int grad = 2, weight = 2;
+    for (int i = 0; i < l.n; ++i) {
+        if (l.e[i].flags & ADAM_GRAD_FP32) grad = 4;
+        if (l.e[i].master || (l.e[i].flags & ADAM_PARAM_FP32)) weight = 4;
+    }
+    auto room = [](int size) { return ADAM_TRIP * size + (W == 4 ? 0 : 128); };
+    AdamRing ring;
+    ring.weight_at = room(grad);
+    ring.m_at = ring.weight_at + room(weight);
+    ring.v_at = ring.m_at + room(STATE8 ? 1 : 4);
+    ring.stage_bytes = ring.v_at + room(STATE8 ? 1 : 4);
+    const int trips = static_cast<int>(std::min<unsigned>(l.trips, 1u << 20));
+    ring.stages = std::min(std::min(ADAM_STAGES, most / ring.stage_bytes), 1 + (trips + p.sm_count * per_sm - 1) / (p.sm_count * per_sm));
+    const dim3 ctas(std::min<unsigned>(l.trips, static_cast<unsigned>(p.sm_count * per_sm)));
+    const size_t smem = static_cast<size_t>(ring.stages) * ring.stage_bytes;
+    auto allow = [&](const void* kern, DeviceOnce& once) {
+        return once.run([&]() { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most); });
+    };
+    static DeviceOnce many, some;
+    if (l.n > ADAM_CAP_SMALL) {
+        auto kern = adam_kernel<ADAM_CAP, W, STATE8, STOCHASTIC>;
+        const cudaError_t e = allow(reinterpret_cast<const void*>(kern), many);
+        return e == cudaSuccess ? launch_pdl(kern, ctas, ADAM_THREADS, smem, stream, 1, l, p, s, ring) : e;
+    }
     AdamList<ADAM_CAP_SMALL> few;
     std::copy(l.e, l.e + l.n, few.e);
     few.n = l.n;
-    few.chunks = l.chunks;
-    return launch_pdl(adam_kernel<ADAM_CAP_SMALL, W, STATE8, STOCHASTIC>, ctas, ADAM_THREADS, 0, stream, 1, few, p, s);
+    few.trips = l.trips;
+    auto kern = adam_kernel<ADAM_CAP_SMALL, W, STATE8, STOCHASTIC>;
+    const cudaError_t e = allow(reinterpret_cast<const void*>(kern), some);
+    return e == cudaSuccess ? launch_pdl(kern, ctas, ADAM_THREADS, smem, stream, 1, few, p, s, ring) : e;
 }
 template <int W>
 static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, const AdamStep& s, cudaStream_t stream) {
@@ -342,7 +489,7 @@ static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, 
     for (int at = 0; at < t.n;) {
         AdamList<ADAM_CAP> l;
         l.n = 0;
-        long long chunks = 0;
+        long long trips = 0;
         for (; at < t.n && l.n < ADAM_CAP; ++at) {
             const long long n = t.numel[at];
             if (n == 0) continue;
@@ -356,17 +503,17 @@ static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, 
             e.v_scale = state8 ? t.v_scale[at] : nullptr;
             e.n = n;
             e.place = place;
-            e.first = static_cast<unsigned>(chunks);
+            e.first = static_cast<unsigned>(trips);
             e.flags = (t.param_dtypes[at] == 1 ? ADAM_PARAM_FP32 : 0) | (t.grad_dtypes[at] == 1 ? ADAM_GRAD_FP32 : 0);
             place += n;
             auto bits = [](const void* q) { return reinterpret_cast<uintptr_t>(q); };
             const uintptr_t state = bits(e.m) | bits(e.v);
-            const bool vectors = ((bits(e.grad) | bits(e.param) | bits(e.master)) & 15) == 0 && (state & (state8 ? 3 : 15)) == 0;
+            const bool vectors = ((bits(e.grad) | bits(e.param) | bits(e.master)) & 15) == 0 && (state & 15) == 0;
             if (vectors != (W == 4)) continue;
             l.e[l.n++] = e;
-            chunks += (n + ADAM_CHUNK - 1) / ADAM_CHUNK;
+            trips += (n + ADAM_TRIP - 1) / ADAM_TRIP;
         }
-        l.chunks = static_cast<unsigned>(chunks);
+        l.trips = static_cast<unsigned>(trips);
         if (l.n == 0) continue;
         const cudaError_t err = state8 ? (stochastic ? launch_adam_list<W, true, true>(l, p, s, stream) : launch_adam_list<W, true, false>(l, p, s, stream))
                                        : (stochastic ? launch_adam_list<W, false, true>(l, p, s, stream) : launch_adam_list<W, false, false>(l, p, s, stream));

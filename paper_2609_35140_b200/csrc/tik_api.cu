@@ -1139,6 +1139,7 @@ tik_status tik_adamw(tik_ctx* ctx, void* const* params, const int* param_dtypes,
     p.eps = static_cast<float>(eps);
     p.seed = seed;
     p.sm_count = ctx->sm_count;
+    p.dev_status = ctx->dev_status;
     bool no_memory = false;
     if (adamw_ranges_overlap(t, p, state8, &no_memory))
         return fail(ctx, TIK_ERR_INVALID_ARG, no_memory ? "out of host memory" : "tensors to be written overlap");

@@ -274,6 +274,7 @@ struct AdamParams {
     float beta1, beta2, one_minus_beta1, one_minus_beta2, eps;
     unsigned seed;
     int sm_count;
+    int* dev_status;
 };
 cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, cudaStream_t stream);
 // whether a range that the step writes meets another of its ranges (or no memory)
