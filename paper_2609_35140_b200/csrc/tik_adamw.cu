@@ -105,12 +105,12 @@ __device__ __forceinline__ void adam_load(float (&x)[ADAM_N], const void* src, b
         }
     }
 }
-template <int W>
+template <int W, bool WHOLE>
 __device__ __forceinline__ void adam_store(const float (&x)[ADAM_N], void* dst, bool fp32, long long at, long long n) {
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && e + W <= n) {
+        if (W == 4 && (WHOLE || e + W <= n)) {
             if (fp32)
                 __stcs(reinterpret_cast<float4*>(static_cast<float*>(dst) + e), make_float4(x[i], x[i + 1 % W], x[i + 2 % W], x[i + 3 % W]));
             else
@@ -119,7 +119,7 @@ __device__ __forceinline__ void adam_store(const float (&x)[ADAM_N], void* dst, 
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                if (e + j < n) {
+                if (WHOLE || e + j < n) {
                     if (fp32) static_cast<float*>(dst)[e + j] = x[i + j];
                     else static_cast<__nv_bfloat16*>(dst)[e + j] = __float2bfloat16_rn(x[i + j]);
                 }
@@ -127,15 +127,31 @@ __device__ __forceinline__ void adam_store(const float (&x)[ADAM_N], void* dst, 
     }
 }
 
+// The upper halves of fp32 values as bf16
+template <int W, bool WHOLE>
+__device__ __forceinline__ void adam_store_upper(const float (&x)[ADAM_N], void* dst, long long at, long long n) {
+#pragma unroll
+    for (int i = 0; i < ADAM_N; i += W) {
+        const long long e = adam_place<W>(at, i);
+        if (W == 4 && (WHOLE || e + W <= n)) {
+            auto pair = [](float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); };
+            __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(dst) + e), make_uint2(pair(x[i], x[i + 1 % W]), pair(x[i + 2 % W], x[i + 3 % W])));
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (WHOLE || e + j < n) static_cast<unsigned short*>(dst)[e + j] = static_cast<unsigned short>(__float_as_uint(x[i + j]) >> 16);
+        }
+    }
+}
+
 __device__ __forceinline__ float adam_scale_value(unsigned byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
 // The scales' bytes of a thread's groups
-template <int W>
+template <int W, bool WHOLE>
 __device__ __forceinline__ void adam_load_scales(unsigned (&byte)[ADAM_N / W], const uint8_t* scale, long long at, long long n) {
+    const uint8_t* p = scale + (at >> 5);
 #pragma unroll
-    for (int k = 0; k < ADAM_N / W; ++k) {
-        const long long e = adam_place<W>(at, W * k);
-        byte[k] = e < n ? scale[e / ADAM_BLOCK] : 0u;
-    }
+    for (int k = 0; k < ADAM_N / W; ++k)                     // (a group of every thread is ADAM_THREADS W elements)
+        byte[k] = WHOLE || adam_place<W>(at, W * k) < n ? p[k * (ADAM_THREADS * W / ADAM_BLOCK)] : 0u;
 }
 // Stored 8-bit values times their block's scale
 template <int W, bool STAGED>
@@ -158,8 +174,7 @@ __device__ __forceinline__ void adam_load8(float (&x)[ADAM_N], const void* src, 
     for (int i = 0; i < ADAM_N; i += 2) {
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[i / 4] >> (8 * (i & 2))), __NV_E4M3);
         const float2 f = __half22float2(__half2(h));
-        x[i] = f.x * adam_scale_value(byte[i / W]);
-        x[i + 1] = f.y * adam_scale_value(byte[(i + 1) / W]);
+        f2_get(f2_mul(f2(f.x, f.y), f2(adam_scale_value(byte[i / W]), adam_scale_value(byte[(i + 1) / W]))), x[i], x[i + 1]);
     }
 }
 __device__ __forceinline__ float max_or_nan(float a, float b) {
@@ -181,20 +196,24 @@ __device__ __forceinline__ float adam_round_e4m3(float y, unsigned random16) {
     const float t = floorf(__fadd_rn(fabsf(y) * per_place, static_cast<float>(random16) * 0x1p-16f));
     return copysignf(t * place, y);
 }
+// Whether one of four e4m3 values is at most the least normal one, unless all are 0.
+__device__ __forceinline__ bool adam_small(unsigned w) {
+    return ((((w & 0x7f7f7f7fu) | 0x80808080u) - 0x09090909u) & 0x80808080u) != 0x80808080u && w != 0u;
+}
 // Stores values and, from each block's first lane, its scale.  POSITIVE: the second moment's roots, of which none above 0 becomes 0.
-template <int W, bool STOCHASTIC, bool POSITIVE>
+template <int W, bool STOCHASTIC, bool POSITIVE, bool WHOLE>
 __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint32_t (&random)[ADAM_N], void* dst, uint8_t* scale, long long at,
                                             long long n) {
     unsigned byte[ADAM_N / W], w[2] = {0u, 0u};
     float y[ADAM_N];
-    bool plain = true;                                       // every value is finite, and 0 or in e4m3's normal range
+    bool rare = false;
 #pragma unroll
     for (int k = 0; k < ADAM_N / W; ++k) {
         float a = 0.0f;
 #pragma unroll
         for (int j = 0; j < W; ++j) a = max_or_nan(a, fabsf(x[W * k + j]));
         if (!finite(a)) {                                    // what is not finite does not count
-            plain = false;
+            rare = true;
             a = 0.0f;
 #pragma unroll
             for (int j = 0; j < W; ++j)
@@ -205,22 +224,24 @@ __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint
         byte[k] = adam_scale_of(a);
     }
 #pragma unroll
-    for (int i = 0; i < ADAM_N; ++i) {
-        y[i] = x[i] * __uint_as_float((254u - byte[i / W]) << 23);
-        plain = plain && (__float_as_uint(fabsf(y[i])) - 1u >= 0x3c800000u - 1u);
-    }
-    if (plain) {
+    for (int i = 0; i < ADAM_N; i += 2)
+        f2_get(f2_mul(f2(x[i], x[i + 1]), f2(__uint_as_float((254u - byte[i / W]) << 23), __uint_as_float((254u - byte[(i + 1) / W]) << 23))), y[i], y[i + 1]);
+#pragma unroll
+    for (int i = 0; i < ADAM_N; i += 2) {
+        float z[2] = {y[i], y[i + 1]};
         if (STOCHASTIC)
 #pragma unroll
-            for (int i = 0; i < ADAM_N; ++i) {
-                // 20 of 23 places are cut off: the number is added below them.  (The same as below in the normal range.)
-                const unsigned r = POSITIVE ? random[i] >> 12 & 0xffff0u : (random[i] & 0xffffu) << 4;
-                y[i] = __uint_as_float((__float_as_uint(y[i]) + r) & 0xfff00000u);
+            for (int j = 0; j < 2; ++j) {
+                // in the normal range 20 of 23 places are cut off, and the number is added below them
+                const unsigned r = POSITIVE ? random[i + j] >> 12 & 0xffff0u : (random[i + j] & 0xffffu) << 4;
+                z[j] = __uint_as_float((__float_as_uint(y[i + j]) + r) & 0xfff00000u);
             }
-#pragma unroll
-        for (int i = 0; i < ADAM_N; i += 2)
-            w[i / 4] |= static_cast<unsigned>(__nv_cvt_float2_to_fp8x2(make_float2(y[i], y[i + 1]), __NV_SATFINITE, __NV_E4M3)) << (8 * (i & 2));
-    } else {
+        w[i / 4] |= static_cast<unsigned>(__nv_cvt_float2_to_fp8x2(make_float2(z[0], z[1]), __NV_SATFINITE, __NV_E4M3)) << (8 * (i & 2));
+    }
+    // Subnormal values, whose places do not follow their exponents, and zeros that may not be: once more, one by one.
+    if (STOCHASTIC || POSITIVE) rare = rare || adam_small(w[0]) || adam_small(w[1]);
+    if (rare) {
+        w[0] = w[1] = 0u;
 #pragma unroll
         for (int i = 0; i < ADAM_N; ++i) {
             float f = y[i];
@@ -235,15 +256,19 @@ __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && e + W <= n) {
+        if (W == 4 && (WHOLE || e + W <= n)) {
             __stcs(reinterpret_cast<unsigned*>(to + e), w[i / 4]);
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                if (e + j < n) to[e + j] = static_cast<uint8_t>(w[i / 4] >> (8 * ((i + j) & 3)));
+                if (WHOLE || e + j < n) to[e + j] = static_cast<uint8_t>(w[i / 4] >> (8 * ((i + j) & 3)));
         }
-        if (e < n && e % ADAM_BLOCK == 0) scale[e / ADAM_BLOCK] = static_cast<uint8_t>(byte[i / W]);
     }
+    uint8_t* s = scale + (at >> 5);
+#pragma unroll
+    for (int k = 0; k < ADAM_N / W; ++k)                     // (trips begin at multiples of 32)
+        if ((static_cast<unsigned>(at) & (ADAM_BLOCK - 1)) == 0u && (WHOLE || adam_place<W>(at, W * k) < n))
+            s[k * (ADAM_THREADS * W / ADAM_BLOCK)] = static_cast<uint8_t>(byte[k]);
 }
 
 // Where a trip's inputs are: the tensor's own arrays, or a stage of the ring whose first elements are the trip's.
@@ -282,44 +307,56 @@ __device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, 
     adam_load<W, STAGED>(x, src.weight, e.master || p32, in, n);
     uint32_t random[ADAM_N] = {};
     if (STOCHASTIC) adam_randoms<W>(random, e.place + at, s.key);
-    const float to_m = p.one_minus_beta1 * clip, to_v = p.one_minus_beta2 * clip * clip;
+    const F2 to_m = f2(p.one_minus_beta1 * clip), to_v = f2(p.one_minus_beta2 * clip * clip), beta1 = f2(p.beta1), beta2 = f2(p.beta2);
+    const F2 decay = f2(s.decay), size = f2(-s.size), root2 = f2(s.root), eps = f2(p.eps);
 #pragma unroll
-    for (int i = 0; i < ADAM_N; ++i) {
-        if (STATE8) v[i] = v[i] * v[i];
-        m[i] = fmaf(p.beta1, m[i], to_m * g[i]);
-        v[i] = fmaf(p.beta2, v[i], to_v * g[i] * g[i]);
-        float root;
-        asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v[i]));
-        float inverse;                                       // (root <= 2^64 and eps >= 2^-126: far inside the range)
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(fmaf(root, s.root, p.eps)));
-        x[i] = fmaf(s.decay, x[i], -s.size * m[i] * inverse);
-        if (STATE8) v[i] = root;
+    for (int i = 0; i < ADAM_N; i += 2) {
+        const F2 g2 = f2(g[i], g[i + 1]), v1 = f2(v[i], v[i + 1]);
+        const F2 m2 = f2_fma(beta1, f2(m[i], m[i + 1]), f2_mul(to_m, g2));
+        const F2 v2 = f2_fma(beta2, STATE8 ? f2_mul(v1, v1) : v1, f2_mul(f2_mul(to_v, g2), g2));
+        f2_get(m2, m[i], m[i + 1]);
+        f2_get(v2, v[i], v[i + 1]);
+        float root[2], inverse[2];
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(root[0]) : "f"(v[i]));
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(root[1]) : "f"(v[i + 1]));
+        f2_get(f2_fma(f2(root[0], root[1]), root2, eps), inverse[0], inverse[1]);
+        // (root <= 2^64 and eps >= 2^-126: far inside the range)
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(inverse[0]));
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(inverse[1]));
+        f2_get(f2_fma(decay, f2(x[i], x[i + 1]), f2_mul(f2_mul(size, m2), f2(inverse[0], inverse[1]))), x[i], x[i + 1]);
+        if (STATE8) v[i] = root[0], v[i + 1] = root[1];
     }
     if (STATE8) {
-        adam_store8<W, STOCHASTIC, false>(m, random, e.m, e.m_scale, at, n);
-        adam_store8<W, STOCHASTIC, true>(v, random, e.v, e.v_scale, at, n);
+        adam_store8<W, STOCHASTIC, false, STAGED>(m, random, e.m, e.m_scale, at, n);
+        adam_store8<W, STOCHASTIC, true, STAGED>(v, random, e.v, e.v_scale, at, n);
     } else {
-        adam_store<W>(m, e.m, true, at, n);
-        adam_store<W>(v, e.v, true, at, n);
+        adam_store<W, STAGED>(m, e.m, true, at, n);
+        adam_store<W, STAGED>(v, e.v, true, at, n);
     }
-    if (e.master) adam_store<W>(x, e.master, true, at, n);
+    if (e.master) adam_store<W, STAGED>(x, e.master, true, at, n);
     if (STOCHASTIC && !e.master && !p32) {
         float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < ADAM_N; ++i) top = max_or_nan(top, fabsf(x[i]));
-        const bool all = finite(top);
+        if (finite(top)) {
+#pragma unroll
+            for (int i = 0; i < ADAM_N; ++i) x[i] = __uint_as_float(__float_as_uint(x[i]) + (adam_mix(random[i]) & 0xffffu));
+            adam_store_upper<W, STAGED>(x, e.param, at, n);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < ADAM_N; ++i)
-            if (all || finite(x[i])) x[i] = __uint_as_float((__float_as_uint(x[i]) + (adam_mix(random[i]) & 0xffffu)) & 0xffff0000u);
+            if (finite(x[i])) x[i] = __uint_as_float((__float_as_uint(x[i]) + (adam_mix(random[i]) & 0xffffu)) & 0xffff0000u);
     }
-    adam_store<W>(x, e.param, p32, at, n);
+    adam_store<W, STAGED>(x, e.param, p32, at, n);
 }
 
-// A trip is ADAM_TRIP elements of one tensor, eight of every thread.  A CTA's trips come through a ring of stages that one
+// A trip is eight elements of every thread, of one tensor, sixteen with 8-bit moments (whose stages are small).  A CTA's trips come through a ring of stages that one
 // thread fills by bulk copies: loads into registers kept too few bytes in flight (466 M elements with 8-bit moments 2435 us).  Bulk
 // copies want multiples of 16 bytes: an array that lies otherwise is copied from the 16 bytes around its ends, which are the
 // tensor's own unless the trip is its first or last; those trips, and ones that are not whole, are read without a stage.
-constexpr int ADAM_TRIP = ADAM_N * ADAM_THREADS;
+__host__ __device__ constexpr int adam_rounds(bool state8) { return state8 ? 2 : 1; }          // of eight elements of every thread
+__host__ __device__ constexpr int adam_trip(bool state8) { return ADAM_N * ADAM_THREADS * adam_rounds(state8); }
 constexpr int ADAM_STAGES = 8;                               // at most
 struct AdamRing {
     int stages, stage_bytes;
@@ -339,10 +376,11 @@ __device__ __forceinline__ void adam_fetch(uint32_t dst, const void* array, long
 }
 
 // CTAs that an SM holds, and the grid has for it: with more of them than it holds, a second wave of a few would have the chip to itself.
-constexpr int adam_ctas_per_sm(int w, bool state8) { return state8 && w == 1 ? 2 : 3; }
+constexpr int adam_ctas_per_sm(int w, bool state8) { return state8 ? (w == 1 ? 2 : 4) : 3; }
 template <int CAP, int W, bool STATE8, bool STOCHASTIC>
 __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) adam_kernel(const __grid_constant__ AdamList<CAP> l, const __grid_constant__ AdamParams p,
                                                                                          const AdamStep given, const AdamRing ring) {
+    constexpr int ROUNDS = adam_rounds(STATE8), TRIP = adam_trip(STATE8);
     extern __shared__ __align__(128) char adam_smem[];
     __shared__ AdamStep from_device;
     __shared__ AdamTrip trips[ADAM_STAGES];
@@ -387,8 +425,8 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
             }
             const AdamEntry& e = l.e[lo];
             t.entry = lo;
-            t.base = static_cast<long long>(c - e.first) * ADAM_TRIP;
-            t.staged = W == 4 ? t.base + ADAM_TRIP <= e.n : t.base > 0 && t.base + ADAM_TRIP + 16 <= e.n;
+            t.base = static_cast<long long>(c - e.first) * TRIP;
+            t.staged = W == 4 ? t.base + TRIP <= e.n : t.base > 0 && t.base + TRIP + 16 <= e.n;
         }
         trips[stage] = t;
         if (!t.staged) {
@@ -399,7 +437,7 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
         const uint32_t dst = stage0 + stage * ring.stage_bytes;
         const int g = e.flags & ADAM_GRAD_FP32 ? 4 : 2, w = e.master || (e.flags & ADAM_PARAM_FP32) ? 4 : 2, st = STATE8 ? 1 : 4;
         const void* weight = e.master ? static_cast<const void*>(e.master) : e.param;
-        auto size = [&](const void* a, int k) { return (adam_skew(a, t.base * k) + static_cast<unsigned>(ADAM_TRIP * k) + 15u) & ~15u; };
+        auto size = [&](const void* a, int k) { return (adam_skew(a, t.base * k) + static_cast<unsigned>(TRIP * k) + 15u) & ~15u; };
         mbar_expect_tx(bar, size(e.grad, g) + size(weight, w) + size(e.m, st) + size(e.v, st));
         adam_fetch(dst, e.grad, t.base * g, size(e.grad, g), bar);
         adam_fetch(dst + ring.weight_at, weight, t.base * w, size(weight, w), bar);
@@ -417,21 +455,34 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
         if (t.entry < 0) break;
         const AdamEntry& e = l.e[t.entry];
         const long long at = t.base + W * tid;
-        unsigned m_byte[ADAM_N / W] = {}, v_byte[ADAM_N / W] = {};
-        if (STATE8) {
-            adam_load_scales<W>(m_byte, e.m_scale, at, e.n);
-            adam_load_scales<W>(v_byte, e.v_scale, at, e.n);
-        }
+        constexpr int ROUND = ADAM_N * ADAM_THREADS;
+        unsigned m_byte[ROUNDS][ADAM_N / W] = {}, v_byte[ROUNDS][ADAM_N / W] = {};
         if (t.staged) {
+            if (STATE8)
+#pragma unroll
+                for (int r = 0; r < ROUNDS; ++r) {
+                    adam_load_scales<W, true>(m_byte[r], e.m_scale, at + r * ROUND, e.n);
+                    adam_load_scales<W, true>(v_byte[r], e.v_scale, at + r * ROUND, e.n);
+                }
             const char* src = adam_smem + stage * ring.stage_bytes;
             const int g = e.flags & ADAM_GRAD_FP32 ? 4 : 2, w = e.master || (e.flags & ADAM_PARAM_FP32) ? 4 : 2, st = STATE8 ? 1 : 4;
             const void* weight = e.master ? static_cast<const void*>(e.master) : e.param;
             const AdamInputs in = W == 4 ? AdamInputs{src, src + ring.weight_at, src + ring.m_at, src + ring.v_at}
                                          : AdamInputs{src + adam_skew(e.grad, t.base * g), src + ring.weight_at + adam_skew(weight, t.base * w),
                                                       src + ring.m_at + adam_skew(e.m, t.base * st), src + ring.v_at + adam_skew(e.v, t.base * st)};
-            adam_elements<W, STATE8, STOCHASTIC, true>(e, at, in, W * tid, m_byte, v_byte, p, s, clip);
+#pragma unroll
+            for (int r = 0; r < ROUNDS; ++r)
+                adam_elements<W, STATE8, STOCHASTIC, true>(e, at + r * ROUND, in, r * ROUND + W * tid, m_byte[r], v_byte[r], p, s, clip);
         } else {
-            adam_elements<W, STATE8, STOCHASTIC, false>(e, at, {e.grad, e.master ? static_cast<const void*>(e.master) : e.param, e.m, e.v}, at, m_byte, v_byte, p, s, clip);
+            const AdamInputs in = {e.grad, e.master ? static_cast<const void*>(e.master) : e.param, e.m, e.v};
+#pragma unroll 1
+            for (int r = 0; r < ROUNDS; ++r) {
+                if (STATE8) {
+                    adam_load_scales<W, false>(m_byte[0], e.m_scale, at + r * ROUND, e.n);
+                    adam_load_scales<W, false>(v_byte[0], e.v_scale, at + r * ROUND, e.n);
+                }
+                adam_elements<W, STATE8, STOCHASTIC, false>(e, at + r * ROUND, in, at + r * ROUND, m_byte[0], v_byte[0], p, s, clip);
+            }
         }
         // the last warp to leave a stage fills it again
         __syncwarp();
@@ -449,25 +500,28 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
 
 template <int W, bool STATE8, bool STOCHASTIC>
 static cudaError_t launch_adam_list(const AdamList<ADAM_CAP>& l, const AdamParams& p, const AdamStep& s, cudaStream_t stream) {
-    // a stage has room for the list's widest tensors; as many stages as an SM's shared memory has room for
-    constexpr int per_sm = adam_ctas_per_sm(W, STATE8), most = 216 * 1024 / per_sm;
+    // A stage has room for the list's widest tensors, and a CTA for as many stages as its share of the SM's shared memory takes, two at
+    // least: a CTA less an SM where the stages are wide (8-bit moments beside a master copy 1515 -> 1417 us).
     int grad = 2, weight = 2;
     for (int i = 0; i < l.n; ++i) {
         if (l.e[i].flags & ADAM_GRAD_FP32) grad = 4;
         if (l.e[i].master || (l.e[i].flags & ADAM_PARAM_FP32)) weight = 4;
     }
-    auto room = [](int size) { return ADAM_TRIP * size + (W == 4 ? 0 : 128); };
+    auto room = [](int size) { return adam_trip(STATE8) * size + (W == 4 ? 0 : 128); };
     AdamRing ring;
     ring.weight_at = room(grad);
     ring.m_at = ring.weight_at + room(weight);
     ring.v_at = ring.m_at + room(STATE8 ? 1 : 4);
     ring.stage_bytes = ring.v_at + room(STATE8 ? 1 : 4);
-    const int trips = static_cast<int>(std::min<unsigned>(l.trips, 1u << 20));
+    constexpr int shared = 216 * 1024;
+    int per_sm = adam_ctas_per_sm(W, STATE8);
+    while (per_sm > 1 && shared / per_sm < 2 * ring.stage_bytes) --per_sm;
+    const int most = shared / per_sm, trips = static_cast<int>(std::min<unsigned>(l.trips, 1u << 20));
     ring.stages = std::min(std::min(ADAM_STAGES, most / ring.stage_bytes), 1 + (trips + p.sm_count * per_sm - 1) / (p.sm_count * per_sm));
     const dim3 ctas(std::min<unsigned>(l.trips, static_cast<unsigned>(p.sm_count * per_sm)));
     const size_t smem = static_cast<size_t>(ring.stages) * ring.stage_bytes;
     auto allow = [&](const void* kern, DeviceOnce& once) {
-        return once.run([&]() { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most); });
+        return once.run([&]() { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, shared); });
     };
     static DeviceOnce many, some;
     if (l.n > ADAM_CAP_SMALL) {
@@ -511,7 +565,7 @@ static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, 
             const bool vectors = ((bits(e.grad) | bits(e.param) | bits(e.master)) & 15) == 0 && (state & 15) == 0;
             if (vectors != (W == 4)) continue;
             l.e[l.n++] = e;
-            trips += (n + ADAM_TRIP - 1) / ADAM_TRIP;
+            trips += (n + adam_trip(state8) - 1) / adam_trip(state8);
         }
         l.trips = static_cast<unsigned>(trips);
         if (l.n == 0) continue;
