@@ -270,8 +270,7 @@ size_t tik_workspace_bytes(int op, int64_t rows_or_batch, int Hq, int Hkv, int d
     if (op == TIK_OP_GRAD_NORM) return rows_or_batch > 0 ? grad_norm_bytes(rows_or_batch) : 0;
     if (op == TIK_OP_TOKEN_LOGPROB_BWD) {
         if (rows_or_batch <= 0 || rows_or_batch >= (1ll << 31) - 256 || H <= 0 || V <= 0 || V > (1 << 30)) return 0;
-        const LogprobBwdPlan g = logprob_bwd_plan(rows_or_batch, H, V);
-        return g.dz_bytes + g.sum_bytes + g.part_bytes;
+        return logprob_bwd_plan(rows_or_batch, H, V).bytes;
     }
     if (op == TIK_OP_POLICY_LOSS) return policy_loss_bytes(max_ctx > 0 ? max_ctx : 0);
     return 0;
@@ -672,13 +671,16 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     if (!d_logprob || !hidden || !lm_head || !target_ids || !lse) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
     if (T >= (1ll << 31) - 256) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31 - 256");
     const LogprobBwdPlan g = logprob_bwd_plan(T, H, V);
-    const size_t need = g.dz_bytes + g.sum_bytes + g.part_bytes;
-    if (!ws || ws_bytes < need) return fail(ctx, TIK_ERR_WORKSPACE, "log-prob gradient workspace too small");
+    if (!ws || ws_bytes < g.bytes) return fail(ctx, TIK_ERR_WORKSPACE, "log-prob gradient workspace too small");
 
+    char* const at = static_cast<char*>(ws);
+    void* const dz = at;
+    auto words = [&](size_t offset) { return g.gather ? reinterpret_cast<const int32_t*>(at + offset) : nullptr; };
     LogprobBwdParams p{};
     p.target = target_ids;
     p.lse = lse;
     p.d_logprob = d_logprob;
+    p.head = static_cast<const __nv_bfloat16*>(lm_head);
     p.T = T;
     p.H = H;
     p.V = V;
@@ -686,36 +688,36 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     p.d_hidden = static_cast<__nv_bfloat16*>(d_hidden);
     p.want_table = d_lm_head != nullptr;
     p.table_fp32 = lm_head_dtype == TIK_DTYPE_FP32;
-    p.sm_count = ctx->sm_count;
     p.dev_status = ctx->dev_status;
-    char* at = static_cast<char*>(ws);
-    void* dz = at;
-    p.sum = reinterpret_cast<float*>(at + g.dz_bytes);
-    p.part = reinterpret_cast<float*>(at + g.dz_bytes + g.sum_bytes);
+    p.sum = reinterpret_cast<float*>(at + g.sum_at);
+    p.part = reinterpret_cast<float*>(at + g.part_at);
+    p.rho = reinterpret_cast<float*>(at + g.rho_at);
+    p.count = words(g.count_at);
+    p.index = words(g.index_at);
+    p.place = words(g.place_at);
+    p.row_target = g.gather ? words(g.target_at) : target_ids;
+    const void* const rows_of = g.gather ? at + g.rows_at : hidden;          // the products' hidden rows
+    p.rows = static_cast<const __nv_bfloat16*>(rows_of);
 
     const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.chunk);
     const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, uT}, rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2};
     const uint32_t rows[2] = {64, 128}, slab[2] = {64, 64}, rows4[2] = {32, 128};    // K-major operands and bf16 output, MN-major, fp32 output
     LogprobBwdMaps m;
     std::string err;
-    bool ok = make_tmap_bf16(ctx, &m.hidden_k, hidden, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
-              make_tmap_bf16(ctx, &m.hidden_mn, hidden, 2, xd, rowH, slab, &err) && make_tmap_bf16(ctx, &m.head_mn, lm_head, 2, wd, rowH, slab, &err) &&
+    bool ok = make_tmap_bf16(ctx, &m.hidden_k, rows_of, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
+              make_tmap_bf16(ctx, &m.hidden_mn, rows_of, 2, xd, rowH, slab, &err) && make_tmap_bf16(ctx, &m.head_mn, lm_head, 2, wd, rowH, slab, &err) &&
               make_tmap_bf16(ctx, &m.dz_out, dz, 2, zd, rowZ, rows, &err) && make_tmap_bf16(ctx, &m.dz_mn, dz, 2, zd, rowZ, slab, &err);
     if (ok && d_lm_head)
         ok = p.table_fp32 ? make_tmap_f32(ctx, &m.table_out, d_lm_head, 2, wd, rowH4, rows4, &err)
                           : make_tmap_bf16(ctx, &m.table_out, d_lm_head, 2, wd, rowH, rows, &err);
     if (ok && d_hidden) {
-        const uint64_t tiles = ((uT + 255) / 256) * ((uH + 255) / 256);
-        const uint64_t parts = (tiles - static_cast<uint64_t>(g.whole)) * g.split;
-        const uint64_t pd[2] = {256, parts * 256}, rowP[1] = {1024};
-        // (a call has whole tiles, split ones, or both; the map of what it has not is not used)
-        if (g.whole > 0) ok = make_tmap_f32(ctx, &m.sum_out, p.sum, 2, xd, rowH4, rows4, &err);
-        if (ok && parts > 0) ok = make_tmap_f32(ctx, &m.part_out, p.part, 2, pd, rowP, rows4, &err);
-        if (g.whole == 0) m.sum_out = m.part_out;
-        if (parts == 0) m.part_out = m.sum_out;
+        const uint64_t pd[2] = {256, static_cast<uint64_t>(g.parts) * 256}, rowP[1] = {1024};
+        ok = make_tmap_f32(ctx, &m.part_out, p.part, 2, pd, rowP, rows4, &err);
+        m.sum_out = m.part_out;                            // (not used by a call of fewer tiles than pairs)
+        if (ok && g.part_at > g.sum_at) ok = make_tmap_f32(ctx, &m.sum_out, p.sum, 2, xd, rowH4, rows4, &err);
     }
     if (!ok) return fail(ctx, TIK_ERR_CUDA, err.c_str());
-    cudaError_t e = launch_logprob_bwd(m, p, g, accumulate != 0, st);
+    cudaError_t e = launch_logprob_bwd(m, p, g, hidden, accumulate != 0, ctx->sm_count, st);
     return e == cudaSuccess ? TIK_OK : cuda_fail(ctx, e, "tik_token_logprob_bwd");
 }
 

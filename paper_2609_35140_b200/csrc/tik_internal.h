@@ -200,32 +200,40 @@ struct LogprobBwdParams {
     const int32_t* target;       // [T]
     const float* lse;            // [T], natural log, from the forward
     const float* d_logprob;      // [T]
+    const __nv_bfloat16* head;   // [V][H]
     int64_t T;
     int H, V;
     float inv_temperature;
     __nv_bfloat16* d_hidden;     // [T][H] or null
     int want_table, table_fp32;
-    float* sum;                  // scratch [T][H]: d_hidden's whole tiles
-    float* part;                 // scratch [parts][split tiles][256][256]
-    int sm_count;
+    int pairs;                   // CTA pairs that a launch has at most
     int* dev_status;
+    // Scratch.  With `count` (more than one row tile) the rows of the products are the tokens that take part, else all.
+    float* sum;                  // [T][H]: d_hidden's whole tiles
+    float* part;                 // [parts][256][256]: the split ones'
+    float* rho;                  // [row]: what d_z lost of the target's term in rounding
+    const int32_t* count;        // their number, or null
+    const int32_t* index;        // [row]: token, or null
+    const int32_t* row_target;   // [row]
+    const int32_t* place;        // [T]: row or -1, or null
+    const __nv_bfloat16* rows;   // [row][H]: their hidden rows
     // of one launch
     int v0, nv;                  // the vocabulary's columns of this chunk
-    int ldz;                     // columns of d_z
-    int row_tiles, col_tiles, nunit;     // 256 x 256 tiles, units
-    int whole, split;            // gradient of the hidden rows: tiles done whole, parts of the others
+    int ldz;                     // columns of d_z, those of a whole chunk
     int add;                     // the output is added to
 };
 struct LogprobBwdPlan {
     int chunks, chunk;           // of the vocabulary, columns of one (a multiple of 256)
-    int whole, split;
-    size_t dz_bytes, sum_bytes, part_bytes;
+    int parts;                   // of split tiles at most
+    bool gather;
+    size_t sum_at, part_at, rho_at, index_at, target_at, place_at, count_at, rows_at, bytes;     // scratch; d_z at 0
 };
 struct LogprobBwdMaps {
     alignas(64) CUtensorMap hidden_k, head_k, hidden_mn, head_mn, dz_out, dz_mn, table_out, sum_out, part_out;
 };
 LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V);
-cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, bool add_table, cudaStream_t stream);
+cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, const void* hidden, bool add_table, int sm_count,
+                               cudaStream_t stream);
 
 // Policy loss (tik_loss.cu).
 constexpr int LOSS_SUM = 0, LOSS_TOKEN_MEAN = 1, LOSS_SEQUENCE_MEAN = 2;

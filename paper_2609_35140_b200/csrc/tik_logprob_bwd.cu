@@ -4,11 +4,14 @@
 //   d_hidden[t]  = sum_v d_z[t][v] lm_head[v],      d_lm_head[v] = sum_t d_z[t][v] hidden[t]
 // Three matrix products of 2 T V H operations each, which is what bounds a call of more than some hundred rows: the logits
 // are computed again (they were never stored), d_z leaves that product's epilogue as bf16 [T][columns of a chunk], and both
-// gradients are products with it.  d_z is the one rounding on the way: every term of a gradient is off by 2^-9 of itself at
-// most, rounded independently, which is less in a sum of them than the sum's own rounding to bf16 at the end.  Sums
-// are fp32 in tensor memory.
+// gradients are products with it.  d_z is the one rounding on the way: every term of a gradient is off by 2^-8 of itself at
+// most, rounded independently.  The target's term is mostly the largest by far, and its rounding would be one error for a whole row, so
+// what it lost is kept (rho [T], fp32) and added to both gradients in fp32 before they are rounded.  Sums are fp32 in tensor memory.
 //
-// One kernel for all three (KIND), persistent CTA pairs that walk units of one 256 x 256 output tile each: a TMA warp streams
+// Tokens without a gradient (d_logprob 0: prompts, padding) take no part.  In calls of more than one row tile the others' rows are
+// gathered first, and everything after goes by their number, which stays on the device: the persistent grids read it.
+//
+// One kernel for all three products (KIND), persistent CTA pairs that walk units of one 256 x 256 output tile each: a TMA warp streams
 // 64-wide slices of the contracted axis through a ring, an MMA warp issues M256 x N256 x K16 MMAs into one of two
 // accumulators, four epilogue warps take the other one out through shared memory and tiled TMA stores.  An operand whose
 // contracted axis is not its contiguous one is read as it lies (MN-major descriptors): nothing is transposed.
@@ -37,6 +40,9 @@ constexpr uint32_t BYTES = OFF_BAR + 256;
 constexpr uint32_t ALLOC = BYTES + 1024;
 constexpr int BAND = 16;                     // DZ: pairs of token tiles whose hidden rows stay in L2 while lm_head streams by
 constexpr int THREADS = 192;                 // warp 0 TMA, warp 1 MMA, warps 2..5 epilogue
+constexpr int HITS = 32;                     // TABLE: targets that a warp's list holds
+constexpr int PAIRS = 74;                    // CTA pairs of a B200, by which HIDDEN's tiles are cut on any device
+constexpr int MOST_PARTS = 4 * PAIRS;        // HIDDEN: split tiles' parts, four rounds
 }  // namespace lpb
 
 // Adds a staged fp32 tile to global memory (bulk async group).
@@ -72,43 +78,110 @@ __device__ __forceinline__ void lpb_take_tensor_memory(volatile uint32_t* slot) 
     tmem_relinquish_pair();
 }
 
+// What a launch has to do, by the number of rows that take part.
+struct LpbShape {
+    int rows;                    // tokens
+    int row_tiles, col_tiles, units;
+    int slices;                  // of 64 of the contracted axis
+    int whole, split;            // HIDDEN: tiles done whole, parts of each of the others
+};
+// The tiles of the last round of pairs, split so that the round costs least in slices, a unit's epilogue and first loads counting as six.
+__device__ __forceinline__ int lpb_split(int rest, int slices, int least_slices) {
+    int best = 1, best_cost = slices + 6;
+    for (int s = 2; s <= least_slices && rest * s <= lpb::MOST_PARTS && s <= 64; ++s) {
+        const int cost = (rest * s + lpb::PAIRS - 1) / lpb::PAIRS * ((slices + s - 1) / s + 6);
+        if (cost < best_cost) best = s, best_cost = cost;
+    }
+    return best;
+}
+template <int KIND>
+__device__ __forceinline__ LpbShape lpb_shape(const LogprobBwdParams& p) {
+    using namespace lpb;
+    LpbShape g;
+    g.rows = p.count ? __ldcg(p.count) : static_cast<int>(p.T);
+    const int tokens = (g.rows + TILE - 1) / TILE, words = (p.nv + TILE - 1) / TILE, channels = (p.H + TILE - 1) / TILE;
+    g.row_tiles = KIND == TABLE ? words : tokens;
+    g.col_tiles = KIND == DZ ? words : channels;
+    g.units = g.row_tiles * g.col_tiles;
+    g.slices = KIND == DZ ? p.H / 64 : KIND == TABLE ? (g.rows + 63) / 64 : (p.nv + 63) / 64;
+    g.whole = g.units;
+    g.split = 1;
+    if (KIND == HIDDEN && g.units > 0) {
+        // by the sizes of a whole chunk and of the last one, so that all chunks' parts are the same
+        const int rest = g.units % PAIRS, most = (min(p.ldz, p.V) + 63) / 64, least = (p.V - (p.V - 1) / p.ldz * p.ldz + 63) / 64;
+        g.whole = g.units - rest;
+        g.split = rest ? lpb_split(rest, most, least) : 1;
+        g.units = g.whole + rest * g.split;
+    }
+    return g;
+}
+
 struct LpbUnit {
     int row, col;                // of the output tile
     int k0, k1;                  // slices of 64 of the contracted axis
     int slot;                    // HIDDEN: part of a split tile (its place in the parts' buffer), -1: a whole tile
 };
 template <int KIND>
-__device__ __forceinline__ LpbUnit lpb_unit(const LogprobBwdParams& p, int u) {
+__device__ __forceinline__ LpbUnit lpb_unit(const LpbShape& g, int u) {
     using namespace lpb;
     LpbUnit x;
     x.slot = -1;
     x.k0 = 0;
+    x.k1 = g.slices;
     if (KIND == DZ) {
         // token tiles fastest inside a band, so that the pairs at work share a few steps of lm_head
-        const int per_band = BAND * p.col_tiles, band = u / per_band, rem = u - band * per_band;
-        const int tiles = min(BAND, p.row_tiles - band * BAND);
+        const int per_band = BAND * g.col_tiles, band = u / per_band, rem = u - band * per_band;
+        const int tiles = min(BAND, g.row_tiles - band * BAND);
         x.row = (band * BAND + rem % tiles) * TILE;
         x.col = rem / tiles * TILE;
-        x.k1 = p.H / 64;
-    } else if (KIND == TABLE) {
-        x.row = u / p.col_tiles * TILE;
-        x.col = u % p.col_tiles * TILE;
-        x.k1 = static_cast<int>((p.T + 63) / 64);
     } else {
-        const int slices = (p.nv + 63) / 64;
         int tile = u;
-        x.k1 = slices;
-        if (u >= p.whole) {
-            const int rest = p.row_tiles * p.col_tiles - p.whole, q = u - p.whole, part = q / rest;
-            tile = p.whole + q % rest;
-            x.k0 = static_cast<int>(static_cast<long long>(slices) * part / p.split);
-            x.k1 = static_cast<int>(static_cast<long long>(slices) * (part + 1) / p.split);
+        if (KIND == HIDDEN && u >= g.whole) {
+            const int rest = g.row_tiles * g.col_tiles - g.whole, q = u - g.whole, part = q / rest;
+            tile = g.whole + q % rest;
+            x.k0 = static_cast<int>(static_cast<long long>(g.slices) * part / g.split);
+            x.k1 = static_cast<int>(static_cast<long long>(g.slices) * (part + 1) / g.split);
             x.slot = q;
         }
-        x.row = tile / p.col_tiles * TILE;
-        x.col = tile % p.col_tiles * TILE;
+        x.row = tile / g.col_tiles * TILE;
+        x.col = tile % g.col_tiles * TILE;
     }
     return x;
+}
+
+// TABLE: calls f(token, row) for the tokens whose target is one of a warp's 32 rows from `first` on, in ascending order; whole warp.
+template <class F>
+__device__ __forceinline__ void lpb_targets(const int32_t* target, int tokens, int first, int lane, F&& f) {
+    for (int t0 = 0; t0 < tokens; t0 += 128) {
+        unsigned row[4], any = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = t0 + 32 * j + lane;
+            row[j] = t < tokens ? static_cast<unsigned>(target[t] - first) : 32u;
+            any |= row[j] < 32u;
+        }
+        if (!__any_sync(0xffffffffu, any)) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            for (unsigned hit = __ballot_sync(0xffffffffu, row[j] < 32u); hit; hit &= hit - 1) {
+                const int src = __ffs(hit) - 1;
+                f(t0 + 32 * j + src, static_cast<int>(__shfl_sync(0xffffffffu, row[j], src)));
+            }
+    }
+}
+// v += a * N bf16 from x on (N a multiple of 8)
+template <int N>
+__device__ __forceinline__ void lpb_add_row(uint32_t (&v)[N], float a, const __nv_bfloat16* x) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+        const uint4 q = *reinterpret_cast<const uint4*>(x + i);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[i + 2 * j] = __float_as_uint(fmaf(a, __uint_as_float(w[j] << 16), __uint_as_float(v[i + 2 * j])));
+            v[i + 2 * j + 1] = __float_as_uint(fmaf(a, __uint_as_float(w[j] & 0xffff0000u), __uint_as_float(v[i + 2 * j + 1])));
+        }
+    }
 }
 
 template <int KIND>
@@ -121,6 +194,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
     const uint32_t rank = cluster_ctarank();     // 0 = the CTA that issues the pair's MMAs
     const int first = static_cast<int>(blockIdx.x >> 1), stride = static_cast<int>(gridDim.x >> 1);
+    __shared__ LpbShape shape;
+    __shared__ int2 hits[KIND == TABLE ? 4 : 1][KIND == TABLE ? HITS : 1];
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -151,13 +226,17 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     }
     if (warp == 1) lpb_take_tensor_memory(tmem_slot);
     pdl_wait();
-    if (tid == 0) *abort_word = (*reinterpret_cast<volatile int*>(p.dev_status) & TIK_DEV_WAIT_EXPIRED) ? 1 : 0;
+    if (tid == 0) {
+        *abort_word = (*reinterpret_cast<volatile int*>(p.dev_status) & TIK_DEV_WAIT_EXPIRED) ? 1 : 0;
+        shape = lpb_shape<KIND>(p);
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();            // the peer's barriers exist before anything signals them
     tc_fence_after();
     pdl_launch_dependents();
     const uint32_t tmem = *tmem_slot;
+    const LpbShape g = shape;
     const uint32_t lead_full = mapa_cluster(bar_full, 0);
     const uint32_t lead_acc_empty = mapa_cluster(bar_acc_empty, 0);
     const uint32_t peer_empty = mapa_cluster(bar_empty, 1);
@@ -168,8 +247,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         // ------------------------------------------------------------ TMA producer
         if (lane == 0) {
             uint32_t it = 0;
-            for (int u = first; u < p.nunit; u += stride) {
-                const LpbUnit x = lpb_unit<KIND>(p, u);
+            for (int u = first; u < g.units; u += stride) {
+                const LpbUnit x = lpb_unit<KIND>(g, u);
                 // each CTA stages its own 128 rows of A and its half of B; what lies outside the tensors arrives as zeros
                 const int a0 = x.row + half, b0 = x.col + half;
                 for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
@@ -199,8 +278,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         if (rank == 0) {
             const uint32_t tmem_u = warp_uniform(tmem);
             uint32_t it = 0, acc = 0;
-            for (int u = first; u < p.nunit; u += stride, ++acc) {
-                const LpbUnit x = lpb_unit<KIND>(p, u);
+            for (int u = first; u < g.units; u += stride, ++acc) {
+                const LpbUnit x = lpb_unit<KIND>(g, u);
                 const int buf = acc & 1;
                 const uint32_t use = acc >> 1;
                 if (use > 0) mbar_wait_warp(bar_acc_empty + 8 * buf, (use - 1) & 1, abort_word, p.dev_status);
@@ -234,24 +313,47 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             named_bar_sync(1, 128);
             return smem + OFF_STG + (piece & 1) * STG_BYTES;
         };
-        for (int u = first; u < p.nunit; u += stride, ++acc) {
-            const LpbUnit x = lpb_unit<KIND>(p, u);
+        for (int u = first; u < g.units; u += stride, ++acc) {
+            const LpbUnit x = lpb_unit<KIND>(g, u);
             const int buf = acc & 1, row0 = x.row + half;
             float c = 0.0f, lse2 = 0.0f;
             int target = -1;
             if (KIND == DZ) {
-                const long long t = static_cast<long long>(row0) + row;
-                if (t < p.T) {
+                if (row0 + row < g.rows) {
+                    const int t = p.index ? p.index[row0 + row] : row0 + row;
                     target = p.target[t];
                     c = __fmul_rn(p.d_logprob[t], p.inv_temperature);
                     lse2 = __fmul_rn(p.lse[t], LOG2E_F);
-                    if (target < 0 || target >= p.V) {     // no gradient
+                    if (c != 0.0f && (target < 0 || target >= p.V)) {      // no gradient
                         c = 0.0f;
                         atomicOr(p.dev_status, TIK_DEV_BAD_TARGET);
                     }
                     target -= p.v0 + x.col;                // column of this tile
                 }
             }
+            int nhits = 0;                                 // tokens whose targets are this warp's rows
+            const int first_row = p.v0 + row0 + quarter * 32;
+            if (KIND == TABLE) {
+                lpb_targets(p.row_target, g.rows, first_row, lane, [&](int t, int r) {
+                    if (nhits < HITS && lane == 0) hits[quarter][nhits] = make_int2(t, r);
+                    ++nhits;
+                    // its hidden row's part comes to L1 while the accumulator is being filled
+                    if (lane < 4 && x.col + 64 * lane < p.H)
+                        asm volatile("prefetch.global.L1 [%0];" ::"l"(p.rows + static_cast<long long>(t) * p.H + x.col + 64 * lane));
+                });
+                __syncwarp();
+            }
+            // what the targets' terms lost in rounding, added to columns col .. of the rows that they belong to
+            auto add_lost = [&](auto& v, int col) {
+                auto one = [&](int t, int r) {
+                    if (lane == r) lpb_add_row(v, p.rho[t], p.rows + static_cast<long long>(t) * p.H + col);
+                };
+                if (nhits <= HITS)
+                    for (int i = 0; i < nhits; ++i) one(hits[quarter][i].x, hits[quarter][i].y);
+                else
+                    lpb_targets(p.row_target, g.rows, first_row, lane, one);
+                __syncwarp();
+            };
             mbar_wait(bar_acc_full + 8 * buf, (acc >> 1) & 1, abort_word, p.dev_status);
             tc_fence_after();
             const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TILE;
@@ -266,16 +368,24 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     tmem_ld32(taddr + 64 * q, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
                     tmem_ld32(taddr + 64 * q + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
                     tmem_wait_ld();
+                    if (KIND == TABLE && x.k1 == 0) {      // no token takes part: the accumulator was not written
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) v[i] = 0u;
+                    }
+                    if (KIND == TABLE && nhits > 0) add_lost(v, x.col + 64 * q);
                     if (KIND == DZ) {
                         const int valid = p.nv - x.col - 64 * q, hit = target - 64 * q;
+                        float at_hit = 0.0f;
 #pragma unroll
                         for (int i = 0; i < 64; ++i) {
                             const float e = ex2_ftz(__fmaf_rn(__uint_as_float(v[i]), scale2, -lse2));
                             float d = __fmul_rn(c, (i == hit ? 1.0f : 0.0f) - e);
                             // a masked row has no gradient whatever its logits are; columns past the vocabulary are read by HIDDEN
                             if (c == 0.0f || i >= valid) d = 0.0f;
+                            if (i == hit) at_hit = d;
                             v[i] = __float_as_uint(d);
                         }
+                        if (hit >= 0 && hit < 64) p.rho[row0 + row] = __fsub_rn(at_hit, __bfloat162float(__float2bfloat16_rn(at_hit)));
                     }
                     uint8_t* stg = stage();
 #pragma unroll
@@ -301,6 +411,11 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     uint32_t v[32];
                     tmem_ld32(taddr + 32 * q, v);
                     tmem_wait_ld();
+                    if (KIND == TABLE && x.k1 == 0) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0u;
+                    }
+                    if (KIND == TABLE && nhits > 0) add_lost(v, x.col + 32 * q);
                     uint8_t* stg = stage();
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16)
@@ -336,69 +451,154 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     if (warp == 1) tmem_dealloc_pair(tmem, LPB_TMEM_COLS);
 }
 
-// d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order.  Thread per eight channels.
-__global__ void __launch_bounds__(256) lpb_fold_kernel(const LogprobBwdParams p, int parts) {
+// d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order, and what the target's term lost.  Zeros
+// for tokens that took no part.  Thread per eight channels.
+__global__ void __launch_bounds__(256) lpb_fold_kernel(const LogprobBwdParams p) {
+    __shared__ LpbShape shape;
     pdl_wait();
     pdl_launch_dependents();
-    const int per_row = p.H / 8, rest = p.row_tiles * p.col_tiles - p.whole;
+    if (threadIdx.x == 0) shape = lpb_shape<lpb::HIDDEN>(p);
+    __syncthreads();
+    const LpbShape g = shape;
+    const int per_row = p.H / 8, rest = g.row_tiles * g.col_tiles - g.whole;
     const long long n = p.T * per_row;
     for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<long long>(gridDim.x) * 256) {
-        const long long t = i / per_row;
-        const int h = static_cast<int>(i - t * per_row) * 8;
-        const int tile = static_cast<int>(t / lpb::TILE) * p.col_tiles + h / lpb::TILE;
-        float f[8];
-        if (tile < p.whole) {
-            const float4* src = reinterpret_cast<const float4*>(p.sum + t * p.H + h);
-            const float4 a = src[0], b = src[1];
-            f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-        } else {
-            const float4* src = reinterpret_cast<const float4*>(
-                p.part + (static_cast<long long>(tile - p.whole) * lpb::TILE + t % lpb::TILE) * lpb::TILE + h % lpb::TILE);
-            const long long next = static_cast<long long>(rest) * lpb::TILE * lpb::TILE / 4;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = 0.0f;
+        const long long row = i / per_row;
+        const int h = static_cast<int>(i - row * per_row) * 8, t = p.place ? p.place[row] : static_cast<int>(row);
+        uint32_t f[8] = {};
+        if (t >= 0) {
+            const int tile = t / lpb::TILE * g.col_tiles + h / lpb::TILE;
+            if (tile < g.whole) {
+                const uint4* src = reinterpret_cast<const uint4*>(p.sum + static_cast<long long>(t) * p.H + h);
+                const uint4 a = src[0], b = src[1];
+                f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+            } else {
+                const float4* src = reinterpret_cast<const float4*>(
+                    p.part + (static_cast<long long>(tile - g.whole) * lpb::TILE + t % lpb::TILE) * lpb::TILE + h % lpb::TILE);
+                const long long next = static_cast<long long>(rest) * lpb::TILE * lpb::TILE / 4;
+                float s[8] = {};
 #pragma unroll 4
-            for (int s = 0; s < parts; ++s, src += next) {
-                const float4 a = src[0], b = src[1];
-                f[0] += a.x, f[1] += a.y, f[2] += a.z, f[3] += a.w, f[4] += b.x, f[5] += b.y, f[6] += b.z, f[7] += b.w;
+                for (int k = 0; k < g.split; ++k, src += next) {
+                    const float4 a = src[0], b = src[1];
+                    s[0] += a.x, s[1] += a.y, s[2] += a.z, s[3] += a.w, s[4] += b.x, s[5] += b.y, s[6] += b.z, s[7] += b.w;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = __float_as_uint(s[j]);
             }
+            const int target = p.row_target[t];
+            if (target >= 0 && target < p.V) lpb_add_row(f, p.rho[t], p.head + static_cast<long long>(target) * p.H + h);
         }
-        *reinterpret_cast<uint4*>(p.d_hidden + t * p.H + h) =
-            make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+        const float* v = reinterpret_cast<const float*>(f);
+        *reinterpret_cast<uint4*>(p.d_hidden + row * p.H + h) =
+            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
     }
 }
 
-// How a call of T rows is cut: columns of a vocabulary chunk, and for HIDDEN the tiles that are done whole, the others' parts.
-//
-// Chunks: as few as keep d_z within 2 GiB (whole vocabularies up to 7000 rows at V 152 064), of equal size.
-// Parts: the tiles of the last round of pairs (74 on a B200), split so that the round costs least in slices, a unit's
-// epilogue and first loads counting as six.
+// The tokens that take part, in order: index [rows] of theirs, their targets, and place [T], -1 for the others; the count.  One CTA:
+// 4096 tokens a step (1.1 us), which is little beside what a step's products take.
+constexpr int LPB_LIST_THREADS = 1024;
+__global__ void __launch_bounds__(LPB_LIST_THREADS) lpb_list_kernel(const LogprobBwdParams p, int32_t* index, int32_t* target, int32_t* place,
+                                                                    int32_t* count) {
+    __shared__ int sums[LPB_LIST_THREADS / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    pdl_wait();
+    pdl_launch_dependents();
+    int total = 0;
+    bool bad = false;
+    for (long long base = 0; base < p.T; base += 4 * LPB_LIST_THREADS) {
+        const long long first = base + 4 * tid;
+        int tgt[4], n = 0;
+        bool on[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            tgt[j] = -1;
+            on[j] = first + j < p.T && p.d_logprob[first + j] != 0.0f;     // (NaN takes part)
+            if (on[j]) {
+                tgt[j] = p.target[first + j];
+                if (tgt[j] < 0 || tgt[j] >= p.V) {
+                    on[j] = false;
+                    bad = true;
+                }
+            }
+            n += on[j];
+        }
+        int before = n;                                    // of this warp's lanes up to this one
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, before, off);
+            if (lane >= off) before += o;
+        }
+        if (lane == 31) sums[warp] = before;
+        __syncthreads();
+        int s = sums[lane];
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, s, off);
+            if (lane >= off) s += o;
+        }
+        int at = total + before - n + (warp ? __shfl_sync(0xffffffffu, s, warp - 1) : 0);
+        total += __shfl_sync(0xffffffffu, s, 31);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (first + j < p.T) place[first + j] = on[j] ? at : -1;
+            if (on[j]) {
+                index[at] = static_cast<int32_t>(first + j);
+                target[at++] = tgt[j];
+            }
+        }
+        __syncthreads();
+    }
+    if (bad) atomicOr(p.dev_status, TIK_DEV_BAD_TARGET);
+    if (tid == 0) *count = total;
+}
+// Their hidden rows, and zeros up to the next multiple of 64 (what TABLE multiplies d_z's zeros with).  A warp per row.
+__global__ void __launch_bounds__(256) lpb_gather_kernel(const LogprobBwdParams p, const __nv_bfloat16* hidden, __nv_bfloat16* rows) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int n = __ldcg(p.count), lane = threadIdx.x & 31, vecs = p.H / 8;
+    const long long end = min(static_cast<long long>((n + 63) / 64) * 64, static_cast<long long>(p.T));
+    for (long long r = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5); r < end; r += static_cast<long long>(gridDim.x) * 8) {
+        uint4* to = reinterpret_cast<uint4*>(rows + r * p.H);
+        if (r >= n) {
+            for (int i = lane; i < vecs; i += 32) to[i] = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        const uint4* from = reinterpret_cast<const uint4*>(hidden + static_cast<long long>(__ldcg(p.index + r)) * p.H);
+#pragma unroll 4
+        for (int i = lane; i < vecs; i += 32) to[i] = from[i];
+    }
+}
+
+// How a call of T rows is cut: columns of a vocabulary chunk, as few chunks as keep d_z within 2 GiB (whole vocabularies up to 7000
+// rows at V 152 064), of equal size; and its scratch.
 LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V) {
-    constexpr int64_t pairs = 74;
+    constexpr int64_t pairs = lpb::PAIRS;
     LogprobBwdPlan g;
     const int64_t steps = (V + 255) / 256;
     const int64_t most = std::max<int64_t>(1, (2ll << 30) / (T * 512));
     g.chunks = static_cast<int>((steps + most - 1) / most);
     g.chunk = static_cast<int>((steps + g.chunks - 1) / g.chunks * 256);
     g.chunks = (V + g.chunk - 1) / g.chunk;
+    g.gather = T > lpb::TILE;
     const int64_t tiles = (T + 255) / 256 * ((H + 255) / 256);
-    const int64_t rest = tiles % pairs;
-    const int slices = (V - (g.chunks - 1) * g.chunk + 63) / 64;          // of the last chunk, the shortest: every part has some
-    const int most_slices = (std::min(g.chunk, V) + 63) / 64;
-    g.whole = static_cast<int>(tiles - rest);
-    g.split = 1;
-    double best = -1.0;
-    for (int s = 1; rest > 0 && s <= 64 && s <= slices; ++s) {
-        const double cost = static_cast<double>((rest * s + pairs - 1) / pairs) * ((most_slices + s - 1) / s + 6);
-        if (best < 0.0 || cost < best) {
-            best = cost;
-            g.split = s;
-        }
-    }
+    g.parts = static_cast<int>(std::min<int64_t>(lpb::MOST_PARTS, std::min(tiles, pairs) * std::min<int64_t>(64, (std::min(g.chunk, V) + 63) / 64)));
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-    g.dz_bytes = up(static_cast<size_t>(T) * g.chunk * 2);
-    g.sum_bytes = g.whole > 0 ? up(static_cast<size_t>(T) * H * 4) : 0;
-    g.part_bytes = static_cast<size_t>(rest) * g.split * lpb::TILE * lpb::TILE * 4;
+    const size_t uT = static_cast<size_t>(T);
+    size_t at = up(uT * g.chunk * 2);
+    auto take = [&](size_t n) {
+        const size_t here = at;
+        at += up(n);
+        return here;
+    };
+    g.sum_at = take(tiles >= pairs ? uT * H * 4 : 0);
+    g.part_at = take(static_cast<size_t>(g.parts) * lpb::TILE * lpb::TILE * 4);
+    g.rho_at = take(uT * 4);
+    g.index_at = take(g.gather ? uT * 4 : 0);
+    g.target_at = take(g.gather ? uT * 4 : 0);
+    g.place_at = take(g.gather ? uT * 4 : 0);
+    g.count_at = take(g.gather ? 4 : 0);
+    g.rows_at = take(g.gather ? uT * H * 2 : 0);
+    g.bytes = at;
     return g;
 }
 
@@ -411,37 +611,36 @@ static cudaError_t launch_lpb(const CUtensorMap& tmA, const CUtensorMap& tmB, co
         return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lpb::ALLOC));
     });
     if (e != cudaSuccess) return e;
-    const int pairs = std::max(1, p.sm_count / 2);
-    return launch_pdl(kern, dim3(static_cast<unsigned>(2 * std::min(pairs, p.nunit))), lpb::THREADS, lpb::ALLOC, stream, 2, tmA, tmB,
+    const long long tokens = (p.T + 255) / 256, words = (p.nv + 255) / 256, channels = (p.H + 255) / 256;
+    const long long units = KIND == lpb::DZ ? tokens * words : KIND == lpb::TABLE ? words * channels : lpb::MOST_PARTS;
+    return launch_pdl(kern, dim3(static_cast<unsigned>(2 * std::min<long long>(p.pairs, units))), lpb::THREADS, lpb::ALLOC, stream, 2, tmA, tmB,
                       tmOut, tmPart, p);
 }
 
-cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, bool add_table, cudaStream_t stream) {
-    const int token_tiles = static_cast<int>((p.T + 255) / 256), h_tiles = (p.H + 255) / 256;
+cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, const void* hidden, bool add_table, int sm_count,
+                               cudaStream_t stream) {
     p.ldz = g.chunk;
-    p.whole = g.whole;
-    p.split = g.split;
+    p.pairs = std::max(1, sm_count / 2);
+    cudaError_t e = cudaSuccess;
+    if (g.gather) {
+        e = launch_pdl(lpb_list_kernel, dim3(1), LPB_LIST_THREADS, 0, stream, 1, p, const_cast<int32_t*>(p.index), const_cast<int32_t*>(p.row_target),
+                       const_cast<int32_t*>(p.place), const_cast<int32_t*>(p.count));
+        if (e != cudaSuccess) return e;
+        e = launch_pdl(lpb_gather_kernel, dim3(static_cast<unsigned>(std::min<long long>((p.T + 7) / 8, 8ll * sm_count))), 256, 0, stream, 1, p,
+                       static_cast<const __nv_bfloat16*>(hidden), const_cast<__nv_bfloat16*>(p.rows));
+        if (e != cudaSuccess) return e;
+    }
     for (int c = 0; c < g.chunks; ++c) {
         p.v0 = c * g.chunk;
         p.nv = std::min(g.chunk, p.V - p.v0);
-        const int v_tiles = (p.nv + 255) / 256;
-        p.row_tiles = token_tiles;
-        p.col_tiles = v_tiles;
-        p.nunit = token_tiles * v_tiles;
-        cudaError_t e = launch_lpb<lpb::DZ>(m.hidden_k, m.head_k, m.dz_out, m.dz_out, p, stream);
+        e = launch_lpb<lpb::DZ>(m.hidden_k, m.head_k, m.dz_out, m.dz_out, p, stream);
         if (e != cudaSuccess) return e;
         if (p.want_table) {
-            p.row_tiles = v_tiles;
-            p.col_tiles = h_tiles;
-            p.nunit = v_tiles * h_tiles;
             p.add = add_table;
             e = launch_lpb<lpb::TABLE>(m.dz_mn, m.hidden_mn, m.table_out, m.table_out, p, stream);
             if (e != cudaSuccess) return e;
         }
         if (p.d_hidden) {
-            p.row_tiles = token_tiles;
-            p.col_tiles = h_tiles;
-            p.nunit = g.whole + (token_tiles * h_tiles - g.whole) * g.split;
             p.add = c > 0;
             e = launch_lpb<lpb::HIDDEN>(m.dz_out, m.head_mn, m.sum_out, m.part_out, p, stream);
             if (e != cudaSuccess) return e;
@@ -449,8 +648,7 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
     }
     if (!p.d_hidden) return cudaSuccess;
     const long long n = p.T * (p.H / 8);
-    return launch_pdl(lpb_fold_kernel, dim3(static_cast<unsigned>(std::min<long long>((n + 255) / 256, 8ll * p.sm_count))), 256, 0, stream, 1,
-                      p, g.split);
+    return launch_pdl(lpb_fold_kernel, dim3(static_cast<unsigned>(std::min<long long>((n + 255) / 256, 8ll * sm_count))), 256, 0, stream, 1, p);
 }
 
 }  // namespace tik

@@ -114,6 +114,51 @@ def test_temperature(f):
     near(dw, b)
 
 
+@pytest.mark.parametrize("T,H,V,masked", [(257, 64, 300, 0.0), (900, 192, 1111, 0.9), (1500, 256, 700, 0.5), (4700, 1024, 513, 0.03), (513, 64, 90, 0.999)])
+def test_tokens_that_take_no_part(T, H, V, masked):
+    """More than one row tile: the others' rows are gathered, by a number that stays on the device."""
+    args = make(T, H, V, seed=21, masked=masked)
+    dh, dw = tik.tik_token_logprob_bwd(*args)
+    a, b = expected(*args)
+    near(dh, a)
+    near(dw, b)
+    assert bool((dh[args[0] == 0] == 0).all())
+
+
+@pytest.mark.parametrize("T", [200, 600])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_no_token_takes_part(T, dtype):
+    d, x, W, ids, lse, f = make(T, 192, 500, seed=22)
+    dw = torch.full((500, 192), 5.0, dtype=dtype, device="cuda")
+    dh, _ = tik.tik_token_logprob_bwd(torch.zeros_like(d), x, W, ids, torch.full_like(lse, float("nan")), f, d_lm_head=dw)
+    assert not dh.any() and not dw.any()
+    keep = torch.full((500, 192), 5.0, device="cuda")
+    tik.tik_token_logprob_bwd(torch.zeros_like(d), x, W, ids, lse, f, need_hidden=False, d_lm_head=keep, accumulate=True)
+    assert bool((keep == 5.0).all())
+
+
+@pytest.mark.parametrize("T,V", [(150, 40), (700, 3), (3000, 1000)])
+def test_targets_that_many_tokens_share(T, V):
+    """More targets among a warp's rows than its list holds."""
+    d, x, W, ids, lse, f = make(T, 128, V, seed=23)
+    ids[::2] = V - 1
+    lse = torch.logsumexp(x.double() @ W.double().T, 1).float()
+    dh, dw = tik.tik_token_logprob_bwd(d, x, W, ids, lse, f)
+    a, b = expected(d, x, W, ids, lse, f)
+    near(dh, a)
+    near(dw, b)
+
+
+def test_the_targets_rounding_is_made_good():
+    """Where the target's term is all there is (its probability near 0, the others' spread), the gradients are as near as their own rounding."""
+    T, H, V = 40, 256, 4096
+    d, x, W, ids, lse, f = make(T, H, V, seed=24, masked=0.0)
+    dh, dw = tik.tik_token_logprob_bwd(d, x, W, ids, lse, f)
+    for got, want in zip((dh, dw), expected(d, x, W, ids, lse, f)):
+        off = (got.double() - want[0]).norm() / want[0].norm()
+        assert off <= 2.0 ** -9 * 1.05                   # a rounding to bf16 is off by 2^-8 / sqrt(3) of the norm at most, by 2^-9 nearly always
+
+
 def test_one_output_alone_has_the_same_bits():
     args = make(333, 256, 1111, seed=1)
     dh, dw = tik.tik_token_logprob_bwd(*args)
@@ -142,8 +187,9 @@ def test_fp32_table_and_accumulation(T, H, V):
     assert torch.equal(d_w, one + alone)                 # one fp32 addition an element
 
 
-def test_masked_tokens_and_bad_targets():
-    d, x, W, ids, lse, f = make(300, 128, 500, seed=4)
+@pytest.mark.parametrize("T", [256, 300])
+def test_masked_tokens_and_bad_targets(T):
+    d, x, W, ids, lse, f = make(T, 128, 500, seed=4)
     clean = tik.tik_token_logprob_bwd(d, x, W, ids, lse, f)
     assert tik.device_status() == 0
     lse2 = torch.where(d == 0, float("nan"), lse)        # what masked tokens hold goes nowhere
@@ -152,9 +198,10 @@ def test_masked_tokens_and_bad_targets():
     assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
     assert bool((got[0][d == 0] == 0).all())
     bad = ids.clone()
-    bad[5], bad[77], bad[299] = -1, 500, 2 ** 31 - 1
+    bad[d == 0] = -100                                   # nobody looks at a masked token's target
+    bad[5], bad[77], bad[T - 1] = -1, 500, 2 ** 31 - 1
     d2 = d.clone()
-    d2[5] = d2[77] = d2[299] = 1.0
+    d2[5] = d2[77] = d2[T - 1] = 1.0
     got = tik.tik_token_logprob_bwd(d2, x, W, bad, lse, f)
     assert tik.device_status() == tik.DEV_BAD_TARGET and tik.device_status() == 0
     want = torch.where((bad < 0) | (bad >= 500), 0.0, d2)

@@ -97,11 +97,11 @@ def test_adamw_of_nothing(ctx, changed):
 
 def test_scratch():
     assert tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, 0, H=64, V=10) == 0
-    # d_z [5][256] bf16 and one tile's part
-    assert tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, 5, H=64, V=10) == 5 * 512 + 256 * 256 * 4
+    # d_z [5][256] bf16, one tile's part, a number per row
+    assert tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, 5, H=64, V=10) == 5 * 512 + 256 * 256 * 4 + 256
     # a chunk's d_z stays within 2 GiB
     for T, V in ((7000, 152064), (16384, 152064), (100000, 152064), (1 << 22, 151936)):
         whole = tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, T, H=256, V=V)
-        assert whole <= (2 << 30) + T * 256 * 4 + (1 << 30)
+        assert whole <= (2 << 30) + T * 256 * 6 + 16 * T + (1 << 27)
     assert tik.workspace_bytes(tik.OP_POLICY_LOSS, 100, max_ctx=7) == 16 + 592 * 5 * 8 + 592 * 4
     assert tik.workspace_bytes(tik.OP_POLICY_LOSS, 100, max_ctx=1001) == 16 + 592 * 5 * 8 + 4016
