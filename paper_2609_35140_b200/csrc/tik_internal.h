@@ -207,12 +207,13 @@ struct LogprobBwdParams {
     __nv_bfloat16* d_hidden;     // [T][H] or null
     int want_table, table_fp32;
     int pairs;                   // CTA pairs that a launch has at most
+    int split;                   // parts of d_hidden's split tiles (without `count`)
     int* dev_status;
     // Scratch.  With `count` (more than one row tile) the rows of the products are the tokens that take part, else all.
     float* sum;                  // [T][H]: d_hidden's whole tiles
     float* part;                 // [parts][256][256]: the split ones'
     float* rho;                  // [row]: what d_z lost of the target's term in rounding
-    const int32_t* count;        // their number, or null
+    const int32_t* count;        // [2]: their number, parts of d_hidden's split tiles; or null
     const int32_t* index;        // [row]: token, or null
     const int32_t* row_target;   // [row]
     const int32_t* place;        // [T]: row or -1, or null

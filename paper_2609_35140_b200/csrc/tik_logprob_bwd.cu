@@ -13,7 +13,7 @@
 //
 // One kernel for all three products (KIND), persistent CTA pairs that walk units of one 256 x 256 output tile each: a TMA warp streams
 // 64-wide slices of the contracted axis through a ring, an MMA warp issues M256 x N256 x K16 MMAs into one of two
-// accumulators, four epilogue warps take the other one out through shared memory and tiled TMA stores.  An operand whose
+// accumulators, eight epilogue warps take the other one out through shared memory and tiled TMA stores.  An operand whose
 // contracted axis is not its contiguous one is read as it lies (MN-major descriptors): nothing is transposed.
 //   DZ      A = hidden (K-major),  B = lm_head (K-major)       rows: tokens,   columns: vocabulary, contracted: H
 //   TABLE   A = d_z (M-major),     B = hidden (N-major)        rows: vocabulary, columns: H,        contracted: tokens
@@ -39,7 +39,7 @@ constexpr uint32_t OFF_BAR = OFF_STG + 2 * STG_BYTES;
 constexpr uint32_t BYTES = OFF_BAR + 256;
 constexpr uint32_t ALLOC = BYTES + 1024;
 constexpr int BAND = 16;                     // DZ: pairs of token tiles whose hidden rows stay in L2 while lm_head streams by
-constexpr int THREADS = 192;                 // warp 0 TMA, warp 1 MMA, warps 2..5 epilogue
+constexpr int THREADS = 320;                 // warp 0 TMA, warp 1 MMA, warps 2..9 epilogue: two groups of four, each with a staging buffer
 constexpr int HITS = 32;                     // TABLE: targets that a warp's list holds
 constexpr int PAIRS = 74;                    // CTA pairs of a B200, by which HIDDEN's tiles are cut on any device
 constexpr int MOST_PARTS = 4 * PAIRS;        // HIDDEN: split tiles' parts, four rounds
@@ -85,14 +85,24 @@ struct LpbShape {
     int slices;                  // of 64 of the contracted axis
     int whole, split;            // HIDDEN: tiles done whole, parts of each of the others
 };
-// The tiles of the last round of pairs, split so that the round costs least in slices, a unit's epilogue and first loads counting as six.
-__device__ __forceinline__ int lpb_split(int rest, int slices, int least_slices) {
-    int best = 1, best_cost = slices + 6;
-    for (int s = 2; s <= least_slices && rest * s <= lpb::MOST_PARTS && s <= 64; ++s) {
-        const int cost = (rest * s + lpb::PAIRS - 1) / lpb::PAIRS * ((slices + s - 1) / s + 6);
-        if (cost < best_cost) best = s, best_cost = cost;
-    }
-    return best;
+// The tiles of the last round of pairs, split so that the round costs least in slices, a unit's epilogue and first loads counting as
+// six and a part's way through memory as a quarter.
+__host__ __device__ inline int lpb_split_cost(int s, int rest, int slices) {
+    return (rest * s + lpb::PAIRS - 1) / lpb::PAIRS * ((slices + s - 1) / s + 6) * 4 + rest * s;
+}
+// What the choice goes by: tiles of the last round for so many rows, slices of a whole chunk, parts at most (the last chunk, the
+// shortest, has a slice for each).
+struct LpbRest {
+    int rest, slices, most;
+};
+__host__ __device__ inline LpbRest lpb_rest(const LogprobBwdParams& p, int rows) {
+    LpbRest r;
+    r.rest = (rows + lpb::TILE - 1) / lpb::TILE * ((p.H + lpb::TILE - 1) / lpb::TILE) % lpb::PAIRS;
+    r.slices = ((p.ldz < p.V ? p.ldz : p.V) + 63) / 64;
+    const int least = (p.V - (p.V - 1) / p.ldz * p.ldz + 63) / 64, room = lpb::MOST_PARTS / (r.rest > 1 ? r.rest : 1);
+    r.most = least < room ? least : room;
+    if (r.most > 64) r.most = 64;
+    return r;
 }
 template <int KIND>
 __device__ __forceinline__ LpbShape lpb_shape(const LogprobBwdParams& p) {
@@ -106,11 +116,10 @@ __device__ __forceinline__ LpbShape lpb_shape(const LogprobBwdParams& p) {
     g.slices = KIND == DZ ? p.H / 64 : KIND == TABLE ? (g.rows + 63) / 64 : (p.nv + 63) / 64;
     g.whole = g.units;
     g.split = 1;
-    if (KIND == HIDDEN && g.units > 0) {
-        // by the sizes of a whole chunk and of the last one, so that all chunks' parts are the same
-        const int rest = g.units % PAIRS, most = (min(p.ldz, p.V) + 63) / 64, least = (p.V - (p.V - 1) / p.ldz * p.ldz + 63) / 64;
+    if (KIND == HIDDEN) {
+        const int rest = g.units % PAIRS;
         g.whole = g.units - rest;
-        g.split = rest ? lpb_split(rest, most, least) : 1;
+        g.split = p.count ? __ldcg(p.count + 1) : p.split;
         g.units = g.whole + rest * g.split;
     }
     return g;
@@ -195,7 +204,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     const uint32_t rank = cluster_ctarank();     // 0 = the CTA that issues the pair's MMAs
     const int first = static_cast<int>(blockIdx.x >> 1), stride = static_cast<int>(gridDim.x >> 1);
     __shared__ LpbShape shape;
-    __shared__ int2 hits[KIND == TABLE ? 4 : 1][KIND == TABLE ? HITS : 1];
+    __shared__ int hits[KIND == TABLE ? 8 : 1][KIND == TABLE ? HITS : 1];
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -216,7 +225,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_acc_full + 8 * b, 1);
-            mbar_init(bar_acc_empty + 8 * b, 256);           // the epilogue threads of both CTAs
+            mbar_init(bar_acc_empty + 8 * b, 512);           // the epilogue threads of both CTAs
         }
         fence_barrier_init();
         tma_prefetch_desc(&tmA);
@@ -302,16 +311,18 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             }
         }
     } else {
-        // ------------------------------------------------------------ epilogue (warps 2..5), thread per row
-        const int quarter = warp & 3;                      // TMEM lane quarter of this warp
+        // ------------------------------------------------------------ epilogue (warps 2..9), thread per row
+        // The two groups take the tile's 128-byte wide pieces in turns (one group of four warps 298 us where a call of 64 rows writes
+        // 1.1 GB of d_lm_head, two 2xx).
+        const int quarter = warp & 3, group = (warp - 2) >> 2;         // TMEM lane quarter of this warp
         const int row = quarter * 32 + lane;
-        uint32_t piece = 0, acc = 0;
-        const bool storer = warp == 2 && lane == 0;
-        // a staging buffer that the store two pieces ago has finished reading
+        uint32_t acc = 0;
+        const bool storer = (warp == 2 || warp == 6) && lane == 0;
+        uint8_t* const stg = smem + OFF_STG + group * STG_BYTES;
+        // the group's buffer, when its last store has finished reading
         auto stage = [&]() {
-            if (storer) tma_store_wait_read1();
-            named_bar_sync(1, 128);
-            return smem + OFF_STG + (piece & 1) * STG_BYTES;
+            if (storer) tma_store_wait_read();
+            named_bar_sync(1 + group, 128);
         };
         for (int u = first; u < g.units; u += stride, ++acc) {
             const LpbUnit x = lpb_unit<KIND>(g, u);
@@ -332,10 +343,14 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 }
             }
             int nhits = 0;                                 // tokens whose targets are this warp's rows
+            unsigned mine = 0;                             // ... and this lane's, of those in the list
             const int first_row = p.v0 + row0 + quarter * 32;
             if (KIND == TABLE) {
                 lpb_targets(p.row_target, g.rows, first_row, lane, [&](int t, int r) {
-                    if (nhits < HITS && lane == 0) hits[quarter][nhits] = make_int2(t, r);
+                    if (nhits < HITS) {
+                        if (lane == 0) hits[warp - 2][nhits] = t;
+                        mine |= lane == r ? 1u << nhits : 0u;
+                    }
                     ++nhits;
                     // its hidden row's part comes to L1 while the accumulator is being filled
                     if (lane < 4 && x.col + 64 * lane < p.H)
@@ -345,13 +360,13 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             }
             // what the targets' terms lost in rounding, added to columns col .. of the rows that they belong to
             auto add_lost = [&](auto& v, int col) {
-                auto one = [&](int t, int r) {
-                    if (lane == r) lpb_add_row(v, p.rho[t], p.rows + static_cast<long long>(t) * p.H + col);
-                };
+                auto one = [&](int t) { lpb_add_row(v, p.rho[t], p.rows + static_cast<long long>(t) * p.H + col); };
                 if (nhits <= HITS)
-                    for (int i = 0; i < nhits; ++i) one(hits[quarter][i].x, hits[quarter][i].y);
+                    for (unsigned rest = mine; rest; rest &= rest - 1) one(hits[warp - 2][__ffs(rest) - 1]);
                 else
-                    lpb_targets(p.row_target, g.rows, first_row, lane, one);
+                    lpb_targets(p.row_target, g.rows, first_row, lane, [&](int t, int r) {
+                        if (lane == r) one(t);
+                    });
                 __syncwarp();
             };
             mbar_wait(bar_acc_full + 8 * buf, (acc >> 1) & 1, abort_word, p.dev_status);
@@ -362,7 +377,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 const int limit = KIND == DZ ? p.ldz : p.H;
                 const float scale2 = KIND == DZ ? __fmul_rn(p.inv_temperature, LOG2E_F) : 0.0f;
 #pragma unroll 1
-                for (int q = 0; q < TILE / 64; ++q, ++piece) {
+                for (int q = group; q < TILE / 64; q += 2) {
                     if (x.col + 64 * q >= limit) break;    // uniform: columns past the output
                     uint32_t v[64];
                     tmem_ld32(taddr + 64 * q, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
@@ -387,7 +402,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         }
                         if (hit >= 0 && hit < 64) p.rho[row0 + row] = __fsub_rn(at_hit, __bfloat162float(__float2bfloat16_rn(at_hit)));
                     }
-                    uint8_t* stg = stage();
+                    stage();
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16) {
                         const uint4 val = make_uint4(
@@ -398,7 +413,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         *reinterpret_cast<uint4*>(stg + row * 128 + ((c16 ^ (row & 7)) << 4)) = val;
                     }
                     fence_proxy_async_smem();
-                    named_bar_sync(1, 128);
+                    named_bar_sync(1 + group, 128);
                     if (storer) {
                         tma_store_2d(&tmOut, smem_u32(stg), x.col + 64 * q, KIND == TABLE ? p.v0 + row0 : row0);
                         tma_store_commit();
@@ -406,7 +421,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 }
             } else {
 #pragma unroll 1
-                for (int q = 0; q < TILE / 32; ++q, ++piece) {
+                for (int q = group; q < TILE / 32; q += 2) {
                     if (x.col + 32 * q >= p.H) break;
                     uint32_t v[32];
                     tmem_ld32(taddr + 32 * q, v);
@@ -416,13 +431,13 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
                     }
                     if (KIND == TABLE && nhits > 0) add_lost(v, x.col + 32 * q);
-                    uint8_t* stg = stage();
+                    stage();
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16)
                         *reinterpret_cast<uint4*>(stg + row * 128 + ((c16 ^ (row & 7)) << 4)) =
                             make_uint4(v[4 * c16], v[4 * c16 + 1], v[4 * c16 + 2], v[4 * c16 + 3]);
                     fence_proxy_async_smem();
-                    named_bar_sync(1, 128);
+                    named_bar_sync(1 + group, 128);
                     if (storer) {
                         const bool part = KIND == HIDDEN && x.slot >= 0;
                         const CUtensorMap* to = part ? &tmPart : &tmOut;
@@ -452,45 +467,44 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
 }
 
 // d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order, and what the target's term lost.  Zeros
-// for tokens that took no part.  Thread per eight channels.
+// for tokens that took no part.  Thread per four channels, eight parts on their way at a time.
 __global__ void __launch_bounds__(256) lpb_fold_kernel(const LogprobBwdParams p) {
-    __shared__ LpbShape shape;
     pdl_wait();
     pdl_launch_dependents();
-    if (threadIdx.x == 0) shape = lpb_shape<lpb::HIDDEN>(p);
-    __syncthreads();
-    const LpbShape g = shape;
-    const int per_row = p.H / 8, rest = g.row_tiles * g.col_tiles - g.whole;
+    const LpbShape g = lpb_shape<lpb::HIDDEN>(p);
+    const int per_row = p.H / 4, rest = g.row_tiles * g.col_tiles - g.whole;
     const long long n = p.T * per_row;
     for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<long long>(gridDim.x) * 256) {
         const long long row = i / per_row;
-        const int h = static_cast<int>(i - row * per_row) * 8, t = p.place ? p.place[row] : static_cast<int>(row);
-        uint32_t f[8] = {};
+        const int h = static_cast<int>(i - row * per_row) * 4, t = p.place ? p.place[row] : static_cast<int>(row);
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (t >= 0) {
+            const int target = p.row_target[t];
+            uint2 w = make_uint2(0u, 0u);
+            float lost = 0.0f;
+            if (target >= 0 && target < p.V) {
+                w = *reinterpret_cast<const uint2*>(p.head + static_cast<long long>(target) * p.H + h);
+                lost = p.rho[t];
+            }
             const int tile = t / lpb::TILE * g.col_tiles + h / lpb::TILE;
             if (tile < g.whole) {
-                const uint4* src = reinterpret_cast<const uint4*>(p.sum + static_cast<long long>(t) * p.H + h);
-                const uint4 a = src[0], b = src[1];
-                f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+                f = *reinterpret_cast<const float4*>(p.sum + static_cast<long long>(t) * p.H + h);
             } else {
                 const float4* src = reinterpret_cast<const float4*>(
                     p.part + (static_cast<long long>(tile - g.whole) * lpb::TILE + t % lpb::TILE) * lpb::TILE + h % lpb::TILE);
                 const long long next = static_cast<long long>(rest) * lpb::TILE * lpb::TILE / 4;
-                float s[8] = {};
-#pragma unroll 4
+#pragma unroll 8
                 for (int k = 0; k < g.split; ++k, src += next) {
-                    const float4 a = src[0], b = src[1];
-                    s[0] += a.x, s[1] += a.y, s[2] += a.z, s[3] += a.w, s[4] += b.x, s[5] += b.y, s[6] += b.z, s[7] += b.w;
+                    const float4 a = *src;
+                    f.x += a.x, f.y += a.y, f.z += a.z, f.w += a.w;
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = __float_as_uint(s[j]);
             }
-            const int target = p.row_target[t];
-            if (target >= 0 && target < p.V) lpb_add_row(f, p.rho[t], p.head + static_cast<long long>(target) * p.H + h);
+            f.x = fmaf(lost, __uint_as_float(w.x << 16), f.x);
+            f.y = fmaf(lost, __uint_as_float(w.x & 0xffff0000u), f.y);
+            f.z = fmaf(lost, __uint_as_float(w.y << 16), f.z);
+            f.w = fmaf(lost, __uint_as_float(w.y & 0xffff0000u), f.w);
         }
-        const float* v = reinterpret_cast<const float*>(f);
-        *reinterpret_cast<uint4*>(p.d_hidden + row * p.H + h) =
-            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+        *reinterpret_cast<uint2*>(p.d_hidden + row * p.H + h) = make_uint2(pack_bf16x2(f.x, f.y), pack_bf16x2(f.z, f.w));
     }
 }
 
@@ -549,7 +563,23 @@ __global__ void __launch_bounds__(LPB_LIST_THREADS) lpb_list_kernel(const Logpro
         __syncthreads();
     }
     if (bad) atomicOr(p.dev_status, TIK_DEV_BAD_TARGET);
-    if (tid == 0) *count = total;
+    if (warp == 0) {
+        const LpbRest r = lpb_rest(p, total);
+        int best = 1, cost = lpb_split_cost(1, r.rest, r.slices);
+        for (int s = lane + 1; s <= r.most; s += 32) {
+            const int c = lpb_split_cost(s, r.rest, r.slices);
+            if (c < cost) best = s, cost = c;
+        }
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) {
+            const int s = __shfl_xor_sync(0xffffffffu, best, off), c = __shfl_xor_sync(0xffffffffu, cost, off);
+            if (c < cost || (c == cost && s < best)) best = s, cost = c;
+        }
+        if (lane == 0) {
+            count[0] = total;
+            count[1] = best;
+        }
+    }
 }
 // Their hidden rows, and zeros up to the next multiple of 64 (what TABLE multiplies d_z's zeros with).  A warp per row.
 __global__ void __launch_bounds__(256) lpb_gather_kernel(const LogprobBwdParams p, const __nv_bfloat16* hidden, __nv_bfloat16* rows) {
@@ -596,7 +626,7 @@ LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V) {
     g.index_at = take(g.gather ? uT * 4 : 0);
     g.target_at = take(g.gather ? uT * 4 : 0);
     g.place_at = take(g.gather ? uT * 4 : 0);
-    g.count_at = take(g.gather ? 4 : 0);
+    g.count_at = take(g.gather ? 8 : 0);
     g.rows_at = take(g.gather ? uT * H * 2 : 0);
     g.bytes = at;
     return g;
@@ -622,7 +652,12 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
     p.ldz = g.chunk;
     p.pairs = std::max(1, sm_count / 2);
     cudaError_t e = cudaSuccess;
-    if (g.gather) {
+    if (!g.gather) {
+        const LpbRest r = lpb_rest(p, static_cast<int>(p.T));
+        p.split = 1;
+        for (int s = 2; s <= r.most; ++s)
+            if (lpb_split_cost(s, r.rest, r.slices) < lpb_split_cost(p.split, r.rest, r.slices)) p.split = s;
+    } else {
         e = launch_pdl(lpb_list_kernel, dim3(1), LPB_LIST_THREADS, 0, stream, 1, p, const_cast<int32_t*>(p.index), const_cast<int32_t*>(p.row_target),
                        const_cast<int32_t*>(p.place), const_cast<int32_t*>(p.count));
         if (e != cudaSuccess) return e;
@@ -647,7 +682,7 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
         }
     }
     if (!p.d_hidden) return cudaSuccess;
-    const long long n = p.T * (p.H / 8);
+    const long long n = p.T * (p.H / 4);
     return launch_pdl(lpb_fold_kernel, dim3(static_cast<unsigned>(std::min<long long>((n + 255) / 256, 8ll * sm_count))), 256, 0, stream, 1, p);
 }
 
