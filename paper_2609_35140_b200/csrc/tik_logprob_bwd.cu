@@ -32,14 +32,14 @@ constexpr int DZ = 0, TABLE = 1, HIDDEN = 2;
 constexpr int TILE = 256;                    // rows (of a pair) and columns of a unit
 constexpr uint32_t OP_BYTES = 128 * 128;     // an operand's share of a stage: 128 rows or columns x 64 of the contracted axis
 constexpr uint32_t STAGE_BYTES = 2 * OP_BYTES;
-constexpr int STAGES = 6;
-constexpr uint32_t STG_BYTES = 128 * 128;    // output staging: 128 rows x 128 bytes, two buffers
+constexpr int STAGES = 5;
+constexpr uint32_t STG_BYTES = 128 * 128;    // output staging: 128 rows x 128 bytes, two buffers for each group of epilogue warps
 constexpr uint32_t OFF_STG = STAGES * STAGE_BYTES;
-constexpr uint32_t OFF_BAR = OFF_STG + 2 * STG_BYTES;
+constexpr uint32_t OFF_BAR = OFF_STG + 4 * STG_BYTES;
 constexpr uint32_t BYTES = OFF_BAR + 256;
 constexpr uint32_t ALLOC = BYTES + 1024;
 constexpr int BAND = 16;                     // DZ: pairs of token tiles whose hidden rows stay in L2 while lm_head streams by
-constexpr int THREADS = 320;                 // warp 0 TMA, warp 1 MMA, warps 2..9 epilogue: two groups of four, each with a staging buffer
+constexpr int THREADS = 320;                 // warp 0 TMA, warp 1 MMA, warps 2..9 epilogue: two groups of four
 constexpr int HITS = 32;                     // TABLE: targets that a warp's list holds
 constexpr int PAIRS = 74;                    // CTA pairs of a B200, by which HIDDEN's tiles are cut on any device
 constexpr int MOST_PARTS = 4 * PAIRS;        // HIDDEN: split tiles' parts, four rounds
@@ -225,7 +225,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar_acc_full + 8 * b, 1);
-            mbar_init(bar_acc_empty + 8 * b, 512);           // the epilogue threads of both CTAs
+            mbar_init(bar_acc_empty + 8 * b, 16);            // the epilogue warps of both CTAs
         }
         fence_barrier_init();
         tma_prefetch_desc(&tmA);
@@ -318,11 +318,12 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         const int row = quarter * 32 + lane;
         uint32_t acc = 0;
         const bool storer = (warp == 2 || warp == 6) && lane == 0;
-        uint8_t* const stg = smem + OFF_STG + group * STG_BYTES;
-        // the group's buffer, when its last store has finished reading
+        uint32_t piece = 0;
+        // the group's buffer of the piece before last, when its store has finished reading
         auto stage = [&]() {
-            if (storer) tma_store_wait_read();
+            if (storer) tma_store_wait_read1();
             named_bar_sync(1 + group, 128);
+            return smem + OFF_STG + (2 * group + (piece++ & 1)) * STG_BYTES;
         };
         for (int u = first; u < g.units; u += stride, ++acc) {
             const LpbUnit x = lpb_unit<KIND>(g, u);
@@ -402,7 +403,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         }
                         if (hit >= 0 && hit < 64) p.rho[row0 + row] = __fsub_rn(at_hit, __bfloat162float(__float2bfloat16_rn(at_hit)));
                     }
-                    stage();
+                    uint8_t* const stg = stage();
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16) {
                         const uint4 val = make_uint4(
@@ -431,7 +432,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
                     }
                     if (KIND == TABLE && nhits > 0) add_lost(v, x.col + 32 * q);
-                    stage();
+                    uint8_t* const stg = stage();
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16)
                         *reinterpret_cast<uint4*>(stg + row * 128 + ((c16 ^ (row & 7)) << 4)) =
@@ -450,7 +451,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             }
             // all TMEM reads of this accumulator are done: hand it back to the MMA warp
             tc_fence_before();
-            mbar_arrive_cluster(lead_acc_empty + 8 * buf);
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(lead_acc_empty + 8 * buf);
         }
         if (storer) tma_store_wait_all();
     }
