@@ -71,6 +71,11 @@ __device__ __forceinline__ void mma_ss_chain4_pair_steps(uint32_t d_tmem, uint64
         : "memory");
 }
 
+// Arrives on a barrier of either CTA.  What it announces is that tensor memory has been read, which the tcgen05 fence before it orders: memory
+// needs no ordering, and a release to the cluster waits for the CTA's stores (2000 clk of a unit's 4600 where the output bounds a call).
+__device__ __forceinline__ void lpb_arrive(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // One warp of both CTAs: all of tensor memory, two 256-column accumulators.  Before the CTA's dependents are released.
 constexpr uint32_t LPB_TMEM_COLS = 512;
 __device__ __forceinline__ void lpb_take_tensor_memory(volatile uint32_t* slot) {
@@ -312,8 +317,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         }
     } else {
         // ------------------------------------------------------------ epilogue (warps 2..9), thread per row
-        // The two groups take the tile's 128-byte wide pieces in turns (one group of four warps 298 us where a call of 64 rows writes
-        // 1.1 GB of d_lm_head, two 2xx).
+        // The two groups take the tile's 128-byte wide pieces in turns (d_lm_head of 64 rows, 1.1 GB: one group 298 us, two
+        // and a buffer more each 286, and with a relaxed arrival 214).
         const int quarter = warp & 3, group = (warp - 2) >> 2;         // TMEM lane quarter of this warp
         const int row = quarter * 32 + lane;
         uint32_t acc = 0;
@@ -452,7 +457,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             // all TMEM reads of this accumulator are done: hand it back to the MMA warp
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(lead_acc_empty + 8 * buf);
+            if (lane == 0) lpb_arrive(lead_acc_empty + 8 * buf);
         }
         if (storer) tma_store_wait_all();
     }
