@@ -757,13 +757,14 @@ tik_status tik_policy_loss(tik_ctx* ctx, const float* logprob, const float* old_
     p.S = S;
     p.adv_per_seq = advantage_per_sequence != 0 && T > 0;
     p.reduction = T > 0 ? reduction : TIK_LOSS_SUM;
-    p.T = T;
+    p.T = static_cast<int>(T);
     p.log_low = std::log1p(-static_cast<double>(clip_low));
     p.log_high = std::log1p(static_cast<double>(clip_high));
-    p.log_dual = clip_dual != 0.0f ? std::log(static_cast<double>(clip_dual)) : INFINITY;
-    p.bound_low = 1.0f - clip_low;
-    p.bound_high = 1.0f + clip_high;
-    p.bound_dual = clip_dual;
+    p.log_dual = clip_dual != 0.0f ? std::log(static_cast<double>(clip_dual)) : 0.0;
+    p.low = clip_low;
+    p.high = clip_high;
+    p.dual = clip_dual != 0.0f;
+    p.dual_less_one = clip_dual - 1.0f;
     p.kl_coef = kl_coef;
     p.scale = scale;
     p.loss = loss;

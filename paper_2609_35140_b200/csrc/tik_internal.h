@@ -245,9 +245,10 @@ struct PolicyLossParams {
     const float* ref;            // [T] or null
     const int32_t* cu;           // [S + 1] or null
     int S, adv_per_seq, reduction;
-    int64_t T;
+    int T;
     double log_low, log_high, log_dual;
-    float bound_low, bound_high, bound_dual;
+    float low, high, dual_less_one;      // the thresholds less one
+    int dual;                    // whether there is a third one
     float kl_coef, scale;
     float* loss;
     float* d_logprob;            // [T] or null

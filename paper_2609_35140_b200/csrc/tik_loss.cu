@@ -7,10 +7,12 @@
 // and over the tokens whose weight w is not 0:  loss = sum_t f_t l_t,  d_logprob = f_t dl_t, with f_t = scale w_t, divided by the
 // number of such tokens (of the whole call, or of the token's sequence).
 //
-// Whether a token is cut is decided on x in 64 bits against the logarithms of the thresholds: r in 32 bits would put tokens on
-// the wrong side of a border where the gradient jumps.  Sums over tokens are fp64 in one fixed order, counts are integers.
-// 20 bytes in and 4 out per token: a call of less than some 100 000 tokens is all latency, and one cluster of up to eight CTAs takes
-// it in one launch, tokens in registers, counts and sums through distributed shared memory.  Longer calls, whose reads need all
+// Per token fp32, but where digits would be lost that matter: whether a token is cut is decided on x in 64 bits against the
+// logarithms of the thresholds (r in 32 bits would put tokens on the wrong side of a border where the gradient jumps); exp(y) - y - 1 comes
+// from its series, not from a difference; -A r goes into the sum as -A and -A (r - 1), the first exact and the second small.  Sums over tokens,
+// which are of both signs and mostly cancel, are fp64 in one fixed order, counts are integers.  (All of it in fp64 took 275 instructions a token.)
+// 20 bytes in and 4 out per token, so a call is all latency: up to 8192 tokens one cluster of up to eight CTAs takes
+// it in one launch, counts and sums through distributed shared memory.  Longer calls, whose arithmetic needs all
 // SMs, take two: one counts, the other computes, and its last CTA folds the sums.
 #include <cstdlib>
 
@@ -23,81 +25,114 @@ namespace tik {
 namespace loss {
 constexpr int MAX_CLUSTER = 8;
 constexpr int SEQ_CAP = 8192;                // sequences' counts that a CTA of a cluster holds
-constexpr int STEPS = 8;                     // tokens of a thread, one per 32 tokens of its warp's stretch
+constexpr int STEPS = 4;                     // tokens of a thread at most, one per 32 tokens of its warp's stretch
+constexpr int CLUSTER_STEPS = 2;             // ... of the cluster's
 constexpr int CLUSTER_THREADS = 512;
 constexpr int GRID_THREADS = 256;
 constexpr int MAX_CTAS = 592;                // of the two-launch form
-constexpr int SUMS = 5;                      // policy, kl, cut, k3, tokens
+constexpr int SUMS = 5;                      // policy, KL, tokens cut, r - 1 - x, tokens that count
 }  // namespace loss
 
-// exp(d) - d - 1 without cancellation: the series where d is small (eight terms: 2e-8 of the value at |d| = 1/2).
-__device__ __forceinline__ float exp_minus_tangent(float d) {
-    if (fabsf(d) > 0.5f) return expm1f(d) - d;
-    float p = 1.0f / 362880.0f;
-    p = fmaf(p, d, 1.0f / 40320.0f);
-    p = fmaf(p, d, 1.0f / 5040.0f);
-    p = fmaf(p, d, 1.0f / 720.0f);
-    p = fmaf(p, d, 1.0f / 120.0f);
-    p = fmaf(p, d, 1.0f / 24.0f);
-    p = fmaf(p, d, 1.0f / 6.0f);
-    p = fmaf(p, d, 0.5f);
-    return p * d * d;
-}
-
 // tokens that a sequence may hold
-__device__ __forceinline__ void loss_range(const PolicyLossParams& p, long long& from, long long& to) {
+__device__ __forceinline__ void loss_range(const PolicyLossParams& p, int& from, int& to) {
     from = 0;
     to = p.T;
     if (p.cu) {
         from = max(p.cu[0], 0);
-        to = min(static_cast<long long>(p.cu[p.S]), to);
+        to = min(p.cu[p.S], to);
     }
 }
 
-struct LossToken {
-    float policy, kl, grad, k3;
-    bool cut;
+// exp(x) - 1 and exp(x) - 1 - x.  x = k ln 2 + f and s = 2^k: exp(x) = s (1 + f + f^2 q), q = sum f^n / (n + 2)! to n = 10.  Up to |x| = 1 k
+// is 0 (the next term is 4e-9 of q), and what would cancel, s - 1 and s f - x, is exactly 0.
+struct Exp {
+    float less_one, remainder;
 };
-__device__ __forceinline__ LossToken loss_token(const PolicyLossParams& p, float lp, float old, float adv, float ref) {
-    LossToken o;
-    const double x = static_cast<double>(lp) - static_cast<double>(old);
-    const float xf = static_cast<float>(x), r = expf(xf);
+__device__ __forceinline__ Exp loss_exp(float x) {
+    const float c = x > 150.0f ? 150.0f : x < -150.0f ? -150.0f : x;       // 2^k in two factors: infinity or 0 beyond fp32 (NaN stays)
+    const float k = fabsf(x) < 1.0f ? 0.0f : rintf(c * LOG2E_F);
+    const float f = fmaf(k, -1.42860677e-6f, fmaf(k, -0.693145752f, c));   // ln 2 in two parts, the first of 16 bits
+    const int i = static_cast<int>(k), half = i >> 1;
+    const float s1 = __int_as_float((half + 127) << 23), s2 = __int_as_float((i - half + 127) << 23);
+    float q = 1.0f / 479001600.0f;
+    q = fmaf(q, f, 1.0f / 39916800.0f);
+    q = fmaf(q, f, 1.0f / 3628800.0f);
+    q = fmaf(q, f, 1.0f / 362880.0f);
+    q = fmaf(q, f, 1.0f / 40320.0f);
+    q = fmaf(q, f, 1.0f / 5040.0f);
+    q = fmaf(q, f, 1.0f / 720.0f);
+    q = fmaf(q, f, 1.0f / 120.0f);
+    q = fmaf(q, f, 1.0f / 24.0f);
+    q = fmaf(q, f, 1.0f / 6.0f);
+    q = fmaf(q, f, 0.5f);
+    const float t = f * f * q;
+    Exp e;
+    if (k == 0.0f) {
+        e.less_one = f + t;
+        e.remainder = t;
+    } else {
+        e.less_one = (1.0f + (f + t)) * s1 * s2 - 1.0f;
+        e.remainder = e.less_one - x;
+    }
+    return e;
+}
+
+// A thread's share of the sums
+struct LossSums {
+    double policy = 0.0, kl = 0.0, remainder = 0.0;
+    int cut = 0, tokens = 0;
+};
+// Adds a token that counts to the sums and returns its gradient; f: its factor.
+__device__ __forceinline__ float loss_token(const PolicyLossParams& p, double f, float lp, float old, float adv, float ref, LossSums& sum) {
+    const float x = lp - old;
+    const Exp r = loss_exp(x);
+    // x against a threshold, in 64 bits where 32 do not settle it
+    auto beyond = [&](double mark, float sign) {
+        const float m = static_cast<float>(mark), d = sign * (x - m), doubt = 1e-6f * (fabsf(x) + 1.0f);
+        if (fabsf(d) > doubt) return d > 0.0f;
+        return sign * ((static_cast<double>(lp) - static_cast<double>(old)) - mark) > 0.0;
+    };
+    float less_one = r.less_one;                           // of what the advantage is multiplied with
     bool cut = false;
-    float at = r;
-    if (adv > 0.0f && x > p.log_high) {
-        cut = true;
-        at = p.bound_high;
-    } else if (adv < 0.0f && x < p.log_low) {
-        cut = true;
-        at = p.bound_low;
-    } else if (adv < 0.0f && x > p.log_dual) {             // (+infinity without a third threshold)
-        cut = true;
-        at = p.bound_dual;
+    if (adv > 0.0f) {
+        if (beyond(p.log_high, 1.0f)) {
+            cut = true;
+            less_one = p.high;
+        }
+    } else if (adv < 0.0f) {
+        if (beyond(p.log_low, -1.0f)) {
+            cut = true;
+            less_one = -p.low;
+        } else if (p.dual && beyond(p.log_dual, 1.0f)) {
+            cut = true;
+            less_one = p.dual_less_one;
+        }
     }
-    o.cut = cut;
-    o.policy = -adv * at;
-    o.grad = cut ? 0.0f : o.policy;
-    o.k3 = exp_minus_tangent(xf);
-    o.kl = 0.0f;
+    float grad = cut ? 0.0f : fmaf(-adv, r.less_one, -adv);
+    sum.policy = fma(-f, static_cast<double>(adv), sum.policy);
+    sum.policy = fma(-f, static_cast<double>(adv * less_one), sum.policy);
     if (p.ref) {
-        const float y = ref - lp;
-        o.kl = exp_minus_tangent(y);
-        o.grad -= p.kl_coef * expm1f(y);
+        const Exp e = loss_exp(ref - lp);
+        sum.kl = fma(f, static_cast<double>(e.remainder), sum.kl);
+        grad -= p.kl_coef * e.less_one;
     }
-    return o;
+    sum.cut += cut;
+    sum.remainder += r.remainder;
+    ++sum.tokens;
+    return static_cast<float>(f) * grad;
 }
 
 // The sequences of a warp's ascending tokens.  `near`: cu[s0 + 1 + lane], the ends of the sequences from s0 on.
 struct LossSeq {
     int s0, near;
     __device__ __forceinline__ void load(const PolicyLossParams& p, int lane) { near = p.cu[min(s0 + 1 + lane, p.S)]; }
-    __device__ __forceinline__ void begin(const PolicyLossParams& p, long long token, int lane) {
+    __device__ __forceinline__ void begin(const PolicyLossParams& p, int token, int lane) {
         s0 = warp_find_sequence(p.cu, p.S, token, lane);
         load(p, lane);
     }
     // The sequence of each lane's token (whole warp, tokens ascending over the lanes and from call to call); some
     // sequence for a token that none holds.
-    __device__ __forceinline__ int of(const PolicyLossParams& p, long long token, int lane) {
+    __device__ __forceinline__ int of(const PolicyLossParams& p, int token, int lane) {
         int n = 0;                                         // ends that the token has reached: a prefix of the 32
 #pragma unroll
         for (int w = 16; w >= 1; w >>= 1)
@@ -155,14 +190,7 @@ __device__ __forceinline__ void loss_results(const PolicyLossParams& p, const do
     }
 }
 // Sums of a block's threads: thread 0 gets the totals, warps in ascending order.
-template <int THREADS>
-__device__ __forceinline__ void loss_block_sums(double (&v)[loss::SUMS], double (*buf)[loss::SUMS], int warps) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < loss::SUMS; ++i) {
-        v[i] = warp_total(v[i]);
-        if (lane == 0) buf[warp][i] = v[i];
-    }
+__device__ __forceinline__ void loss_block_fold(double (&v)[loss::SUMS], const double (*buf)[loss::SUMS], int warps) {
     __syncthreads();
     if (threadIdx.x == 0)
 #pragma unroll
@@ -170,6 +198,15 @@ __device__ __forceinline__ void loss_block_sums(double (&v)[loss::SUMS], double 
             v[i] = 0.0;
             for (int w = 0; w < warps; ++w) v[i] += buf[w][i];
         }
+}
+__device__ __forceinline__ void loss_block_sums(const LossSums& s, double (&v)[loss::SUMS], double (*buf)[loss::SUMS], int warps) {
+    const double policy = warp_total(s.policy), kl = warp_total(s.kl), remainder = warp_total(s.remainder);
+    const int cut = __reduce_add_sync(0xffffffffu, s.cut), tokens = __reduce_add_sync(0xffffffffu, s.tokens);
+    if ((threadIdx.x & 31) == 0) {
+        double* const to = buf[threadIdx.x >> 5];
+        to[0] = policy, to[1] = kl, to[2] = cut, to[3] = remainder, to[4] = tokens;
+    }
+    loss_block_fold(v, buf, warps);
 }
 
 // One cluster.  A thread holds `steps` tokens (at most STEPS): those of its lane in each 32 of its warp's stretch.
@@ -189,28 +226,31 @@ __global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(con
     if (tid == 0) cta_count = 0;
     pdl_wait();
     pdl_launch_dependents();
-    const long long t0 = (static_cast<long long>(rank) * warps + warp) * 32 * steps + lane;
-    long long from, to;
-    loss_range(p, from, to);
+    const int t0 = (rank * warps + warp) * 32 * steps + lane;
+    constexpr int STEPS = CLUSTER_STEPS;
     float lp[STEPS], old[STEPS], adv[STEPS], w[STEPS], ref[STEPS];
     int seq[STEPS];
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
-        const long long t = t0 + 32 * j;
-        const bool in = j < steps && t >= from && t < to;
+        const int t = t0 + 32 * j;
+        const bool in = j < steps && t < p.T;
         w[j] = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f;
         lp[j] = in ? p.logprob[t] : 0.0f;
         old[j] = in ? p.old_logprob[t] : 0.0f;
         adv[j] = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
         ref[j] = in && p.ref ? p.ref[t] : 0.0f;
     }
-    if (find) {
-        LossSeq q;
-        q.begin(p, t0 - lane, lane);
+    int from, to;
+    loss_range(p, from, to);
+    LossSeq q;
+    if (find) q.begin(p, t0 - lane, lane);
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
-            if (j < steps) seq[j] = q.of(p, t0 + 32 * j, lane);
-            if (j < steps && p.adv_per_seq && w[j] != 0.0f) adv[j] = p.advantage[seq[j]];
+    for (int j = 0; j < STEPS; ++j) {
+        const int t = t0 + 32 * j;
+        if (t < from || t >= to) w[j] = 0.0f;
+        if (find && j < steps) {
+            seq[j] = q.of(p, t, lane);
+            if (p.adv_per_seq && w[j] != 0.0f) adv[j] = p.advantage[seq[j]];
         }
     }
     if (ctas > 1) cluster_sync_all();                      // zeroed counts, and every CTA of the cluster has begun
@@ -237,35 +277,29 @@ __global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(con
     else __syncthreads();
     int all = 0;
     for (int c = 0; c < ctas; ++c) all += dsmem_read_int(mapa_cluster(smem_u32(&cta_count), c));
-    float f = p.scale;
-    if (p.reduction == LOSS_TOKEN_MEAN) f = static_cast<float>(static_cast<double>(p.scale) / (all > 1 ? all : 1));
-    double sum[SUMS] = {};
+    double f = p.scale;
+    if (p.reduction == LOSS_TOKEN_MEAN) f /= all > 1 ? all : 1;
+    LossSums mine;
 #pragma unroll
     for (int j = 0; j < STEPS; ++j) {
-        const long long t = t0 + 32 * j;
+        const int t = t0 + 32 * j;
         if (j >= steps || t >= p.T) break;
         float d = 0.0f;
         if (w[j] != 0.0f) {
-            float fj = f;
+            double fj = f * w[j];
             if (per_sequence) {
                 const int s = seq[j], owner = s / per;
                 const int n = count_seq ? dsmem_read_int(mapa_cluster(smem_u32(&seq_count[s - owner * per]), owner)) : p.cu[s + 1] - p.cu[s];
-                fj = __fdiv_rn(f, static_cast<float>(n > 1 ? n : 1));
+                fj /= n > 1 ? n : 1;
             }
-            fj *= w[j];
-            const LossToken o = loss_token(p, lp[j], old[j], adv[j], ref[j]);
-            d = fj * o.grad;
-            sum[0] += static_cast<double>(fj) * o.policy;
-            sum[1] += static_cast<double>(fj) * o.kl;
-            sum[2] += o.cut ? 1.0 : 0.0;
-            sum[3] += o.k3;
+            d = loss_token(p, fj, lp[j], old[j], adv[j], ref[j], mine);
         }
         if (p.d_logprob) p.d_logprob[t] = d;
     }
-    loss_block_sums<CLUSTER_THREADS>(sum, sums, warps);
+    double sum[SUMS];
+    loss_block_sums(mine, sum, sums, warps);
     if (ctas == 1) {
         if (tid == 0) {
-            sum[4] = all;
             loss_results(p, sum);
         }
         return;
@@ -278,7 +312,6 @@ __global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(con
         for (int c = 1; c < ctas; ++c)
 #pragma unroll
             for (int i = 0; i < SUMS; ++i) sum[i] += dsmem_read(mapa_cluster(smem_u32(&cta_sums[i]), c));
-        sum[4] = all;
         loss_results(p, sum);
     }
     cluster_sync_all();                                    // nobody leaves while its sums may still be read
@@ -293,17 +326,19 @@ __global__ void __launch_bounds__(loss::GRID_THREADS) loss_count_kernel(const Po
     pdl_launch_dependents();
     if (blockIdx.x == 0 && tid == 0) *p.ticket = 0;
     if (!p.weight) return;
-    long long lo, hi;
+    int lo, hi;
     loss_range(p, lo, hi);
-    long long from = lo + static_cast<long long>(blockIdx.x) * GRID_THREADS, to = hi, step = static_cast<long long>(gridDim.x) * GRID_THREADS;
+    unsigned from = lo + blockIdx.x * GRID_THREADS, to = hi, step = gridDim.x * GRID_THREADS;
     if (p.reduction == LOSS_SEQUENCE_MEAN) {
-        from = max(lo, static_cast<long long>(p.cu[blockIdx.x]));
-        to = min(hi, static_cast<long long>(p.cu[blockIdx.x + 1]));
+        from = max(lo, p.cu[blockIdx.x]);
+        to = max(min(hi, p.cu[blockIdx.x + 1]), 0);
         step = GRID_THREADS;
+    } else if (hi < 0) {
+        to = 0;
     }
     int n = 0;
 #pragma unroll 8
-    for (long long t = from + tid; t < to; t += step) n += p.weight[t] != 0.0f;
+    for (unsigned t = from + tid; t < to; t += step) n += p.weight[t] != 0.0f;
     n = warp_total(n);
     if ((tid & 31) == 0) buf[tid >> 5] = n;
     __syncthreads();
@@ -313,7 +348,7 @@ __global__ void __launch_bounds__(loss::GRID_THREADS) loss_count_kernel(const Po
     }
 }
 
-__global__ void __launch_bounds__(loss::GRID_THREADS) loss_grid_kernel(const PolicyLossParams p, int counts) {
+__global__ void __launch_bounds__(loss::GRID_THREADS, 4) loss_grid_kernel(const PolicyLossParams p, int counts, int steps) {
     using namespace loss;
     constexpr int WARPS = GRID_THREADS / 32;
     __shared__ double sums[WARPS][SUMS];
@@ -323,11 +358,28 @@ __global__ void __launch_bounds__(loss::GRID_THREADS) loss_grid_kernel(const Pol
     const bool per_sequence = p.reduction == LOSS_SEQUENCE_MEAN, find = p.adv_per_seq || per_sequence;
     pdl_wait();
     pdl_launch_dependents();
-    long long lo, hi;
+    // (unsigned: the last step of a call of nearly 2^31 tokens passes them)
+    const unsigned stretch = 32u * steps, step = gridDim.x * WARPS * stretch, T = static_cast<unsigned>(p.T);
+    unsigned base = (blockIdx.x * WARPS + warp) * stretch;
+    float lp[STEPS], old[STEPS], adv[STEPS], w[STEPS], ref[STEPS];
+    auto load = [&]() {
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            const unsigned t = base + 32 * j + lane;
+            const bool in = j < steps && t < T;
+            w[j] = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f;
+            lp[j] = in ? p.logprob[t] : 0.0f;
+            old[j] = in ? p.old_logprob[t] : 0.0f;
+            adv[j] = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
+            ref[j] = in && p.ref ? p.ref[t] : 0.0f;
+        }
+    };
+    load();                                                // on its way while the counts are folded
+    int lo, hi;
     loss_range(p, lo, hi);
-    float f = p.scale;
+    double f = p.scale;
     if (p.reduction == LOSS_TOKEN_MEAN) {
-        long long all = hi - lo;
+        int all = hi - lo;
         if (p.weight) {
             int n = 0;
             for (int i = tid; i < counts; i += GRID_THREADS) n += p.count[i];
@@ -337,48 +389,34 @@ __global__ void __launch_bounds__(loss::GRID_THREADS) loss_grid_kernel(const Pol
             all = 0;
             for (int w = 0; w < WARPS; ++w) all += buf[w];
         }
-        f = static_cast<float>(static_cast<double>(p.scale) / (all > 1 ? all : 1));
+        f /= static_cast<double>(all > 1 ? all : 1);
     }
-    double sum[SUMS] = {};
-    const long long stretch = 32 * STEPS, step = static_cast<long long>(gridDim.x) * WARPS * stretch;
-    for (long long base = (static_cast<long long>(blockIdx.x) * WARPS + warp) * stretch; base < p.T; base += step) {
-        float lp[STEPS], old[STEPS], adv[STEPS], w[STEPS], ref[STEPS];
-#pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
-            const long long t = base + 32 * j + lane;
-            const bool in = t >= lo && t < hi;
-            w[j] = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f;
-            lp[j] = in ? p.logprob[t] : 0.0f;
-            old[j] = in ? p.old_logprob[t] : 0.0f;
-            adv[j] = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
-            ref[j] = in && p.ref ? p.ref[t] : 0.0f;
-        }
+    LossSums mine;
+    while (base < T) {
         LossSeq q;
-        if (find) q.begin(p, base, lane);
+        if (find) q.begin(p, static_cast<int>(base), lane);
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) {
-            const long long t = base + 32 * j + lane;
+            if (j >= steps) break;
+            const unsigned at = base + 32 * j + lane;
+            const int t = at < T ? static_cast<int>(at) : p.T - 1;
             const int s = find ? q.of(p, t, lane) : 0;
             float d = 0.0f;
-            if (w[j] != 0.0f) {
-                float fj = f;
+            if (w[j] != 0.0f && t >= lo && t < hi) {
+                double fj = f * w[j];
                 if (per_sequence) {
                     const int n = p.weight ? p.count[s] : p.cu[s + 1] - p.cu[s];
-                    fj = __fdiv_rn(f, static_cast<float>(n > 1 ? n : 1));
+                    fj /= n > 1 ? n : 1;
                 }
-                fj *= w[j];
-                const LossToken o = loss_token(p, lp[j], old[j], p.adv_per_seq ? p.advantage[s] : adv[j], ref[j]);
-                d = fj * o.grad;
-                sum[0] += static_cast<double>(fj) * o.policy;
-                sum[1] += static_cast<double>(fj) * o.kl;
-                sum[2] += o.cut ? 1.0 : 0.0;
-                sum[3] += o.k3;
-                sum[4] += 1.0;
+                d = loss_token(p, fj, lp[j], old[j], p.adv_per_seq ? p.advantage[s] : adv[j], ref[j], mine);
             }
-            if (p.d_logprob && t < p.T) p.d_logprob[t] = d;
+            if (p.d_logprob && at < T) p.d_logprob[at] = d;
         }
+        base += step;
+        if (base < T) load();
     }
-    loss_block_sums<GRID_THREADS>(sum, sums, WARPS);
+    double sum[SUMS];
+    loss_block_sums(mine, sum, sums, WARPS);
     if (tid == 0) {
 #pragma unroll
         for (int i = 0; i < SUMS; ++i) p.part[blockIdx.x * SUMS + i] = sum[i];
@@ -389,12 +427,23 @@ __global__ void __launch_bounds__(loss::GRID_THREADS) loss_grid_kernel(const Pol
     if (!last) return;
     __threadfence();
     // the CTAs' sums in one order, whichever CTA is the last
+    double part[(MAX_CTAS + GRID_THREADS - 1) / GRID_THREADS][SUMS];
 #pragma unroll
-    for (int i = 0; i < SUMS; ++i) sum[i] = 0.0;
-    for (int c = tid; c < static_cast<int>(gridDim.x); c += GRID_THREADS)
+    for (int k = 0; k < (MAX_CTAS + GRID_THREADS - 1) / GRID_THREADS; ++k)
 #pragma unroll
-        for (int i = 0; i < SUMS; ++i) sum[i] += __ldcg(&p.part[c * SUMS + i]);
-    loss_block_sums<GRID_THREADS>(sum, sums, WARPS);
+        for (int i = 0; i < SUMS; ++i) {
+            const int c = tid + k * GRID_THREADS;
+            part[k][i] = c < static_cast<int>(gridDim.x) ? __ldcg(&p.part[c * SUMS + i]) : 0.0;
+        }
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i) {
+        double v = part[0][i];
+#pragma unroll
+        for (int k = 1; k < (MAX_CTAS + GRID_THREADS - 1) / GRID_THREADS; ++k) v += part[k][i];
+        v = warp_total(v);
+        if (lane == 0) sums[warp][i] = v;
+    }
+    loss_block_fold(sum, sums, WARPS);
     if (tid == 0) loss_results(p, sum);
 }
 
@@ -407,11 +456,11 @@ size_t policy_loss_bytes(int64_t S) {
 cudaError_t launch_policy_loss(PolicyLossParams& p, void* ws, cudaStream_t stream) {
     using namespace loss;
     const bool counts_seq = p.reduction == LOSS_SEQUENCE_MEAN && p.weight;
-    const int64_t most = static_cast<int64_t>(MAX_CLUSTER) * CLUSTER_THREADS * STEPS;
+    const int64_t most = static_cast<int64_t>(MAX_CLUSTER) * CLUSTER_THREADS * CLUSTER_STEPS;
     if (p.T <= most && (!counts_seq || p.S <= SEQ_CAP)) {
-        // as many CTAs as leave a thread two tokens, and then as many tokens as it takes
+        // as many CTAs as leave a thread one token, and then as many tokens as it takes
         int ctas = 1;
-        while (ctas < MAX_CLUSTER && p.T > 2ll * ctas * CLUSTER_THREADS) ctas *= 2;
+        while (ctas < MAX_CLUSTER && p.T > static_cast<int64_t>(ctas) * CLUSTER_THREADS) ctas *= 2;
         const int threads = p.T > CLUSTER_THREADS ? CLUSTER_THREADS : p.T > 32 ? static_cast<int>((p.T + 31) / 32 * 32) : 32;
         const int steps = static_cast<int>((p.T + static_cast<int64_t>(ctas) * threads - 1) / (static_cast<int64_t>(ctas) * threads));
         const size_t smem = counts_seq ? static_cast<size_t>((p.S + ctas - 1) / ctas) * sizeof(int) : 0;
@@ -420,12 +469,15 @@ cudaError_t launch_policy_loss(PolicyLossParams& p, void* ws, cudaStream_t strea
     p.ticket = static_cast<int*>(ws);
     p.part = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);
     p.count = reinterpret_cast<int*>(p.part + SUMS * MAX_CTAS);
-    const int64_t stretches = (p.T + GRID_THREADS * STEPS - 1) / (GRID_THREADS * STEPS);
+    // as few tokens a thread as MAX_CTAS allow: what a thread does one after the other is what a call waits for
+    const int64_t waves = (p.T + static_cast<int64_t>(MAX_CTAS) * GRID_THREADS - 1) / (static_cast<int64_t>(MAX_CTAS) * GRID_THREADS);
+    const int steps = static_cast<int>(waves < STEPS ? waves : STEPS);
+    const int64_t stretches = (p.T + static_cast<int64_t>(GRID_THREADS) * steps - 1) / (static_cast<int64_t>(GRID_THREADS) * steps);
     const int ctas = static_cast<int>(stretches < MAX_CTAS ? stretches : MAX_CTAS);
     const int counts = !p.weight ? 1 : p.reduction == LOSS_SEQUENCE_MEAN ? p.S : ctas;
     cudaError_t e = launch_pdl(loss_count_kernel, dim3(static_cast<unsigned>(counts)), GRID_THREADS, 0, stream, 1, p);
     if (e != cudaSuccess) return e;
-    return launch_pdl(loss_grid_kernel, dim3(static_cast<unsigned>(ctas)), GRID_THREADS, 0, stream, 1, p, counts);
+    return launch_pdl(loss_grid_kernel, dim3(static_cast<unsigned>(ctas)), GRID_THREADS, 0, stream, 1, p, counts, steps);
 }
 
 }  // namespace tik
