@@ -43,35 +43,29 @@ __device__ __forceinline__ void loss_range(const PolicyLossParams& p, int& from,
     }
 }
 
-// exp(x) - 1 and exp(x) - 1 - x.  x = k ln 2 + f and s = 2^k: exp(x) = s (1 + f + f^2 q), q = sum f^n / (n + 2)! to n = 10.  Up to |x| = 1 k
-// is 0 (the next term is 4e-9 of q), and what would cancel, s - 1 and s f - x, is exactly 0.
+// exp(x) - 1 and exp(x) - 1 - x.  Up to |x| = 1, where nearly all tokens are, from x^2 q(x) with q = sum x^n / (n + 2)! to n = 10 (the next
+// term is 4e-9 of q): nothing cancels.  Beyond, where little does, through expf.
 struct Exp {
     float less_one, remainder;
 };
 __device__ __forceinline__ Exp loss_exp(float x) {
-    const float c = x > 150.0f ? 150.0f : x < -150.0f ? -150.0f : x;       // 2^k in two factors: infinity or 0 beyond fp32 (NaN stays)
-    const float k = fabsf(x) < 1.0f ? 0.0f : rintf(c * LOG2E_F);
-    const float f = fmaf(k, -1.42860677e-6f, fmaf(k, -0.693145752f, c));   // ln 2 in two parts, the first of 16 bits
-    const int i = static_cast<int>(k), half = i >> 1;
-    const float s1 = __int_as_float((half + 127) << 23), s2 = __int_as_float((i - half + 127) << 23);
-    float q = 1.0f / 479001600.0f;
-    q = fmaf(q, f, 1.0f / 39916800.0f);
-    q = fmaf(q, f, 1.0f / 3628800.0f);
-    q = fmaf(q, f, 1.0f / 362880.0f);
-    q = fmaf(q, f, 1.0f / 40320.0f);
-    q = fmaf(q, f, 1.0f / 5040.0f);
-    q = fmaf(q, f, 1.0f / 720.0f);
-    q = fmaf(q, f, 1.0f / 120.0f);
-    q = fmaf(q, f, 1.0f / 24.0f);
-    q = fmaf(q, f, 1.0f / 6.0f);
-    q = fmaf(q, f, 0.5f);
-    const float t = f * f * q;
     Exp e;
-    if (k == 0.0f) {
-        e.less_one = f + t;
-        e.remainder = t;
+    if (fabsf(x) < 1.0f) {
+        float q = 1.0f / 479001600.0f;
+        q = fmaf(q, x, 1.0f / 39916800.0f);
+        q = fmaf(q, x, 1.0f / 3628800.0f);
+        q = fmaf(q, x, 1.0f / 362880.0f);
+        q = fmaf(q, x, 1.0f / 40320.0f);
+        q = fmaf(q, x, 1.0f / 5040.0f);
+        q = fmaf(q, x, 1.0f / 720.0f);
+        q = fmaf(q, x, 1.0f / 120.0f);
+        q = fmaf(q, x, 1.0f / 24.0f);
+        q = fmaf(q, x, 1.0f / 6.0f);
+        q = fmaf(q, x, 0.5f);
+        e.remainder = x * x * q;
+        e.less_one = x + e.remainder;
     } else {
-        e.less_one = (1.0f + (f + t)) * s1 * s2 - 1.0f;
+        e.less_one = expf(x) - 1.0f;
         e.remainder = e.less_one - x;
     }
     return e;
@@ -88,25 +82,16 @@ __device__ __forceinline__ float loss_token(const PolicyLossParams& p, double f,
     const Exp r = loss_exp(x);
     // x against a threshold, in 64 bits where 32 do not settle it
     auto beyond = [&](double mark, float sign) {
-        const float m = static_cast<float>(mark), d = sign * (x - m), doubt = 1e-6f * (fabsf(x) + 1.0f);
-        if (fabsf(d) > doubt) return d > 0.0f;
+        const float d = sign * (x - static_cast<float>(mark));
+        if (fabsf(d) > 1e-6f * (fabsf(x) + 1.0f)) return d > 0.0f;
         return sign * ((static_cast<double>(lp) - static_cast<double>(old)) - mark) > 0.0;
     };
-    float less_one = r.less_one;                           // of what the advantage is multiplied with
-    bool cut = false;
-    if (adv > 0.0f) {
-        if (beyond(p.log_high, 1.0f)) {
-            cut = true;
-            less_one = p.high;
-        }
-    } else if (adv < 0.0f) {
-        if (beyond(p.log_low, -1.0f)) {
-            cut = true;
-            less_one = -p.low;
-        } else if (p.dual && beyond(p.log_dual, 1.0f)) {
-            cut = true;
-            less_one = p.dual_less_one;
-        }
+    const bool up = adv > 0.0f, down = adv < 0.0f;
+    bool cut = (up || down) && beyond(up ? p.log_high : p.log_low, up ? 1.0f : -1.0f);
+    float less_one = cut ? (up ? p.high : -p.low) : r.less_one;            // of what the advantage is multiplied with
+    if (p.dual && down && !cut && beyond(p.log_dual, 1.0f)) {
+        cut = true;
+        less_one = p.dual_less_one;
     }
     float grad = cut ? 0.0f : fmaf(-adv, r.less_one, -adv);
     sum.policy = fma(-f, static_cast<double>(adv), sum.policy);
