@@ -318,3 +318,86 @@ def grad_norm(grads) -> float:
     """Square root of the sum of the squares of all elements of a list of arrays."""
     with np.errstate(all="ignore"):
         return float(np.sqrt(sum(float((_f64(g) ** 2).sum()) for g in grads)))
+
+
+# ---------------------------------------------------------------- a policy update's objective, its way back, the optimiser (numpy, fp64)
+
+def policy_loss(logprob, old_logprob, advantage, weight=None, ref_logprob=None, cu_seqlens=None, clip_low: float = 0.2,
+                clip_high: float = 0.2, clip_dual: float = 0.0, kl_coef: float = 0.0, reduction: str = "token", scale: float = 1.0):
+    """(loss, its gradient with respect to logprob [T], [policy part, KL part, share of tokens cut, mean of r - 1 - log r, tokens that
+    count]).  advantage [T], or [S,1] per sequence."""
+    lp, old, adv, ref = (_f64(a) for a in (logprob, old_logprob, advantage, ref_logprob))
+    T = len(lp)
+    w = np.ones(T) if weight is None else _f64(weight)
+    seq = np.full(T, -1)
+    if cu_seqlens is None:
+        seq[:] = 0
+    else:
+        for s in range(len(cu_seqlens) - 1):
+            seq[cu_seqlens[s]:cu_seqlens[s + 1]] = s
+    on = (seq >= 0) & (w != 0)
+    loss, kl_sum, cut_sum, k3, d = 0.0, 0.0, 0, 0.0, np.zeros(T)
+    for t in np.flatnonzero(on):
+        n = {"sum": 1, "token": int(on.sum()), "sequence": int((on & (seq == seq[t])).sum())}[reduction]
+        f, A = scale * w[t] / n, float(adv[seq[t], 0] if adv.ndim == 2 else adv[t])
+        x = lp[t] - old[t]
+        r = np.exp(x)
+        value, slope, cut = -A * r, -A * r, False
+        if A > 0 and x > np.log1p(clip_high):
+            value, slope, cut = -A * (1 + clip_high), 0.0, True
+        elif A < 0 and x < np.log1p(-clip_low):
+            value, slope, cut = -A * (1 - clip_low), 0.0, True
+        elif A < 0 and clip_dual and x > np.log(clip_dual):
+            value, slope, cut = -A * clip_dual, 0.0, True
+        if ref is not None:
+            y = ref[t] - lp[t]
+            kl_sum += f * (np.expm1(y) - y)
+            slope -= kl_coef * np.expm1(y)
+        loss += f * value
+        cut_sum += cut
+        k3 += np.expm1(x) - x
+        d[t] = f * slope
+    n = max(1, int(on.sum()))
+    return loss + kl_coef * kl_sum, d, np.array([loss, kl_sum, cut_sum / n, k3 / n, on.sum()])
+
+
+def token_logprob_bwd(d_logprob, hidden, lm_head, target_ids, lse, inv_temperature: float = 1.0):
+    """(d_hidden [T,H], d_lm_head [V,H], d_z [T,V]): gradients of logprob[t] = z[t][target[t]] - lse[t], z = inv_temperature * hidden @ lm_head.T,
+    with the lse given.  Tokens with d_logprob 0 or a target outside the vocabulary have none."""
+    g, x, W, lse = (_f64(a) for a in (d_logprob, hidden, lm_head, lse))
+    ids = np.asarray(target_ids, dtype=np.int64)
+    dz = np.zeros((len(x), len(W)))
+    for t in range(len(x)):
+        if g[t] != 0 and 0 <= ids[t] < len(W):
+            dz[t] = -np.exp(inv_temperature * (W @ x[t]) - lse[t])
+            dz[t, ids[t]] += 1.0
+            dz[t] *= inv_temperature * g[t]
+    return dz @ W, dz.T @ x, dz
+
+
+def adamw(param, grad, exp_avg, exp_avg_sq, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+          weight_decay: float = 0.0, clip: float = 1.0):
+    """(weights, first moments, second moments) after a step."""
+    p, g, m, v = (_f64(a) for a in (param, grad, exp_avg, exp_avg_sq))
+    g = clip * g
+    m, v = beta1 * m + (1 - beta1) * g, beta2 * v + (1 - beta2) * g * g
+    return (1 - lr * weight_decay) * p - lr * (m / (1 - beta1 ** step)) / (np.sqrt(v / (1 - beta2 ** step)) + eps), m, v
+
+
+def e4m3_values():
+    """What the 256 codes of e4m3 (bias 7, no infinities, one NaN per sign) stand for."""
+    out = np.empty(256)
+    for c in range(256):
+        e, m = c >> 3 & 15, c & 7
+        mag = np.nan if e == 15 and m == 7 else m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10)
+        out[c] = -mag if c & 128 else mag
+    return out
+
+
+def block_scale(x):
+    """k >= -127, the smallest with which the largest of a block fits 448 * 2^k."""
+    top = float(np.max(np.abs(_f64(x)), initial=0.0))
+    k = -127
+    while top > 448.0 * 2.0 ** k:
+        k += 1
+    return k

@@ -13,6 +13,9 @@ median and minimum, the algorithmic work and the resulting rate.
   python -m paper_2609_35140_b200.microbench embed_bwd --rows 16001 --hidden 3584 --vocab 152064      (also embed)
   python -m paper_2609_35140_b200.microbench norm_bwd  --rows 16001 --hidden 3584                     (also norm)
   python -m paper_2609_35140_b200.microbench clip      --rows 100000 --hidden 3584                    (rows x hidden elements)
+  python -m paper_2609_35140_b200.microbench logprob_bwd --rows 2048 --hidden 1536 --vocab 151936
+  python -m paper_2609_35140_b200.microbench loss      --rows 1000000                                 (rows tokens)
+  python -m paper_2609_35140_b200.microbench adamw     --rows 30000 --hidden 3584                     (also adamw8: rows x hidden elements)
 """
 from __future__ import annotations
 
@@ -171,6 +174,40 @@ def run(a) -> dict:
             byt = (8.0 if a.case == "norm" else 12.0) * T * H
         med, mn = _time(fn, a.reps, a.warmup, flush)
         out.update(shape={"rows": T, "hidden": H, "vocab": V}, bytes=byt, gbs=byt / (med * 1e-3) / 1e9, gbs_best=byt / (mn * 1e-3) / 1e9)
+    elif a.case == "logprob_bwd":
+        gen = torch.Generator(device=dev).manual_seed(4321)
+        T, H, V = a.rows, a.hidden, a.vocab
+        x, W = synth._randn_bf16((T, H), gen, dev), synth._randn_bf16((V, H), gen, dev, std=0.02, chunk_rows=1 << 14)
+        tgt = torch.randint(0, V, (T,), generator=gen, device=dev).to(torch.int32)
+        lse, d = torch.empty(T, device=dev), torch.randn(T, generator=gen, device=dev)
+        tik.tik_token_logprob(x, W, tgt, lse=lse)
+        dx, dW = torch.empty_like(x), torch.empty_like(W)
+        ws = torch.empty(tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, T, H=H, V=V), dtype=torch.uint8, device=dev)
+        med, mn = _time(lambda: tik.tik_token_logprob_bwd(d, x, W, tgt, lse, d_hidden=dx, d_lm_head=dW, ws=ws), a.reps, a.warmup, flush)
+        fl, byt = 6.0 * T * H * V, 4.0 * H * (T + V)
+        out.update(shape={"rows": T, "hidden": H, "vocab": V}, flops=fl, tflops=fl / (med * 1e-3) / 1e12, bytes=byt, gbs=byt / (med * 1e-3) / 1e9)
+    elif a.case in ("loss", "adamw", "adamw8"):
+        gen = torch.Generator(device=dev).manual_seed(4321)
+        if a.case == "loss":
+            old, adv = -torch.rand(a.rows, generator=gen, device=dev), torch.randn(a.rows, generator=gen, device=dev)
+            lp, ref = (old + 0.1 * torch.randn(a.rows, generator=gen, device=dev) for _ in range(2))
+            w = (torch.rand(a.rows, generator=gen, device=dev) > 0.3).float()
+            fn = lambda: tik.tik_policy_loss(lp, old, adv, weight=w, ref_logprob=ref, kl_coef=0.05)
+            byt = 24.0 * a.rows
+        else:
+            n = a.rows * a.hidden
+            p, g = (synth._randn_bf16((1, n), gen, dev)[0] for _ in range(2))
+            if a.case == "adamw":
+                master, m, v = p.float(), torch.zeros(n, device=dev), torch.zeros(n, device=dev)
+                fn = lambda: tik.tik_adamw([p], [g], [m], [v], 1e-4, 10, master=[master])
+                byt = 28.0 * n
+            else:
+                m, v = (torch.zeros(n, dtype=torch.float8_e4m3fn, device=dev) for _ in range(2))
+                ms, vs = (torch.zeros((n + 31) // 32, dtype=torch.uint8, device=dev) for _ in range(2))
+                fn = lambda: tik.tik_adamw([p], [g], [m], [v], 1e-4, 10, exp_avg_scale=[ms], exp_avg_sq_scale=[vs], seed=1)
+                byt = 10.125 * n
+        med, mn = _time(fn, a.reps, a.warmup, flush)
+        out.update(shape={"rows": a.rows, "hidden": a.hidden}, bytes=byt, gbs=byt / (med * 1e-3) / 1e9, gbs_best=byt / (mn * 1e-3) / 1e9)
     else:
         raise SystemExit("unknown case " + a.case)
     out.update(ms=med, ms_best=mn, reps=a.reps, device_flags=tik.device_status())
@@ -180,7 +217,7 @@ def run(a) -> dict:
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("case", choices=["train", "prefill", "decode", "logprob", "linear", "embed", "embed_bwd", "norm",
-                                     "norm_bwd", "clip"])
+                                     "norm_bwd", "clip", "logprob_bwd", "loss", "adamw", "adamw8"])
     ap.add_argument("--seqs", type=int, default=1)
     ap.add_argument("--len", type=int, default=4096)
     ap.add_argument("--lens", default="", help="comma-separated lengths (overrides --seqs/--len)")
