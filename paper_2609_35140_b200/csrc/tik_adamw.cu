@@ -73,8 +73,9 @@ __device__ __forceinline__ uint32_t adam_random(long long place, uint32_t key) {
     return adam_mix(static_cast<uint32_t>(place) * 0x632BE5ABu + key + static_cast<uint32_t>(place >> 32) * 0x85157AF5u);
 }
 
-// A thread's eight elements, in groups of W neighbours, a group of every thread after the other: W = 4 where a tensor lies at multiples of
-// 16 bytes (a warp's access is one run of 128 bytes or more, whole sectors), else W = 1.  A block of 32 is a group of 32 / W lanes.
+// A thread's eight elements, in groups of W neighbours, a group of every thread after the other.  Where a tensor lies at multiples of 16
+// bytes W is 4, so that a warp's access is one run of whole sectors, and with 8-bit moments 8: a block of 32, held by 32 / W lanes, then takes two
+// shuffles for a maximum and one thread's scale goes for all its elements.  Else W is 1.
 constexpr int ADAM_N = 8;
 template <int W>
 __device__ __forceinline__ long long adam_place(long long at, int i) { return at + i % W + (i / W) * (W * ADAM_THREADS); }
@@ -85,16 +86,27 @@ __device__ __forceinline__ void adam_load(float (&x)[ADAM_N], const void* src, b
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && (STAGED || e + W <= n)) {
+        if (W > 1 && (STAGED || e + W <= n)) {
             if (fp32) {
-                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(src) + e);
-                const float4 a = STAGED ? *p : __ldcs(p);
-                x[i] = a.x, x[i + 1 % W] = a.y, x[i + 2 % W] = a.z, x[i + 3 % W] = a.w;
+#pragma unroll
+                for (int j = 0; j < W; j += 4) {
+                    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(src) + e + j);
+                    const float4 a = STAGED ? *p : __ldcs(p);
+                    x[i + j] = a.x, x[i + j + 1 % W] = a.y, x[i + j + 2 % W] = a.z, x[i + j + 3 % W] = a.w;
+                }
             } else {
                 const uint2* p = reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(src) + e);
-                const uint2 a = STAGED ? *p : __ldcs(p);
-                x[i] = __uint_as_float(a.x << 16), x[i + 1 % W] = __uint_as_float(a.x & 0xffff0000u);
-                x[i + 2 % W] = __uint_as_float(a.y << 16), x[i + 3 % W] = __uint_as_float(a.y & 0xffff0000u);
+                uint4 a = make_uint4(0, 0, 0, 0);
+                if (W == 8) {
+                    a = STAGED ? *reinterpret_cast<const uint4*>(p) : __ldcs(reinterpret_cast<const uint4*>(p));
+                } else {
+                    const uint2 b = STAGED ? *p : __ldcs(p);
+                    a.x = b.x;
+                    a.y = b.y;
+                }
+                const unsigned w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int j = 0; j < W; ++j) x[i + j] = __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
             }
         } else {
 #pragma unroll
@@ -105,17 +117,28 @@ __device__ __forceinline__ void adam_load(float (&x)[ADAM_N], const void* src, b
         }
     }
 }
+// W bf16 from their words
+template <int W>
+__device__ __forceinline__ void adam_store_words(__nv_bfloat16* to, const unsigned (&w)[4]) {
+    if (W == 8) __stcs(reinterpret_cast<uint4*>(to), make_uint4(w[0], w[1], w[2], w[3]));
+    else __stcs(reinterpret_cast<uint2*>(to), make_uint2(w[0], w[1]));
+}
 template <int W, bool WHOLE>
 __device__ __forceinline__ void adam_store(const float (&x)[ADAM_N], void* dst, bool fp32, long long at, long long n) {
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && (WHOLE || e + W <= n)) {
-            if (fp32)
-                __stcs(reinterpret_cast<float4*>(static_cast<float*>(dst) + e), make_float4(x[i], x[i + 1 % W], x[i + 2 % W], x[i + 3 % W]));
-            else
-                __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(dst) + e),
-                       make_uint2(pack_bf16x2(x[i], x[i + 1 % W]), pack_bf16x2(x[i + 2 % W], x[i + 3 % W])));
+        if (W > 1 && (WHOLE || e + W <= n)) {
+            if (fp32) {
+#pragma unroll
+                for (int j = 0; j < W; j += 4)
+                    __stcs(reinterpret_cast<float4*>(static_cast<float*>(dst) + e + j), make_float4(x[i + j], x[i + j + 1 % W], x[i + j + 2 % W], x[i + j + 3 % W]));
+            } else {
+                unsigned w[4] = {};
+#pragma unroll
+                for (int j = 0; j < W; j += 2) w[j / 2] = pack_bf16x2(x[i + j], x[i + j + 1 % W]);
+                adam_store_words<W>(static_cast<__nv_bfloat16*>(dst) + e, w);
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
@@ -133,9 +156,11 @@ __device__ __forceinline__ void adam_store_upper(const float (&x)[ADAM_N], void*
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && (WHOLE || e + W <= n)) {
-            auto pair = [](float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); };
-            __stcs(reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(dst) + e), make_uint2(pair(x[i], x[i + 1 % W]), pair(x[i + 2 % W], x[i + 3 % W])));
+        if (W > 1 && (WHOLE || e + W <= n)) {
+            unsigned w[4] = {};
+#pragma unroll
+            for (int j = 0; j < W; j += 2) w[j / 2] = __byte_perm(__float_as_uint(x[i + j]), __float_as_uint(x[i + j + 1 % W]), 0x7632);
+            adam_store_words<W>(static_cast<__nv_bfloat16*>(dst) + e, w);
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
@@ -161,13 +186,15 @@ __device__ __forceinline__ void adam_load8(float (&x)[ADAM_N], const void* src, 
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && (STAGED || e + W <= n)) {
-            const unsigned* p = reinterpret_cast<const unsigned*>(q + e);
-            w[i / 4] = STAGED ? *p : __ldcs(p);
+        if (W == 8 && (STAGED || e + W <= n)) {
+            const uint2* p = reinterpret_cast<const uint2*>(q + e);
+            const uint2 a = STAGED ? *p : __ldcs(p);
+            w[0] = a.x;
+            w[1] = a.y;
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                if (STAGED || e + j < n) w[i / 4] |= static_cast<unsigned>(q[e + j]) << (8 * ((i + j) & 3));
+                if (STAGED || e + j < n) w[(i + j) / 4] |= static_cast<unsigned>(q[e + j]) << (8 * ((i + j) & 3));
         }
     }
 #pragma unroll
@@ -233,8 +260,8 @@ __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 // in the normal range 20 of 23 places are cut off, and the number is added below them
-                const unsigned r = POSITIVE ? random[i + j] >> 12 & 0xffff0u : (random[i + j] & 0xffffu) << 4;
-                z[j] = __uint_as_float((__float_as_uint(y[i + j]) + r) & 0xfff00000u);
+                const unsigned r = POSITIVE ? random[i + j] >> 16 : random[i + j] & 0xffffu;
+                z[j] = __uint_as_float((__float_as_uint(y[i + j]) + 16u * r) & 0xfff00000u);
             }
         w[i / 4] |= static_cast<unsigned>(__nv_cvt_float2_to_fp8x2(make_float2(z[0], z[1]), __NV_SATFINITE, __NV_E4M3)) << (8 * (i & 2));
     }
@@ -256,12 +283,12 @@ __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += W) {
         const long long e = adam_place<W>(at, i);
-        if (W == 4 && (WHOLE || e + W <= n)) {
-            __stcs(reinterpret_cast<unsigned*>(to + e), w[i / 4]);
+        if (W == 8 && (WHOLE || e + W <= n)) {
+            __stcs(reinterpret_cast<uint2*>(to + e), make_uint2(w[0], w[1]));
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                if (WHOLE || e + j < n) to[e + j] = static_cast<uint8_t>(w[i / 4] >> (8 * ((i + j) & 3)));
+                if (WHOLE || e + j < n) to[e + j] = static_cast<uint8_t>(w[(i + j) / 4] >> (8 * ((i + j) & 3)));
         }
     }
     uint8_t* s = scale + (at >> 5);
@@ -288,6 +315,12 @@ __device__ __forceinline__ void adam_randoms(uint32_t (&random)[ADAM_N], long lo
 #pragma unroll
             for (int j = 1; j < W; ++j) random[i + j] = adam_random(first + j, key);
     }
+}
+// Subnormal v count as 0 where issue slots are what bounds the kernel.
+template <bool STATE8>
+__device__ __forceinline__ void adam_root(float& root, float v) {
+    if (STATE8) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v));
+    else asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
 }
 // Eight elements of each of a warp's lanes: at `at` of the tensor, and `in` of the inputs.
 template <int W, bool STATE8, bool STOCHASTIC, bool STAGED>
@@ -317,8 +350,8 @@ __device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, 
         f2_get(m2, m[i], m[i + 1]);
         f2_get(v2, v[i], v[i + 1]);
         float root[2], inverse[2];
-        asm("sqrt.approx.f32 %0, %1;" : "=f"(root[0]) : "f"(v[i]));
-        asm("sqrt.approx.f32 %0, %1;" : "=f"(root[1]) : "f"(v[i + 1]));
+        adam_root<STATE8>(root[0], v[i]);
+        adam_root<STATE8>(root[1], v[i + 1]);
         f2_get(f2_fma(f2(root[0], root[1]), root2, eps), inverse[0], inverse[1]);
         // (root <= 2^64 and eps >= 2^-126: far inside the range)
         asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(inverse[0]));
@@ -426,7 +459,7 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
             const AdamEntry& e = l.e[lo];
             t.entry = lo;
             t.base = static_cast<long long>(c - e.first) * TRIP;
-            t.staged = W == 4 ? t.base + TRIP <= e.n : t.base > 0 && t.base + TRIP + 16 <= e.n;
+            t.staged = W > 1 ? t.base + TRIP <= e.n : t.base > 0 && t.base + TRIP + 16 <= e.n;
         }
         trips[stage] = t;
         if (!t.staged) {
@@ -467,7 +500,7 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
             const char* src = adam_smem + stage * ring.stage_bytes;
             const int g = e.flags & ADAM_GRAD_FP32 ? 4 : 2, w = e.master || (e.flags & ADAM_PARAM_FP32) ? 4 : 2, st = STATE8 ? 1 : 4;
             const void* weight = e.master ? static_cast<const void*>(e.master) : e.param;
-            const AdamInputs in = W == 4 ? AdamInputs{src, src + ring.weight_at, src + ring.m_at, src + ring.v_at}
+            const AdamInputs in = W > 1 ? AdamInputs{src, src + ring.weight_at, src + ring.m_at, src + ring.v_at}
                                          : AdamInputs{src + adam_skew(e.grad, t.base * g), src + ring.weight_at + adam_skew(weight, t.base * w),
                                                       src + ring.m_at + adam_skew(e.m, t.base * st), src + ring.v_at + adam_skew(e.v, t.base * st)};
 #pragma unroll
@@ -507,7 +540,7 @@ static cudaError_t launch_adam_list(const AdamList<ADAM_CAP>& l, const AdamParam
         if (l.e[i].flags & ADAM_GRAD_FP32) grad = 4;
         if (l.e[i].master || (l.e[i].flags & ADAM_PARAM_FP32)) weight = 4;
     }
-    auto room = [](int size) { return adam_trip(STATE8) * size + (W == 4 ? 0 : 128); };
+    auto room = [](int size) { return adam_trip(STATE8) * size + (W > 1 ? 0 : 128); };
     AdamRing ring;
     ring.weight_at = room(grad);
     ring.m_at = ring.weight_at + room(weight);
@@ -537,7 +570,7 @@ static cudaError_t launch_adam_list(const AdamList<ADAM_CAP>& l, const AdamParam
     const cudaError_t e = allow(reinterpret_cast<const void*>(kern), some);
     return e == cudaSuccess ? launch_pdl(kern, ctas, ADAM_THREADS, smem, stream, 1, few, p, s, ring) : e;
 }
-template <int W>
+template <bool VECTORS>
 static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, const AdamStep& s, cudaStream_t stream) {
     long long place = 0;
     for (int at = 0; at < t.n;) {
@@ -563,14 +596,15 @@ static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, 
             auto bits = [](const void* q) { return reinterpret_cast<uintptr_t>(q); };
             const uintptr_t state = bits(e.m) | bits(e.v);
             const bool vectors = ((bits(e.grad) | bits(e.param) | bits(e.master)) & 15) == 0 && (state & 15) == 0;
-            if (vectors != (W == 4)) continue;
+            if (vectors != VECTORS) continue;
             l.e[l.n++] = e;
             trips += (n + adam_trip(state8) - 1) / adam_trip(state8);
         }
         l.trips = static_cast<unsigned>(trips);
         if (l.n == 0) continue;
-        const cudaError_t err = state8 ? (stochastic ? launch_adam_list<W, true, true>(l, p, s, stream) : launch_adam_list<W, true, false>(l, p, s, stream))
-                                       : (stochastic ? launch_adam_list<W, false, true>(l, p, s, stream) : launch_adam_list<W, false, false>(l, p, s, stream));
+        constexpr int W8 = VECTORS ? 8 : 1, W32 = VECTORS ? 4 : 1;
+        const cudaError_t err = state8 ? (stochastic ? launch_adam_list<W8, true, true>(l, p, s, stream) : launch_adam_list<W8, true, false>(l, p, s, stream))
+                                       : (stochastic ? launch_adam_list<W32, false, true>(l, p, s, stream) : launch_adam_list<W32, false, false>(l, p, s, stream));
         if (err != cudaSuccess) return err;
     }
     return cudaSuccess;
@@ -579,8 +613,8 @@ static cudaError_t launch_adam_lists(const AdamTensors& t, const AdamParams& p, 
 // Tensors that lie at odd addresses take launches of their own, behind the others'.
 cudaError_t launch_adamw(const AdamTensors& t, const AdamParams& p, bool state8, bool stochastic, cudaStream_t stream) {
     const AdamStep s = adam_step(p, p.lr, p.step);
-    const cudaError_t e = launch_adam_lists<4>(t, p, state8, stochastic, s, stream);
-    return e == cudaSuccess ? launch_adam_lists<1>(t, p, state8, stochastic, s, stream) : e;
+    const cudaError_t e = launch_adam_lists<true>(t, p, state8, stochastic, s, stream);
+    return e == cudaSuccess ? launch_adam_lists<false>(t, p, state8, stochastic, s, stream) : e;
 }
 
 bool adamw_ranges_overlap(const AdamTensors& t, const AdamParams& p, bool state8, bool* no_memory) {
