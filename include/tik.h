@@ -276,11 +276,11 @@ tik_status tik_token_logprob(tik_ctx* ctx, const void* hidden, const void* lm_he
  * each term of a sum but the target's is off by 2^-8 of itself at most.  A token with d_logprob 0 (masked) takes no part, whatever
  * its target and lse; one whose target is outside [0, V) gives no gradient and raises TIK_DEV_BAD_TARGET.  hidden must be finite, masked
  * tokens' rows included.
- * Deterministic: fixed orders, no atomics on values.  Outputs overlap neither inputs nor each other.
+ * Deterministic: fixed orders, no atomics on values.  Outputs overlap neither inputs nor each other (TIK_ERR_INVALID_ARG).
  * H must be a multiple of 64, V <= 2^30, T < 2^31 - 256.  ws: tik_workspace_bytes(TIK_OP_TOKEN_LOGPROB_BWD, T, ..., H, V) bytes (d_z
  * of a vocabulary chunk, 2 GiB at most up to T = 2^22, fp32 sums, gathered rows); concurrent calls (and captured graphs that may run at the
- * same time) need buffers of their own.  Two kernels where T > 256, per vocabulary chunk one and one more for each gradient, and one at the
- * end for d_hidden. */
+ * same time) need buffers of their own.  Two kernels where T > 256, per vocabulary chunk one and one more for each
+ * gradient (small calls: for both), and one at the end for d_hidden. */
 tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const void* hidden, const void* lm_head,
                                  const int32_t* target_ids, const float* lse, void* d_hidden, void* d_lm_head, int lm_head_dtype,
                                  int accumulate, int64_t T, int H, int V, float inv_temperature, void* ws, size_t ws_bytes,

@@ -529,6 +529,11 @@ __global__ void __launch_bounds__(ADAM_THREADS, adam_ctas_per_sm(W, STATE8)) ada
         }
         __syncwarp();
     }
+    if (*static_cast<volatile int*>(&abort_word)) {          // let copies in flight finish before shared memory is released
+        const unsigned long long t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 1000000ull) {
+        }
+    }
 }
 
 template <int W, bool STATE8, bool STOCHASTIC>

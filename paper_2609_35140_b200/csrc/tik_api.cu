@@ -670,6 +670,23 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     }
     if (!d_logprob || !hidden || !lm_head || !target_ids || !lse) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
     if (T >= (1ll << 31) - 256) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31 - 256");
+    {
+        struct Range {
+            const void* p;
+            size_t bytes;
+        };
+        const size_t rows = static_cast<size_t>(T), width = static_cast<size_t>(H), words = static_cast<size_t>(V);
+        const Range in[] = {{hidden, rows * width * 2}, {lm_head, words * width * 2}, {d_logprob, rows * 4}, {target_ids, rows * 4}, {lse, rows * 4}};
+        const Range out[] = {{d_hidden, rows * width * 2}, {d_lm_head, words * width * (lm_head_dtype == TIK_DTYPE_FP32 ? 4 : 2)}};
+        auto meet = [](const Range& a, const Range& b) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+            return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+        };
+        bool overlap = meet(out[0], out[1]);
+        for (const Range& o : out)
+            for (const Range& i : in) overlap = overlap || meet(o, i);
+        if (overlap) return fail(ctx, TIK_ERR_INVALID_ARG, "an output overlaps an input or the other output");
+    }
     const LogprobBwdPlan g = logprob_bwd_plan(T, H, V);
     if (!ws || ws_bytes < g.bytes) return fail(ctx, TIK_ERR_WORKSPACE, "log-prob gradient workspace too small");
 
@@ -702,7 +719,7 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.chunk);
     const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, uT}, rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2};
     const uint32_t rows[2] = {64, 128}, slab[2] = {64, 64}, rows4[2] = {32, 128};    // K-major operands and bf16 output, MN-major, fp32 output
-    LogprobBwdMaps m;
+    LogprobBwdMaps m{};
     std::string err;
     bool ok = make_tmap_bf16(ctx, &m.hidden_k, rows_of, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
               make_tmap_bf16(ctx, &m.hidden_mn, rows_of, 2, xd, rowH, slab, &err) && make_tmap_bf16(ctx, &m.head_mn, lm_head, 2, wd, rowH, slab, &err) &&

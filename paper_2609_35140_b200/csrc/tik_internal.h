@@ -221,7 +221,7 @@ struct LogprobBwdParams {
     // of one launch
     int v0, nv;                  // the vocabulary's columns of this chunk
     int ldz;                     // columns of d_z, those of a whole chunk
-    int add;                     // the output is added to
+    int add_table, add_hidden;   // the outputs are added to
 };
 struct LogprobBwdPlan {
     int chunks, chunk;           // of the vocabulary, columns of one (a multiple of 256)

@@ -11,7 +11,7 @@
 // Tokens without a gradient (d_logprob 0: prompts, padding) take no part.  In calls of more than one row tile the others' rows are
 // gathered first, and everything after goes by their number, which stays on the device: the persistent grids read it.
 //
-// One kernel for all three products (KIND), persistent CTA pairs that walk units of one 256 x 256 output tile each: a TMA warp streams
+// One kernel, launched for DZ and then for the gradients: persistent CTA pairs that walk units of one 256 x 256 output tile each: a TMA warp streams
 // 64-wide slices of the contracted axis through a ring, an MMA warp issues M256 x N256 x K16 MMAs into one of two
 // accumulators, eight epilogue warps take the other one out through shared memory and tiled TMA stores.  An operand whose
 // contracted axis is not its contiguous one is read as it lies (MN-major descriptors): nothing is transposed.
@@ -19,7 +19,7 @@
 //   TABLE   A = d_z (M-major),     B = hidden (N-major)        rows: vocabulary, columns: H,        contracted: tokens
 //   HIDDEN  A = d_z (K-major),     B = lm_head (N-major)       rows: tokens,   columns: H,          contracted: vocabulary
 // HIDDEN has few tiles with a long contracted axis (4001 x 3584: 224 tiles, 2376 slices, for 74 pairs), so the tiles of the last,
-// partial round are split along it, into parts that are summed in ascending order by lpb_fold_kernel.  Vocabularies whose d_z
+// partial round are split along it, into parts that are summed in ascending order by lpb_fold_kernel; TABLE's many short units follow.  Vocabularies whose d_z
 // exceeds the scratch are taken in chunks; the sums behind d_hidden then grow in fp32, one addition an element and chunk, in order.
 #include "tik_core.cuh"
 #include "tik_internal.h"
@@ -28,7 +28,7 @@
 namespace tik {
 
 namespace lpb {
-constexpr int DZ = 0, TABLE = 1, HIDDEN = 2;
+constexpr int DZ = 0, TABLE = 1, HIDDEN = 2, BOTH = 3;        // what a launch does
 constexpr int TILE = 256;                    // rows (of a pair) and columns of a unit
 constexpr uint32_t OP_BYTES = 128 * 128;     // an operand's share of a stage: 128 rows or columns x 64 of the contracted axis
 constexpr uint32_t STAGE_BYTES = 2 * OP_BYTES;
@@ -86,9 +86,9 @@ __device__ __forceinline__ void lpb_take_tensor_memory(volatile uint32_t* slot) 
 // What a launch has to do, by the number of rows that take part.
 struct LpbShape {
     int rows;                    // tokens
-    int row_tiles, col_tiles, units;
-    int slices;                  // of 64 of the contracted axis
+    int tokens, words, channels; // tiles of 256 of the tokens, the chunk's vocabulary, H
     int whole, split;            // HIDDEN: tiles done whole, parts of each of the others
+    int hidden_units, units;     // BOTH: HIDDEN's units come first
 };
 // The tiles of the last round of pairs, split so that the round costs least in slices, a unit's epilogue and first loads counting as
 // six and a part's way through memory as a quarter.
@@ -109,57 +109,60 @@ __host__ __device__ inline LpbRest lpb_rest(const LogprobBwdParams& p, int rows)
     if (r.most > 64) r.most = 64;
     return r;
 }
-template <int KIND>
-__device__ __forceinline__ LpbShape lpb_shape(const LogprobBwdParams& p) {
+__device__ __forceinline__ LpbShape lpb_shape(const LogprobBwdParams& p, int kind) {
     using namespace lpb;
     LpbShape g;
     g.rows = p.count ? __ldcg(p.count) : static_cast<int>(p.T);
-    const int tokens = (g.rows + TILE - 1) / TILE, words = (p.nv + TILE - 1) / TILE, channels = (p.H + TILE - 1) / TILE;
-    g.row_tiles = KIND == TABLE ? words : tokens;
-    g.col_tiles = KIND == DZ ? words : channels;
-    g.units = g.row_tiles * g.col_tiles;
-    g.slices = KIND == DZ ? p.H / 64 : KIND == TABLE ? (g.rows + 63) / 64 : (p.nv + 63) / 64;
-    g.whole = g.units;
-    g.split = 1;
-    if (KIND == HIDDEN) {
-        const int rest = g.units % PAIRS;
-        g.whole = g.units - rest;
-        g.split = p.count ? __ldcg(p.count + 1) : p.split;
-        g.units = g.whole + rest * g.split;
-    }
+    g.tokens = (g.rows + TILE - 1) / TILE;
+    g.words = (p.nv + TILE - 1) / TILE;
+    g.channels = (p.H + TILE - 1) / TILE;
+    const int tiles = g.tokens * g.channels, rest = tiles % PAIRS;
+    g.whole = tiles - rest;
+    g.split = p.count ? __ldcg(p.count + 1) : p.split;
+    g.hidden_units = kind == HIDDEN || kind == BOTH ? g.whole + rest * g.split : 0;
+    g.units = kind == DZ ? g.tokens * g.words : g.hidden_units + (kind == HIDDEN ? 0 : g.words * g.channels);
     return g;
 }
 
 struct LpbUnit {
+    bool table;                  // TABLE's, of the gradients'
     int row, col;                // of the output tile
     int k0, k1;                  // slices of 64 of the contracted axis
     int slot;                    // HIDDEN: part of a split tile (its place in the parts' buffer), -1: a whole tile
 };
 template <int KIND>
-__device__ __forceinline__ LpbUnit lpb_unit(const LpbShape& g, int u) {
+__device__ __forceinline__ LpbUnit lpb_unit(const LogprobBwdParams& p, const LpbShape& g, int u) {
     using namespace lpb;
     LpbUnit x;
     x.slot = -1;
     x.k0 = 0;
-    x.k1 = g.slices;
+    x.table = KIND == TABLE || (KIND == BOTH && u >= g.hidden_units);
     if (KIND == DZ) {
         // token tiles fastest inside a band, so that the pairs at work share a few steps of lm_head
-        const int per_band = BAND * g.col_tiles, band = u / per_band, rem = u - band * per_band;
-        const int tiles = min(BAND, g.row_tiles - band * BAND);
+        const int per_band = BAND * g.words, band = u / per_band, rem = u - band * per_band;
+        const int tiles = min(BAND, g.tokens - band * BAND);
         x.row = (band * BAND + rem % tiles) * TILE;
         x.col = rem / tiles * TILE;
-    } else {
-        int tile = u;
-        if (KIND == HIDDEN && u >= g.whole) {
-            const int rest = g.row_tiles * g.col_tiles - g.whole, q = u - g.whole, part = q / rest;
+        x.k1 = p.H / 64;
+        return x;
+    }
+    int tile = u;
+    if (!x.table) {
+        const int slices = (p.nv + 63) / 64;
+        x.k1 = slices;
+        if (u >= g.whole) {
+            const int rest = g.tokens * g.channels - g.whole, q = u - g.whole, part = q / rest;
             tile = g.whole + q % rest;
-            x.k0 = static_cast<int>(static_cast<long long>(g.slices) * part / g.split);
-            x.k1 = static_cast<int>(static_cast<long long>(g.slices) * (part + 1) / g.split);
+            x.k0 = static_cast<int>(static_cast<long long>(slices) * part / g.split);
+            x.k1 = static_cast<int>(static_cast<long long>(slices) * (part + 1) / g.split);
             x.slot = q;
         }
-        x.row = tile / g.col_tiles * TILE;
-        x.col = tile % g.col_tiles * TILE;
+    } else {
+        tile = u - g.hidden_units;
+        x.k1 = (g.rows + 63) / 64;
     }
+    x.row = tile / g.channels * TILE;
+    x.col = tile % g.channels * TILE;
     return x;
 }
 
@@ -199,17 +202,14 @@ __device__ __forceinline__ void lpb_add_row(uint32_t (&v)[N], float a, const __n
 }
 
 template <int KIND>
-__global__ void __launch_bounds__(lpb::THREADS, 1)
-lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmOut,
-           const __grid_constant__ CUtensorMap tmPart, const LogprobBwdParams p) {
+__global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_constant__ LogprobBwdMaps maps, const __grid_constant__ LogprobBwdParams p) {
     using namespace lpb;
-    constexpr bool A_MN = KIND == TABLE, B_MN = KIND != DZ;
-    constexpr uint32_t IDESC = mma_idesc_bf16(256, TILE, B_MN, A_MN);
+    constexpr bool GRADS = KIND != DZ, TABLES = KIND == TABLE || KIND == BOTH;
     const int tid = threadIdx.x, warp = warp_uniform(tid >> 5), lane = tid & 31;
     const uint32_t rank = cluster_ctarank();     // 0 = the CTA that issues the pair's MMAs
     const int first = static_cast<int>(blockIdx.x >> 1), stride = static_cast<int>(gridDim.x >> 1);
     __shared__ LpbShape shape;
-    __shared__ int hits[KIND == TABLE ? 8 : 1][KIND == TABLE ? HITS : 1];
+    __shared__ int hits[TABLES ? 8 : 1][TABLES ? HITS : 1];
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -233,16 +233,15 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             mbar_init(bar_acc_empty + 8 * b, 16);            // the epilogue warps of both CTAs
         }
         fence_barrier_init();
-        tma_prefetch_desc(&tmA);
-        tma_prefetch_desc(&tmB);
-        tma_prefetch_desc(&tmOut);
-        if (KIND == HIDDEN) tma_prefetch_desc(&tmPart);
+        tma_prefetch_desc(&maps.dz_out);
+        tma_prefetch_desc(GRADS ? &maps.head_mn : &maps.head_k);
+        tma_prefetch_desc(GRADS ? &maps.hidden_mn : &maps.hidden_k);
     }
     if (warp == 1) lpb_take_tensor_memory(tmem_slot);
     pdl_wait();
     if (tid == 0) {
         *abort_word = (*reinterpret_cast<volatile int*>(p.dev_status) & TIK_DEV_WAIT_EXPIRED) ? 1 : 0;
-        shape = lpb_shape<KIND>(p);
+        shape = lpb_shape(p, KIND);
     }
     tc_fence_before();
     __syncthreads();
@@ -262,7 +261,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         if (lane == 0) {
             uint32_t it = 0;
             for (int u = first; u < g.units; u += stride) {
-                const LpbUnit x = lpb_unit<KIND>(g, u);
+                const LpbUnit x = lpb_unit<KIND>(p, g, u);
                 // each CTA stages its own 128 rows of A and its half of B; what lies outside the tensors arrives as zeros
                 const int a0 = x.row + half, b0 = x.col + half;
                 for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
@@ -271,18 +270,21 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     const uint32_t use = it / STAGES, dst = sbase + s * STAGE_BYTES;
                     if (use > 0) mbar_wait(bar_empty + 8 * s, (use - 1) & 1, abort_word, p.dev_status);
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * STAGE_BYTES);   // both CTAs' bytes
-                    if (A_MN) {
-                        tma_load_2d_pair(dst, &tmA, lead_full + 8 * s, a0, kb * 64);
-                        tma_load_2d_pair(dst + OP_BYTES / 2, &tmA, lead_full + 8 * s, a0 + 64, kb * 64);
+                    const uint32_t bar = lead_full + 8 * s;
+                    if (!GRADS) {
+                        tma_load_2d_pair(dst, &maps.hidden_k, bar, kb * 64, a0);
+                        tma_load_2d_pair(dst + OP_BYTES, &maps.head_k, bar, kb * 64, p.v0 + b0);
                     } else {
-                        tma_load_2d_pair(dst, &tmA, lead_full + 8 * s, kb * 64, a0);
-                    }
-                    if (B_MN) {
-                        const int k = kb * 64 + (KIND == HIDDEN ? p.v0 : 0);
-                        tma_load_2d_pair(dst + OP_BYTES, &tmB, lead_full + 8 * s, b0, k);
-                        tma_load_2d_pair(dst + OP_BYTES + OP_BYTES / 2, &tmB, lead_full + 8 * s, b0 + 64, k);
-                    } else {
-                        tma_load_2d_pair(dst + OP_BYTES, &tmB, lead_full + 8 * s, kb * 64, p.v0 + b0);
+                        if (x.table) {
+                            tma_load_2d_pair(dst, &maps.dz_mn, bar, a0, kb * 64);
+                            tma_load_2d_pair(dst + OP_BYTES / 2, &maps.dz_mn, bar, a0 + 64, kb * 64);
+                        } else {
+                            tma_load_2d_pair(dst, &maps.dz_out, bar, kb * 64, a0);
+                        }
+                        const CUtensorMap* const b = x.table ? &maps.hidden_mn : &maps.head_mn;
+                        const int k = kb * 64 + (x.table ? 0 : p.v0);
+                        tma_load_2d_pair(dst + OP_BYTES, b, bar, b0, k);
+                        tma_load_2d_pair(dst + OP_BYTES + OP_BYTES / 2, b, bar, b0 + 64, k);
                     }
                 }
             }
@@ -293,7 +295,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             const uint32_t tmem_u = warp_uniform(tmem);
             uint32_t it = 0, acc = 0;
             for (int u = first; u < g.units; u += stride, ++acc) {
-                const LpbUnit x = lpb_unit<KIND>(g, u);
+                const LpbUnit x = lpb_unit<KIND>(p, g, u);
                 const int buf = acc & 1;
                 const uint32_t use = acc >> 1;
                 if (use > 0) mbar_wait_warp(bar_acc_empty + 8 * buf, (use - 1) & 1, abort_word, p.dev_status);
@@ -305,9 +307,15 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     tc_fence_after();
                     const uint32_t a = sbase + s * STAGE_BYTES, b = a + OP_BYTES;
                     // MN-major: 64 columns of the axis per 128-byte row, the next 64 half an operand further
-                    mma_ss_chain4_pair_steps<A_MN ? 128 : 2, B_MN ? 128 : 2>(
-                        tmem_u + buf * TILE, smem_desc_sw128(a, A_MN ? OP_BYTES / 2 : 0, 1024),
-                        smem_desc_sw128(b, B_MN ? OP_BYTES / 2 : 0, 1024), IDESC, kb > x.k0 ? 1u : 0u);
+                    const uint32_t more = kb > x.k0 ? 1u : 0u, d = tmem_u + buf * TILE;
+                    if (!GRADS)
+                        mma_ss_chain4_pair_steps<2, 2>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, 0, 1024), mma_idesc_bf16(256, TILE, false, false), more);
+                    else if (x.table)
+                        mma_ss_chain4_pair_steps<128, 128>(d, smem_desc_sw128(a, OP_BYTES / 2, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024),
+                                                           mma_idesc_bf16(256, TILE, true, true), more);
+                    else
+                        mma_ss_chain4_pair_steps<2, 128>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024),
+                                                         mma_idesc_bf16(256, TILE, true, false), more);
                     mma_commit_pair(bar_empty + 8 * s);
                     mma_commit_pair(peer_empty + 8 * s);
                 }
@@ -331,11 +339,11 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             return smem + OFF_STG + (2 * group + (piece++ & 1)) * STG_BYTES;
         };
         for (int u = first; u < g.units; u += stride, ++acc) {
-            const LpbUnit x = lpb_unit<KIND>(g, u);
+            const LpbUnit x = lpb_unit<KIND>(p, g, u);
             const int buf = acc & 1, row0 = x.row + half;
             float c = 0.0f, lse2 = 0.0f;
             int target = -1;
-            if (KIND == DZ) {
+            if (!GRADS) {
                 if (row0 + row < g.rows) {
                     const int t = p.index ? p.index[row0 + row] : row0 + row;
                     target = p.target[t];
@@ -351,7 +359,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             int nhits = 0;                                 // tokens whose targets are this warp's rows
             unsigned mine = 0;                             // ... and this lane's, of those in the list
             const int first_row = p.v0 + row0 + quarter * 32;
-            if (KIND == TABLE) {
+            const bool table = TABLES && x.table;
+            if (table) {
                 lpb_targets(p.row_target, g.rows, first_row, lane, [&](int t, int r) {
                     if (nhits < HITS) {
                         if (lane == 0) hits[warp - 2][nhits] = t;
@@ -378,10 +387,10 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             mbar_wait(bar_acc_full + 8 * buf, (acc >> 1) & 1, abort_word, p.dev_status);
             tc_fence_after();
             const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TILE;
-            const bool f32_out = KIND == HIDDEN || (KIND == TABLE && p.table_fp32);
+            const bool f32_out = GRADS && (!table || p.table_fp32);
             if (!f32_out) {
-                const int limit = KIND == DZ ? p.ldz : p.H;
-                const float scale2 = KIND == DZ ? __fmul_rn(p.inv_temperature, LOG2E_F) : 0.0f;
+                const int limit = !GRADS ? p.ldz : p.H;
+                const float scale2 = !GRADS ? __fmul_rn(p.inv_temperature, LOG2E_F) : 0.0f;
 #pragma unroll 1
                 for (int q = group; q < TILE / 64; q += 2) {
                     if (x.col + 64 * q >= limit) break;    // uniform: columns past the output
@@ -389,12 +398,12 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     tmem_ld32(taddr + 64 * q, *reinterpret_cast<uint32_t(*)[32]>(&v[0]));
                     tmem_ld32(taddr + 64 * q + 32, *reinterpret_cast<uint32_t(*)[32]>(&v[32]));
                     tmem_wait_ld();
-                    if (KIND == TABLE && x.k1 == 0) {      // no token takes part: the accumulator was not written
+                    if (table && x.k1 == 0) {      // no token takes part: the accumulator was not written
 #pragma unroll
                         for (int i = 0; i < 64; ++i) v[i] = 0u;
                     }
-                    if (KIND == TABLE && nhits > 0) add_lost(v, x.col + 64 * q);
-                    if (KIND == DZ) {
+                    if (table && nhits > 0) add_lost(v, x.col + 64 * q);
+                    if (!GRADS) {
                         const int valid = p.nv - x.col - 64 * q, hit = target - 64 * q;
                         float at_hit = 0.0f;
 #pragma unroll
@@ -421,7 +430,7 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     fence_proxy_async_smem();
                     named_bar_sync(1 + group, 128);
                     if (storer) {
-                        tma_store_2d(&tmOut, smem_u32(stg), x.col + 64 * q, KIND == TABLE ? p.v0 + row0 : row0);
+                        tma_store_2d(GRADS ? &maps.table_out : &maps.dz_out, smem_u32(stg), x.col + 64 * q, GRADS ? p.v0 + row0 : row0);
                         tma_store_commit();
                     }
                 }
@@ -432,11 +441,11 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     uint32_t v[32];
                     tmem_ld32(taddr + 32 * q, v);
                     tmem_wait_ld();
-                    if (KIND == TABLE && x.k1 == 0) {
+                    if (table && x.k1 == 0) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
                     }
-                    if (KIND == TABLE && nhits > 0) add_lost(v, x.col + 32 * q);
+                    if (table && nhits > 0) add_lost(v, x.col + 32 * q);
                     uint8_t* const stg = stage();
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16)
@@ -445,10 +454,10 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     fence_proxy_async_smem();
                     named_bar_sync(1 + group, 128);
                     if (storer) {
-                        const bool part = KIND == HIDDEN && x.slot >= 0;
-                        const CUtensorMap* to = part ? &tmPart : &tmOut;
-                        const int c0 = (part ? 0 : x.col) + 32 * q, c1 = part ? x.slot * TILE + half : KIND == TABLE ? p.v0 + row0 : row0;
-                        if (p.add) tma_add_2d(to, smem_u32(stg), c0, c1);
+                        const bool part = x.slot >= 0;
+                        const CUtensorMap* to = table ? &maps.table_out : part ? &maps.part_out : &maps.sum_out;
+                        const int c0 = (part ? 0 : x.col) + 32 * q, c1 = part ? x.slot * TILE + half : table ? p.v0 + row0 : row0;
+                        if (table ? p.add_table : p.add_hidden) tma_add_2d(to, smem_u32(stg), c0, c1);
                         else tma_store_2d(to, smem_u32(stg), c0, c1);
                         tma_store_commit();
                     }
@@ -478,8 +487,8 @@ lpb_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
 __global__ void __launch_bounds__(256) lpb_fold_kernel(const LogprobBwdParams p) {
     pdl_wait();
     pdl_launch_dependents();
-    const LpbShape g = lpb_shape<lpb::HIDDEN>(p);
-    const int per_row = p.H / 4, rest = g.row_tiles * g.col_tiles - g.whole;
+    const LpbShape g = lpb_shape(p, lpb::HIDDEN);
+    const int per_row = p.H / 4, rest = g.tokens * g.channels - g.whole;
     const long long n = p.T * per_row;
     for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<long long>(gridDim.x) * 256) {
         const long long row = i / per_row;
@@ -493,7 +502,7 @@ __global__ void __launch_bounds__(256) lpb_fold_kernel(const LogprobBwdParams p)
                 w = *reinterpret_cast<const uint2*>(p.head + static_cast<long long>(target) * p.H + h);
                 lost = p.rho[t];
             }
-            const int tile = t / lpb::TILE * g.col_tiles + h / lpb::TILE;
+            const int tile = t / lpb::TILE * g.channels + h / lpb::TILE;
             if (tile < g.whole) {
                 f = *reinterpret_cast<const float4*>(p.sum + static_cast<long long>(t) * p.H + h);
             } else {
@@ -640,18 +649,17 @@ LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V) {
 }
 
 template <int KIND>
-static cudaError_t launch_lpb(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmOut, const CUtensorMap& tmPart,
-                              const LogprobBwdParams& p, cudaStream_t stream) {
+static cudaError_t launch_lpb(const LogprobBwdMaps& maps, const LogprobBwdParams& p, cudaStream_t stream) {
     auto kern = lpb_kernel<KIND>;
     static DeviceOnce configured;     // the opt-in belongs to the (function, device) pair
     cudaError_t e = configured.run([&]() {
         return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lpb::ALLOC));
     });
     if (e != cudaSuccess) return e;
+    // no more pairs than there may be units
     const long long tokens = (p.T + 255) / 256, words = (p.nv + 255) / 256, channels = (p.H + 255) / 256;
-    const long long units = KIND == lpb::DZ ? tokens * words : KIND == lpb::TABLE ? words * channels : lpb::MOST_PARTS;
-    return launch_pdl(kern, dim3(static_cast<unsigned>(2 * std::min<long long>(p.pairs, units))), lpb::THREADS, lpb::ALLOC, stream, 2, tmA, tmB,
-                      tmOut, tmPart, p);
+    const long long units = KIND == lpb::DZ ? tokens * words : KIND == lpb::HIDDEN ? lpb::MOST_PARTS : words * channels + (KIND == lpb::BOTH ? lpb::MOST_PARTS : 0);
+    return launch_pdl(kern, dim3(static_cast<unsigned>(2 * std::min<long long>(p.pairs, units))), lpb::THREADS, lpb::ALLOC, stream, 2, maps, p);
 }
 
 cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, const void* hidden, bool add_table, int sm_count,
@@ -675,18 +683,18 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
     for (int c = 0; c < g.chunks; ++c) {
         p.v0 = c * g.chunk;
         p.nv = std::min(g.chunk, p.V - p.v0);
-        e = launch_lpb<lpb::DZ>(m.hidden_k, m.head_k, m.dz_out, m.dz_out, p, stream);
+        p.add_table = add_table;
+        p.add_hidden = c > 0;
+        e = launch_lpb<lpb::DZ>(m, p, stream);
+        // Both gradients in one launch where d_lm_head is a few rounds of units and launches are what a call takes (256 x 256, vocabulary
+        // 2048: 27.1 -> 21.5 us).  In long calls the pairs come to d_lm_head's units one after the other and no longer share their
+        // operands in L2 (501 x 1536, vocabulary 151 936: 647 us apart, 659 together).
+        const int words = (p.nv + 255) / 256, channels = (p.H + 255) / 256;
+        const bool both = p.want_table && p.d_hidden && static_cast<long long>(words) * channels <= 4 * lpb::PAIRS;
+        if (both && e == cudaSuccess) e = launch_lpb<lpb::BOTH>(m, p, stream);
+        if (!both && p.want_table && e == cudaSuccess) e = launch_lpb<lpb::TABLE>(m, p, stream);
+        if (!both && p.d_hidden && e == cudaSuccess) e = launch_lpb<lpb::HIDDEN>(m, p, stream);
         if (e != cudaSuccess) return e;
-        if (p.want_table) {
-            p.add = add_table;
-            e = launch_lpb<lpb::TABLE>(m.dz_mn, m.hidden_mn, m.table_out, m.table_out, p, stream);
-            if (e != cudaSuccess) return e;
-        }
-        if (p.d_hidden) {
-            p.add = c > 0;
-            e = launch_lpb<lpb::HIDDEN>(m.dz_out, m.head_mn, m.sum_out, m.part_out, p, stream);
-            if (e != cudaSuccess) return e;
-        }
     }
     if (!p.d_hidden) return cudaSuccess;
     const long long n = p.T * (p.H / 4);

@@ -34,7 +34,8 @@ LOGPROB = dict(d=A, x=B, w=C, ids=D, lse=E, dx=F, dw=G, type=0, accumulate=0, T=
     (dict(dx=None, dw=None), INVALID), (dict(H=96), UNSUPPORTED), (dict(V=(1 << 30) + 1), UNSUPPORTED), (dict(d=None), INVALID), (dict(x=None), INVALID),
     (dict(w=None), INVALID), (dict(ids=None), INVALID), (dict(lse=None), INVALID), (dict(x=B + 8), UNSUPPORTED), (dict(w=C + 2), UNSUPPORTED),
     (dict(dx=F + 4), UNSUPPORTED), (dict(dw=G + 8), UNSUPPORTED), (dict(ws=H_ + 8), UNSUPPORTED), (dict(T=(1 << 31) - 256), UNSUPPORTED),
-    (dict(ws=None), WORKSPACE), (dict(ws_bytes=100), WORKSPACE), (dict(T=0, dx=None, dw=None), OK),
+    (dict(dx=B), INVALID), (dict(dx=C + 16), INVALID), (dict(dw=B + 512), INVALID), (dict(dw=F), INVALID), (dict(dw=E), INVALID),
+    (dict(dx=F, dw=F + 624, type=1), INVALID), (dict(ws=None), WORKSPACE), (dict(ws_bytes=100), WORKSPACE), (dict(T=0, dx=None, dw=None), OK),
     (dict(T=0, dw=None, d=None, x=None, ids=None, lse=None), OK), (dict(T=0, type=1, accumulate=1, d=None, x=None, ws=None), OK)])
 def test_logprob_bwd(ctx, changed, code):
     args = dict(LOGPROB, **changed)
