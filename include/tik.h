@@ -305,7 +305,7 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
  *   of r - 1 - x, and their number.
  * fp32 per token, sums over tokens in fp64 in one fixed order: the same inputs give the same bits on every call.  T < 2^31; tensors
  * aligned to their elements.  ws: tik_workspace_bytes(TIK_OP_POLICY_LOSS, T, ..., S as max_ctx, ...) bytes, as above.  One kernel up
- * to 8192 tokens (with weights and per-sequence means also at most 8192 sequences), else two. */
+ * to 4096 tokens (with weights and per-sequence means also at most 8192 sequences), else two. */
 tik_status tik_policy_loss(tik_ctx* ctx, const float* logprob, const float* old_logprob, const float* advantage,
                            int advantage_per_sequence, const float* weight, const float* ref_logprob, const int32_t* cu_seqlens, int S,
                            int64_t T, float clip_low, float clip_high, float clip_dual, float kl_coef, int reduction, float scale,

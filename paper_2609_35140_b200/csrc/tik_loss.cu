@@ -11,8 +11,8 @@
 // logarithms of the thresholds (r in 32 bits would put tokens on the wrong side of a border where the gradient jumps); exp(y) - y - 1 comes
 // from its series, not from a difference; -A r goes into the sum as -A and -A (r - 1), the first exact and the second small.  Sums over tokens,
 // which are of both signs and mostly cancel, are fp64 in one fixed order, counts are integers.  (All of it in fp64 took 275 instructions a token.)
-// 20 bytes in and 4 out per token, so a call is all latency: up to 8192 tokens one cluster of up to eight CTAs takes
-// it in one launch, counts and sums through distributed shared memory.  Longer calls, whose arithmetic needs all
+// 20 bytes in and 4 out per token, so a call is all latency: up to 4096 tokens one cluster of up to eight CTAs takes
+// it in one launch, a token a thread, counts and sums through distributed shared memory.  Longer calls, whose arithmetic needs all
 // SMs, take two: one counts, the other computes, and its last CTA folds the sums.
 #include <cstdlib>
 
@@ -26,7 +26,6 @@ namespace loss {
 constexpr int MAX_CLUSTER = 8;
 constexpr int SEQ_CAP = 8192;                // sequences' counts that a CTA of a cluster holds
 constexpr int STEPS = 4;                     // tokens of a thread at most, one per 32 tokens of its warp's stretch
-constexpr int CLUSTER_STEPS = 2;             // ... of the cluster's
 constexpr int CLUSTER_THREADS = 512;
 constexpr int GRID_THREADS = 256;
 constexpr int MAX_CTAS = 592;                // of the two-launch form
@@ -194,99 +193,74 @@ __device__ __forceinline__ void loss_block_sums(const LossSums& s, double (&v)[l
     loss_block_fold(v, buf, warps);
 }
 
-// One cluster.  A thread holds `steps` tokens (at most STEPS): those of its lane in each 32 of its warp's stretch.
-__global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(const PolicyLossParams p, int steps) {
+// One cluster, a token a thread.
+__global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(const PolicyLossParams p) {
     using namespace loss;
     extern __shared__ int seq_count[];                     // [per]: tokens of the sequences rank * per ...
     __shared__ double sums[CLUSTER_THREADS / 32][SUMS];
     __shared__ double cta_sums[SUMS];
     __shared__ int cta_count;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warps = blockDim.x >> 5;
     const int ctas = static_cast<int>(gridDim.x), rank = static_cast<int>(blockIdx.x);
     const bool per_sequence = p.reduction == LOSS_SEQUENCE_MEAN, count_seq = per_sequence && p.weight;
     const int per = (p.S + ctas - 1) / ctas;
-    const bool find = p.adv_per_seq || per_sequence;
     if (count_seq)
         for (int i = tid; i < per; i += blockDim.x) seq_count[i] = 0;
     if (tid == 0) cta_count = 0;
     pdl_wait();
     pdl_launch_dependents();
-    const int t0 = (rank * warps + warp) * 32 * steps + lane;
-    constexpr int STEPS = CLUSTER_STEPS;
-    float lp[STEPS], old[STEPS], adv[STEPS], w[STEPS], ref[STEPS];
-    int seq[STEPS];
-#pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-        const int t = t0 + 32 * j;
-        const bool in = j < steps && t < p.T;
-        w[j] = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f;
-        lp[j] = in ? p.logprob[t] : 0.0f;
-        old[j] = in ? p.old_logprob[t] : 0.0f;
-        adv[j] = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
-        ref[j] = in && p.ref ? p.ref[t] : 0.0f;
-    }
-    int from, to;
+    const int t = rank * static_cast<int>(blockDim.x) + tid;
+    const bool in = t < p.T;
+    float w = in ? (p.weight ? p.weight[t] : 1.0f) : 0.0f, adv = in && !p.adv_per_seq ? p.advantage[t] : 0.0f;
+    const float lp = in ? p.logprob[t] : 0.0f, old = in ? p.old_logprob[t] : 0.0f, ref = in && p.ref ? p.ref[t] : 0.0f;
+    int from, to, seq = 0;
     loss_range(p, from, to);
-    LossSeq q;
-    if (find) q.begin(p, t0 - lane, lane);
-#pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-        const int t = t0 + 32 * j;
-        if (t < from || t >= to) w[j] = 0.0f;
-        if (find && j < steps) {
-            seq[j] = q.of(p, t, lane);
-            if (p.adv_per_seq && w[j] != 0.0f) adv[j] = p.advantage[seq[j]];
-        }
+    if (t < from || t >= to) w = 0.0f;
+    if (p.adv_per_seq || per_sequence) {
+        LossSeq q;
+        q.begin(p, t - lane, lane);
+        seq = q.of(p, t, lane);
+        if (p.adv_per_seq && w != 0.0f) adv = p.advantage[seq];
     }
     if (ctas > 1) cluster_sync_all();                      // zeroed counts, and every CTA of the cluster has begun
     else __syncthreads();
-    int total = 0;
-#pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-        const unsigned on = __ballot_sync(0xffffffffu, w[j] != 0.0f);
-        total += __popc(on);
-        if (count_seq && j < steps) {
-            // a warp's tokens are mostly of one sequence: one addition for each run of equal ones
-            const int before = __shfl_up_sync(0xffffffffu, seq[j], 1);
-            const unsigned heads = __ballot_sync(0xffffffffu, lane == 0 || before != seq[j]);
-            if (heads >> lane & 1u) {
-                const unsigned later = lane == 31 ? 0u : heads & (0xffffffffu << (lane + 1));
-                const unsigned run = (later ? (1u << (__ffs(later) - 1)) - 1u : 0xffffffffu) & (0xffffffffu << lane);
-                const int n = __popc(on & run), owner = seq[j] / per;
-                if (n > 0) dsmem_add(mapa_cluster(smem_u32(&seq_count[seq[j] - owner * per]), owner), n);
-            }
+    const unsigned on = __ballot_sync(0xffffffffu, w != 0.0f);
+    if (lane == 0 && on) atomicAdd(&cta_count, __popc(on));
+    if (count_seq) {
+        // a warp's tokens are mostly of one sequence: one addition for each run of equal ones
+        const int before = __shfl_up_sync(0xffffffffu, seq, 1);
+        const unsigned heads = __ballot_sync(0xffffffffu, lane == 0 || before != seq);
+        if (heads >> lane & 1u) {
+            const unsigned later = lane == 31 ? 0u : heads & (0xffffffffu << (lane + 1));
+            const unsigned run = (later ? (1u << (__ffs(later) - 1)) - 1u : 0xffffffffu) & (0xffffffffu << lane);
+            const int n = __popc(on & run), owner = seq / per;
+            if (n > 0) dsmem_add(mapa_cluster(smem_u32(&seq_count[seq - owner * per]), owner), n);
         }
     }
-    if (lane == 0 && total > 0) atomicAdd(&cta_count, total);
     if (ctas > 1) cluster_sync_all();
     else __syncthreads();
-    int all = 0;
-    for (int c = 0; c < ctas; ++c) all += dsmem_read_int(mapa_cluster(smem_u32(&cta_count), c));
     double f = p.scale;
-    if (p.reduction == LOSS_TOKEN_MEAN) f /= all > 1 ? all : 1;
-    LossSums mine;
-#pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-        const int t = t0 + 32 * j;
-        if (j >= steps || t >= p.T) break;
-        float d = 0.0f;
-        if (w[j] != 0.0f) {
-            double fj = f * w[j];
-            if (per_sequence) {
-                const int s = seq[j], owner = s / per;
-                const int n = count_seq ? dsmem_read_int(mapa_cluster(smem_u32(&seq_count[s - owner * per]), owner)) : p.cu[s + 1] - p.cu[s];
-                fj /= n > 1 ? n : 1;
-            }
-            d = loss_token(p, fj, lp[j], old[j], adv[j], ref[j], mine);
-        }
-        if (p.d_logprob) p.d_logprob[t] = d;
+    if (p.reduction == LOSS_TOKEN_MEAN) {
+        int all = 0;
+        for (int c = 0; c < ctas; ++c) all += dsmem_read_int(mapa_cluster(smem_u32(&cta_count), c));
+        f /= all > 1 ? all : 1;
     }
+    LossSums mine;
+    float d = 0.0f;
+    if (w != 0.0f) {
+        f *= w;
+        if (per_sequence) {
+            const int owner = seq / per;
+            const int n = count_seq ? dsmem_read_int(mapa_cluster(smem_u32(&seq_count[seq - owner * per]), owner)) : p.cu[seq + 1] - p.cu[seq];
+            f /= n > 1 ? n : 1;
+        }
+        d = loss_token(p, f, lp, old, adv, ref, mine);
+    }
+    if (p.d_logprob && in) p.d_logprob[t] = d;
     double sum[SUMS];
     loss_block_sums(mine, sum, sums, warps);
     if (ctas == 1) {
-        if (tid == 0) {
-            loss_results(p, sum);
-        }
+        if (tid == 0) loss_results(p, sum);
         return;
     }
     if (tid == 0)
@@ -441,15 +415,13 @@ size_t policy_loss_bytes(int64_t S) {
 cudaError_t launch_policy_loss(PolicyLossParams& p, void* ws, cudaStream_t stream) {
     using namespace loss;
     const bool counts_seq = p.reduction == LOSS_SEQUENCE_MEAN && p.weight;
-    const int64_t most = static_cast<int64_t>(MAX_CLUSTER) * CLUSTER_THREADS * CLUSTER_STEPS;
-    if (p.T <= most && (!counts_seq || p.S <= SEQ_CAP)) {
-        // as many CTAs as leave a thread one token, and then as many tokens as it takes
+    // (Two tokens a thread of the cluster: 8000 tokens 8.5 us, 7.0 by two launches; 4000 tokens 6.3 either way, and a launch less of the host.)
+    if (p.T <= MAX_CLUSTER * CLUSTER_THREADS && (!counts_seq || p.S <= SEQ_CAP)) {
         int ctas = 1;
-        while (ctas < MAX_CLUSTER && p.T > static_cast<int64_t>(ctas) * CLUSTER_THREADS) ctas *= 2;
-        const int threads = p.T > CLUSTER_THREADS ? CLUSTER_THREADS : p.T > 32 ? static_cast<int>((p.T + 31) / 32 * 32) : 32;
-        const int steps = static_cast<int>((p.T + static_cast<int64_t>(ctas) * threads - 1) / (static_cast<int64_t>(ctas) * threads));
+        while (p.T > ctas * CLUSTER_THREADS) ctas *= 2;
+        const int threads = p.T > CLUSTER_THREADS ? CLUSTER_THREADS : p.T > 32 ? (p.T + 31) / 32 * 32 : 32;
         const size_t smem = counts_seq ? static_cast<size_t>((p.S + ctas - 1) / ctas) * sizeof(int) : 0;
-        return launch_pdl(loss_cluster_kernel, dim3(ctas), static_cast<unsigned>(threads), smem, stream, static_cast<unsigned>(ctas), p, steps);
+        return launch_pdl(loss_cluster_kernel, dim3(ctas), static_cast<unsigned>(threads), smem, stream, static_cast<unsigned>(ctas), p);
     }
     p.ticket = static_cast<int*>(ws);
     p.part = reinterpret_cast<double*>(static_cast<char*>(ws) + 16);

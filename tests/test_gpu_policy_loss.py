@@ -90,7 +90,7 @@ def both(a, **kw):
     return got
 
 
-@pytest.mark.parametrize("T,S", [(1, 1), (2, 3), (31, 1), (32, 5), (33, 40), (257, 7), (512, 3), (513, 513), (1025, 64), (4099, 17), (8193, 2),
+@pytest.mark.parametrize("T,S", [(1, 1), (2, 3), (31, 1), (32, 5), (33, 40), (257, 7), (512, 3), (513, 513), (1025, 64), (4096, 17), (4097, 2), (8193, 2),
                                  (20000, 700), (32768, 1), (32769, 9), (60013, 64), (70001, 9000), (300007, 1024)])
 @pytest.mark.parametrize("reduction", ["sum", "token", "sequence"])
 def test_lengths(T, S, reduction):

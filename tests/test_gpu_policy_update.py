@@ -189,8 +189,8 @@ def test_launch_counts(tik):
         f()
         return tik.kernel_launches() - n
     z = lambda n: torch.zeros(n, device="cuda")  # noqa: E731
-    assert launches(lambda: tik.tik_policy_loss(z(8192), z(8192), z(8192))) == 1
-    assert launches(lambda: tik.tik_policy_loss(z(8193), z(8193), z(8193))) == 2
+    assert launches(lambda: tik.tik_policy_loss(z(4096), z(4096), z(4096))) == 1
+    assert launches(lambda: tik.tik_policy_loss(z(4097), z(4097), z(4097))) == 2
     x, W = torch.zeros(300, 64, device="cuda", dtype=BF), torch.zeros(500, 64, device="cuda", dtype=BF)
     back = lambda n, **kw: tik.tik_token_logprob_bwd(z(n), x[:n], W, z(n).int(), z(n), **kw)  # noqa: E731
     assert launches(lambda: back(256)) == 3 and launches(lambda: back(257)) == 5
