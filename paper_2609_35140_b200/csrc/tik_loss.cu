@@ -75,6 +75,9 @@ struct LossSums {
     double policy = 0.0, kl = 0.0, remainder = 0.0;
     int cut = 0, tokens = 0;
 };
+// tokens of a sequence, those of the call (without weights: all count)
+__device__ __forceinline__ int loss_length(const PolicyLossParams& p, int s) { return min(p.cu[s + 1], p.T) - max(p.cu[s], 0); }
+
 // Adds a token that counts to the sums and returns its gradient; f: its factor.
 __device__ __forceinline__ float loss_token(const PolicyLossParams& p, double f, float lp, float old, float adv, float ref, LossSums& sum) {
     const float x = lp - old;
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(loss::CLUSTER_THREADS) loss_cluster_kernel(con
         f *= w;
         if (per_sequence) {
             const int owner = seq / per;
-            const int n = count_seq ? dsmem_read_int(mapa_cluster(smem_u32(&seq_count[seq - owner * per]), owner)) : p.cu[seq + 1] - p.cu[seq];
+            const int n = count_seq ? dsmem_read_int(mapa_cluster(smem_u32(&seq_count[seq - owner * per]), owner)) : loss_length(p, seq);
             f /= n > 1 ? n : 1;
         }
         d = loss_token(p, f, lp, old, adv, ref, mine);
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(loss::GRID_THREADS, 4) loss_grid_kernel(const 
             if (w[j] != 0.0f && t >= lo && t < hi) {
                 double fj = f * w[j];
                 if (per_sequence) {
-                    const int n = p.weight ? p.count[s] : p.cu[s + 1] - p.cu[s];
+                    const int n = p.weight ? p.count[s] : loss_length(p, s);
                     fj /= n > 1 ? n : 1;
                 }
                 d = loss_token(p, fj, lp[j], old[j], p.adv_per_seq ? p.advantage[s] : adv[j], ref[j], mine);
