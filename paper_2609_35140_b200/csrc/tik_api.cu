@@ -716,14 +716,14 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     const void* const rows_of = g.gather ? at + g.rows_at : hidden;          // the products' hidden rows
     p.rows = static_cast<const __nv_bfloat16*>(rows_of);
 
-    const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.chunk);
-    const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, uT}, rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2};
+    const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.ldt);
+    const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, static_cast<uint64_t>(g.chunk)}, sd[2] = {uZ, uH}, rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2}, rowZ4[1] = {uZ * 4};
     const uint32_t rows[2] = {64, 128}, slab[2] = {64, 64}, rows4[2] = {32, 128};    // K-major operands and bf16 output, MN-major, fp32 output
     LogprobBwdMaps m{};
     std::string err;
     bool ok = make_tmap_bf16(ctx, &m.hidden_k, rows_of, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
               make_tmap_bf16(ctx, &m.hidden_mn, rows_of, 2, xd, rowH, slab, &err) && make_tmap_bf16(ctx, &m.head_mn, lm_head, 2, wd, rowH, slab, &err) &&
-              make_tmap_bf16(ctx, &m.dz_out, dz, 2, zd, rowZ, rows, &err) && make_tmap_bf16(ctx, &m.dz_mn, dz, 2, zd, rowZ, slab, &err);
+              make_tmap_bf16(ctx, &m.dz_k, dz, 2, zd, rowZ, rows, &err) && make_tmap_bf16(ctx, &m.dz_mn, dz, 2, zd, rowZ, slab, &err);
     if (ok && d_lm_head)
         ok = p.table_fp32 ? make_tmap_f32(ctx, &m.table_out, d_lm_head, 2, wd, rowH4, rows4, &err)
                           : make_tmap_bf16(ctx, &m.table_out, d_lm_head, 2, wd, rowH, rows, &err);
@@ -731,7 +731,7 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
         const uint64_t pd[2] = {256, static_cast<uint64_t>(g.parts) * 256}, rowP[1] = {1024};
         ok = make_tmap_f32(ctx, &m.part_out, p.part, 2, pd, rowP, rows4, &err);
         m.sum_out = m.part_out;                            // (not used by a call of fewer tiles than pairs)
-        if (ok && g.part_at > g.sum_at) ok = make_tmap_f32(ctx, &m.sum_out, p.sum, 2, xd, rowH4, rows4, &err);
+        if (ok && g.part_at > g.sum_at) ok = make_tmap_f32(ctx, &m.sum_out, p.sum, 2, sd, rowZ4, rows4, &err);
     }
     if (!ok) return fail(ctx, TIK_ERR_CUDA, err.c_str());
     cudaError_t e = launch_logprob_bwd(m, p, g, hidden, accumulate != 0, ctx->sm_count, st);

@@ -210,8 +210,8 @@ struct LogprobBwdParams {
     int split;                   // parts of d_hidden's split tiles (without `count`)
     int* dev_status;
     // Scratch.  With `count` (more than one row tile) the rows of the products are the tokens that take part, else all.
-    float* sum;                  // [T][H]: d_hidden's whole tiles
-    float* part;                 // [parts][256][256]: the split ones'
+    float* sum;                  // [H][ldt]: d_hidden's whole tiles
+    float* part;                 // [parts][256 channels][256 tokens]: the split ones'
     float* rho;                  // [row]: what d_z lost of the target's term in rounding
     const int32_t* count;        // [2]: their number, parts of d_hidden's split tiles; or null
     const int32_t* index;        // [row]: token, or null
@@ -220,17 +220,19 @@ struct LogprobBwdParams {
     const __nv_bfloat16* rows;   // [row][H]: their hidden rows
     // of one launch
     int v0, nv;                  // the vocabulary's columns of this chunk
-    int ldz;                     // columns of d_z, those of a whole chunk
+    int chunk;                   // words of a whole chunk
+    int ldt;                     // tokens that a row of d_z and of the sums has room for
     int add_table, add_hidden;   // the outputs are added to
 };
 struct LogprobBwdPlan {
     int chunks, chunk;           // of the vocabulary, columns of one (a multiple of 256)
     int parts;                   // of split tiles at most
+    int ldt;                     // T up to a multiple of 64
     bool gather;
     size_t sum_at, part_at, rho_at, index_at, target_at, place_at, count_at, rows_at, bytes;     // scratch; d_z at 0
 };
 struct LogprobBwdMaps {
-    alignas(64) CUtensorMap hidden_k, head_k, hidden_mn, head_mn, dz_out, dz_mn, table_out, sum_out, part_out;
+    alignas(64) CUtensorMap hidden_k, head_k, hidden_mn, head_mn, dz_k, dz_mn, table_out, sum_out, part_out;
 };
 LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V);
 cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, const void* hidden, bool add_table, int sm_count,

@@ -3,7 +3,7 @@
 //   d_z[t][v]    = f d_logprob[t] ([v == target[t]] - p[t][v])
 //   d_hidden[t]  = sum_v d_z[t][v] lm_head[v],      d_lm_head[v] = sum_t d_z[t][v] hidden[t]
 // Three matrix products of 2 T V H operations each, which is what bounds a call of more than some hundred rows: the logits
-// are computed again (they were never stored), d_z leaves that product's epilogue as bf16 [T][columns of a chunk], and both
+// are computed again (they were never stored), d_z leaves that product's epilogue as bf16 [rows of a chunk][T], and both
 // gradients are products with it.  d_z is the one rounding on the way: every term of a gradient is off by 2^-8 of itself at
 // most, rounded independently.  The target's term is mostly the largest by far, and its rounding would be one error for a whole row, so
 // what it lost is kept (rho [T], fp32) and added to both gradients in fp32 before they are rounded.  Sums are fp32 in tensor memory.
@@ -15,9 +15,11 @@
 // 64-wide slices of the contracted axis through a ring, an MMA warp issues M256 x N256 x K16 MMAs into one of two
 // accumulators, eight epilogue warps take the other one out through shared memory and tiled TMA stores.  An operand whose
 // contracted axis is not its contiguous one is read as it lies (MN-major descriptors): nothing is transposed.
-//   DZ      A = hidden (K-major),  B = lm_head (K-major)       rows: tokens,   columns: vocabulary, contracted: H
-//   TABLE   A = d_z (M-major),     B = hidden (N-major)        rows: vocabulary, columns: H,        contracted: tokens
-//   HIDDEN  A = d_z (K-major),     B = lm_head (N-major)       rows: tokens,   columns: H,          contracted: vocabulary
+//   DZ      A = lm_head (K-major), B = hidden (K-major)        rows: vocabulary, columns: tokens, contracted: H
+//   TABLE   A = d_z (K-major),     B = hidden (N-major)        rows: vocabulary, columns: H,      contracted: tokens
+//   HIDDEN  A = lm_head (M-major), B = d_z (N-major)           rows: H,          columns: tokens, contracted: vocabulary
+// Tokens are columns wherever they are not contracted: an MMA has 256 rows whatever is in them, but 64, 128 or 192 columns where
+// the last tile has no more.  So d_z lies as [vocabulary][tokens] and the sums behind d_hidden as [H][tokens]; the fold turns them.
 // HIDDEN has few tiles with a long contracted axis (4001 x 3584: 224 tiles, 2376 slices, for 74 pairs), so the tiles of the last,
 // partial round are split along it, into parts that are summed in ascending order by lpb_fold_kernel; TABLE's many short units follow.  Vocabularies whose d_z
 // exceeds the scratch are taken in chunks; the sums behind d_hidden then grow in fp32, one addition an element and chunk, in order.
@@ -37,8 +39,8 @@ constexpr uint32_t STG_BYTES = 128 * 128;    // output staging: 128 rows x 128 b
 constexpr uint32_t OFF_STG = STAGES * STAGE_BYTES;
 constexpr uint32_t OFF_BAR = OFF_STG + 4 * STG_BYTES;
 constexpr uint32_t BYTES = OFF_BAR + 256;
-constexpr uint32_t ALLOC = BYTES + 1024;
-constexpr int BAND = 16;                     // DZ: pairs of token tiles whose hidden rows stay in L2 while lm_head streams by
+constexpr uint32_t ALLOC = BYTES + 1024;     // (1792 bytes are left for what is declared in the kernel)
+constexpr int BAND = 16;                     // DZ: token tiles whose hidden rows stay in L2 while lm_head streams by
 constexpr int THREADS = 320;                 // warp 0 TMA, warp 1 MMA, warps 2..9 epilogue: two groups of four
 constexpr int HITS = 32;                     // TABLE: targets that a warp's list holds
 constexpr int PAIRS = 74;                    // CTA pairs of a B200, by which HIDDEN's tiles are cut on any device
@@ -103,8 +105,8 @@ struct LpbRest {
 __host__ __device__ inline LpbRest lpb_rest(const LogprobBwdParams& p, int rows) {
     LpbRest r;
     r.rest = (rows + lpb::TILE - 1) / lpb::TILE * ((p.H + lpb::TILE - 1) / lpb::TILE) % lpb::PAIRS;
-    r.slices = ((p.ldz < p.V ? p.ldz : p.V) + 63) / 64;
-    const int least = (p.V - (p.V - 1) / p.ldz * p.ldz + 63) / 64, room = lpb::MOST_PARTS / (r.rest > 1 ? r.rest : 1);
+    r.slices = ((p.chunk < p.V ? p.chunk : p.V) + 63) / 64;
+    const int least = (p.V - (p.V - 1) / p.chunk * p.chunk + 63) / 64, room = lpb::MOST_PARTS / (r.rest > 1 ? r.rest : 1);
     r.most = least < room ? least : room;
     if (r.most > 64) r.most = 64;
     return r;
@@ -126,10 +128,12 @@ __device__ __forceinline__ LpbShape lpb_shape(const LogprobBwdParams& p, int kin
 
 struct LpbUnit {
     bool table;                  // TABLE's, of the gradients'
-    int row, col;                // of the output tile
+    int row, col, cols;          // of the output tile; its columns, 256 or fewer
     int k0, k1;                  // slices of 64 of the contracted axis
     int slot;                    // HIDDEN: part of a split tile (its place in the parts' buffer), -1: a whole tile
 };
+// Columns of a token tile
+__device__ __forceinline__ int lpb_cols(const LpbShape& g, int first) { return min(lpb::TILE, (g.rows - first + 63) / 64 * 64); }
 template <int KIND>
 __device__ __forceinline__ LpbUnit lpb_unit(const LogprobBwdParams& p, const LpbShape& g, int u) {
     using namespace lpb;
@@ -138,31 +142,37 @@ __device__ __forceinline__ LpbUnit lpb_unit(const LogprobBwdParams& p, const Lpb
     x.k0 = 0;
     x.table = KIND == TABLE || (KIND == BOTH && u >= g.hidden_units);
     if (KIND == DZ) {
-        // token tiles fastest inside a band, so that the pairs at work share a few steps of lm_head
+        // token tiles fastest inside a band, so that the pairs at work share a few steps of lm_head, and another one first for each
+        // step: the narrow last tiles go to all pairs in turn
         const int per_band = BAND * g.words, band = u / per_band, rem = u - band * per_band;
-        const int tiles = min(BAND, g.tokens - band * BAND);
-        x.row = (band * BAND + rem % tiles) * TILE;
-        x.col = rem / tiles * TILE;
+        const int tiles = min(BAND, g.tokens - band * BAND), word = rem / tiles;
+        x.row = word * TILE;
+        x.col = (band * BAND + (rem + word) % tiles) * TILE;
+        x.cols = lpb_cols(g, x.col);
         x.k1 = p.H / 64;
         return x;
     }
-    int tile = u;
-    if (!x.table) {
-        const int slices = (p.nv + 63) / 64;
-        x.k1 = slices;
-        if (u >= g.whole) {
-            const int rest = g.tokens * g.channels - g.whole, q = u - g.whole, part = q / rest;
-            tile = g.whole + q % rest;
-            x.k0 = static_cast<int>(static_cast<long long>(slices) * part / g.split);
-            x.k1 = static_cast<int>(static_cast<long long>(slices) * (part + 1) / g.split);
-            x.slot = q;
-        }
-    } else {
-        tile = u - g.hidden_units;
+    if (x.table) {
+        const int tile = u - g.hidden_units;
+        x.row = tile / g.channels * TILE;
+        x.col = tile % g.channels * TILE;
+        x.cols = TILE;
         x.k1 = (g.rows + 63) / 64;
+        return x;
     }
-    x.row = tile / g.channels * TILE;
-    x.col = tile % g.channels * TILE;
+    const int slices = (p.nv + 63) / 64;
+    int tile = u;
+    x.k1 = slices;
+    if (u >= g.whole) {
+        const int rest = g.tokens * g.channels - g.whole, q = u - g.whole, part = q / rest;
+        tile = g.whole + q % rest;
+        x.k0 = static_cast<int>(static_cast<long long>(slices) * part / g.split);
+        x.k1 = static_cast<int>(static_cast<long long>(slices) * (part + 1) / g.split);
+        x.slot = q;
+    }
+    x.row = tile % g.channels * TILE;                      // (the last token tile's come last, mostly among the split ones)
+    x.col = tile / g.channels * TILE;
+    x.cols = lpb_cols(g, x.col);
     return x;
 }
 
@@ -210,6 +220,8 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
     const int first = static_cast<int>(blockIdx.x >> 1), stride = static_cast<int>(gridDim.x >> 1);
     __shared__ LpbShape shape;
     __shared__ int hits[TABLES ? 8 : 1][TABLES ? HITS : 1];
+    __shared__ __align__(16) float token_factor[2][GRADS ? 1 : 64], token_lse2[2][GRADS ? 1 : 64];
+    __shared__ __align__(16) int token_target[2][GRADS ? 1 : 64];
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -233,7 +245,7 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
             mbar_init(bar_acc_empty + 8 * b, 16);            // the epilogue warps of both CTAs
         }
         fence_barrier_init();
-        tma_prefetch_desc(&maps.dz_out);
+        tma_prefetch_desc(&maps.dz_k);
         tma_prefetch_desc(GRADS ? &maps.head_mn : &maps.head_k);
         tma_prefetch_desc(GRADS ? &maps.hidden_mn : &maps.hidden_k);
     }
@@ -262,8 +274,9 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
             uint32_t it = 0;
             for (int u = first; u < g.units; u += stride) {
                 const LpbUnit x = lpb_unit<KIND>(p, g, u);
-                // each CTA stages its own 128 rows of A and its half of B; what lies outside the tensors arrives as zeros
-                const int a0 = x.row + half, b0 = x.col + half;
+                // each CTA stages its own 128 rows of A and its half of B's columns (and what is behind them, up to 128); what lies outside
+                // the tensors arrives as zeros
+                const int a0 = x.row + half, b0 = x.col + x.cols / 2 * static_cast<int>(rank);
                 for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
                     if (*abort_word) break;      // a wait expired somewhere: stop issuing copies
                     const int s = it % STAGES;
@@ -272,19 +285,18 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * STAGE_BYTES);   // both CTAs' bytes
                     const uint32_t bar = lead_full + 8 * s;
                     if (!GRADS) {
-                        tma_load_2d_pair(dst, &maps.hidden_k, bar, kb * 64, a0);
-                        tma_load_2d_pair(dst + OP_BYTES, &maps.head_k, bar, kb * 64, p.v0 + b0);
+                        tma_load_2d_pair(dst, &maps.head_k, bar, kb * 64, p.v0 + a0);
+                        tma_load_2d_pair(dst + OP_BYTES, &maps.hidden_k, bar, kb * 64, b0);
                     } else {
                         if (x.table) {
-                            tma_load_2d_pair(dst, &maps.dz_mn, bar, a0, kb * 64);
-                            tma_load_2d_pair(dst + OP_BYTES / 2, &maps.dz_mn, bar, a0 + 64, kb * 64);
+                            tma_load_2d_pair(dst, &maps.dz_k, bar, kb * 64, a0);
                         } else {
-                            tma_load_2d_pair(dst, &maps.dz_out, bar, kb * 64, a0);
+                            tma_load_2d_pair(dst, &maps.head_mn, bar, a0, p.v0 + kb * 64);
+                            tma_load_2d_pair(dst + OP_BYTES / 2, &maps.head_mn, bar, a0 + 64, p.v0 + kb * 64);
                         }
-                        const CUtensorMap* const b = x.table ? &maps.hidden_mn : &maps.head_mn;
-                        const int k = kb * 64 + (x.table ? 0 : p.v0);
-                        tma_load_2d_pair(dst + OP_BYTES, b, bar, b0, k);
-                        tma_load_2d_pair(dst + OP_BYTES + OP_BYTES / 2, b, bar, b0 + 64, k);
+                        const CUtensorMap* const b = x.table ? &maps.hidden_mn : &maps.dz_mn;
+                        tma_load_2d_pair(dst + OP_BYTES, b, bar, b0, kb * 64);
+                        tma_load_2d_pair(dst + OP_BYTES + OP_BYTES / 2, b, bar, b0 + 64, kb * 64);
                     }
                 }
             }
@@ -308,14 +320,13 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                     const uint32_t a = sbase + s * STAGE_BYTES, b = a + OP_BYTES;
                     // MN-major: 64 columns of the axis per 128-byte row, the next 64 half an operand further
                     const uint32_t more = kb > x.k0 ? 1u : 0u, d = tmem_u + buf * TILE;
+                    const uint32_t idesc = mma_idesc_bf16(256, KIND == TABLE ? TILE : x.cols, GRADS, KIND == HIDDEN || (KIND == BOTH && !x.table));
                     if (!GRADS)
-                        mma_ss_chain4_pair_steps<2, 2>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, 0, 1024), mma_idesc_bf16(256, TILE, false, false), more);
+                        mma_ss_chain4_pair_steps<2, 2>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, 0, 1024), idesc, more);
                     else if (x.table)
-                        mma_ss_chain4_pair_steps<128, 128>(d, smem_desc_sw128(a, OP_BYTES / 2, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024),
-                                                           mma_idesc_bf16(256, TILE, true, true), more);
+                        mma_ss_chain4_pair_steps<2, 128>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024), idesc, more);
                     else
-                        mma_ss_chain4_pair_steps<2, 128>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024),
-                                                         mma_idesc_bf16(256, TILE, true, false), more);
+                        mma_ss_chain4_pair_steps<128, 128>(d, smem_desc_sw128(a, OP_BYTES / 2, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024), idesc, more);
                     mma_commit_pair(bar_empty + 8 * s);
                     mma_commit_pair(peer_empty + 8 * s);
                 }
@@ -341,11 +352,12 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
         for (int u = first; u < g.units; u += stride, ++acc) {
             const LpbUnit x = lpb_unit<KIND>(p, g, u);
             const int buf = acc & 1, row0 = x.row + half;
-            float c = 0.0f, lse2 = 0.0f;
-            int target = -1;
+            float c = 0.0f, lse2 = 0.0f;                   // DZ: what a token of the group's pieces has of its own, a token a thread;
+            int target = -1;                               // one that takes no part has factor 0
             if (!GRADS) {
-                if (row0 + row < g.rows) {
-                    const int t = p.index ? p.index[row0 + row] : row0 + row;
+                const int k = tid & 127, r = x.col + 64 * (group + 2 * (k >> 6)) + (k & 63);
+                if (r < g.rows) {
+                    const int t = p.index ? p.index[r] : r;
                     target = p.target[t];
                     c = __fmul_rn(p.d_logprob[t], p.inv_temperature);
                     lse2 = __fmul_rn(p.lse[t], LOG2E_F);
@@ -353,7 +365,6 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                         c = 0.0f;
                         atomicOr(p.dev_status, TIK_DEV_BAD_TARGET);
                     }
-                    target -= p.v0 + x.col;                // column of this tile
                 }
             }
             int nhits = 0;                                 // tokens whose targets are this warp's rows
@@ -389,7 +400,8 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
             const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TILE;
             const bool f32_out = GRADS && (!table || p.table_fp32);
             if (!f32_out) {
-                const int limit = !GRADS ? p.ldz : p.H;
+                const int limit = !GRADS ? x.col + x.cols : p.H;           // (of a token tile all 64 columns of a piece)
+                const int v_row = p.v0 + row0 + row;                       // DZ: this thread's word
                 const float scale2 = !GRADS ? __fmul_rn(p.inv_temperature, LOG2E_F) : 0.0f;
 #pragma unroll 1
                 for (int q = group; q < TILE / 64; q += 2) {
@@ -403,21 +415,24 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                         for (int i = 0; i < 64; ++i) v[i] = 0u;
                     }
                     if (table && nhits > 0) add_lost(v, x.col + 64 * q);
-                    if (!GRADS) {
-                        const int valid = p.nv - x.col - 64 * q, hit = target - 64 * q;
-                        float at_hit = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) {
-                            const float e = ex2_ftz(__fmaf_rn(__uint_as_float(v[i]), scale2, -lse2));
-                            float d = __fmul_rn(c, (i == hit ? 1.0f : 0.0f) - e);
-                            // a masked row has no gradient whatever its logits are; columns past the vocabulary are read by HIDDEN
-                            if (c == 0.0f || i >= valid) d = 0.0f;
-                            if (i == hit) at_hit = d;
-                            v[i] = __float_as_uint(d);
-                        }
-                        if (hit >= 0 && hit < 64) p.rho[row0 + row] = __fsub_rn(at_hit, __bfloat162float(__float2bfloat16_rn(at_hit)));
+                    if (!GRADS && (tid & 127) >> 6 == q >> 1) {            // (the last piece's have been read: the group met since)
+                        token_factor[group][tid & 63] = c;
+                        token_lse2[group][tid & 63] = lse2;
+                        token_target[group][tid & 63] = target;
                     }
                     uint8_t* const stg = stage();
+                    if (!GRADS) {
+                        const bool word = v_row < p.V;                 // words past the vocabulary are read by HIDDEN
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) {
+                            const float f = token_factor[group][i], e = ex2_ftz(__fmaf_rn(__uint_as_float(v[i]), scale2, -token_lse2[group][i]));
+                            const bool hit = token_target[group][i] == v_row;
+                            float d = __fmul_rn(f, (hit ? 1.0f : 0.0f) - e);
+                            if (f == 0.0f || !word) d = 0.0f;          // a masked token has no gradient whatever its logits are
+                            if (hit) p.rho[x.col + 64 * q + i] = __fsub_rn(d, __bfloat162float(__float2bfloat16_rn(d)));
+                            v[i] = __float_as_uint(d);
+                        }
+                    }
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16) {
                         const uint4 val = make_uint4(
@@ -430,14 +445,14 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                     fence_proxy_async_smem();
                     named_bar_sync(1 + group, 128);
                     if (storer) {
-                        tma_store_2d(GRADS ? &maps.table_out : &maps.dz_out, smem_u32(stg), x.col + 64 * q, GRADS ? p.v0 + row0 : row0);
+                        tma_store_2d(GRADS ? &maps.table_out : &maps.dz_k, smem_u32(stg), x.col + 64 * q, GRADS ? p.v0 + row0 : row0);
                         tma_store_commit();
                     }
                 }
             } else {
 #pragma unroll 1
                 for (int q = group; q < TILE / 32; q += 2) {
-                    if (x.col + 32 * q >= p.H) break;
+                    if (table ? x.col + 32 * q >= p.H : 32 * q >= x.cols) break;
                     uint32_t v[32];
                     tmem_ld32(taddr + 32 * q, v);
                     tmem_wait_ld();
@@ -482,46 +497,70 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
     if (warp == 1) tmem_dealloc_pair(tmem, LPB_TMEM_COLS);
 }
 
-// d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order, and what the target's term lost.  Zeros
-// for tokens that took no part.  Thread per four channels, eight parts on their way at a time.
-__global__ void __launch_bounds__(256) lpb_fold_kernel(const LogprobBwdParams p) {
+// d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order, and what the target's term lost; zeros
+// for tokens that took no part.  The sums lie as [H][tokens]: a CTA turns 32 tokens x 32 channels in shared memory.  A thread adds the parts
+// of four tokens at a channel, sixteen parts on their way at a time, and writes four channels of a token.  (Rows of the result go by
+// tokens that take part; the others' rows are zeroed by the CTAs of the first channels.)
+__global__ void __launch_bounds__(256, 2) lpb_fold_kernel(const LogprobBwdParams p) {
+    __shared__ float turn[32][33];
     pdl_wait();
     pdl_launch_dependents();
     const LpbShape g = lpb_shape(p, lpb::HIDDEN);
-    const int per_row = p.H / 4, rest = g.tokens * g.channels - g.whole;
-    const long long n = p.T * per_row;
-    for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<long long>(gridDim.x) * 256) {
-        const long long row = i / per_row;
-        const int h = static_cast<int>(i - row * per_row) * 4, t = p.place ? p.place[row] : static_cast<int>(row);
-        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (t >= 0) {
-            const int target = p.row_target[t];
-            uint2 w = make_uint2(0u, 0u);
-            float lost = 0.0f;
+    const int tid = threadIdx.x, rest = g.tokens * g.channels - g.whole;
+    const int bands = (p.H + 31) / 32;
+    const long long blocks = static_cast<long long>((g.rows + 31) / 32) * bands;
+    for (long long b = blockIdx.x; b < blocks; b += gridDim.x) {
+        const int t0 = static_cast<int>(b / bands) * 32, h0 = static_cast<int>(b % bands) * 32;
+        const int tile = t0 / lpb::TILE * g.channels + h0 / lpb::TILE;
+        // what is written, and what it needs beside the sums
+        const int r = tid / 8, h = tid % 8 * 4;
+        uint2 w = make_uint2(0u, 0u);
+        float lost = 0.0f;
+        long long row = t0 + r;
+        if (t0 + r < g.rows) {
+            const int target = p.row_target[t0 + r];
             if (target >= 0 && target < p.V) {
-                w = *reinterpret_cast<const uint2*>(p.head + static_cast<long long>(target) * p.H + h);
-                lost = p.rho[t];
+                w = *reinterpret_cast<const uint2*>(p.head + static_cast<long long>(target) * p.H + h0 + h);
+                lost = p.rho[t0 + r];
             }
-            const int tile = t / lpb::TILE * g.channels + h / lpb::TILE;
+            if (p.index) row = p.index[t0 + r];
+        }
+        {
+            const int h = h0 + tid / 8, t = t0 + tid % 8 * 4;
+            float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (tile < g.whole) {
-                f = *reinterpret_cast<const float4*>(p.sum + static_cast<long long>(t) * p.H + h);
+                f = *reinterpret_cast<const float4*>(p.sum + static_cast<long long>(h) * p.ldt + t);
             } else {
                 const float4* src = reinterpret_cast<const float4*>(
-                    p.part + (static_cast<long long>(tile - g.whole) * lpb::TILE + t % lpb::TILE) * lpb::TILE + h % lpb::TILE);
+                    p.part + (static_cast<long long>(tile - g.whole) * lpb::TILE + h % lpb::TILE) * lpb::TILE + t % lpb::TILE);
                 const long long next = static_cast<long long>(rest) * lpb::TILE * lpb::TILE / 4;
-#pragma unroll 8
-                for (int k = 0; k < g.split; ++k, src += next) {
-                    const float4 a = *src;
-                    f.x += a.x, f.y += a.y, f.z += a.z, f.w += a.w;
+                for (int k = 0; k < g.split; k += 16) {
+                    float4 a[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        a[i] = k + i < g.split ? __ldcg(src + i * next) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) f.x += a[i].x, f.y += a[i].y, f.z += a[i].z, f.w += a[i].w;
+                    src += 16 * next;
                 }
             }
-            f.x = fmaf(lost, __uint_as_float(w.x << 16), f.x);
-            f.y = fmaf(lost, __uint_as_float(w.x & 0xffff0000u), f.y);
-            f.z = fmaf(lost, __uint_as_float(w.y << 16), f.z);
-            f.w = fmaf(lost, __uint_as_float(w.y & 0xffff0000u), f.w);
+            __syncthreads();                               // (the last block has been read)
+            float* const to = &turn[tid / 8][tid % 8 * 4];
+            to[0] = f.x, to[1] = f.y, to[2] = f.z, to[3] = f.w;
         }
-        *reinterpret_cast<uint2*>(p.d_hidden + row * p.H + h) = make_uint2(pack_bf16x2(f.x, f.y), pack_bf16x2(f.z, f.w));
+        __syncthreads();
+        if (t0 + r < g.rows) {
+            const float x0 = fmaf(lost, __uint_as_float(w.x << 16), turn[h][r]), x1 = fmaf(lost, __uint_as_float(w.x & 0xffff0000u), turn[h + 1][r]);
+            const float x2 = fmaf(lost, __uint_as_float(w.y << 16), turn[h + 2][r]), x3 = fmaf(lost, __uint_as_float(w.y & 0xffff0000u), turn[h + 3][r]);
+            *reinterpret_cast<uint2*>(p.d_hidden + row * p.H + h0 + h) = make_uint2(pack_bf16x2(x0, x1), pack_bf16x2(x2, x3));
+        }
     }
+    // the others' rows, a warp each
+    if (!p.place) return;
+    const int lane = tid & 31;
+    for (long long row = static_cast<long long>(blockIdx.x) * 8 + (tid >> 5); row < p.T; row += static_cast<long long>(gridDim.x) * 8)
+        if (p.place[row] < 0)
+            for (int h = 8 * lane; h < p.H; h += 256) *reinterpret_cast<uint4*>(p.d_hidden + row * p.H + h) = make_uint4(0, 0, 0, 0);
 }
 
 // The tokens that take part, in order: index [rows] of theirs, their targets, and place [T], -1 for the others; the count.  One CTA:
@@ -620,8 +659,9 @@ __global__ void __launch_bounds__(256) lpb_gather_kernel(const LogprobBwdParams 
 LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V) {
     constexpr int64_t pairs = lpb::PAIRS;
     LogprobBwdPlan g;
+    g.ldt = static_cast<int>((T + 63) / 64 * 64);
     const int64_t steps = (V + 255) / 256;
-    const int64_t most = std::max<int64_t>(1, (2ll << 30) / (T * 512));
+    const int64_t most = std::max<int64_t>(1, (2ll << 30) / (g.ldt * 512ll));
     g.chunks = static_cast<int>((steps + most - 1) / most);
     g.chunk = static_cast<int>((steps + g.chunks - 1) / g.chunks * 256);
     g.chunks = (V + g.chunk - 1) / g.chunk;
@@ -630,13 +670,13 @@ LogprobBwdPlan logprob_bwd_plan(int64_t T, int H, int V) {
     g.parts = static_cast<int>(std::min<int64_t>(lpb::MOST_PARTS, std::min(tiles, pairs) * std::min<int64_t>(64, (std::min(g.chunk, V) + 63) / 64)));
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     const size_t uT = static_cast<size_t>(T);
-    size_t at = up(uT * g.chunk * 2);
+    size_t at = up(static_cast<size_t>(g.ldt) * g.chunk * 2);
     auto take = [&](size_t n) {
         const size_t here = at;
         at += up(n);
         return here;
     };
-    g.sum_at = take(tiles >= pairs ? uT * H * 4 : 0);
+    g.sum_at = take(tiles >= pairs ? static_cast<size_t>(g.ldt) * H * 4 : 0);
     g.part_at = take(static_cast<size_t>(g.parts) * lpb::TILE * lpb::TILE * 4);
     g.rho_at = take(uT * 4);
     g.index_at = take(g.gather ? uT * 4 : 0);
@@ -664,7 +704,8 @@ static cudaError_t launch_lpb(const LogprobBwdMaps& maps, const LogprobBwdParams
 
 cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, const LogprobBwdPlan& g, const void* hidden, bool add_table, int sm_count,
                                cudaStream_t stream) {
-    p.ldz = g.chunk;
+    p.chunk = g.chunk;
+    p.ldt = g.ldt;
     p.pairs = std::max(1, sm_count / 2);
     cudaError_t e = cudaSuccess;
     if (!g.gather) {
@@ -697,8 +738,8 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
         if (e != cudaSuccess) return e;
     }
     if (!p.d_hidden) return cudaSuccess;
-    const long long n = p.T * (p.H / 4);
-    return launch_pdl(lpb_fold_kernel, dim3(static_cast<unsigned>(std::min<long long>((n + 255) / 256, 8ll * sm_count))), 256, 0, stream, 1, p);
+    const long long blocks = (p.T + 31) / 32 * ((p.H + 31) / 32);
+    return launch_pdl(lpb_fold_kernel, dim3(static_cast<unsigned>(std::min<long long>(blocks, 8ll * sm_count))), 256, 0, stream, 1, p);
 }
 
 }  // namespace tik

@@ -98,8 +98,8 @@ def test_adamw_of_nothing(ctx, changed):
 
 def test_scratch():
     assert tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, 0, H=64, V=10) == 0
-    # d_z [5][256] bf16, one tile's part, a number per row
-    assert tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, 5, H=64, V=10) == 5 * 512 + 256 * 256 * 4 + 256
+    # d_z [256][64] bf16, one tile's part, a number per row
+    assert tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, 5, H=64, V=10) == 64 * 512 + 256 * 256 * 4 + 256
     # a chunk's d_z stays within 2 GiB
     for T, V in ((7000, 152064), (16384, 152064), (100000, 152064), (1 << 22, 151936)):
         whole = tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, T, H=256, V=V)
