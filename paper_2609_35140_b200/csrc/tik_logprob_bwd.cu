@@ -18,8 +18,8 @@
 //   DZ      A = lm_head (K-major), B = hidden (K-major)        rows: vocabulary, columns: tokens, contracted: H
 //   TABLE   A = d_z (K-major),     B = hidden (N-major)        rows: vocabulary, columns: H,      contracted: tokens
 //   HIDDEN  A = lm_head (M-major), B = d_z (N-major)           rows: H,          columns: tokens, contracted: vocabulary
-// Tokens are columns wherever they are not contracted: an MMA has 256 rows whatever is in them, but 64, 128 or 192 columns where
-// the last tile has no more.  So d_z lies as [vocabulary][tokens] and the sums behind d_hidden as [H][tokens]; the fold turns them.
+// Tokens are columns wherever they are not contracted: an MMA has 256 rows whatever is in them, but as few as 32 columns where the
+// last tile has no more (contracted, they end at a multiple of 16).  So d_z lies as [vocabulary][tokens] and the sums behind d_hidden as [H][tokens]; the fold turns them.
 // HIDDEN has few tiles with a long contracted axis (4001 x 3584: 224 tiles, 2376 slices, for 74 pairs), so the tiles of the last,
 // partial round are split along it, into parts that are summed in ascending order by lpb_fold_kernel; TABLE's many short units follow.  Vocabularies whose d_z
 // exceeds the scratch are taken in chunks; the sums behind d_hidden then grow in fp32, one addition an element and chunk, in order.
@@ -70,6 +70,23 @@ __device__ __forceinline__ void mma_ss_chain4_pair_steps(uint32_t d_tmem, uint64
         "add.u64 da, %1, %7;\n\tadd.u64 db, %2, %10;\n\t"
         "@e tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, pt;\n\t"
         "}" ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "n"(SA), "n"(2 * SA), "n"(3 * SA), "n"(SB), "n"(2 * SB), "n"(3 * SB)
+        : "memory");
+}
+// The same for the first `steps` (1..4) of the four.
+template <int SA, int SB>
+__device__ __forceinline__ void mma_ss_chain_pair_steps(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, int steps) {
+    asm volatile(
+        "{\n\t.reg .pred p0, pt, e, e1, e2, e3;\n\telect.sync _|e, 0xffffffff;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.b32 p0, %4, 0;\n\tsetp.eq.b32 pt, 0, 0;\n\t"
+        "setp.gt.and.s32 e1, %11, 1, e;\n\tsetp.gt.and.s32 e2, %11, 2, e;\n\tsetp.gt.and.s32 e3, %11, 3, e;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p0;\n\t"
+        "add.u64 da, %1, %5;\n\tadd.u64 db, %2, %8;\n\t"
+        "@e1 tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.u64 da, %1, %6;\n\tadd.u64 db, %2, %9;\n\t"
+        "@e2 tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.u64 da, %1, %7;\n\tadd.u64 db, %2, %10;\n\t"
+        "@e3 tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "}" ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "n"(SA), "n"(2 * SA), "n"(3 * SA), "n"(SB), "n"(2 * SB), "n"(3 * SB), "r"(steps)
         : "memory");
 }
 
@@ -132,8 +149,8 @@ struct LpbUnit {
     int k0, k1;                  // slices of 64 of the contracted axis
     int slot;                    // HIDDEN: part of a split tile (its place in the parts' buffer), -1: a whole tile
 };
-// Columns of a token tile
-__device__ __forceinline__ int lpb_cols(const LpbShape& g, int first) { return min(lpb::TILE, (g.rows - first + 63) / 64 * 64); }
+// Columns of a token tile, in steps of the pair MMA's 32.  (What its accumulator holds behind them is not used.)
+__device__ __forceinline__ int lpb_cols(const LpbShape& g, int first) { return min(lpb::TILE, (g.rows - first + 31) / 32 * 32); }
 template <int KIND>
 __device__ __forceinline__ LpbUnit lpb_unit(const LogprobBwdParams& p, const LpbShape& g, int u) {
     using namespace lpb;
@@ -324,7 +341,8 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                     if (!GRADS)
                         mma_ss_chain4_pair_steps<2, 2>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, 0, 1024), idesc, more);
                     else if (x.table)
-                        mma_ss_chain4_pair_steps<2, 128>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024), idesc, more);
+                        mma_ss_chain_pair_steps<2, 128>(d, smem_desc_sw128(a, 0, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024), idesc, more,
+                                                        min(4, (g.rows - 64 * kb + 15) / 16));      // (no more than there are tokens)
                     else
                         mma_ss_chain4_pair_steps<128, 128>(d, smem_desc_sw128(a, OP_BYTES / 2, 1024), smem_desc_sw128(b, OP_BYTES / 2, 1024), idesc, more);
                     mma_commit_pair(bar_empty + 8 * s);
@@ -400,7 +418,7 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
             const uint32_t taddr = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TILE;
             const bool f32_out = GRADS && (!table || p.table_fp32);
             if (!f32_out) {
-                const int limit = !GRADS ? x.col + x.cols : p.H;           // (of a token tile all 64 columns of a piece)
+                const int limit = !GRADS ? x.col + x.cols : p.H;           // (of a token tile all 64 columns of a piece, zeros behind the last)
                 const int v_row = p.v0 + row0 + row;                       // DZ: this thread's word
                 const float scale2 = !GRADS ? __fmul_rn(p.inv_temperature, LOG2E_F) : 0.0f;
 #pragma unroll 1
