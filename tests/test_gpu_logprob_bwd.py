@@ -211,6 +211,20 @@ def test_masked_tokens_and_bad_targets(T):
     assert not zero[0].any() and not zero[1].any()
 
 
+@pytest.mark.parametrize("T", [1, 31, 33, 95, 161, 225, 289, 353, 600, 1100])
+def test_what_an_earlier_call_left(T):
+    """Scratch and accumulators full of NaN: token tiles of every width, what lies behind their last columns is not used."""
+    d, x, W, ids, lse, f = make(1024, 128, 19000, seed=31)
+    old = tik.tik_token_logprob_bwd(torch.full_like(d, float("nan")), torch.full_like(x, float("nan")), W, ids, lse, f)
+    assert bool(old[0].isnan().all()) and bool(old[1].isnan().any())
+    args = make(T, 128, 700, seed=T)
+    ws = torch.full((tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, T, H=128, V=700),), 255, dtype=torch.uint8, device="cuda")
+    dh, dw = tik.tik_token_logprob_bwd(*args, ws=ws)
+    a, b = expected(*args)
+    near(dh, a)
+    near(dw, b)
+
+
 def test_no_rows():
     W = torch.randn(40, 64, device="cuda").bfloat16()
     e = torch.empty(0, device="cuda")
