@@ -23,6 +23,8 @@
 // HIDDEN has few tiles with a long contracted axis (4001 x 3584: 224 tiles, 2376 slices, for 74 pairs), so the tiles of the last,
 // partial round are split along it, into parts that are summed in ascending order by lpb_fold_kernel; TABLE's many short units follow.  Vocabularies whose d_z
 // exceeds the scratch are taken in chunks; the sums behind d_hidden then grow in fp32, one addition an element and chunk, in order.
+#include <type_traits>
+
 #include "tik_core.cuh"
 #include "tik_internal.h"
 #include "tik_ptx.cuh"
@@ -441,15 +443,22 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
                     uint8_t* const stg = stage();
                     if (!GRADS) {
                         const bool word = v_row < p.V;                 // words past the vocabulary are read by HIDDEN
+                        // Shared memory's bandwidth is what the MMAs live on: their targets are looked at one by one only where one of
+                        // the piece's is a row of the warp's (2048 x 1536: 640 -> 610 us).
+                        auto gradients = [&](auto targets) {
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) {
-                            const float f = token_factor[group][i], e = ex2_ftz(__fmaf_rn(__uint_as_float(v[i]), scale2, -token_lse2[group][i]));
-                            const bool hit = token_target[group][i] == v_row;
-                            float d = __fmul_rn(f, (hit ? 1.0f : 0.0f) - e);
-                            if (f == 0.0f || !word) d = 0.0f;          // a masked token has no gradient whatever its logits are
-                            if (hit) p.rho[x.col + 64 * q + i] = __fsub_rn(d, __bfloat162float(__float2bfloat16_rn(d)));
-                            v[i] = __float_as_uint(d);
-                        }
+                            for (int i = 0; i < 64; ++i) {
+                                const float f = token_factor[group][i], e = ex2_ftz(__fmaf_rn(__uint_as_float(v[i]), scale2, -token_lse2[group][i]));
+                                const bool hit = targets.value && token_target[group][i] == v_row;
+                                float d = __fmul_rn(f, (hit ? 1.0f : 0.0f) - e);
+                                if (f == 0.0f || !word) d = 0.0f;      // a masked token has no gradient whatever its logits are
+                                if (hit) p.rho[x.col + 64 * q + i] = __fsub_rn(d, __bfloat162float(__float2bfloat16_rn(d)));
+                                v[i] = __float_as_uint(d);
+                            }
+                        };
+                        const unsigned t0 = token_target[group][lane] - first_row, t1 = token_target[group][lane + 32] - first_row;
+                        if (__any_sync(0xffffffffu, t0 < 32u || t1 < 32u)) gradients(std::true_type());
+                        else gradients(std::false_type());
                     }
 #pragma unroll
                     for (int c16 = 0; c16 < 8; ++c16) {
@@ -519,7 +528,8 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
 // for tokens that took no part.  The sums lie as [H][tokens]: a CTA turns 32 tokens x 32 channels in shared memory.  A thread adds the parts
 // of four tokens at a channel, sixteen parts on their way at a time, and writes four channels of a token.  (Rows of the result go by
 // tokens that take part; the others' rows are zeroed by the CTAs of the first channels.)
-__global__ void __launch_bounds__(256, 2) lpb_fold_kernel(const LogprobBwdParams p) {
+template <int AT_ONCE>
+__global__ void __launch_bounds__(256, AT_ONCE == 16 ? 2 : 4) lpb_fold_kernel(const LogprobBwdParams p) {
     __shared__ float turn[32][33];
     pdl_wait();
     pdl_launch_dependents();
@@ -552,14 +562,14 @@ __global__ void __launch_bounds__(256, 2) lpb_fold_kernel(const LogprobBwdParams
                 const float4* src = reinterpret_cast<const float4*>(
                     p.part + (static_cast<long long>(tile - g.whole) * lpb::TILE + h % lpb::TILE) * lpb::TILE + t % lpb::TILE);
                 const long long next = static_cast<long long>(rest) * lpb::TILE * lpb::TILE / 4;
-                for (int k = 0; k < g.split; k += 16) {
-                    float4 a[16];
+                for (int k = 0; k < g.split; k += AT_ONCE) {
+                    float4 a[AT_ONCE];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
+                    for (int i = 0; i < AT_ONCE; ++i)
                         a[i] = k + i < g.split ? __ldcg(src + i * next) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) f.x += a[i].x, f.y += a[i].y, f.z += a[i].z, f.w += a[i].w;
-                    src += 16 * next;
+                    for (int i = 0; i < AT_ONCE; ++i) f.x += a[i].x, f.y += a[i].y, f.z += a[i].z, f.w += a[i].w;
+                    src += AT_ONCE * next;
                 }
             }
             __syncthreads();                               // (the last block has been read)
@@ -757,7 +767,9 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
     }
     if (!p.d_hidden) return cudaSuccess;
     const long long blocks = (p.T + 31) / 32 * ((p.H + 31) / 32);
-    return launch_pdl(lpb_fold_kernel, dim3(static_cast<unsigned>(std::min<long long>(blocks, 8ll * sm_count))), 256, 0, stream, 1, p);
+    // calls of a few CTAs wait for one part after the other, others for how much is on its way
+    if (blocks <= 2ll * sm_count) return launch_pdl(lpb_fold_kernel<16>, dim3(static_cast<unsigned>(blocks)), 256, 0, stream, 1, p);
+    return launch_pdl(lpb_fold_kernel<8>, dim3(static_cast<unsigned>(std::min<long long>(blocks, 8ll * sm_count))), 256, 0, stream, 1, p);
 }
 
 }  // namespace tik
