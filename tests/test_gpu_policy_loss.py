@@ -204,6 +204,28 @@ def test_without_a_gradient_and_in_place():
         assert d3.data_ptr() == b["logprob"].data_ptr() and torch.equal(d3, d) and torch.equal(l3, loss)
 
 
+@pytest.mark.parametrize("T", [4097, 60013, 1000003])
+def test_a_chain_of_calls_on_one_tensor(T):
+    """A call reads what the call before it wrote, without a synchronisation in between: its kernels begin under that call's tail."""
+    a = make(T, 12, seed=14)
+    kw = dict(kl_coef=0.05, reduction="sum", scale=1e-3)          # (x -> 1e-3 w (-A) exp(x - old): |x| < 1 throughout; with 0.5 it grows to infinity)
+
+    def chain(sync):
+        b = dict(a, logprob=a["logprob"].clone(), weight=a["weight"].clone())
+        losses = []
+        for i in range(12):
+            losses.append(tik.tik_policy_loss(**b, **kw, d_logprob=b["weight" if i % 3 == 2 else "logprob"])[0])
+            if sync:
+                torch.cuda.synchronize()
+        return torch.stack(losses), b["logprob"], b["weight"]
+
+    want = chain(True)
+    assert bool(want[0].isfinite().all())
+    for _ in range(3):
+        for x, y in zip(chain(False), want):
+            assert torch.equal(x, y)
+
+
 def test_views_at_odd_addresses():
     T = 1000
     flat = {k: (v if k == "cu_seqlens" else torch.cat([v[:1], v])[1:]) for k, v in make(T, 5, seed=11).items()}
