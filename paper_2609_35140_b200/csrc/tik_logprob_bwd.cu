@@ -526,8 +526,9 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
 
 // d_hidden in bf16 from the whole tiles' sums and the others' parts, these in ascending order, and what the target's term lost; zeros
 // for tokens that took no part.  The sums lie as [H][tokens]: a CTA turns 32 tokens x 32 channels in shared memory.  A thread adds the parts
-// of four tokens at a channel, sixteen parts on their way at a time, and writes four channels of a token.  (Rows of the result go by
-// tokens that take part; the others' rows are zeroed by the CTAs of the first channels.)
+// of four tokens at a channel, AT_ONCE of them on their way at a time, and writes four channels of a token.  (Rows of the result go by
+// tokens that take part; the others' rows come last.)  256 x 256 with 32 parts 4.7 us with sixteen at a time, 7.5 with eight; 2048 x 1536 with six
+// parts 19 with eight and four CTAs an SM, 28.6 with sixteen and two.
 template <int AT_ONCE>
 __global__ void __launch_bounds__(256, AT_ONCE == 16 ? 2 : 4) lpb_fold_kernel(const LogprobBwdParams p) {
     __shared__ float turn[32][33];
