@@ -717,7 +717,8 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     p.rows = static_cast<const __nv_bfloat16*>(rows_of);
 
     const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.ldt);
-    const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, static_cast<uint64_t>(g.chunk)}, sd[2] = {uZ, uH}, rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2}, rowZ4[1] = {uZ * 4};
+    const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, static_cast<uint64_t>(g.chunk)}, sd[2] = {uZ, uH};
+    const uint64_t rowH[1] = {uH * 2}, rowH4[1] = {uH * 4}, rowZ[1] = {uZ * 2}, rowZ4[1] = {uZ * 4};
     const uint32_t rows[2] = {64, 128}, slab[2] = {64, 64}, rows4[2] = {32, 128};    // K-major operands and bf16 output, MN-major, fp32 output
     LogprobBwdMaps m{};
     std::string err;
