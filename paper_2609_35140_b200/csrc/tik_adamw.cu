@@ -223,9 +223,10 @@ __device__ __forceinline__ float adam_round_e4m3(float y, unsigned random16) {
     const float t = floorf(__fadd_rn(fabsf(y) * per_place, static_cast<float>(random16) * 0x1p-16f));
     return copysignf(t * place, y);
 }
-// Whether one of four e4m3 values is at most the least normal one, unless all are 0.
-__device__ __forceinline__ bool adam_small(unsigned w) {
-    return ((((w & 0x7f7f7f7fu) | 0x80808080u) - 0x09090909u) & 0x80808080u) != 0x80808080u && w != 0u;
+// Whether one of four e4m3 values is at most the least normal one, unless what they stand for, `x`, is all 0.
+__device__ __forceinline__ bool adam_small(unsigned w, const float* x) {
+    if (((((w & 0x7f7f7f7fu) | 0x80808080u) - 0x09090909u) & 0x80808080u) == 0x80808080u) return false;
+    return w != 0u || x[0] != 0.0f || x[1] != 0.0f || x[2] != 0.0f || x[3] != 0.0f;
 }
 // Stores values and, from each block's first lane, its scale.  POSITIVE: the second moment's roots, of which none above 0 becomes 0.
 template <int W, bool STOCHASTIC, bool POSITIVE, bool WHOLE>
@@ -266,7 +267,7 @@ __device__ __forceinline__ void adam_store8(const float (&x)[ADAM_N], const uint
         w[i / 4] |= static_cast<unsigned>(__nv_cvt_float2_to_fp8x2(make_float2(z[0], z[1]), __NV_SATFINITE, __NV_E4M3)) << (8 * (i & 2));
     }
     // Subnormal values, whose places do not follow their exponents, and zeros that may not be: once more, one by one.
-    if (STOCHASTIC || POSITIVE) rare = rare || adam_small(w[0]) || adam_small(w[1]);
+    if (STOCHASTIC || POSITIVE) rare = rare || adam_small(w[0], x) || adam_small(w[1], x + 4);
     if (rare) {
         w[0] = w[1] = 0u;
 #pragma unroll
