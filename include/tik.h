@@ -436,7 +436,7 @@ tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* ou
  *   step: this step's number, from 1 on.  lr_device, step_device: device fp32 [1], int32 [1], or NULL; read in place of lr and step
  *   when the kernel runs, so that a captured step follows them.
  *   norm: device fp32 [1] or NULL (c = 1): the gradients' norm, as tik_grad_norm leaves it.  c = max_norm / norm where max_norm < norm
- *   < infinity, else 1, and a norm that is not finite skips the step: nothing is written.
+ *   < infinity, else 1, and a norm that is not finite skips the step: nothing is written.  c grad is rounded to fp32, as tik_grad_clip does.
  *   stochastic != 0: 8-bit moments and bf16 weights without a master copy are rounded to one of their two neighbours, up with
  *   the probability of the distance from the lower one: 16 bits of a hash of the element's place in the call (elements of the tensors before it
  *   counted), seed and step decide.  Else to the nearest.

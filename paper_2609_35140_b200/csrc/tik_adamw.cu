@@ -341,11 +341,12 @@ __device__ __forceinline__ void adam_elements(const AdamEntry& e, long long at, 
     adam_load<W, STAGED>(x, src.weight, e.master || p32, in, n);
     uint32_t random[ADAM_N] = {};
     if (STOCHASTIC) adam_randoms<W>(random, e.place + at, s.key);
-    const F2 to_m = f2(p.one_minus_beta1 * clip), to_v = f2(p.one_minus_beta2 * clip * clip), beta1 = f2(p.beta1), beta2 = f2(p.beta2);
+    const F2 clip2 = f2(clip), to_m = f2(p.one_minus_beta1), to_v = f2(p.one_minus_beta2), beta1 = f2(p.beta1), beta2 = f2(p.beta2);
     const F2 decay = f2(s.decay), size = f2(-s.size), root2 = f2(s.root), eps = f2(p.eps);
 #pragma unroll
     for (int i = 0; i < ADAM_N; i += 2) {
-        const F2 g2 = f2(g[i], g[i + 1]), v1 = f2(v[i], v[i + 1]);
+        // (clipped before it is squared: the square of a small clip has no digits in fp32, that of a clipped gradient has)
+        const F2 g2 = f2_mul(clip2, f2(g[i], g[i + 1])), v1 = f2(v[i], v[i + 1]);
         const F2 m2 = f2_fma(beta1, f2(m[i], m[i + 1]), f2_mul(to_m, g2));
         const F2 v2 = f2_fma(beta2, STATE8 ? f2_mul(v1, v1) : v1, f2_mul(f2_mul(to_v, g2), g2));
         f2_get(m2, m[i], m[i + 1]);
