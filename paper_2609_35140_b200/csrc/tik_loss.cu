@@ -95,7 +95,8 @@ __device__ __forceinline__ float loss_token(const PolicyLossParams& p, double f,
         cut = true;
         less_one = p.dual_less_one;
     }
-    float grad = cut ? 0.0f : fmaf(-adv, r.less_one, -adv);
+    if (adv == 0.0f && fabsf(x) <= 3.402823466e38f) less_one = 0.0f;       // nothing times a ratio beyond fp32 (x beyond it goes on)
+    float grad = cut ? 0.0f : fmaf(-adv, less_one, -adv);
     sum.policy = fma(-f, static_cast<double>(adv), sum.policy);
     sum.policy = fma(-f, static_cast<double>(adv * less_one), sum.policy);
     if (p.ref) {
