@@ -9,7 +9,8 @@
 //
 // Per token fp32, but where digits would be lost that matter: whether a token is cut is decided on x in 64 bits against the
 // logarithms of the thresholds (r in 32 bits would put tokens on the wrong side of a border where the gradient jumps); exp(y) - y - 1 comes
-// from its series, not from a difference; -A r goes into the sum as -A and -A (r - 1), the first exact and the second small.  Sums over tokens,
+// from its series, not from a difference; -A r goes into the sum as -A and -A (r - 1), the first exact and the second small, and from x = -1 down,
+// where r - 1 has lost digits of r (half of them at x = -8, all at -18), as it is, in the gradient too.  Sums over tokens,
 // which are of both signs and mostly cancel, are fp64 in one fixed order, counts are integers.  (All of it in fp64 took 275 instructions a token.)
 // 20 bytes in and 4 out per token, so a call is all latency: up to 4096 tokens one cluster of up to eight CTAs takes
 // it in one launch, a token a thread, counts and sums through distributed shared memory.  Longer calls, whose arithmetic needs all
@@ -45,7 +46,7 @@ __device__ __forceinline__ void loss_range(const PolicyLossParams& p, int& from,
 // exp(x) - 1 and exp(x) - 1 - x.  Up to |x| = 1, where nearly all tokens are, from x^2 q(x) with q = sum x^n / (n + 2)! to n = 10 (the next
 // term is 4e-9 of q): nothing cancels.  Beyond, where little does, through expf.
 struct Exp {
-    float less_one, remainder;
+    float less_one, remainder, whole;                      // whole: exp(x), from x = -1 down, where exp(x) - 1 has lost digits of it
 };
 __device__ __forceinline__ Exp loss_exp(float x) {
     Exp e;
@@ -63,8 +64,10 @@ __device__ __forceinline__ Exp loss_exp(float x) {
         q = fmaf(q, x, 0.5f);
         e.remainder = x * x * q;
         e.less_one = x + e.remainder;
+        e.whole = 0.0f;
     } else {
-        e.less_one = expf(x) - 1.0f;
+        e.whole = expf(x);
+        e.less_one = e.whole - 1.0f;
         e.remainder = e.less_one - x;
     }
     return e;
@@ -96,9 +99,12 @@ __device__ __forceinline__ float loss_token(const PolicyLossParams& p, double f,
         less_one = p.dual_less_one;
     }
     if (adv == 0.0f && fabsf(x) <= 3.402823466e38f) less_one = 0.0f;       // nothing times a ratio beyond fp32 (x beyond it goes on)
-    float grad = cut ? 0.0f : fmaf(-adv, less_one, -adv);
-    sum.policy = fma(-f, static_cast<double>(adv), sum.policy);
-    sum.policy = fma(-f, static_cast<double>(adv * less_one), sum.policy);
+    // -A r from r itself where r is small
+    const bool small = !cut && x <= -1.0f;
+    const float base = small ? 0.0f : -adv, part = -adv * (small ? r.whole : less_one);
+    float grad = cut ? 0.0f : small ? part : fmaf(-adv, less_one, -adv);
+    sum.policy = fma(f, static_cast<double>(base), sum.policy);
+    sum.policy = fma(f, static_cast<double>(part), sum.policy);
     if (p.ref) {
         const Exp e = loss_exp(ref - lp);
         sum.kl = fma(f, static_cast<double>(e.remainder), sum.kl);

@@ -44,3 +44,30 @@ def test_no_advantage_and_a_ratio_beyond_fp32(T, per_seq, dual):
         a["logprob"][at] = bad
         loss, d, _ = tik.tik_policy_loss(**a)
         assert math.isnan(float(loss)) and math.isnan(float(d[at]))
+
+
+@pytest.mark.parametrize("T", [1] + SIZES)
+@pytest.mark.parametrize("reduction", ["sum", "token", "sequence"])
+def test_ratios_far_below_one_keep_their_digits(T, reduction):
+    """Advantages above 0 of tokens that the policy has left, which no threshold cuts: r down to e^-80."""
+    a = make(T, 3, seed=2, weight=False, ref=False)
+    t = torch.arange(T, device="cuda")
+    a["advantage"] = 0.1 + a["advantage"].abs()
+    far = torch.linspace(1.0, 80.0, T, device="cuda") if T > 1 else torch.tensor([12.5], device="cuda")
+    a["logprob"] = a["old_logprob"] - far
+    _, d, _ = compare(a, stats=range(5), reduction=reduction)
+    assert bool((d < 0).all())
+    # beside others, and as the smaller side of a threshold
+    a["advantage"][t % 3 == 1] *= -1.0
+    a["logprob"][t % 4 == 2] = a["old_logprob"][t % 4 == 2] + 0.1
+    for ref in (None, a["old_logprob"] + 0.3):
+        compare(dict(a, ref_logprob=ref), stats=range(5), reduction=reduction, kl_coef=0.0 if ref is None else 0.05)
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_around_the_ends_of_the_series(sign):
+    """x within some steps of -1 and 1, where one way of taking r ends and another begins."""
+    old = torch.full((64,), -3.0, device="cuda")
+    x = (1.0 + torch.arange(-32, 32, device="cuda") * 2.0 ** -21) * sign
+    a = dict(logprob=old + x, old_logprob=old, advantage=torch.linspace(-2, 2, 64, device="cuda"))
+    compare(a, stats=range(5), clip_low=0.9, clip_high=9.0)
