@@ -297,7 +297,7 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
  *   mean over sequences of their means)
  * What a token that does not count holds (infinities, NaN) goes nowhere; others pass theirs on.  A ratio beyond fp32 is infinite, but for an
  * advantage of 0, whose policy term and gradient are 0 whatever finite numbers its ratio is of.
- *   logprob, old_logprob, weight (or NULL), ref_logprob (or NULL: no KL term, kl_coef 0): fp32 [T]
+ *   logprob, old_logprob, weight (or NULL), ref_logprob (or NULL: no KL term, kl_coef 0; with kl_coef 0 it goes into stats alone): fp32 [T]
  *   advantage: fp32 [T], or [S] with advantage_per_sequence
  *   cu_seqlens: int32 [S+1] or NULL; needed per sequence.  Where given, tokens before cu_seqlens[0] or from cu_seqlens[S] on
  *   (a padded batch) do not count.

@@ -108,7 +108,7 @@ __device__ __forceinline__ float loss_token(const PolicyLossParams& p, double f,
     if (p.ref) {
         const Exp e = loss_exp(ref - lp);
         sum.kl = fma(f, static_cast<double>(e.remainder), sum.kl);
-        grad -= p.kl_coef * e.less_one;
+        if (p.kl_coef != 0.0f) grad -= p.kl_coef * e.less_one;             // (0 times what may be beyond fp32)
     }
     sum.cut += cut;
     sum.remainder += r.remainder;
@@ -174,7 +174,7 @@ __device__ __forceinline__ void dsmem_add(uint32_t addr, int v) {
 
 __device__ __forceinline__ void loss_results(const PolicyLossParams& p, const double (&sum)[loss::SUMS]) {
     const double n = sum[4] > 1.0 ? sum[4] : 1.0;
-    *p.loss = static_cast<float>(sum[0] + static_cast<double>(p.kl_coef) * sum[1]);
+    *p.loss = static_cast<float>(p.kl_coef != 0.0f ? sum[0] + static_cast<double>(p.kl_coef) * sum[1] : sum[0]);
     if (p.stats) {
         p.stats[0] = static_cast<float>(sum[0]);
         p.stats[1] = static_cast<float>(sum[1]);

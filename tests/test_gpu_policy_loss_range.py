@@ -71,3 +71,17 @@ def test_around_the_ends_of_the_series(sign):
     x = (1.0 + torch.arange(-32, 32, device="cuda") * 2.0 ** -21) * sign
     a = dict(logprob=old + x, old_logprob=old, advantage=torch.linspace(-2, 2, 64, device="cuda"))
     compare(a, stats=range(5), clip_low=0.9, clip_high=9.0)
+
+
+@pytest.mark.parametrize("T", SIZES)
+def test_a_kl_term_that_is_only_looked_at(T):
+    """kl_coef 0 beside a reference: the loss and its gradient are those without one, however far off the reference is."""
+    a = make(T, 4, seed=3)
+    none = dict(a, ref_logprob=None)
+    for reduction in ("sum", "token", "sequence"):
+        near, far = tik.tik_policy_loss(**a, reduction=reduction), dict(a, ref_logprob=a["logprob"] + 95.0)
+        want, got = tik.tik_policy_loss(**none, reduction=reduction), tik.tik_policy_loss(**far, reduction=reduction)
+        for x in (near, got):
+            assert torch.equal(x[0], want[0]) and torch.equal(x[1], want[1])
+            assert torch.equal(x[2][[0, 2, 3, 4]], want[2][[0, 2, 3, 4]])
+        assert 0 < float(near[2][1]) < math.inf and float(got[2][1]) == math.inf
