@@ -301,7 +301,8 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
  *   advantage: fp32 [T], or [S] with advantage_per_sequence
  *   cu_seqlens: int32 [S+1] or NULL; needed per sequence.  Where given, tokens before cu_seqlens[0] or from cu_seqlens[S] on
  *   (a padded batch) do not count.
- *   loss: fp32 [1];  d_logprob: fp32 [T] or NULL, each element written, may be one of the inputs [T];
+ *   loss: fp32 [1];  d_logprob: fp32 [T] or NULL, each element written, may be one of the inputs [T] from its first element on;
+ *   outputs overlap inputs and each other in no other way (TIK_ERR_INVALID_ARG);
  *   stats: fp32 [5] or NULL: sum f policy, sum f (exp(y) - y - 1), and over the tokens that count the share that is cut, the mean
  *   of r - 1 - x, and their number.
  * fp32 per token, sums over tokens in fp64 in one fixed order: the same inputs give the same bits on every call.  T < 2^31; tensors

@@ -58,6 +58,15 @@ static tik_status cuda_fail(tik_ctx* ctx, cudaError_t e, const char* where) {
     ctx->last_error = std::string(where) + ": " + cudaGetErrorString(e);
     return TIK_ERR_CUDA;
 }
+// Bytes of memory, and whether two of them meet (an absent one, or one of none, meets nothing).
+struct Range {
+    const void* p;
+    size_t bytes;
+};
+static bool meet(const Range& a, const Range& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
+}
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static bool page_ok(int page) { return page == 16 || page == 32 || page == 64 || page == 128; }
 static float scale_to_c(float softmax_scale) { return softmax_scale * LOG2E_F; }
@@ -671,17 +680,9 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     if (!d_logprob || !hidden || !lm_head || !target_ids || !lse) return fail(ctx, TIK_ERR_INVALID_ARG, "null pointer");
     if (T >= (1ll << 31) - 256) return fail(ctx, TIK_ERR_UNSUPPORTED, "T must be < 2^31 - 256");
     {
-        struct Range {
-            const void* p;
-            size_t bytes;
-        };
         const size_t rows = static_cast<size_t>(T), width = static_cast<size_t>(H), words = static_cast<size_t>(V);
         const Range in[] = {{hidden, rows * width * 2}, {lm_head, words * width * 2}, {d_logprob, rows * 4}, {target_ids, rows * 4}, {lse, rows * 4}};
         const Range out[] = {{d_hidden, rows * width * 2}, {d_lm_head, words * width * (lm_head_dtype == TIK_DTYPE_FP32 ? 4 : 2)}};
-        auto meet = [](const Range& a, const Range& b) {
-            const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-            return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
-        };
         bool overlap = meet(out[0], out[1]);
         for (const Range& o : out)
             for (const Range& i : in) overlap = overlap || meet(o, i);
@@ -763,6 +764,20 @@ tik_status tik_policy_loss(tik_ctx* ctx, const float* logprob, const float* old_
                           static_cast<const void*>(loss), static_cast<const void*>(d_logprob), static_cast<const void*>(stats)})
         if (reinterpret_cast<uintptr_t>(q) & 3u) return fail(ctx, TIK_ERR_UNSUPPORTED, "a tensor must be aligned to its elements");
     if (!aligned16(ws)) return fail(ctx, TIK_ERR_UNSUPPORTED, "pointers must be 16-byte aligned");
+    {
+        // d_logprob may be one of the inputs of a number per token, each of which only the thread that writes there reads
+        const size_t rows = static_cast<size_t>(T) * 4, seqs = static_cast<size_t>(S) * 4;
+        const bool by_seq = advantage_per_sequence != 0;
+        const Range token[] = {{logprob, rows}, {old_logprob, rows}, {by_seq ? nullptr : advantage, rows}, {weight, rows}, {ref_logprob, rows}};
+        const Range seq[] = {{T > 0 && by_seq ? advantage : nullptr, seqs}, {T > 0 && S > 0 ? cu_seqlens : nullptr, seqs + 4}};
+        const Range out[] = {{loss, 4}, {stats, 20}, {d_logprob, rows}};
+        bool overlap = meet(out[0], out[1]) || meet(out[0], out[2]) || meet(out[1], out[2]);
+        for (const Range& o : out) {
+            for (const Range& i : token) overlap = overlap || (meet(o, i) && !(o.p == d_logprob && i.p == d_logprob));
+            for (const Range& i : seq) overlap = overlap || meet(o, i);
+        }
+        if (overlap) return fail(ctx, TIK_ERR_INVALID_ARG, "an output overlaps an input or another output");
+    }
     const size_t need = tik_workspace_bytes(TIK_OP_POLICY_LOSS, T, 0, 0, 0, S, 0, 0);
     if (!ws || ws_bytes < need) return fail(ctx, TIK_ERR_WORKSPACE, "policy loss workspace too small");
     PolicyLossParams p{};
