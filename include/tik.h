@@ -274,8 +274,7 @@ tik_status tik_token_logprob(tik_ctx* ctx, const void* hidden, const void* lm_he
  * accumulate != 0 (fp32 only): d_lm_head is added to, as by the later micro-batches of a step; else every row is written,
  * with zeros for T == 0.  Logits are computed again, d_z is rounded to bf16 and is the operand of both products, sums are fp32:
  * each term of a sum but the target's is off by 2^-8 of itself at most.  A token with d_logprob 0 (masked) takes no part, whatever
- * its target and lse; one whose target is outside [0, V) gives no gradient and raises TIK_DEV_BAD_TARGET.  hidden must be finite, masked
- * tokens' rows included.
+ * its target, lse and hidden row hold; nor does one whose target is outside [0, V), which raises TIK_DEV_BAD_TARGET.
  * Deterministic: fixed orders, no atomics on values.  Outputs overlap neither inputs nor each other (TIK_ERR_INVALID_ARG).
  * H must be a multiple of 64, V <= 2^30, T < 2^31 - 256.  ws: tik_workspace_bytes(TIK_OP_TOKEN_LOGPROB_BWD, T, ..., H, V) bytes (d_z
  * of a vocabulary chunk, 2 GiB at most up to T = 2^22, fp32 sums, gathered rows); concurrent calls (and captured graphs that may run at the

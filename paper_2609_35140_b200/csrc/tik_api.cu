@@ -714,8 +714,13 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     p.index = words(g.index_at);
     p.place = words(g.place_at);
     p.row_target = g.gather ? words(g.target_at) : target_ids;
-    const void* const rows_of = g.gather ? at + g.rows_at : hidden;          // the products' hidden rows
+    // The hidden rows that d_lm_head multiplies, without those of tokens that take no part: gathered, or up to a row tile copied in place.  The copy lies
+    // where d_hidden will (its last kernel writes it), or where the parts of its sums would.
+    const bool copied = !g.gather && d_lm_head;
+    void* const rows_of = g.gather ? at + g.rows_at : copied ? (d_hidden ? d_hidden : at + g.part_at) : const_cast<void*>(hidden);
     p.rows = static_cast<const __nv_bfloat16*>(rows_of);
+    p.clean = copied ? static_cast<__nv_bfloat16*>(rows_of) : nullptr;
+    p.hidden = static_cast<const __nv_bfloat16*>(hidden);
 
     const uint64_t uT = static_cast<uint64_t>(T), uH = static_cast<uint64_t>(H), uV = static_cast<uint64_t>(V), uZ = static_cast<uint64_t>(g.ldt);
     const uint64_t xd[2] = {uH, uT}, wd[2] = {uH, uV}, zd[2] = {uZ, static_cast<uint64_t>(g.chunk)}, sd[2] = {uZ, uH};
@@ -723,7 +728,7 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     const uint32_t rows[2] = {64, 128}, slab[2] = {64, 64}, rows4[2] = {32, 128};    // K-major operands and bf16 output, MN-major, fp32 output
     LogprobBwdMaps m{};
     std::string err;
-    bool ok = make_tmap_bf16(ctx, &m.hidden_k, rows_of, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
+    bool ok = make_tmap_bf16(ctx, &m.hidden_k, g.gather ? rows_of : hidden, 2, xd, rowH, rows, &err) && make_tmap_bf16(ctx, &m.head_k, lm_head, 2, wd, rowH, rows, &err) &&
               make_tmap_bf16(ctx, &m.hidden_mn, rows_of, 2, xd, rowH, slab, &err) && make_tmap_bf16(ctx, &m.head_mn, lm_head, 2, wd, rowH, slab, &err) &&
               make_tmap_bf16(ctx, &m.dz_k, dz, 2, zd, rowZ, rows, &err) && make_tmap_bf16(ctx, &m.dz_mn, dz, 2, zd, rowZ, slab, &err);
     if (ok && d_lm_head)

@@ -218,6 +218,8 @@ struct LogprobBwdParams {
     const int32_t* row_target;   // [row]
     const int32_t* place;        // [T]: row or -1, or null
     const __nv_bfloat16* rows;   // [row][H]: their hidden rows
+    __nv_bfloat16* clean;        // [T][H] without `count`: the hidden rows, zeros for tokens without a gradient (rows, then); or null
+    const __nv_bfloat16* hidden; // [T][H]: what it is copied from
     // of one launch
     int v0, nv;                  // the vocabulary's columns of this chunk
     int chunk;                   // words of a whole chunk

@@ -10,6 +10,8 @@
 //
 // Tokens without a gradient (d_logprob 0: prompts, padding) take no part.  In calls of more than one row tile the others' rows are
 // gathered first, and everything after goes by their number, which stays on the device: the persistent grids read it.
+// In calls of one, whose launches are what they take, all rows go through: d_z is 0 for such tokens, and DZ leaves TABLE a copy of the hidden
+// rows with zeros for theirs, whatever they hold.
 //
 // One kernel, launched for DZ and then for the gradients: persistent CTA pairs that walk units of one 256 x 256 output tile each: a TMA warp streams
 // 64-wide slices of the contracted axis through a ring, an MMA warp issues M256 x N256 x K16 MMAs into one of two
@@ -360,6 +362,16 @@ __global__ void __launch_bounds__(lpb::THREADS, 1) lpb_kernel(const __grid_const
         // and a buffer more each 286, and with a relaxed arrival 214).
         const int quarter = warp & 3, group = (warp - 2) >> 2;         // TMEM lane quarter of this warp
         const int row = quarter * 32 + lane;
+        if (!GRADS && p.clean) {
+            // 256 channels of a token a warp, while the first accumulator is being filled
+            const int pieces = (p.H + 255) / 256, T = static_cast<int>(p.T);
+            for (int i = static_cast<int>(blockIdx.x) * 8 + warp - 2; i < T * pieces; i += static_cast<int>(gridDim.x) * 8) {
+                const int t = i / pieces, h = (i - t * pieces) * 256 + 8 * lane, target = p.target[t];
+                const bool on = __fmul_rn(p.d_logprob[t], p.inv_temperature) != 0.0f && target >= 0 && target < p.V;
+                const long long at = static_cast<long long>(t) * p.H + h;
+                if (h < p.H) *reinterpret_cast<uint4*>(p.clean + at) = on ? *reinterpret_cast<const uint4*>(p.hidden + at) : make_uint4(0, 0, 0, 0);
+            }
+        }
         uint32_t acc = 0;
         const bool storer = (warp == 2 || warp == 6) && lane == 0;
         uint32_t piece = 0;
@@ -756,6 +768,7 @@ cudaError_t launch_logprob_bwd(const LogprobBwdMaps& m, LogprobBwdParams p, cons
         p.add_table = add_table;
         p.add_hidden = c > 0;
         e = launch_lpb<lpb::DZ>(m, p, stream);
+        p.clean = nullptr;                                 // (once is enough)
         // Both gradients in one launch where d_lm_head is a few rounds of units and launches are what a call takes (256 x 256, vocabulary
         // 2048: 27.1 -> 21.5 us).  In long calls the pairs come to d_lm_head's units one after the other and no longer share their
         // operands in L2 (501 x 1536, vocabulary 151 936: 647 us apart, 659 together).
