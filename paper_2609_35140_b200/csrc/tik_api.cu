@@ -715,9 +715,10 @@ tik_status tik_token_logprob_bwd(tik_ctx* ctx, const float* d_logprob, const voi
     p.place = words(g.place_at);
     p.row_target = g.gather ? words(g.target_at) : target_ids;
     // The hidden rows that d_lm_head multiplies, without those of tokens that take no part: gathered, or up to a row tile copied in place.  The copy lies
-    // where d_hidden will (its last kernel writes it), or where the parts of its sums would.
+    // where d_hidden will (its last kernel writes it), or where its sums would: whole tiles' are ldt x H numbers, and where there are none the parts' at least
+    // 256 x 256 for every 256 channels.
     const bool copied = !g.gather && d_lm_head;
-    void* const rows_of = g.gather ? at + g.rows_at : copied ? (d_hidden ? d_hidden : at + g.part_at) : const_cast<void*>(hidden);
+    void* const rows_of = g.gather ? at + g.rows_at : copied ? (d_hidden ? d_hidden : at + g.sum_at) : const_cast<void*>(hidden);
     p.rows = static_cast<const __nv_bfloat16*>(rows_of);
     p.clean = copied ? static_cast<__nv_bfloat16*>(rows_of) : nullptr;
     p.hidden = static_cast<const __nv_bfloat16*>(hidden);

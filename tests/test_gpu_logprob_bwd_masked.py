@@ -76,3 +76,19 @@ def test_vocabulary_in_chunks_of_a_short_call():
     assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
     short = torch.where(ids < 64, ids, ids - (V - 128))    # the same words' rows alone
     near(got[1][at], expected(d, x, W[at], short, lse, 1.0)[1])
+
+
+@pytest.mark.parametrize("T,H,V", [(256, 65_536, 40), (256, 18_944, 64), (255, 19_200, 65), (250, 40_000, 1), (1, 65_600, 40), (256, 256, 1)])
+@pytest.mark.parametrize("hidden", [False, True])
+def test_wide_rows_stay_inside_the_workspace(T, H, V, hidden):
+    """The rows' copy is wider than the parts of so small a vocabulary's sums; what lies behind the workspace stays."""
+    args = make(T, H, V, seed=43, masked=0.3)
+    args[0][0] = 1.0
+    need = tik.workspace_bytes(tik.OP_TOKEN_LOGPROB_BWD, T, H=H, V=V)
+    buf = torch.full((need + (64 << 20),), 171, dtype=torch.uint8, device="cuda")
+    dh, dw = tik.tik_token_logprob_bwd(*args, need_hidden=hidden, ws=buf[:need])
+    assert bool((buf[need:] == 171).all())
+    a, b = expected(*args)
+    near(dw, b)
+    if hidden:
+        near(dh, a)
