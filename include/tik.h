@@ -441,7 +441,7 @@ tik_status tik_grad_clip(tik_ctx* ctx, const void* const* grads, void* const* ou
  *   stochastic != 0: 8-bit moments and bf16 weights without a master copy are rounded to one of their two neighbours, up with
  *   the probability of the distance from the lower one: 16 bits of a hash of the element's place in the call (elements of the tensors before it
  *   counted), seed and step decide.  Else to the nearest.
- * fp32 arithmetic; with 8-bit moments a v below 2^-126 counts as 0.  Tensors that are written overlap neither each other nor an input
+ * fp32 arithmetic, roots and reciprocals to 2^-23 of themselves; with 8-bit moments a v below 2^-126 counts as 0.  Tensors that are written overlap neither each other nor an input
  * (TIK_ERR_INVALID_ARG).  No workspace.  A kernel per four hundred tensors, and another where some of them, but not all, lie at other
  * addresses than multiples of 16 bytes. */
 tik_status tik_adamw(tik_ctx* ctx, void* const* params, const int* param_dtypes, const void* const* grads, const int* grad_dtypes,

@@ -229,7 +229,7 @@ def tik_token_logprob_bwd(d_logprob, hidden, lm_head, target_ids, lse, inv_tempe
                           d_lm_head: Optional[torch.Tensor] = None, accumulate: bool = False, ws: Optional[torch.Tensor] = None):
     """Gradient of tik_token_logprob: d_logprob fp32 [T] and the forward's inputs and lse [T] -> (d_hidden [T,H] bf16, d_lm_head
     [V,H]: bf16, or the bf16 or fp32 tensor passed), None for what is not needed.  accumulate: added to d_lm_head (fp32).  Tokens with
-    d_logprob 0 give no gradient.  Deterministic.  Scratch is d_z of a vocabulary chunk in bf16, up to 2 GiB."""
+    d_logprob 0 give no gradient, whatever their rows hold.  Deterministic.  Scratch is d_z of a vocabulary chunk in bf16, up to 2 GiB."""
     return (_native or _load_native()).token_logprob_bwd(d_logprob, hidden, lm_head, target_ids, lse, inv_temperature, bool(need_hidden),
                                                          bool(need_lm_head), d_hidden, d_lm_head, bool(accumulate), ws)
 
@@ -239,7 +239,7 @@ def tik_policy_loss(logprob, old_logprob, advantage, weight=None, ref_logprob=No
                     grad: bool = True, d_logprob: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """Clipped policy loss with a KL term over packed tokens, fp32 [T]; advantage [T], or [S,1] per sequence; weight: 0 masks a token,
     anything else is its factor; cu_seqlens int32 [S+1].  reduction: "sum", "token" (mean over the tokens that count) or "sequence"
-    (scale times the sum over sequences of their means).  Returns (loss [1], d_logprob [T] (None without grad), stats [5]: policy
+    (scale times the sum over sequences of their means).  d_logprob may be one of the inputs [T].  Returns (loss [1], d_logprob [T] (None without grad), stats [5]: policy
     part, KL part, share of tokens cut, mean of r - 1 - log r, tokens that count).  loss and stats always are parts of one storage,
     d_logprob and the scratch too where all is small (1 MiB together)."""
     if reduction not in LOSS_REDUCTIONS:
